@@ -23,6 +23,9 @@
  *   dopr_decoder_layer the whole decoder layer around that attention.
  *   dopr_salience      offline: which document positions become prefix
  *                      slots (Sec. 3.2.1 salience, top-K selection).
+ *   dopr_quantize_rows, dopr_quant_matmul, dopr_norm_residual, dopr_rotary
+ *                      the operators of a layer around its attention, with
+ *                      8-bit integer products and for other layer families.
  *
  * Conventions shared by every call
  *   - All device buffers are allocated by the caller and passed as raw device
@@ -448,6 +451,188 @@ dopr_status_t dopr_salience(const dopr_salience_args_t *args, void *stream);
  * ties to the lower position.  No workspace. */
 dopr_status_t dopr_select_top_k(const dopr_salience_args_t *args,
                                 void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* Operators of a decoder layer around its attention: rows in 8-bit integers,
+ * products of 8-bit integer matrices, the norms around a gated residual, and
+ * rotary positions.  They make up a layer with 8-bit products (the weights
+ * take half the bytes of bf16 and the matrix cores run at twice the rate),
+ * layers of other families than the one dopr_decoder_layer runs, and the
+ * prefix keys that dopr_store_put takes (Sec. 3.3: the selected states are
+ * forwarded as prefix inputs and their keys and values kept).
+ *
+ * Activations are bf16, fp16 or fp32 (`dtype`); sums, norms and scales are
+ * fp32, and every output is rounded once, to nearest even.  Strides are in
+ * elements; rows may start at any element-aligned address and lie any
+ * distance of at least their length apart.  Everything is asynchronous on
+ * `stream`, and outputs do not vary from run to run.                       */
+typedef enum { DOPR_BF16 = 0, DOPR_F16 = 1, DOPR_F32 = 2 } dopr_dtype_t;
+
+/* Rows in 8-bit integers: v = x, or SiLU(x) * up when `up` is given; with
+ * a = max(max_k |v[k]|, 127 * 2^-126) of a row,
+ *   scale = a / 127,  q[k] = round-to-nearest-even(v[k] * (127 / a)),
+ * each operation in fp32, so |q| <= 127 and v ~ q * scale.  A row of zeros
+ * has q = 0.  A row with a value that is not finite has q = 0 and scale NaN,
+ * so that every product with it is NaN.  Weights [out, in] are quantised per
+ * output channel by the same call.                                         */
+typedef struct {
+  int32_t dtype;            /* of x and up                                  */
+  int64_t rows;             /* >= 0                                         */
+  int64_t width;            /* 8 .. 65536                                   */
+  const void *x;            /* dev [rows, width]                            */
+  int64_t x_row_stride;
+  const void *up;           /* dev [rows, width] or NULL                    */
+  int64_t up_row_stride;
+  int8_t *q;                /* dev [rows, width]                            */
+  int64_t q_row_stride;
+  float *scale;             /* dev fp32 [rows]                              */
+} dopr_quantize_args_t;
+
+dopr_status_t dopr_quantize_rows(const dopr_quantize_args_t *args,
+                                 void *stream);
+
+/* Product of 8-bit integer matrices with a scale per row and per column, in
+ * the stored-weight convention (w is [out, in]):
+ *   y[m, n] = (sum_k x[m, k] w[n, k]) * x_scale[m] * w_scale[n]
+ *             + bias[n] + residual[m, n]
+ * The integer sum is exact (32 bits).  y may be the residual (same address
+ * and stride).  The bytes between a row's end and its stride are never read.
+ * Rows on 16-byte addresses (x, w and both strides multiples of 16) take the
+ * fast kernels.                                                            */
+typedef struct {
+  int32_t dtype;            /* of bias, residual and y                      */
+  int64_t rows;             /* M >= 0                                       */
+  int64_t cols;             /* N >= 0                                       */
+  int64_t depth;            /* K, 0 .. 131071                               */
+  const int8_t *x;          /* dev [M, K]                                   */
+  int64_t x_row_stride;
+  const float *x_scale;     /* dev fp32 [M]                                 */
+  const int8_t *w;          /* dev [N, K]                                   */
+  int64_t w_row_stride;
+  const float *w_scale;     /* dev fp32 [N]                                 */
+  const void *bias;         /* dev [N] or NULL                              */
+  const void *residual;     /* dev [M, N] or NULL                           */
+  int64_t residual_row_stride;
+  void *y;                  /* dev [M, N]                                   */
+  int64_t y_row_stride;
+  void *workspace;          /* dev scratch, 256-byte aligned, of at least
+                               dopr_quant_matmul_workspace() bytes (NULL
+                               where that is 0)                             */
+  size_t workspace_bytes;
+} dopr_quant_matmul_args_t;
+
+/* Workspace bytes for these rows, cols and depth (host arithmetic). */
+dopr_status_t dopr_quant_matmul_workspace(const dopr_quant_matmul_args_t *args,
+                                          size_t *bytes);
+
+dopr_status_t dopr_quant_matmul(const dopr_quant_matmul_args_t *args,
+                                void *stream);
+
+/* The norms on either side of a block, fused with its gate and residual:
+ *   n = RMSNorm(x) * post_norm_w       (x itself when post_norm_w is NULL)
+ *   h = residual_scale * residual + gate * n   (either factor left out when
+ *                                               its pointer is NULL)
+ *   z = RMSNorm(h) * pre_norm_w        (h itself when pre_norm_w is NULL)
+ * x is a block's output, h the residual stream behind it and z the next
+ * block's input.  RMSNorm is over the row with epsilon rms_eps.  Outputs: h,
+ * and z as dtype (`z`) and / or in 8 bits (`q`, `q_scale`, as
+ * dopr_quantize_rows makes them from the unrounded z); at least one.  The
+ * second norm reads h before its rounding to residual_dtype.  h may be the
+ * residual or x (same address, stride and type), z may be x.               */
+typedef struct {
+  int32_t dtype;            /* of x, post_norm_w, gate, pre_norm_w and z    */
+  int32_t residual_dtype;   /* of residual and h: dtype or DOPR_F32         */
+  int64_t rows;             /* >= 0                                         */
+  int64_t width;            /* 8 .. 65536                                   */
+  const void *x;            /* dev [rows, width]                            */
+  int64_t x_row_stride;
+  const void *post_norm_w;  /* dev [width] or NULL                          */
+  const void *gate;         /* dev [rows, width], or [width] with
+                               gate_row_stride 0 (one for all rows), or
+                               NULL                                         */
+  int64_t gate_row_stride;
+  const void *residual;     /* dev [rows, width] or NULL                    */
+  int64_t residual_row_stride;
+  const void *pre_norm_w;   /* dev [width] or NULL                          */
+  float residual_scale;     /* finite                                       */
+  float rms_eps;            /* finite, >= 0                                 */
+  void *h;                  /* dev [rows, width] or NULL                    */
+  int64_t h_row_stride;
+  void *z;                  /* dev [rows, width] or NULL                    */
+  int64_t z_row_stride;
+  int8_t *q;                /* dev [rows, width] or NULL                    */
+  int64_t q_row_stride;
+  float *q_scale;           /* dev fp32 [rows], with q                      */
+} dopr_norm_residual_args_t;
+
+dopr_status_t dopr_norm_residual(const dopr_norm_residual_args_t *args,
+                                 void *stream);
+
+/* Rotary positions of query and key heads.  With R = rotary_dim and
+ * t = positions[row] * inv_freq[i], pair i < R/2 of a head, (a, b) =
+ * (x[i], x[i + R/2]), or (x[2i], x[2i + 1]) when `interleaved`, becomes
+ *   attention_factor * (a cos t - b sin t, b cos t + a sin t)
+ * (`inverse`: t -> -t); x[R ..] passes through.  With a norm gain, the
+ * head's RMSNorm over all of head_dim, times the gain, comes first
+ * (dopr_prefix_attn's order).  A prefix attention of heads that are already
+ * normed and rotated takes both gains NULL and rope_inv_freq all zero.
+ * Outputs may be the inputs (same addresses and strides); other overlaps
+ * are not allowed.  Heads lie head_stride apart, so a head-major layout or
+ * the q and k parts of one projection's rows are read as they are.         */
+typedef struct {
+  int32_t dtype;
+  int32_t n_q_heads;        /* >= 0                                         */
+  int32_t n_kv_heads;       /* >= 0                                         */
+  int32_t head_dim;         /* D, 2 .. 512                                  */
+  int32_t rotary_dim;       /* R, even, 2 .. D                              */
+  int32_t interleaved;      /* 0 or 1                                       */
+  int32_t inverse;          /* 0 or 1; 1 takes no norm gains                */
+  float attention_factor;   /* finite                                       */
+  float rms_eps;            /* finite, >= 0                                 */
+  int64_t rows;             /* tokens >= 0                                  */
+  const int32_t *positions; /* dev int32 [rows]                             */
+  const float *inv_freq;    /* dev fp32 [R/2]                               */
+  const void *q;            /* dev [rows, n_q_heads, D]; NULL with 0 heads  */
+  int64_t q_row_stride, q_head_stride;
+  void *q_out;
+  int64_t q_out_row_stride, q_out_head_stride;
+  const void *k;            /* dev [rows, n_kv_heads, D]                    */
+  int64_t k_row_stride, k_head_stride;
+  void *k_out;
+  int64_t k_out_row_stride, k_out_head_stride;
+  const void *q_norm_w;     /* dev [D] or NULL                              */
+  const void *k_norm_w;     /* dev [D] or NULL                              */
+} dopr_rotary_args_t;
+
+dopr_status_t dopr_rotary(const dopr_rotary_args_t *args, void *stream);
+
+/* Rotation frequencies for contexts longer than the trained one.  With
+ * w_i = theta^(-2i/R), i < R/2, and s = factor:
+ *   DOPR_ROPE_PLAIN   w_i
+ *   DOPR_ROPE_LINEAR  w_i / s
+ *   DOPR_ROPE_BASE    (theta * s^(R/(R-2)))^(-2i/R): the base is stretched so
+ *                     that the slowest pair turns s times slower (R > 2)
+ *   DOPR_ROPE_RAMP    w_i (g_i + (1 - g_i) / s), g_i = 1 for pairs that turn
+ *                     at least turns_high times within original_len, 0 for
+ *                     at most turns_low, linear in the pair's index between
+ *                     the two (real-valued) indices where the turns are met
+ *   DOPR_ROPE_BANDS   the same with g_i linear in the number of turns
+ * *attention_factor receives 0.1 ln s + 1 for RAMP with s > 1, else 1.
+ * Host arithmetic in 64 bits; inv_freq is a HOST array of R/2 floats.      */
+typedef enum {
+  DOPR_ROPE_PLAIN = 0,
+  DOPR_ROPE_LINEAR = 1,
+  DOPR_ROPE_BASE = 2,
+  DOPR_ROPE_RAMP = 3,
+  DOPR_ROPE_BANDS = 4
+} dopr_rope_scaling_t;
+
+dopr_status_t dopr_rotary_frequencies(int32_t rotary_dim, double theta,
+                                      dopr_rope_scaling_t scaling,
+                                      double factor, double original_len,
+                                      double turns_low, double turns_high,
+                                      float *inv_freq,
+                                      float *attention_factor);
 
 /* ------------------------------------------------------------------------ */
 /* Exports used by the bit-exact tests of the integer steps.               */

@@ -95,6 +95,64 @@ class _SalienceArgs(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t)]
 
 
+class _QuantizeArgs(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("width", ctypes.c_int64), ("x", ctypes.c_void_p),
+                ("x_row_stride", ctypes.c_int64), ("up", ctypes.c_void_p),
+                ("up_row_stride", ctypes.c_int64), ("q", ctypes.c_void_p),
+                ("q_row_stride", ctypes.c_int64), ("scale", ctypes.c_void_p)]
+
+
+class _QuantMatmulArgs(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("depth", ctypes.c_int64),
+                ("x", ctypes.c_void_p), ("x_row_stride", ctypes.c_int64),
+                ("x_scale", ctypes.c_void_p), ("w", ctypes.c_void_p),
+                ("w_row_stride", ctypes.c_int64),
+                ("w_scale", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("residual", ctypes.c_void_p),
+                ("residual_row_stride", ctypes.c_int64),
+                ("y", ctypes.c_void_p), ("y_row_stride", ctypes.c_int64),
+                ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
+class _NormResidualArgs(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("residual_dtype", ctypes.c_int32),
+                ("rows", ctypes.c_int64), ("width", ctypes.c_int64),
+                ("x", ctypes.c_void_p), ("x_row_stride", ctypes.c_int64),
+                ("post_norm_w", ctypes.c_void_p), ("gate", ctypes.c_void_p),
+                ("gate_row_stride", ctypes.c_int64),
+                ("residual", ctypes.c_void_p),
+                ("residual_row_stride", ctypes.c_int64),
+                ("pre_norm_w", ctypes.c_void_p),
+                ("residual_scale", ctypes.c_float),
+                ("rms_eps", ctypes.c_float), ("h", ctypes.c_void_p),
+                ("h_row_stride", ctypes.c_int64), ("z", ctypes.c_void_p),
+                ("z_row_stride", ctypes.c_int64), ("q", ctypes.c_void_p),
+                ("q_row_stride", ctypes.c_int64),
+                ("q_scale", ctypes.c_void_p)]
+
+
+class _RotaryArgs(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("inverse", ctypes.c_int32),
+                ("attention_factor", ctypes.c_float),
+                ("rms_eps", ctypes.c_float), ("rows", ctypes.c_int64),
+                ("positions", ctypes.c_void_p), ("inv_freq", ctypes.c_void_p),
+                ("q", ctypes.c_void_p), ("q_row_stride", ctypes.c_int64),
+                ("q_head_stride", ctypes.c_int64), ("q_out", ctypes.c_void_p),
+                ("q_out_row_stride", ctypes.c_int64),
+                ("q_out_head_stride", ctypes.c_int64),
+                ("k", ctypes.c_void_p), ("k_row_stride", ctypes.c_int64),
+                ("k_head_stride", ctypes.c_int64), ("k_out", ctypes.c_void_p),
+                ("k_out_row_stride", ctypes.c_int64),
+                ("k_out_head_stride", ctypes.c_int64),
+                ("q_norm_w", ctypes.c_void_p), ("k_norm_w", ctypes.c_void_p)]
+
+
 EXPORTS = {
     "dopr_store_bytes": ([ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p],
                          ctypes.c_int),
@@ -135,6 +193,17 @@ EXPORTS = {
                                 ctypes.c_int),
     "dopr_salience": ([ctypes.c_void_p, ctypes.c_void_p], ctypes.c_int),
     "dopr_select_top_k": ([ctypes.c_void_p, ctypes.c_void_p], ctypes.c_int),
+    "dopr_quantize_rows": ([ctypes.c_void_p, ctypes.c_void_p], ctypes.c_int),
+    "dopr_quant_matmul_workspace": ([ctypes.c_void_p, ctypes.c_void_p],
+                                    ctypes.c_int),
+    "dopr_quant_matmul": ([ctypes.c_void_p, ctypes.c_void_p], ctypes.c_int),
+    "dopr_norm_residual": ([ctypes.c_void_p, ctypes.c_void_p], ctypes.c_int),
+    "dopr_rotary": ([ctypes.c_void_p, ctypes.c_void_p], ctypes.c_int),
+    "dopr_rotary_frequencies": ([ctypes.c_int32, ctypes.c_double,
+                                 ctypes.c_int, ctypes.c_double,
+                                 ctypes.c_double, ctypes.c_double,
+                                 ctypes.c_double, ctypes.c_void_p,
+                                 ctypes.c_void_p], ctypes.c_int),
     "dopr_check_status": ([ctypes.c_void_p, ctypes.c_void_p], ctypes.c_int),
     "dopr_status_str": ([ctypes.c_int], ctypes.c_char_p),
     "dopr_last_error": ([], ctypes.c_char_p),
@@ -513,6 +582,198 @@ def dopr_select_top_k(cu_doclens, cu_select, u, selected, *, max_doclen,
                        u.numel(), selected.numel(), cu_doclens, cu_select,
                        None, None, u, selected, None, status, None)
     _check(lib().dopr_select_top_k(ctypes.byref(a), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# Operators of a layer around its attention.  These take any strides that the
+# C ABI takes, so the wrappers check what a pointer and a size cannot show:
+# types, shapes and unit strides.
+
+_dtypes = {}
+
+
+def _dtype_code(t, what: str) -> int:
+    if not _dtypes:
+        import torch
+        _dtypes.update({torch.bfloat16: 0, torch.float16: 1,
+                        torch.float32: 2})
+    code = _dtypes.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{what} must be bfloat16, float16 or float32, not "
+                         f"{t.dtype}")
+    return code
+
+
+def _expect(t, what: str, shape, dtype):
+    """t has this shape and type, on a GPU, its last dimension contiguous."""
+    if t.dtype != dtype or t.shape != shape or not t.is_cuda or (
+            shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(
+            f"{what} must be a {dtype} GPU tensor of shape {tuple(shape)} "
+            f"with unit last stride, not {t.dtype} {tuple(t.shape)}, strides "
+            f"{t.stride()}, on {t.device}")
+
+
+def _row_stride(t) -> int:
+    """Elements between rows; a single row has no stride to speak of."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _optional_row(t, what, shape, dtype):
+    """(pointer, row stride) of an optional [rows, width] operand."""
+    if t is None:
+        return None, 0
+    _expect(t, what, shape, dtype)
+    return t.data_ptr(), _row_stride(t)
+
+
+def dopr_quantize_rows(x, q, scale, *, up=None, stream=None):
+    """Rows of x [rows, width] (or SiLU(x) * up) in 8-bit integers: q int8
+    [rows, width], scale fp32 [rows]."""
+    import torch
+    shape = x.shape
+    code = _dtype_code(x, "x")
+    _expect(x, "x", shape, x.dtype)
+    _expect(q, "q", shape, torch.int8)
+    _expect(scale, "scale", shape[:1], torch.float32)
+    up_p, up_s = _optional_row(up, "up", shape, x.dtype)
+    a = _QuantizeArgs(code, shape[0], shape[1], x.data_ptr(), _row_stride(x),
+                      up_p, up_s, q.data_ptr(), _row_stride(q),
+                      scale.data_ptr())
+    _check(lib().dopr_quantize_rows(ctypes.byref(a), _stream(stream)))
+
+
+def dopr_quant_matmul_workspace(rows: int, cols: int, depth: int) -> int:
+    """Workspace bytes of a product (host arithmetic; 0: none is needed)."""
+    a = _QuantMatmulArgs()
+    a.rows, a.cols, a.depth = rows, cols, depth
+    n = ctypes.c_size_t(0)
+    _check(lib().dopr_quant_matmul_workspace(ctypes.byref(a),
+                                             ctypes.byref(n)))
+    return n.value
+
+
+def dopr_quant_matmul(x, x_scale, w, w_scale, y, *, bias=None, residual=None,
+                      workspace=None, stream=None):
+    """y [M, N] = (x w^T) * x_scale * w_scale (+ bias) (+ residual) with x
+    int8 [M, K] and w int8 [N, K]; y, bias [N] and residual [M, N] share one
+    type.  y may be the residual."""
+    import torch
+    m, k = x.shape
+    n = w.shape[0]
+    code = _dtype_code(y, "y")
+    _expect(x, "x", (m, k), torch.int8)
+    _expect(w, "w", (n, k), torch.int8)
+    _expect(y, "y", (m, n), y.dtype)
+    _expect(x_scale, "x_scale", (m,), torch.float32)
+    _expect(w_scale, "w_scale", (n,), torch.float32)
+    if bias is not None:
+        _expect(bias, "bias", (n,), y.dtype)
+    res_p, res_s = _optional_row(residual, "residual", (m, n), y.dtype)
+    ws_bytes = 0 if workspace is None else (
+        workspace.numel() * workspace.element_size())
+    a = _QuantMatmulArgs(code, m, n, k, x.data_ptr(), _row_stride(x),
+                         x_scale.data_ptr(), w.data_ptr(), _row_stride(w),
+                         w_scale.data_ptr(), _ptr(bias), res_p, res_s,
+                         y.data_ptr(), _row_stride(y), _ptr(workspace),
+                         ws_bytes)
+    _check(lib().dopr_quant_matmul(ctypes.byref(a), _stream(stream)))
+
+
+def dopr_norm_residual(x, *, residual=None, post_norm_w=None, gate=None,
+                       residual_scale=1.0, pre_norm_w=None, h=None, z=None,
+                       q=None, q_scale=None, rms_eps=1e-6, stream=None):
+    """h = residual_scale * residual + gate * norm(x, post_norm_w) and
+    z = norm(h, pre_norm_w), z also or instead in 8 bits (q int8 [rows,
+    width], q_scale fp32 [rows]).  gate is [width] or [rows, width]; residual
+    and h share one type, x's or fp32."""
+    import torch
+    shape = x.shape
+    code = _dtype_code(x, "x")
+    _expect(x, "x", shape, x.dtype)
+    for t, what in ((post_norm_w, "post_norm_w"), (pre_norm_w, "pre_norm_w")):
+        if t is not None:
+            _expect(t, what, shape[1:], x.dtype)
+    gate_p = gate_s = 0
+    if gate is not None and gate.dim() == 1:
+        _expect(gate, "gate", shape[1:], x.dtype)
+        gate_p = gate.data_ptr()
+    elif gate is not None:
+        gate_p, gate_s = _optional_row(gate, "gate", shape, x.dtype)
+    # residual and h: x's type, or fp32 kept wider than it
+    rt = (residual if residual is not None else x if h is None else h).dtype
+    if rt != x.dtype and rt != torch.float32:
+        raise ValueError(f"residual and h must be {x.dtype} or float32")
+    res_p, res_s = _optional_row(residual, "residual", shape, rt)
+    h_p, h_s = _optional_row(h, "h", shape, rt)
+    z_p, z_s = _optional_row(z, "z", shape, x.dtype)
+    q_p, q_s = _optional_row(q, "q", shape, torch.int8)
+    if q_scale is not None:
+        _expect(q_scale, "q_scale", shape[:1], torch.float32)
+    a = _NormResidualArgs(code, _dtypes[rt], shape[0], shape[1], x.data_ptr(),
+                          _row_stride(x), _ptr(post_norm_w), gate_p, gate_s,
+                          res_p, res_s, _ptr(pre_norm_w),
+                          float(residual_scale), float(rms_eps), h_p, h_s,
+                          z_p, z_s, q_p, q_s, _ptr(q_scale))
+    _check(lib().dopr_norm_residual(ctypes.byref(a), _stream(stream)))
+
+
+def dopr_rotary(q, k, positions, inv_freq, q_out, k_out, *, interleaved=False,
+                inverse=False, attention_factor=1.0, q_norm_w=None,
+                k_norm_w=None, rms_eps=1e-6, stream=None):
+    """Rotary positions (after an optional per-head RMSNorm) of q [rows, Hq,
+    D] and k [rows, Hkv, D]; either may be None.  positions int32 [rows];
+    inv_freq fp32 [R/2] rotates the first R elements of a head.  Outputs may
+    be the inputs."""
+    import torch
+    first = q if q is not None else k
+    if first is None:
+        raise ValueError("q and k are both None")
+    rows, _, d = first.shape
+    dt = first.dtype
+    code = _dtype_code(first, "q")
+    parts = []
+    for x, out, name in ((q, q_out, "q"), (k, k_out, "k")):
+        if x is None:
+            parts.append((0, None, 0, 0, None, 0, 0))
+            continue
+        shape = (rows, x.shape[1], d)
+        _expect(x, name, shape, dt)
+        _expect(out, name + "_out", shape, dt)
+        parts.append((shape[1], x.data_ptr(), x.stride(0), x.stride(1),
+                      out.data_ptr(), out.stride(0), out.stride(1)))
+    _expect(positions, "positions", (rows,), torch.int32)
+    _expect(inv_freq, "inv_freq", inv_freq.shape, torch.float32)
+    for t, what in ((q_norm_w, "q_norm_w"), (k_norm_w, "k_norm_w")):
+        if t is not None:
+            _expect(t, what, (d,), dt)
+    a = _RotaryArgs(code, parts[0][0], parts[1][0], d, 2 * inv_freq.numel(),
+                    int(interleaved), int(inverse), float(attention_factor),
+                    float(rms_eps), rows, positions.data_ptr(),
+                    inv_freq.data_ptr(), *parts[0][1:], *parts[1][1:],
+                    _ptr(q_norm_w), _ptr(k_norm_w))
+    _check(lib().dopr_rotary(ctypes.byref(a), _stream(stream)))
+
+
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3, "bands": 4}
+
+
+def dopr_rotary_frequencies(rotary_dim: int, theta: float, *,
+                            scaling="plain", factor=1.0, original_len=0.0,
+                            turns_low=1.0, turns_high=32.0):
+    """Rotation frequencies for a context `factor` times the trained one
+    (host arithmetic): (fp32 CPU tensor [rotary_dim / 2], attention factor).
+    scaling: plain, linear, base, ramp or bands (the C enum's names)."""
+    import torch
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(ROPE_SCALINGS)}")
+    out = torch.empty(max(int(rotary_dim) // 2, 1), dtype=torch.float32)
+    f = ctypes.c_float(0.0)
+    _check(lib().dopr_rotary_frequencies(
+        int(rotary_dim), float(theta), ROPE_SCALINGS[scaling], float(factor),
+        float(original_len), float(turns_low), float(turns_high),
+        out.data_ptr(), ctypes.byref(f)))
+    return out, f.value
 
 
 def dopr_check_status(store: Store, stream=None) -> int:

@@ -929,6 +929,274 @@ dopr_status_t dopr_select_top_k(const dopr_salience_args_t *a, void *stream) {
   return ok();
 }
 
+// ---------------------------------------------------------------------------
+// Operators around the attention
+
+namespace {
+
+constexpr int64_t kMaxRowWidth = 65536;   // a row held by 1,024 threads
+constexpr int64_t kMaxDepth = 131071;     // 128^2 * depth < 2^31
+
+bool is_dtype(int32_t t) {
+  return t == DOPR_BF16 || t == DOPR_F16 || t == DOPR_F32;
+}
+
+bool aligned_to(const void *p, int32_t dtype) {
+  const uintptr_t e = dtype == DOPR_F32 ? 4 : 2;
+  return reinterpret_cast<uintptr_t>(p) % e == 0;
+}
+
+dopr_status_t check_rows(int32_t dtype, int64_t rows, int64_t width) {
+  if (!is_dtype(dtype)) return fail(DOPR_ERR_INVALID_ARG, "unknown dtype");
+  if (rows < 0 || rows > INT32_MAX)
+    return fail(DOPR_ERR_INVALID_ARG, "rows must be in [0, 2^31)");
+  if (width < 1) return fail(DOPR_ERR_INVALID_ARG, "width < 1");
+  if (width < 8 || width > kMaxRowWidth)
+    return fail(DOPR_ERR_UNSUPPORTED, "width must be in [8, 65536]");
+  return DOPR_OK;
+}
+
+}  // namespace
+
+dopr_status_t dopr_quantize_rows(const dopr_quantize_args_t *a,
+                                 void *stream) {
+  if (!a) return fail(DOPR_ERR_INVALID_ARG, "args is NULL");
+  dopr_status_t s = check_rows(a->dtype, a->rows, a->width);
+  if (s != DOPR_OK) return s;
+  if (a->x_row_stride < a->width || a->q_row_stride < a->width ||
+      (a->up && a->up_row_stride < a->width))
+    return fail(DOPR_ERR_INVALID_ARG, "row strides must be >= width");
+  if (a->rows == 0) return ok();
+  if (!a->x || !a->q || !a->scale)
+    return fail(DOPR_ERR_INVALID_ARG, "NULL buffer");
+  if (!aligned_to(a->x, a->dtype) || !aligned_to(a->up, a->dtype) ||
+      !aligned_to(a->scale, DOPR_F32))
+    return fail(DOPR_ERR_INVALID_ARG, "buffers must be element-aligned");
+  hipError_t e = launch_quantize_rows(*a, as_stream(stream));
+  if (e != hipSuccess) return hip_fail(e, "quantize launch");
+  return ok();
+}
+
+namespace {
+
+dopr_status_t check_product(const dopr_quant_matmul_args_t *a) {
+  if (!a) return fail(DOPR_ERR_INVALID_ARG, "args is NULL");
+  if (a->rows < 0 || a->cols < 0 || a->depth < 0 || a->rows > INT32_MAX ||
+      a->cols > INT32_MAX)
+    return fail(DOPR_ERR_INVALID_ARG,
+                "rows and cols must be in [0, 2^31), depth >= 0");
+  if (a->depth > kMaxDepth)
+    return fail(DOPR_ERR_UNSUPPORTED,
+                "depth over 131071 may exceed 32-bit sums");
+  if (((a->rows + 15) / 16) * ((a->cols + 15) / 16) > INT32_MAX)
+    return fail(DOPR_ERR_UNSUPPORTED, "more than 2^31 16 x 16 output blocks");
+  return DOPR_OK;
+}
+
+}  // namespace
+
+dopr_status_t dopr_quant_matmul_workspace(const dopr_quant_matmul_args_t *a,
+                                          size_t *bytes) {
+  if (!bytes) return fail(DOPR_ERR_INVALID_ARG, "bytes is NULL");
+  dopr_status_t s = check_product(a);
+  if (s != DOPR_OK) return s;
+  *bytes = product_workspace(a->rows, a->cols, a->depth);
+  return ok();
+}
+
+dopr_status_t dopr_quant_matmul(const dopr_quant_matmul_args_t *a,
+                                void *stream) {
+  dopr_status_t s = check_product(a);
+  if (s != DOPR_OK) return s;
+  if (!is_dtype(a->dtype)) return fail(DOPR_ERR_INVALID_ARG, "unknown dtype");
+  if (a->x_row_stride < a->depth || a->w_row_stride < a->depth ||
+      a->y_row_stride < a->cols ||
+      (a->residual && a->residual_row_stride < a->cols))
+    return fail(DOPR_ERR_INVALID_ARG,
+                "row strides must be at least the rows' length");
+  if (a->rows == 0 || a->cols == 0) return ok();
+  if (!a->x_scale || !a->w_scale || !a->y ||
+      (a->depth > 0 && (!a->x || !a->w)))
+    return fail(DOPR_ERR_INVALID_ARG, "NULL buffer");
+  if (!aligned_to(a->x_scale, DOPR_F32) || !aligned_to(a->w_scale, DOPR_F32) ||
+      !aligned_to(a->bias, a->dtype) || !aligned_to(a->residual, a->dtype) ||
+      !aligned_to(a->y, a->dtype))
+    return fail(DOPR_ERR_INVALID_ARG, "buffers must be element-aligned");
+  const size_t need = product_workspace(a->rows, a->cols, a->depth);
+  if (need > 0) {
+    if (!a->workspace || a->workspace_bytes < need)
+      return fail(DOPR_ERR_WORKSPACE,
+                  "workspace holds " +
+                      std::to_string(a->workspace ? a->workspace_bytes : 0) +
+                      " bytes, needs " + std::to_string(need));
+    if (reinterpret_cast<uintptr_t>(a->workspace) % kAlign)
+      return fail(DOPR_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  }
+  hipError_t e = launch_product(*a, as_stream(stream));
+  if (e != hipSuccess) return hip_fail(e, "product launch");
+  return ok();
+}
+
+dopr_status_t dopr_norm_residual(const dopr_norm_residual_args_t *a,
+                                 void *stream) {
+  if (!a) return fail(DOPR_ERR_INVALID_ARG, "args is NULL");
+  dopr_status_t s = check_rows(a->dtype, a->rows, a->width);
+  if (s != DOPR_OK) return s;
+  if (a->residual_dtype != a->dtype && a->residual_dtype != DOPR_F32)
+    return fail(DOPR_ERR_INVALID_ARG,
+                "residual_dtype must be dtype or DOPR_F32");
+  if (!std::isfinite(a->residual_scale))
+    return fail(DOPR_ERR_INVALID_ARG, "residual_scale must be finite");
+  if (!(a->rms_eps >= 0.f) || !std::isfinite(a->rms_eps))
+    return fail(DOPR_ERR_INVALID_ARG, "rms_eps must be finite and >= 0");
+  const int64_t w = a->width;
+  if (a->x_row_stride < w || (a->residual && a->residual_row_stride < w) ||
+      (a->gate && a->gate_row_stride != 0 && a->gate_row_stride < w) ||
+      (a->h && a->h_row_stride < w) || (a->z && a->z_row_stride < w) ||
+      (a->q && a->q_row_stride < w))
+    return fail(DOPR_ERR_INVALID_ARG,
+                "row strides must be >= width (the gate's may be 0)");
+  if (!a->h && !a->z && !a->q)
+    return fail(DOPR_ERR_INVALID_ARG, "no output: h, z and q are NULL");
+  if (!a->q != !a->q_scale)
+    return fail(DOPR_ERR_INVALID_ARG, "q and q_scale go together");
+  if (a->rows == 0) return ok();
+  if (!a->x) return fail(DOPR_ERR_INVALID_ARG, "x is NULL");
+  const void *el[] = {a->x, a->post_norm_w, a->gate, a->pre_norm_w, a->z};
+  for (const void *p : el)
+    if (!aligned_to(p, a->dtype))
+      return fail(DOPR_ERR_INVALID_ARG, "buffers must be element-aligned");
+  if (!aligned_to(a->residual, a->residual_dtype) ||
+      !aligned_to(a->h, a->residual_dtype) ||
+      !aligned_to(a->q_scale, DOPR_F32))
+    return fail(DOPR_ERR_INVALID_ARG, "buffers must be element-aligned");
+  hipError_t e = launch_norm_residual(*a, as_stream(stream));
+  if (e != hipSuccess) return hip_fail(e, "norm launch");
+  return ok();
+}
+
+namespace {
+
+// Heads [rows][heads][D] at these strides do not overlap one another, token-
+// or head-major.
+bool heads_apart(int64_t rows, int64_t heads, int64_t D, int64_t row,
+                 int64_t head) {
+  if (row < 0 || head < 0) return false;
+  if (heads <= 1) return rows <= 1 || row >= D;
+  if (rows <= 1) return head >= D;
+  return (head >= D && row >= (heads - 1) * head + D) ||
+         (row >= D && head >= (rows - 1) * row + D);
+}
+
+}  // namespace
+
+dopr_status_t dopr_rotary(const dopr_rotary_args_t *a, void *stream) {
+  if (!a) return fail(DOPR_ERR_INVALID_ARG, "args is NULL");
+  if (!is_dtype(a->dtype)) return fail(DOPR_ERR_INVALID_ARG, "unknown dtype");
+  if (a->n_q_heads < 0 || a->n_kv_heads < 0 ||
+      (int64_t)a->n_q_heads + a->n_kv_heads > (1 << 20))
+    return fail(DOPR_ERR_INVALID_ARG, "heads must be in [0, 2^20]");
+  if (a->rows < 0 || a->rows > INT32_MAX)
+    return fail(DOPR_ERR_INVALID_ARG, "rows must be in [0, 2^31)");
+  if (a->head_dim < 2 || a->rotary_dim < 2 || a->rotary_dim % 2 ||
+      a->rotary_dim > a->head_dim)
+    return fail(DOPR_ERR_INVALID_ARG,
+                "rotary_dim must be even, in [2, head_dim]");
+  if (a->head_dim > 512)
+    return fail(DOPR_ERR_UNSUPPORTED, "head_dim over 512");
+  if ((a->interleaved & ~1) || (a->inverse & ~1))
+    return fail(DOPR_ERR_INVALID_ARG, "interleaved and inverse are 0 or 1");
+  if (a->inverse && (a->q_norm_w || a->k_norm_w))
+    return fail(DOPR_ERR_INVALID_ARG,
+                "an inverse rotation takes no norm gains");
+  if (!std::isfinite(a->attention_factor))
+    return fail(DOPR_ERR_INVALID_ARG, "attention_factor must be finite");
+  if (!(a->rms_eps >= 0.f) || !std::isfinite(a->rms_eps))
+    return fail(DOPR_ERR_INVALID_ARG, "rms_eps must be finite and >= 0");
+  if (a->rows == 0 || a->n_q_heads + a->n_kv_heads == 0) return ok();
+  if (!a->positions || !a->inv_freq || (a->n_q_heads && (!a->q || !a->q_out)) ||
+      (a->n_kv_heads && (!a->k || !a->k_out)))
+    return fail(DOPR_ERR_INVALID_ARG, "NULL buffer");
+  if ((a->n_q_heads &&
+       !(heads_apart(a->rows, a->n_q_heads, a->head_dim, a->q_out_row_stride,
+                     a->q_out_head_stride) &&
+         a->q_row_stride >= 0 && a->q_head_stride >= 0)) ||
+      (a->n_kv_heads &&
+       !(heads_apart(a->rows, a->n_kv_heads, a->head_dim, a->k_out_row_stride,
+                     a->k_out_head_stride) &&
+         a->k_row_stride >= 0 && a->k_head_stride >= 0)))
+    return fail(DOPR_ERR_INVALID_ARG,
+                "strides must be >= 0 and output heads must not overlap");
+  const void *el[] = {a->q, a->q_out, a->k, a->k_out, a->q_norm_w,
+                      a->k_norm_w};
+  for (const void *p : el)
+    if (!aligned_to(p, a->dtype))
+      return fail(DOPR_ERR_INVALID_ARG, "buffers must be element-aligned");
+  if (!aligned_to(a->positions, DOPR_F32) || !aligned_to(a->inv_freq, DOPR_F32))
+    return fail(DOPR_ERR_INVALID_ARG, "buffers must be element-aligned");
+  hipError_t e = launch_rotary(*a, as_stream(stream));
+  if (e != hipSuccess) return hip_fail(e, "rotary launch");
+  return ok();
+}
+
+dopr_status_t dopr_rotary_frequencies(int32_t R, double theta,
+                                      dopr_rope_scaling_t scaling,
+                                      double factor, double original_len,
+                                      double turns_low, double turns_high,
+                                      float *inv_freq,
+                                      float *attention_factor) {
+  if (!inv_freq || !attention_factor)
+    return fail(DOPR_ERR_INVALID_ARG, "NULL buffer");
+  if (R < 2 || R % 2)
+    return fail(DOPR_ERR_INVALID_ARG, "rotary_dim must be even and >= 2");
+  if (!(theta > 1.0) || !std::isfinite(theta))
+    return fail(DOPR_ERR_INVALID_ARG, "theta must be finite and > 1");
+  const int kind = (int)scaling;
+  if (kind < DOPR_ROPE_PLAIN || kind > DOPR_ROPE_BANDS)
+    return fail(DOPR_ERR_INVALID_ARG, "unknown scaling");
+  if (kind != DOPR_ROPE_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor)))
+    return fail(DOPR_ERR_INVALID_ARG, "factor must be finite and >= 1");
+  if (kind == DOPR_ROPE_BASE && R == 2)
+    return fail(DOPR_ERR_INVALID_ARG, "a stretched base needs two pairs");
+  const bool parts = kind == DOPR_ROPE_RAMP || kind == DOPR_ROPE_BANDS;
+  if (parts && (!(original_len > 0.0) || !std::isfinite(original_len) ||
+                !(turns_low > 0.0) || !(turns_high > turns_low) ||
+                !std::isfinite(turns_high)))
+    return fail(DOPR_ERR_INVALID_ARG,
+                "original_len and 0 < turns_low < turns_high must be finite");
+  const double two_pi = 6.283185307179586477;
+  // the (real) index of the pair that turns `turns` times in original_len
+  auto index_of = [&](double turns) {
+    return 0.5 * R * std::log(original_len / (two_pi * turns)) /
+           std::log(theta);
+  };
+  for (int i = 0; i < R / 2; ++i) {
+    double w = std::pow(theta, -2.0 * i / R);
+    if (kind == DOPR_ROPE_LINEAR) {
+      w /= factor;
+    } else if (kind == DOPR_ROPE_BASE) {
+      w = std::pow(theta * std::pow(factor, (double)R / (R - 2)),
+                   -2.0 * i / R);
+    } else if (parts) {
+      const double turns = original_len * w / two_pi;
+      double g;
+      if (kind == DOPR_ROPE_RAMP) {
+        const double fast = index_of(turns_high), slow = index_of(turns_low);
+        g = (slow - i) / (slow - fast);
+      } else {
+        g = (turns - turns_low) / (turns_high - turns_low);
+      }
+      g = std::min(1.0, std::max(0.0, g));
+      w *= g + (1.0 - g) / factor;
+    }
+    inv_freq[i] = (float)w;
+  }
+  *attention_factor = kind == DOPR_ROPE_RAMP && factor > 1.0
+                          ? (float)(0.1 * std::log(factor) + 1.0)
+                          : 1.f;
+  return ok();
+}
+
 dopr_status_t dopr_check_status(dopr_store_t st, void *stream) {
   if (!st) return fail(DOPR_ERR_INVALID_ARG, "store is NULL");
   hipStream_t hs = as_stream(stream);

@@ -1,0 +1,305 @@
+// rotary.hip -- rotary positions of query and key heads (k_rotary), with the
+// heads' RMSNorm in front.
+//
+// Pair i of a head (elements (i, i + R/2), or (2i, 2i+1) where the layout is
+// interleaved) turns by position * inv_freq[i]; elements from R on pass
+// through.  A wave takes one token: its lanes form the token's R/2 rotations
+// once, then every head uses them.  A lane holds 8 pairs (16 elements) of a
+// head, so a rotation never leaves the lane, in-place calls are safe, and a
+// head's sum of squares is a butterfly over the 1 to 64 lanes of that head.
+// Bound by HBM: each head is read and written once.
+//
+// The angle's whole turns are dropped in 64 bits (four operations per pair
+// and token): in 32 bits the product of a position and a frequency is off by
+// up to 2^-25 of itself, at position 2^17 0.004 rad, more than a bf16
+// rounding.
+#include "rowio.hpp"
+
+namespace dopr {
+namespace {
+
+constexpr int kRotaryWaves = 4;
+constexpr int kRotaryBatch = 4;  // head groups whose loads are in flight
+
+struct RotaryHeads {
+  const void *x;
+  void *out;
+  const void *norm_w;
+  int64_t row, head, out_row, out_head;  // strides in elements
+};
+
+struct RotaryParams {
+  RotaryHeads q, k;
+  const int32_t *positions;
+  const float *inv_freq;
+  int64_t items;             // tokens * splits
+  int32_t n_q, n_heads;      // query heads, all heads
+  int32_t D, R;
+  int32_t group_log2;        // lanes per head
+  int32_t pair_units, units; // 16-element units of a head: rotated, all
+  int32_t splits;            // waves that share a token's heads
+  float factor, sign, eps;
+};
+
+// A unit's two runs of 8 elements, of which [lo, n) are its own.
+struct Unit {
+  int pa, pb, lo_a, lo_b, n_a, n_b;
+  int pair;  // first pair, or -1: passes through
+};
+
+// SMALL: runs are cut at their ends (element loads); else the last run of a
+// part moves back to end with it and keeps its own tail.
+template <bool INTER, bool SMALL>
+__device__ __forceinline__ Unit unit_of(int u, int pair_units, int D, int R) {
+  Unit k;
+  k.n_a = k.n_b = 8;
+  const int half = R / 2;
+  if (u < pair_units) {
+    int i0 = 8 * u, lo = 0;
+    if (!SMALL && i0 + 8 > half) {
+      lo = i0 + 8 - half;
+      i0 = half - 8;
+    }
+    k.pair = i0;
+    if (INTER) {
+      k.pa = 2 * i0;
+      k.pb = 2 * i0 + 8;
+      k.lo_a = min(2 * lo, 8);
+      k.lo_b = max(2 * lo - 8, 0);
+      if (SMALL) {
+        k.n_a = min(8, R - k.pa);
+        k.n_b = max(0, min(8, R - k.pb));
+      }
+    } else {
+      k.pa = i0;
+      k.pb = i0 + half;
+      k.lo_a = k.lo_b = lo;
+      if (SMALL) k.n_a = k.n_b = min(8, half - i0);
+    }
+  } else {
+    int c = R + 16 * (u - pair_units), lo = 0;
+    if (!SMALL && c + 16 > D) {
+      lo = c + 16 - D;
+      c = D - 16;
+    }
+    k.pair = -1;
+    k.pa = c;
+    k.pb = c + 8;
+    k.lo_a = min(lo, 8);
+    k.lo_b = max(lo - 8, 0);
+    if (SMALL) {
+      k.n_a = max(0, min(8, D - k.pa));
+      k.n_b = max(0, min(8, D - k.pb));
+    }
+  }
+  return k;
+}
+
+// A run of 8 elements; SMALL reads and writes elements [lo, n) one by one.
+template <typename T, bool SMALL>
+struct Run {
+  Raw8<T> raw;
+  float f[SMALL ? 8 : 1];
+  __device__ __forceinline__ void load(const T *p, int n) {
+    if constexpr (SMALL) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = e < n ? to_f32<T>(p[e]) : 0.f;
+    } else {
+      raw.load(p);
+    }
+  }
+  __device__ __forceinline__ void get(float *g) const {
+    if constexpr (SMALL) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) g[e] = f[e];
+    } else {
+      raw.get(g);
+    }
+  }
+  static __device__ __forceinline__ void store(T *p, int lo, int n,
+                                               const float *g) {
+    if constexpr (SMALL) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < n) p[e] = from_f32<T>(g[e]);
+    } else {
+      store8<T>(p, lo, g);
+    }
+  }
+};
+
+template <typename T, bool INTER, bool SMALL>
+__global__ __launch_bounds__(64 * kRotaryWaves) void k_rotary(RotaryParams P) {
+  __shared__ float2 table[kRotaryWaves][256];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t item = (int64_t)blockIdx.x * kRotaryWaves + wave;
+  if (item >= P.items) return;  // no block barrier below
+  const int64_t tok = item / P.splits;
+  const int split = (int)(item - tok * P.splits);
+  const int per_wave = 64 >> P.group_log2;
+  const int sub = lane >> P.group_log2;          // head of a group
+  const int u_raw = lane & ((1 << P.group_log2) - 1);
+  const int u = min(u_raw, P.units - 1);
+  const Unit k = unit_of<INTER, SMALL>(u, P.pair_units, P.D, P.R);
+  const int step = per_wave * P.splits;
+
+  // the token's rotations, times the factor
+  const double pos = (double)P.positions[tok];
+  for (int i = lane; i < P.R / 2; i += 64) {
+    const double turns =
+        pos * (double)P.inv_freq[i] * 0.15915494309189533577;
+    const float r = (float)(turns - rint(turns));
+    float s, c;
+    sincospif(2.f * r, &s, &c);
+    table[wave][i] = make_float2(c * P.factor, s * P.factor * P.sign);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  float c[8], s[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    // (pairs behind a small part's end belong to no element)
+    const int i = k.pair + e;
+    const bool in = k.pair >= 0 && i < P.R / 2;
+    const float2 t = table[wave][in ? i : 0];
+    c[e] = in ? t.x : 1.f;
+    s[e] = in ? t.y : 0.f;
+  }
+
+  for (int h0 = split * per_wave; h0 < P.n_heads; h0 += step * kRotaryBatch) {
+    Run<T, SMALL> ra[kRotaryBatch], rb[kRotaryBatch];
+#pragma unroll
+    for (int b = 0; b < kRotaryBatch; ++b) {
+      const int h = min(h0 + b * step + sub, P.n_heads - 1);
+      const bool is_k = h >= P.n_q;
+      const RotaryHeads &H = is_k ? P.k : P.q;
+      const T *x = static_cast<const T *>(H.x) + tok * H.row +
+                   (int64_t)(is_k ? h - P.n_q : h) * H.head;
+      ra[b].load(x + k.pa, k.n_a);
+      rb[b].load(x + k.pb, k.n_b);
+    }
+#pragma unroll
+    for (int b = 0; b < kRotaryBatch; ++b) {
+      const int hr = h0 + b * step + sub;
+      if (h0 + b * step >= P.n_heads) break;
+      const int h = min(hr, P.n_heads - 1);
+      const bool is_k = h >= P.n_q;
+      const RotaryHeads &H = is_k ? P.k : P.q;
+      float fa[8], fb[8];
+      ra[b].get(fa);
+      rb[b].get(fb);
+      if (P.q.norm_w || P.k.norm_w) {
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float a = e >= k.lo_a && u == u_raw ? fa[e] : 0.f;
+          const float b2 = e >= k.lo_b && u == u_raw ? fb[e] : 0.f;
+          ss = fmaf(a, a, fmaf(b2, b2, ss));
+        }
+        for (int off = (1 << P.group_log2) >> 1; off > 0; off >>= 1)
+          ss += __shfl_xor(ss, off, 64);
+        if (H.norm_w) {
+          const float inv = 1.0f / sqrtf(ss / (float)P.D + P.eps);
+          const T *w = static_cast<const T *>(H.norm_w);
+          Run<T, SMALL> wa, wb;
+          wa.load(w + k.pa, k.n_a);
+          wb.load(w + k.pb, k.n_b);
+          float ga[8], gb[8];
+          wa.get(ga);
+          wb.get(gb);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            fa[e] = fa[e] * inv * ga[e];
+            fb[e] = fb[e] * inv * gb[e];
+          }
+        }
+      }
+      if (k.pair >= 0) {
+        float a[8], b2[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          a[e] = INTER ? (e < 4 ? fa[2 * e] : fb[2 * e - 8]) : fa[e];
+          b2[e] = INTER ? (e < 4 ? fa[2 * e + 1] : fb[2 * e - 7]) : fb[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float x0 = a[e] * c[e] - b2[e] * s[e];
+          const float x1 = b2[e] * c[e] + a[e] * s[e];
+          if (INTER) {
+            (e < 4 ? fa[2 * e] : fb[2 * e - 8]) = x0;
+            (e < 4 ? fa[2 * e + 1] : fb[2 * e - 7]) = x1;
+          } else {
+            fa[e] = x0;
+            fb[e] = x1;
+          }
+        }
+      }
+      if (hr < P.n_heads && u == u_raw) {
+        T *o = static_cast<T *>(H.out) + tok * H.out_row +
+               (int64_t)(is_k ? h - P.n_q : h) * H.out_head;
+        Run<T, SMALL>::store(o + k.pa, k.lo_a, k.n_a, fa);
+        Run<T, SMALL>::store(o + k.pb, k.lo_b, k.n_b, fb);
+      }
+    }
+  }
+}
+
+template <typename T, bool INTER>
+void launch(const RotaryParams &P, bool small, hipStream_t s) {
+  const dim3 grid((unsigned)((P.items + kRotaryWaves - 1) / kRotaryWaves));
+  const dim3 block(64 * kRotaryWaves);
+  if (small)
+    hipLaunchKernelGGL((k_rotary<T, INTER, true>), grid, block, 0, s, P);
+  else
+    hipLaunchKernelGGL((k_rotary<T, INTER, false>), grid, block, 0, s, P);
+}
+
+template <typename T>
+void launch(const RotaryParams &P, bool inter, bool small, hipStream_t s) {
+  if (inter)
+    launch<T, true>(P, small, s);
+  else
+    launch<T, false>(P, small, s);
+}
+
+}  // namespace
+
+hipError_t launch_rotary(const dopr_rotary_args_t &a, hipStream_t s) {
+  RotaryParams P{};
+  P.q = {a.q, a.q_out, a.q_norm_w, a.q_row_stride, a.q_head_stride,
+         a.q_out_row_stride, a.q_out_head_stride};
+  P.k = {a.k, a.k_out, a.k_norm_w, a.k_row_stride, a.k_head_stride,
+         a.k_out_row_stride, a.k_out_head_stride};
+  P.positions = a.positions;
+  P.inv_freq = a.inv_freq;
+  P.n_q = a.n_q_heads;
+  P.n_heads = a.n_q_heads + a.n_kv_heads;
+  P.D = a.head_dim;
+  P.R = a.rotary_dim;
+  P.pair_units = (a.rotary_dim / 2 + 7) / 8;
+  P.units = P.pair_units + (a.head_dim - a.rotary_dim + 15) / 16;
+  while ((1 << P.group_log2) < P.units) ++P.group_log2;
+  P.factor = a.attention_factor;
+  P.sign = a.inverse ? -1.f : 1.f;
+  P.eps = a.rms_eps;
+  const int rest = a.head_dim - a.rotary_dim;
+  const bool small = a.rotary_dim < 16 || (rest > 0 && rest < 16);
+  // few tokens: a token's head groups go to several waves (each forms the
+  // rotations again) until about eight waves a SIMD are there
+  const int groups = (P.n_heads + (64 >> P.group_log2) - 1) /
+                     (64 >> P.group_log2);
+  P.splits = 1;
+  while (P.splits < groups && a.rows * P.splits < 8192) P.splits *= 2;
+  if (P.splits > groups) P.splits = groups;
+  P.items = a.rows * P.splits;
+  if (a.dtype == DOPR_BF16)
+    launch<bf16_t>(P, a.interleaved, small, s);
+  else if (a.dtype == DOPR_F16)
+    launch<_Float16>(P, a.interleaved, small, s);
+  else
+    launch<float>(P, a.interleaved, small, s);
+  return hipGetLastError();
+}
+
+}  // namespace dopr

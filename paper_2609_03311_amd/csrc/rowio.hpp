@@ -1,0 +1,156 @@
+// rowio.hpp -- element types of the row operators (rows.hip, rotary.hip,
+// qproduct.hip): loads and stores of 8 elements at any element alignment, in
+// fp32.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "internal.hpp"
+
+namespace dopr {
+
+struct bf16_t {
+  uint16_t bits;
+};
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2v __attribute__((ext_vector_type(2)));
+// 16 and 8 bytes that may start at any byte: one global load or store each
+// (global memory is accessed in unaligned mode), at full speed where the
+// address happens to be aligned
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x4 u32x4_any __attribute__((aligned(1)));
+typedef u32x2 u32x2_any __attribute__((aligned(1)));
+
+template <typename T>
+__device__ __forceinline__ float to_f32(T v);
+template <>
+__device__ __forceinline__ float to_f32<bf16_t>(bf16_t v) {
+  return __uint_as_float((uint32_t)v.bits << 16);
+}
+template <>
+__device__ __forceinline__ float to_f32<_Float16>(_Float16 v) {
+  return (float)v;
+}
+template <>
+__device__ __forceinline__ float to_f32<float>(float v) {
+  return v;
+}
+
+// rounded to nearest even; NaN stays NaN
+template <typename T>
+__device__ __forceinline__ T from_f32(float f);
+template <>
+__device__ __forceinline__ bf16_t from_f32<bf16_t>(float f) {
+  return bf16_t{__builtin_bit_cast(uint16_t, (__bf16)f)};
+}
+template <>
+__device__ __forceinline__ _Float16 from_f32<_Float16>(float f) {
+  return (_Float16)f;
+}
+template <>
+__device__ __forceinline__ float from_f32<float>(float f) {
+  return f;
+}
+
+template <typename T>
+__device__ __forceinline__ void unpack2(uint32_t u, float &a, float &b);
+template <>
+__device__ __forceinline__ void unpack2<bf16_t>(uint32_t u, float &a,
+                                                float &b) {
+  a = __uint_as_float(u << 16);
+  b = __uint_as_float(u & 0xffff0000u);
+}
+template <>
+__device__ __forceinline__ void unpack2<_Float16>(uint32_t u, float &a,
+                                                  float &b) {
+  const f16x2v h = __builtin_bit_cast(f16x2v, u);
+  a = (float)h.x;
+  b = (float)h.y;
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float a, float b);
+template <>
+__device__ __forceinline__ uint32_t pack2<bf16_t>(float a, float b) {
+  const f32x2 f = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2v));
+}
+template <>
+__device__ __forceinline__ uint32_t pack2<_Float16>(float a, float b) {
+  const f32x2 f = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, f16x2v));
+}
+
+// 8 elements as they lie in memory
+template <typename T>
+struct Raw8 {
+  u32x4 u;
+  __device__ __forceinline__ void load(const T *p) {
+    u = *reinterpret_cast<const u32x4_any *>(p);
+  }
+  __device__ __forceinline__ void get(float *f) const {
+    unpack2<T>(u.x, f[0], f[1]);
+    unpack2<T>(u.y, f[2], f[3]);
+    unpack2<T>(u.z, f[4], f[5]);
+    unpack2<T>(u.w, f[6], f[7]);
+  }
+};
+template <>
+struct Raw8<float> {
+  u32x4 u, v;
+  __device__ __forceinline__ void load(const float *p) {
+    u = *reinterpret_cast<const u32x4_any *>(p);
+    v = *reinterpret_cast<const u32x4_any *>(p + 4);
+  }
+  __device__ __forceinline__ void get(float *f) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[i] = __uint_as_float(u[i]);
+      f[4 + i] = __uint_as_float(v[i]);
+    }
+  }
+};
+
+// The 8 elements of a row of `width` that start at c0, as one load that stays
+// inside the row: chunks behind the end read the row's first elements and
+// keep none, the row's last partial chunk reads the last 8 and keeps those
+// from `lo` on.  `width` is at least 8.
+struct Chunk {
+  int c, lo;
+  __device__ __forceinline__ Chunk(int c0, int width) {
+    const int n = width - c0;
+    c = n >= 8 ? c0 : n > 0 ? width - 8 : 0;
+    lo = n >= 8 ? 0 : n > 0 ? 8 - n : 8;
+  }
+  __device__ __forceinline__ void mask(float *f) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = e >= lo ? f[e] : 0.f;
+  }
+};
+
+// Elements lo..7 of f to p[lo..7].
+template <typename T>
+__device__ __forceinline__ void store8(T *p, int lo, const float *f) {
+  if (lo == 0) {
+    if constexpr (sizeof(T) == 2) {
+      const u32x4 u = {pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]),
+                       pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7])};
+      *reinterpret_cast<u32x4_any *>(p) = u;
+    } else {
+      const u32x4 u = {__float_as_uint(f[0]), __float_as_uint(f[1]),
+                       __float_as_uint(f[2]), __float_as_uint(f[3])};
+      const u32x4 v = {__float_as_uint(f[4]), __float_as_uint(f[5]),
+                       __float_as_uint(f[6]), __float_as_uint(f[7])};
+      *reinterpret_cast<u32x4_any *>(p) = u;
+      *reinterpret_cast<u32x4_any *>(p + 4) = v;
+    }
+  } else if (lo < 8) {
+#pragma unroll
+    for (int e = 1; e < 8; ++e)
+      if (e >= lo) p[e] = from_f32<T>(f[e]);
+  }
+}
+
+}  // namespace dopr
