@@ -187,8 +187,220 @@ __global__ __launch_bounds__(256) void k_product_any(ProductParams P,
   }
 }
 
+// ---------------------------------------------------------------------------
+// Rows on 16-byte addresses: WGM x WGN waves of 16 FM x 64, the depth in steps
+// of 64 bytes that go straight from memory to LDS, kStages steps deep.
+//
+// Step t's operands are read from LDS to registers during step t - 1's
+// products, so at a barrier every wave is done with the LDS buffer of the
+// step it starts to multiply, and the loads of step t + kStages go there: a
+// load has kStages - 1 steps to arrive.
+
+constexpr int kStep = 64;
+constexpr int kStages = 4;
+constexpr int kGroupM = 8;  // tile rows that share w tiles while in L2
+
+// 64 lanes' 16 bytes each from base + off to LDS, in lane order from m0 on.
+// (The compiler does not know of the LDS write: stage_wait orders it.)
+__device__ __forceinline__ void dma16(uint32_t lds, const void *base,
+                                      uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\t"
+               "global_load_lds_dwordx4 %1, %2"
+               :: "s"(lds), "v"(off), "s"(base)
+               : "m0");
+}
+
+// At most `left` of this wave's loads are on their way, its LDS reads have
+// returned, and every wave is here.
+template <int left>
+__device__ __forceinline__ void stage_wait() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(left)
+               : "memory");
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3)))
+                                   void *)p;
+}
+
+// Tile of block b: the blocks of one XCD (b % 8) take consecutive tiles, in
+// groups of kGroupM tile rows, so the 32 that run together cover 8 x 4 tiles.
+__device__ __forceinline__ void tile_of(int64_t b, int64_t tm, int64_t tn,
+                                        int64_t &m, int64_t &n) {
+  const int64_t all = tm * tn, per = all / 8, rem = all % 8, xcd = b % 8;
+  const int64_t t = xcd * per + (xcd < rem ? xcd : rem) + b / 8;
+  const int64_t g = t / (kGroupM * tn);
+  const int64_t rows = min((int64_t)kGroupM, tm - g * kGroupM);
+  const int64_t in = t - g * kGroupM * tn;
+  m = g * kGroupM + in % rows;
+  n = in / rows;
+}
+
+template <typename T, int FM, int WGM, int WGN>
+__global__ __launch_bounds__(64 * WGM * WGN, 2) void k_product(
+    ProductParams P, int64_t tm, int64_t tn) {
+  constexpr int kBM = 16 * FM * WGM, kBN = 64 * WGN;
+  // a wave's loads of a step: 16 rows of 64 bytes each
+  constexpr int kXLoads = FM / WGN, kWLoads = 4 / WGM;
+  constexpr int kLoads = kXLoads + kWLoads;
+  static_assert(kXLoads * WGN == FM && kWLoads * WGM == 4, "even shares");
+  constexpr int kStageBytes = (kBM + kBN) * kStep;
+  extern __shared__ u32x4 lds[];  // [kStages][x rows | w rows]
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int64_t bm, bn;
+  tile_of(blockIdx.x, tm, tn, bm, bn);
+  const int64_t m0 = bm * kBM, n0 = bn * kBN;
+  // rows behind the end repeat the last one; their results are not stored
+  const int last_m = (int)min(P.M - 1 - m0, (int64_t)kBM - 1);
+  const int last_n = (int)min(P.N - 1 - n0, (int64_t)kBN - 1);
+  const int8_t *xbase = P.x + m0 * P.ldx, *wbase = P.w + n0 * P.ldw;
+  const int full = (int)(P.K / kStep);
+
+  // LDS row r of a part holds its 16-byte chunk c at slot any_slot(r, c); the
+  // lanes of a load fill 64 slots in order
+  auto x_row = [&](int i) { return (wave * kXLoads + i) * 16 + (lane >> 2); };
+  auto w_lds_row = [&](int i) {
+    return (wave * kWLoads + i) * 16 + (lane >> 2);
+  };
+  const int chunk = ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
+  uint32_t xoff[kXLoads], woff[kWLoads];
+#pragma unroll
+  for (int i = 0; i < kXLoads; ++i)
+    xoff[i] = (uint32_t)min(x_row(i), last_m) * (uint32_t)P.ldx + chunk;
+#pragma unroll
+  for (int i = 0; i < kWLoads; ++i)
+    woff[i] =
+        (uint32_t)min(w_row(w_lds_row(i)), last_n) * (uint32_t)P.ldw + chunk;
+  const uint32_t xdst = lds_address(lds) + wave * kXLoads * 1024;
+  const uint32_t wdst =
+      lds_address(lds) + kBM * kStep + wave * kWLoads * 1024;
+  auto issue = [&](int s) {
+    const uint32_t b = (s % kStages) * kStageBytes;
+#pragma unroll
+    for (int i = 0; i < kXLoads; ++i)
+      dma16(xdst + b + i * 1024, xbase + (int64_t)s * kStep, xoff[i]);
+#pragma unroll
+    for (int i = 0; i < kWLoads; ++i)
+      dma16(wdst + b + i * 1024, wbase + (int64_t)s * kStep, woff[i]);
+  };
+
+  const int wm = (wave / WGN) * (16 * FM), wn = (wave % WGN) * 64;
+  const int slot = any_slot(lane & 15, lane >> 4);
+  const int xslot = wm * 4 + slot, wslot = (kBM + wn) * 4 + slot;
+  i32x4 acc[FM][4] = {};
+  auto read = [&](int s, i32x4 *x, i32x4 *w) {
+    const u32x4 *p = lds + (s % kStages) * (kStageBytes / 16);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      w[j] = __builtin_bit_cast(i32x4, p[wslot + j * 64]);
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+      x[i] = __builtin_bit_cast(i32x4, p[xslot + i * 64]);
+  };
+  auto multiply = [&](const i32x4 *x, const i32x4 *w) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[j], x[i],
+                                                          acc[i][j], 0, 0, 0);
+  };
+
+#pragma unroll 1
+  for (int s = 0; s < kStages - 1 && s < full; ++s) issue(s);
+  i32x4 xa[FM], wa[4], xb[FM], wb[4];
+  if (P.K % kStep) {
+    // the partial step comes first, through the last buffer, while the first
+    // loads are on their way: zeros from the depth on
+    u32x4 *p = lds + (kStages - 1) * (kStageBytes / 16) + lane;
+    const int64_t k = (int64_t)full * kStep + chunk;
+#pragma unroll 1
+    for (int i = 0; i < kXLoads; ++i)
+      p[(wave * kXLoads + i) * 64] = row_bytes(
+          xbase + (int64_t)min(x_row(i), last_m) * P.ldx, k, P.K);
+#pragma unroll 1
+    for (int i = 0; i < kWLoads; ++i)
+      p[kBM * 4 + (wave * kWLoads + i) * 64] =
+          row_bytes(wbase + (int64_t)min(w_row(w_lds_row(i)), last_n) * P.ldw,
+                    k, P.K);
+    __syncthreads();
+    read(kStages - 1, xa, wa);
+    multiply(xa, wa);
+    __syncthreads();
+  }
+  if (full > 0) {
+    if (full >= kStages) issue(kStages - 1);
+    stage_wait<0>();
+    read(0, xa, wa);
+    // products of step s, held in (x, w), while step s + 1 is read into
+    // (y, v); behind the last step that is a stale buffer, never used
+    int s = 0;
+    auto step = [&](const i32x4 *x, const i32x4 *w, i32x4 *y, i32x4 *v) {
+      stage_wait<(kStages - 2) * kLoads>();
+      issue(s + kStages);
+      read(s + 1, y, v);
+      multiply(x, w);
+      ++s;
+    };
+    while (s + kStages + 1 < full) {
+      step(xa, wa, xb, wb);
+      step(xb, wb, xa, wa);
+    }
+#pragma unroll 1
+    for (; s < full; ++s) {
+      stage_wait<0>();
+      if (s + kStages < full) issue(s + kStages);
+      read(s + 1, xb, wb);
+      multiply(xa, wa);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) xa[i] = xb[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) wa[j] = wb[j];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    float v[16];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * j + e] = (float)acc[i][j][e];
+    store16<T>(P, m0 + wm + 16 * i + (lane & 15), n0 + wn + 16 * (lane >> 4),
+               v);
+  }
+}
+
+template <typename T, int FM, int WGM, int WGN>
+hipError_t product_tiles(const ProductParams &P, hipStream_t s) {
+  constexpr int kBM = 16 * FM * WGM, kBN = 64 * WGN;
+  const int64_t tm = (P.M + kBM - 1) / kBM, tn = (P.N + kBN - 1) / kBN;
+  const size_t lds = (size_t)kStages * (kBM + kBN) * kStep;
+  const auto kernel = &k_product<T, FM, WGM, WGN>;
+  // (the runtime's own limit is 64 KB until a kernel asks for more)
+  static const hipError_t allowed = hipFuncSetAttribute(
+      reinterpret_cast<const void *>(kernel),
+      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (allowed != hipSuccess) return allowed;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(tm * tn)),
+                     dim3(64 * WGM * WGN), lds, s, P, tm, tn);
+  return hipGetLastError();
+}
+
+// x, w and their strides on 16 bytes, and a tile's rows within 32-bit offsets
+bool aligned_rows(const ProductParams &P) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(P.x) |
+                      reinterpret_cast<uintptr_t>(P.w) | (uintptr_t)P.ldx |
+                      (uintptr_t)P.ldw;
+  return a % 16 == 0 && P.ldx < (1 << 22) && P.ldw < (1 << 22);
+}
+
 template <typename T>
 hipError_t product(const ProductParams &P, hipStream_t s) {
+  if (aligned_rows(P)) {
+    if (P.M > 512) return product_tiles<T, 8, 2, 4>(P, s);
+    return product_tiles<T, 4, 2, 2>(P, s);
+  }
   const int64_t tm = (P.M + kAnyTile - 1) / kAnyTile,
                 tn = (P.N + kAnyTile - 1) / kAnyTile;
   hipLaunchKernelGGL((k_product_any<T>), dim3((unsigned)(tm * tn)), dim3(256),
