@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -243,9 +244,13 @@ def _ptr(t) -> Optional[int]:
 
 
 def _stream(stream) -> Optional[int]:
+    """Handle of `stream`, or of the current device's current stream."""
     if stream is None:
         import torch
-        stream = torch.cuda.current_stream()
+        try:  # the handle alone: no Stream object is made for it
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        except AttributeError:
+            stream = torch.cuda.current_stream()
     return stream.cuda_stream
 
 
@@ -604,43 +609,64 @@ def _dtype_code(t, what: str) -> int:
     return code
 
 
-def _expect(t, what: str, shape, dtype):
-    """t has this shape and type, on a GPU, its last dimension contiguous."""
-    if t.dtype != dtype or t.shape != shape or not t.is_cuda or (
-            shape[-1] > 1 and t.stride(-1) != 1):
-        raise ValueError(
-            f"{what} must be a {dtype} GPU tensor of shape {tuple(shape)} "
-            f"with unit last stride, not {t.dtype} {tuple(t.shape)}, strides "
-            f"{t.stride()}, on {t.device}")
+def _packer(struct_type):
+    """bytes(fields...) in the layout of a ctypes structure.  These calls are
+    a few microseconds of GPU work at their smallest, and packing is a quarter
+    of what filling a Structure costs."""
+    codes = {ctypes.c_int32: "i", ctypes.c_int64: "q", ctypes.c_void_p: "P",
+             ctypes.c_float: "f", ctypes.c_size_t: "N"}
+    fmt = "@" + "".join(codes[c] for _, c in struct_type._fields_)
+    return struct.Struct(fmt).pack
 
 
-def _row_stride(t) -> int:
-    """Elements between rows; a single row has no stride to speak of."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+_pack_quantize = _packer(_QuantizeArgs)
+_pack_product = _packer(_QuantMatmulArgs)
+_pack_norm = _packer(_NormResidualArgs)
+_pack_rotary = _packer(_RotaryArgs)
 
 
-def _optional_row(t, what, shape, dtype):
-    """(pointer, row stride) of an optional [rows, width] operand."""
+def _refuse(t, what, shape, dtype):
+    raise ValueError(
+        f"{what} must be a {dtype} GPU tensor of shape {tuple(shape)} with "
+        f"unit last stride, not {t.dtype} {tuple(t.shape)}, strides "
+        f"{t.stride()}, on {t.device}")
+
+
+def _vector(t, what, n, dtype) -> int:
+    """Address of a contiguous [n] vector of this type (0 for None)."""
     if t is None:
-        return None, 0
-    _expect(t, what, shape, dtype)
-    return t.data_ptr(), _row_stride(t)
+        return 0
+    if (t.dtype is not dtype or t.shape != (n,) or not t.is_cuda or
+            (n > 1 and t.stride(0) != 1)):
+        _refuse(t, what, (n,), dtype)
+    return t.data_ptr()
+
+
+def _matrix(t, what, shape, dtype):
+    """(address, row stride) of a matrix with unit column stride ((0, 0) for
+    None); a single row has no stride to speak of."""
+    if t is None:
+        return 0, 0
+    s = t.stride()
+    if (t.dtype is not dtype or t.shape != shape or not t.is_cuda or
+            (s[1] != 1 and shape[1] > 1)):
+        _refuse(t, what, shape, dtype)
+    return t.data_ptr(), s[0] if shape[0] > 1 else max(s[0], shape[1])
 
 
 def dopr_quantize_rows(x, q, scale, *, up=None, stream=None):
     """Rows of x [rows, width] (or SiLU(x) * up) in 8-bit integers: q int8
     [rows, width], scale fp32 [rows]."""
     import torch
-    shape = x.shape
-    code = _dtype_code(x, "x")
-    _expect(x, "x", shape, x.dtype)
-    _expect(q, "q", shape, torch.int8)
-    _expect(scale, "scale", shape[:1], torch.float32)
-    up_p, up_s = _optional_row(up, "up", shape, x.dtype)
-    a = _QuantizeArgs(code, shape[0], shape[1], x.data_ptr(), _row_stride(x),
-                      up_p, up_s, q.data_ptr(), _row_stride(q),
-                      scale.data_ptr())
-    _check(lib().dopr_quantize_rows(ctypes.byref(a), _stream(stream)))
+    shape, dt = x.shape, x.dtype
+    rows, width = shape
+    _check(lib().dopr_quantize_rows(
+        _pack_quantize(_dtype_code(x, "x"), rows, width,
+                       *_matrix(x, "x", shape, dt),
+                       *_matrix(up, "up", shape, dt),
+                       *_matrix(q, "q", shape, torch.int8),
+                       _vector(scale, "scale", rows, torch.float32)),
+        _stream(stream)))
 
 
 def dopr_quant_matmul_workspace(rows: int, cols: int, depth: int) -> int:
@@ -661,23 +687,19 @@ def dopr_quant_matmul(x, x_scale, w, w_scale, y, *, bias=None, residual=None,
     import torch
     m, k = x.shape
     n = w.shape[0]
-    code = _dtype_code(y, "y")
-    _expect(x, "x", (m, k), torch.int8)
-    _expect(w, "w", (n, k), torch.int8)
-    _expect(y, "y", (m, n), y.dtype)
-    _expect(x_scale, "x_scale", (m,), torch.float32)
-    _expect(w_scale, "w_scale", (n,), torch.float32)
-    if bias is not None:
-        _expect(bias, "bias", (n,), y.dtype)
-    res_p, res_s = _optional_row(residual, "residual", (m, n), y.dtype)
-    ws_bytes = 0 if workspace is None else (
-        workspace.numel() * workspace.element_size())
-    a = _QuantMatmulArgs(code, m, n, k, x.data_ptr(), _row_stride(x),
-                         x_scale.data_ptr(), w.data_ptr(), _row_stride(w),
-                         w_scale.data_ptr(), _ptr(bias), res_p, res_s,
-                         y.data_ptr(), _row_stride(y), _ptr(workspace),
-                         ws_bytes)
-    _check(lib().dopr_quant_matmul(ctypes.byref(a), _stream(stream)))
+    dt, i8, f32 = y.dtype, torch.int8, torch.float32
+    _check(lib().dopr_quant_matmul(
+        _pack_product(_dtype_code(y, "y"), m, n, k,
+                      *_matrix(x, "x", (m, k), i8),
+                      _vector(x_scale, "x_scale", m, f32),
+                      *_matrix(w, "w", (n, k), i8),
+                      _vector(w_scale, "w_scale", n, f32),
+                      _vector(bias, "bias", n, dt),
+                      *_matrix(residual, "residual", (m, n), dt),
+                      *_matrix(y, "y", (m, n), dt),
+                      0 if workspace is None else workspace.data_ptr(),
+                      0 if workspace is None else workspace.nbytes),
+        _stream(stream)))
 
 
 def dopr_norm_residual(x, *, residual=None, post_norm_w=None, gate=None,
@@ -688,34 +710,42 @@ def dopr_norm_residual(x, *, residual=None, post_norm_w=None, gate=None,
     width], q_scale fp32 [rows]).  gate is [width] or [rows, width]; residual
     and h share one type, x's or fp32."""
     import torch
-    shape = x.shape
+    shape, dt = x.shape, x.dtype
+    rows, width = shape
     code = _dtype_code(x, "x")
-    _expect(x, "x", shape, x.dtype)
-    for t, what in ((post_norm_w, "post_norm_w"), (pre_norm_w, "pre_norm_w")):
-        if t is not None:
-            _expect(t, what, shape[1:], x.dtype)
-    gate_p = gate_s = 0
-    if gate is not None and gate.dim() == 1:
-        _expect(gate, "gate", shape[1:], x.dtype)
-        gate_p = gate.data_ptr()
-    elif gate is not None:
-        gate_p, gate_s = _optional_row(gate, "gate", shape, x.dtype)
     # residual and h: x's type, or fp32 kept wider than it
     rt = (residual if residual is not None else x if h is None else h).dtype
-    if rt != x.dtype and rt != torch.float32:
-        raise ValueError(f"residual and h must be {x.dtype} or float32")
-    res_p, res_s = _optional_row(residual, "residual", shape, rt)
-    h_p, h_s = _optional_row(h, "h", shape, rt)
-    z_p, z_s = _optional_row(z, "z", shape, x.dtype)
-    q_p, q_s = _optional_row(q, "q", shape, torch.int8)
-    if q_scale is not None:
-        _expect(q_scale, "q_scale", shape[:1], torch.float32)
-    a = _NormResidualArgs(code, _dtypes[rt], shape[0], shape[1], x.data_ptr(),
-                          _row_stride(x), _ptr(post_norm_w), gate_p, gate_s,
-                          res_p, res_s, _ptr(pre_norm_w),
-                          float(residual_scale), float(rms_eps), h_p, h_s,
-                          z_p, z_s, q_p, q_s, _ptr(q_scale))
-    _check(lib().dopr_norm_residual(ctypes.byref(a), _stream(stream)))
+    if rt is not dt and rt is not torch.float32:
+        raise ValueError(f"residual and h must be {dt} or float32")
+    _check(lib().dopr_norm_residual(
+        _pack_norm(code, _dtypes[rt], rows, width,
+                   *_matrix(x, "x", shape, dt),
+                   _vector(post_norm_w, "post_norm_w", width, dt),
+                   *((_vector(gate, "gate", width, dt), 0)
+                     if gate is not None and gate.dim() == 1 else
+                     _matrix(gate, "gate", shape, dt)),
+                   *_matrix(residual, "residual", shape, rt),
+                   _vector(pre_norm_w, "pre_norm_w", width, dt),
+                   residual_scale, rms_eps, *_matrix(h, "h", shape, rt),
+                   *_matrix(z, "z", shape, dt),
+                   *_matrix(q, "q", shape, torch.int8),
+                   _vector(q_scale, "q_scale", rows, torch.float32)),
+        _stream(stream)))
+
+
+def _heads(x, out, name, rows, d, dt):
+    """Both tensors' addresses and strides for [rows, heads, d]."""
+    if x is None:
+        return 0, 0, 0, 0, 0, 0
+    shape = (rows, x.shape[1], d)
+    parts = ()
+    for t, what in ((x, name), (out, name + "_out")):
+        s = t.stride()
+        if (t.dtype is not dt or t.shape != shape or not t.is_cuda or
+                (s[2] != 1 and d > 1)):
+            _refuse(t, what, shape, dt)
+        parts += (t.data_ptr(), s[0], s[1])
+    return parts
 
 
 def dopr_rotary(q, k, positions, inv_freq, q_out, k_out, *, interleaved=False,
@@ -731,28 +761,19 @@ def dopr_rotary(q, k, positions, inv_freq, q_out, k_out, *, interleaved=False,
         raise ValueError("q and k are both None")
     rows, _, d = first.shape
     dt = first.dtype
-    code = _dtype_code(first, "q")
-    parts = []
-    for x, out, name in ((q, q_out, "q"), (k, k_out, "k")):
-        if x is None:
-            parts.append((0, None, 0, 0, None, 0, 0))
-            continue
-        shape = (rows, x.shape[1], d)
-        _expect(x, name, shape, dt)
-        _expect(out, name + "_out", shape, dt)
-        parts.append((shape[1], x.data_ptr(), x.stride(0), x.stride(1),
-                      out.data_ptr(), out.stride(0), out.stride(1)))
-    _expect(positions, "positions", (rows,), torch.int32)
-    _expect(inv_freq, "inv_freq", inv_freq.shape, torch.float32)
-    for t, what in ((q_norm_w, "q_norm_w"), (k_norm_w, "k_norm_w")):
-        if t is not None:
-            _expect(t, what, (d,), dt)
-    a = _RotaryArgs(code, parts[0][0], parts[1][0], d, 2 * inv_freq.numel(),
-                    int(interleaved), int(inverse), float(attention_factor),
-                    float(rms_eps), rows, positions.data_ptr(),
-                    inv_freq.data_ptr(), *parts[0][1:], *parts[1][1:],
-                    _ptr(q_norm_w), _ptr(k_norm_w))
-    _check(lib().dopr_rotary(ctypes.byref(a), _stream(stream)))
+    half = inv_freq.numel()
+    _check(lib().dopr_rotary(
+        _pack_rotary(_dtype_code(first, "q"), 0 if q is None else q.shape[1],
+                     0 if k is None else k.shape[1], d, 2 * half,
+                     bool(interleaved), bool(inverse), attention_factor,
+                     rms_eps, rows,
+                     _vector(positions, "positions", rows, torch.int32),
+                     _vector(inv_freq, "inv_freq", half, torch.float32),
+                     *_heads(q, q_out, "q", rows, d, dt),
+                     *_heads(k, k_out, "k", rows, d, dt),
+                     _vector(q_norm_w, "q_norm_w", d, dt),
+                     _vector(k_norm_w, "k_norm_w", d, dt)),
+        _stream(stream)))
 
 
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3, "bands": 4}

@@ -82,23 +82,40 @@ __device__ __forceinline__ void store16(const ProductParams &P, int64_t m,
   }
 }
 
+// 16 bytes of a row from depth k, zeros from K on.  Nothing behind the row is
+// read: the row's last 16 bytes, shifted down.
+__device__ __forceinline__ u32x4 row_bytes(const int8_t *p, int64_t k,
+                                           int64_t K) {
+  if (K < 16) {  // (k = 0 or past the end)
+    u32x4 u = {0u, 0u, 0u, 0u};
+#pragma unroll 1
+    for (int e = (int)(K - k) - 1; e >= 0; --e) {
+      u.w = u.w << 8 | u.z >> 24;
+      u.z = u.z << 8 | u.y >> 24;
+      u.y = u.y << 8 | u.x >> 24;
+      u.x = u.x << 8 | (uint8_t)p[k + e];
+    }
+    return u;
+  }
+  const int64_t at = min(k, K - 16);
+  u32x4 u = *reinterpret_cast<const u32x4_any *>(p + at);
+  const uint32_t s = (uint32_t)min(k - at, (int64_t)16);
+  if (s & 16) u = u32x4{0u, 0u, 0u, 0u};
+  if (s & 8) u = u32x4{u.z, u.w, 0u, 0u};
+  if (s & 4) u = u32x4{u.y, u.z, u.w, 0u};
+  const uint32_t b = s & 3;
+  return u32x4{__builtin_amdgcn_alignbyte(u.y, u.x, b),
+               __builtin_amdgcn_alignbyte(u.z, u.y, b),
+               __builtin_amdgcn_alignbyte(u.w, u.z, b),
+               __builtin_amdgcn_alignbyte(0u, u.w, b)};
+}
+
 // ---------------------------------------------------------------------------
 // Any strides and alignment: 128 x 128 tiles, 4 waves of 64 x 64, depth in
 // steps of 64 bytes through registers into two LDS buffers.
 
 constexpr int kAnyTile = 128;
 constexpr int kAnyStep = 64;
-
-// 16 bytes of a row from depth k, zeros from K on
-__device__ __forceinline__ u32x4 row_bytes(const int8_t *p, int64_t k,
-                                           int64_t K) {
-  if (k + 16 <= K) return *reinterpret_cast<const u32x4_any *>(p + k);
-  u32x4 u = {0u, 0u, 0u, 0u};
-#pragma unroll
-  for (int e = 0; e < 16; ++e)
-    if (k + e < K) u[e >> 2] |= (uint32_t)(uint8_t)p[k + e] << (8 * (e & 3));
-  return u;
-}
 
 // LDS address (16-byte units) of chunk c of 64-byte row r: 16 rows' equal
 // chunks fall on all 64 banks
@@ -387,6 +404,145 @@ hipError_t product_tiles(const ProductParams &P, hipStream_t s) {
   return hipGetLastError();
 }
 
+// ---------------------------------------------------------------------------
+// Few rows: a block's WK waves share one strip of 16 FN w rows and split the
+// depth, in batches of U steps of 64 bytes, each wave's operands coming
+// straight from memory to its registers, one batch ahead of the products.
+// The waves' sums meet in LDS (integers: the split does not show).
+
+// 4 results of y row m from column n on.
+template <typename T>
+__device__ __forceinline__ void store4(const ProductParams &P, int64_t m,
+                                       int64_t n, const i32x4 &acc) {
+  if (m >= P.M || n >= P.N) return;
+  const float xs = P.x_scale[m];
+  const T *bias = static_cast<const T *>(P.bias);
+  const T *res = static_cast<const T *>(P.res) + m * P.ldr;
+  T *y = static_cast<T *>(P.y) + m * P.ldy;
+  const int left = (int)min(P.N - n, (int64_t)4);
+  float v[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int64_t c = n + min(e, left - 1);
+    v[e] = (float)acc[e] * xs * P.w_scale[c];
+    if (P.bias) v[e] += to_f32<T>(bias[c]);
+    if (P.res) v[e] += to_f32<T>(res[c]);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (e < left) y[n + e] = from_f32<T>(v[e]);
+}
+
+template <typename T, int FM, int FN, int U, int WK>
+__global__ __launch_bounds__(64 * WK) void k_product_few(ProductParams P) {
+  __shared__ i32x4 sums[WK][FM * FN][64];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t n0 = (int64_t)blockIdx.x * (16 * FN);
+  const int64_t m0 = (int64_t)blockIdx.y * (16 * FM);
+  const int kc = (lane >> 4) * 16;
+  // rows behind the end repeat the last one; their results are not stored
+  const int8_t *xp[FM], *wp[FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+    xp[i] = P.x + min(m0 + 16 * i + (lane & 15), P.M - 1) * P.ldx + kc;
+#pragma unroll
+  for (int j = 0; j < FN; ++j)
+    wp[j] = P.w + min(n0 + 16 * j + (lane & 15), P.N - 1) * P.ldw + kc;
+  constexpr int kBatch = U * kStep;
+  i32x4 acc[FM][FN] = {};
+  struct Batch {
+    u32x4 x[U][FM], w[U][FN];
+  };
+  auto fetch = [&](int64_t batch, Batch &b) {
+    const int64_t k = batch * kBatch;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+        b.w[u][j] =
+            *reinterpret_cast<const u32x4_any *>(wp[j] + k + u * kStep);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+        b.x[u][i] =
+            *reinterpret_cast<const u32x4_any *>(xp[i] + k + u * kStep);
+    }
+  };
+  auto product1 = [&](const u32x4 *x, const u32x4 *w) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+            __builtin_bit_cast(i32x4, w[j]), __builtin_bit_cast(i32x4, x[i]),
+            acc[i][j], 0, 0, 0);
+  };
+  auto multiply = [&](const Batch &b) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) product1(b.x[u], b.w[u]);
+  };
+  const int batches = (int)(P.K / kBatch);
+  Batch a, b;
+  if (wave < batches) fetch(wave, a);
+  for (int i = wave; i < batches; i += 2 * WK) {
+    if (i + WK < batches) fetch(i + WK, b);
+    multiply(a);
+    if (i + WK >= batches) break;
+    if (i + 2 * WK < batches) fetch(i + 2 * WK, a);
+    multiply(b);
+  }
+  // steps behind the last whole batch, one at a time, first to the waves that
+  // had a batch less
+  const int first = batches * U;
+#pragma unroll 1
+  for (int s = first + (wave + WK - batches % WK) % WK;
+       (int64_t)s * kStep < P.K; s += WK) {
+    u32x4 x[FM], w[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+      w[j] = row_bytes(wp[j] - kc, (int64_t)s * kStep + kc, P.K);
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+      x[i] = row_bytes(xp[i] - kc, (int64_t)s * kStep + kc, P.K);
+    product1(x, w);
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) sums[wave][i * FN + j][lane] = acc[i][j];
+  __syncthreads();
+  for (int f = wave; f < FM * FN; f += WK) {
+    i32x4 s = sums[0][f][lane];
+#pragma unroll
+    for (int w = 1; w < WK; ++w) s += sums[w][f][lane];
+    store4<T>(P, m0 + 16 * (f / FN) + (lane & 15),
+              n0 + 16 * (f % FN) + 4 * (lane >> 4), s);
+  }
+}
+
+template <typename T, int FM, int FN, int U, int WK>
+hipError_t product_few(const ProductParams &P, hipStream_t s) {
+  const unsigned strips = (unsigned)((P.N + 16 * FN - 1) / (16 * FN));
+  const unsigned rows = (unsigned)((P.M + 16 * FM - 1) / (16 * FM));
+  hipLaunchKernelGGL((k_product_few<T, FM, FN, U, WK>), dim3(strips, rows),
+                     dim3(64 * WK), 0, s, P);
+  return hipGetLastError();
+}
+
+// Depth split over 4, 8 or 16 waves: until some 16 waves a CU have work, as
+// long as a wave keeps a batch.
+template <typename T, int FM, int FN, int U>
+hipError_t product_few(const ProductParams &P, hipStream_t s) {
+  const int64_t strips = (P.N + 16 * FN - 1) / (16 * FN);
+  const int64_t batches = P.K / (U * kStep);
+  if constexpr (FM < 4)  // (four x operands of 16 waves would spill)
+    if (strips * 8 < 4096 && batches > 8)
+      return product_few<T, FM, FN, U, 16>(P, s);
+  if (strips * 4 < 4096 && batches > 4)
+    return product_few<T, FM, FN, U, 8>(P, s);
+  return product_few<T, FM, FN, U, 4>(P, s);
+}
+
 // x, w and their strides on 16 bytes, and a tile's rows within 32-bit offsets
 bool aligned_rows(const ProductParams &P) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(P.x) |
@@ -397,6 +553,9 @@ bool aligned_rows(const ProductParams &P) {
 
 template <typename T>
 hipError_t product(const ProductParams &P, hipStream_t s) {
+  if (P.M <= 16) return product_few<T, 1, 1, 4>(P, s);
+  if (P.M <= 32) return product_few<T, 2, 1, 4>(P, s);
+  if (P.M <= 64) return product_few<T, 4, 2, 2>(P, s);
   if (aligned_rows(P)) {
     if (P.M > 512) return product_tiles<T, 8, 2, 4>(P, s);
     return product_tiles<T, 4, 2, 2>(P, s);
