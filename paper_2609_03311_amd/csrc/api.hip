@@ -990,6 +990,9 @@ dopr_status_t check_product(const dopr_quant_matmul_args_t *a) {
                 "depth over 131071 may exceed 32-bit sums");
   if (((a->rows + 15) / 16) * ((a->cols + 15) / 16) > INT32_MAX)
     return fail(DOPR_ERR_UNSUPPORTED, "more than 2^31 16 x 16 output blocks");
+  // (row and column numbers of a tile that reaches past the end stay int)
+  if (a->rows > INT32_MAX - 1024 || a->cols > INT32_MAX - 1024)
+    return fail(DOPR_ERR_UNSUPPORTED, "rows and cols must be < 2^31 - 1024");
   return DOPR_OK;
 }
 

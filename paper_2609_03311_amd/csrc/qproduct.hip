@@ -28,78 +28,107 @@ struct ProductParams {
   const void *bias, *res;
   void *y;
   int64_t M, N, K, ldx, ldw, ldr, ldy;
+  int32_t *parts;  // [splits][M][parts_row(N)] sums of a split depth
+  int32_t splits;  // 1: y is written at once
 };
+
+// Elements between rows of the sums: stores of 16 need no bound.
+__host__ __device__ inline int64_t parts_row(int64_t N) {
+  return (N + 15) & ~(int64_t)15;
+}
 
 // w row (of 64) behind LDS row p
 __device__ __forceinline__ int w_row(int p) {
   return (p & ~63) + ((p & 15) >> 2) * 16 + ((p >> 4) & 3) * 4 + (p & 3);
 }
 
-// 16 results of y row m from column n on: scales, bias, residual, store.
+// Finishes 16 consecutive columns of y, row by row: the columns' scales are
+// read once and the rows' addresses stepped from one to the next.
 template <typename T>
-__device__ __forceinline__ void store16(const ProductParams &P, int64_t m,
-                                        int64_t n, const float *acc) {
-  if (m >= P.M || n >= P.N) return;
-  const float xs = P.x_scale[m];
-  const T *bias = static_cast<const T *>(P.bias);
-  const T *res = static_cast<const T *>(P.res) + m * P.ldr;
-  T *y = static_cast<T *>(P.y) + m * P.ldy;
-  float v[16];
-  if (n + 16 <= P.N) {
+struct Columns {
+  float scale[16];
+  const T *bias, *res;
+  T *y;
+  const float *x_scale;
+  int m, left;  // row, columns to the end of the row
+  __device__ __forceinline__ Columns(const ProductParams &P, int m0, int n)
+      : m(m0), left((int)P.N - n) {
+    const float *s = P.w_scale + n;
+    if (left >= 16) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        Raw8<float> r;
+        r.load(s + 8 * h);
+        r.get(scale + 8 * h);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) scale[e] = s[min(e, left - 1)];
+    }
+    bias = static_cast<const T *>(P.bias) + n;
+    res = static_cast<const T *>(P.res) + m * P.ldr + n;
+    y = static_cast<T *>(P.y) + m * P.ldy + n;
+    x_scale = P.x_scale + m;
+  }
+  // `rows` rows further down
+  __device__ __forceinline__ void next(const ProductParams &P, int rows) {
+    m += rows;
+    x_scale += rows;
+    y += rows * P.ldy;
+    if (P.res) res += rows * P.ldr;
+  }
+  // v: the row's integer sums
+  __device__ __forceinline__ void store(const ProductParams &P, float *v) const {
+    if (m >= (int)P.M) return;
+    const float xs = *x_scale;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = v[e] * xs * scale[e];
+    if (left >= 16) {
+      if (P.bias) add16(bias, v);
+      if (P.res) add16(res, v);
+      store8<T>(y, 0, v);
+      store8<T>(y + 8, 0, v + 8);
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < 15; ++e)
+      if (e < left) {
+        if (P.bias) v[e] += to_f32<T>(bias[e]);
+        if (P.res) v[e] += to_f32<T>(res[e]);
+        y[e] = from_f32<T>(v[e]);
+      }
+  }
+  static __device__ __forceinline__ void add16(const T *p, float *v) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      float s[8], b[8];
-      Raw8<float> rs;
-      Raw8<T> rb;
-      rs.load(P.w_scale + n + 8 * h);
-      rs.get(s);
+      float b[8];
+      Raw8<T> r;
+      r.load(p + 8 * h);
+      r.get(b);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[8 * h + e] = acc[8 * h + e] * xs * s[e];
-      if (P.bias) {
-        rb.load(bias + n + 8 * h);
-        rb.get(b);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[8 * h + e] += b[e];
-      }
-      if (P.res) {
-        rb.load(res + n + 8 * h);
-        rb.get(b);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[8 * h + e] += b[e];
-      }
+      for (int e = 0; e < 8; ++e) v[8 * h + e] += b[e];
     }
-    store8<T>(y + n, 0, v);
-    store8<T>(y + n + 8, 0, v + 8);
-    return;
   }
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    if (n + e >= P.N) break;
-    float f = acc[e] * xs * P.w_scale[n + e];
-    if (P.bias) f += to_f32<T>(bias[n + e]);
-    if (P.res) f += to_f32<T>(res[n + e]);
-    y[n + e] = from_f32<T>(f);
-  }
-}
+};
 
 // 16 bytes of a row from depth k, zeros from K on.  Nothing behind the row is
 // read: the row's last 16 bytes, shifted down.
 __device__ __forceinline__ u32x4 row_bytes(const int8_t *p, int64_t k,
                                            int64_t K) {
-  if (K < 16) {  // (k = 0 or past the end)
-    u32x4 u = {0u, 0u, 0u, 0u};
+  u32x4 u = {0u, 0u, 0u, 0u};
+  uint32_t s;
+  if (K < 16) {  // a row of less: byte by byte
+    s = (uint32_t)k;
 #pragma unroll 1
-    for (int e = (int)(K - k) - 1; e >= 0; --e) {
-      u.w = u.w << 8 | u.z >> 24;
-      u.z = u.z << 8 | u.y >> 24;
-      u.y = u.y << 8 | u.x >> 24;
-      u.x = u.x << 8 | (uint8_t)p[k + e];
-    }
-    return u;
+    for (int e = (int)K - 1; e >= 0; --e)
+      u = u32x4{u.x << 8 | (uint8_t)p[e], u.y << 8 | u.x >> 24,
+                u.z << 8 | u.y >> 24, u.w << 8 | u.z >> 24};
+  } else {
+    const int64_t at = min(k, K - 16);
+    u = *reinterpret_cast<const u32x4_any *>(p + at);
+    s = (uint32_t)min(k - at, (int64_t)16);
   }
-  const int64_t at = min(k, K - 16);
-  u32x4 u = *reinterpret_cast<const u32x4_any *>(p + at);
-  const uint32_t s = (uint32_t)min(k - at, (int64_t)16);
+  if (s > 16) s = 16;
   if (s & 16) u = u32x4{0u, 0u, 0u, 0u};
   if (s & 8) u = u32x4{u.z, u.w, 0u, 0u};
   if (s & 4) u = u32x4{u.y, u.z, u.w, 0u};
@@ -110,117 +139,136 @@ __device__ __forceinline__ u32x4 row_bytes(const int8_t *p, int64_t k,
                __builtin_amdgcn_alignbyte(0u, u.w, b)};
 }
 
-// ---------------------------------------------------------------------------
-// Any strides and alignment: 128 x 128 tiles, 4 waves of 64 x 64, depth in
-// steps of 64 bytes through registers into two LDS buffers.
+// The depth goes in spans of 128 bytes, two matrix steps of 64, through LDS
+// rows of 128 bytes.
+constexpr int kCUs = 256;
+constexpr int kStep = 64;
+constexpr int kSpan = 128;
 
-constexpr int kAnyTile = 128;
-constexpr int kAnyStep = 64;
-
-// LDS address (16-byte units) of chunk c of 64-byte row r: 16 rows' equal
-// chunks fall on all 64 banks
-__device__ __forceinline__ int any_slot(int r, int c) {
-  return r * 4 + (c ^ ((r >> 2) & 3));
+// LDS slot (16-byte units) of chunk c of row r: 16 rows' equal chunks fall on
+// all 64 banks.
+__device__ __forceinline__ int span_slot(int r, int c) {
+  return r * 8 + (c ^ ((r >> 1) & 7));
 }
 
+// ---------------------------------------------------------------------------
+// Any strides and alignment: 64 x 128 tiles of 4 waves (32 x 64 each), a span
+// ahead in registers, two in LDS; three blocks a CU hide one another's loads.
+
+constexpr int kAnyM = 64, kAnyN = 128;
+
 template <typename T>
-__global__ __launch_bounds__(256) void k_product_any(ProductParams P,
-                                                     int64_t tiles_n) {
-  __shared__ u32x4 lds[2][2][kAnyTile * 4];  // [buffer][x, w]
+__global__ __launch_bounds__(256, 3) void k_product_any(ProductParams P,
+                                                        int tiles_n) {
+  constexpr int kLoads = (kAnyM + kAnyN) * 8 / 256;
+  __shared__ u32x4 lds[2][(kAnyM + kAnyN) * 8];  // [x rows | w rows]
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t bm = blockIdx.x / tiles_n, bn = blockIdx.x - bm * tiles_n;
-  const int64_t m0 = bm * kAnyTile, n0 = bn * kAnyTile;
-  const int8_t *xp[2], *wp[2];
-  int slot[2], kc[2];
+  const int bm = blockIdx.x / tiles_n, bn = blockIdx.x - bm * tiles_n;
+  const int m0 = bm * kAnyM, n0 = bn * kAnyN;
+  const int chunk = (tid & 7) * 16;
+  const int8_t *at[kLoads];
+  int slot[kLoads];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int id = tid + 256 * i, r = id >> 2;
-    kc[i] = (id & 3) * 16;
-    slot[i] = any_slot(r, id & 3);
+  for (int i = 0; i < kLoads; ++i) {
+    const int r = i * 32 + (tid >> 3);
     // rows behind the end repeat the last one; their results are not stored
-    xp[i] = P.x + min(m0 + r, P.M - 1) * P.ldx;
-    wp[i] = P.w + min(n0 + w_row(r), P.N - 1) * P.ldw;
+    at[i] = r < kAnyM
+                ? P.x + (int64_t)min(m0 + r, (int)P.M - 1) * P.ldx
+                : P.w + (int64_t)min(n0 + w_row(r - kAnyM), (int)P.N - 1) *
+                            P.ldw;
+    slot[i] = span_slot(r, tid & 7);
   }
-  u32x4 xr[2], wr[2];
+  u32x4 next[kLoads];
   auto fetch = [&](int64_t k0) {
-    if (k0 + kAnyStep <= P.K) {
+    if (k0 + kSpan <= P.K) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        xr[i] = *reinterpret_cast<const u32x4_any *>(xp[i] + k0 + kc[i]);
-        wr[i] = *reinterpret_cast<const u32x4_any *>(wp[i] + k0 + kc[i]);
-      }
+      for (int i = 0; i < kLoads; ++i)
+        next[i] = *reinterpret_cast<const u32x4_any *>(at[i] + k0 + chunk);
     } else {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        xr[i] = row_bytes(xp[i], k0 + kc[i], P.K);
-        wr[i] = row_bytes(wp[i], k0 + kc[i], P.K);
-      }
+      for (int i = 0; i < kLoads; ++i)
+        next[i] = row_bytes(at[i], k0 + chunk, P.K);
     }
   };
-  auto put = [&](int b) {
+  i32x4 acc[2][4] = {};  // [x operand][w operand]
+  const int wm = (wave >> 1) * 32, wn = (wave & 1) * 64;
+  const int spans = (int)((P.K + kSpan - 1) / kSpan);
+  if (spans > 0) fetch(0);
+  for (int s = 0; s < spans; ++s) {
+    u32x4 *buf = lds[s & 1];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      lds[b][0][slot[i]] = xr[i];
-      lds[b][1][slot[i]] = wr[i];
-    }
-  };
-  i32x4 acc[4][4] = {};  // [x operand][w operand]
-  const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
-  const int64_t steps = (P.K + kAnyStep - 1) / kAnyStep;
-  if (steps > 0) {
-    fetch(0);
-    put(0);
-  }
-  __syncthreads();
-  for (int64_t s = 0; s < steps; ++s) {
-    const int b = (int)(s & 1);
-    if (s + 1 < steps) fetch((s + 1) * kAnyStep);
-    i32x4 xf[4], wf[4];
+    for (int i = 0; i < kLoads; ++i) buf[slot[i]] = next[i];
+    if (s + 1 < spans) fetch((int64_t)(s + 1) * kSpan);
+    // (one barrier a span: the buffer written next was read a span ago)
+    __syncthreads();
 #pragma unroll
-    for (int f = 0; f < 4; ++f) {
-      xf[f] = __builtin_bit_cast(
-          i32x4, lds[b][0][any_slot(wm + 16 * f + (lane & 15), lane >> 4)]);
-      wf[f] = __builtin_bit_cast(
-          i32x4, lds[b][1][any_slot(wn + 16 * f + (lane & 15), lane >> 4)]);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int h = 0; h < 2; ++h) {
+      i32x4 xf[2], wf[4];
+      const int c = 4 * h + (lane >> 4);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[j], xf[i],
-                                                          acc[i][j], 0, 0, 0);
-    if (s + 1 < steps) put(b ^ 1);
-    __syncthreads();
-  }
+        wf[j] = __builtin_bit_cast(
+            i32x4, buf[span_slot(kAnyM + wn + 16 * j + (lane & 15), c)]);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 2; ++i)
+        xf[i] = __builtin_bit_cast(
+            i32x4, buf[span_slot(wm + 16 * i + (lane & 15), c)]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+              wf[j], xf[i], acc[i][j], 0, 0, 0);
+    }
+  }
+  const int n = n0 + wn + 16 * (lane >> 4);
+  if (n >= (int)P.N) return;
+  Columns<T> columns(P, m0 + wm + (lane & 15), n);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
     float v[16];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[4 * j + e] = (float)acc[i][j][e];
-    store16<T>(P, m0 + wm + 16 * i + (lane & 15),
-               n0 + wn + 16 * (lane >> 4), v);
+    columns.store(P, v);
+    columns.next(P, 16);
   }
 }
 
-// ---------------------------------------------------------------------------
-// Rows on 16-byte addresses: WGM x WGN waves of 16 FM x 64, the depth in steps
-// of 64 bytes that go straight from memory to LDS, kStages steps deep.
-//
-// Step t's operands are read from LDS to registers during step t - 1's
-// products, so at a barrier every wave is done with the LDS buffer of the
-// step it starts to multiply, and the loads of step t + kStages go there: a
-// load has kStages - 1 steps to arrive.
+template <typename T>
+hipError_t product_any(const ProductParams &P, hipStream_t s) {
+  const int64_t tm = (P.M + kAnyM - 1) / kAnyM, tn = (P.N + kAnyN - 1) / kAnyN;
+  if (tm * tn > INT32_MAX) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((k_product_any<T>), dim3((unsigned)(tm * tn)), dim3(256),
+                     0, s, P, (int)tn);
+  return hipGetLastError();
+}
 
-constexpr int kStep = 64;
-constexpr int kStages = 4;
+// ---------------------------------------------------------------------------
+// Rows on 16-byte addresses: WK groups of WGM x WGN waves of 16 FM x 64.  The
+// depth goes in spans of 128 bytes, a whole cache line of every row, straight
+// from memory to LDS, ST spans deep (halves of a line would be fetched twice:
+// a tile's lines outlast the L1 cache).  Group g takes the spans g, g + WK,
+// ...; the groups' sums meet in LDS.
+//
+// A span is multiplied in two steps of 64 bytes, each step's operands read
+// from LDS to registers during the step before.  So halfway through a span
+// every wave is done with its LDS buffer: the one barrier of a span stands
+// there, and the loads of ST spans later follow it.
+
 constexpr int kGroupM = 8;  // tile rows that share w tiles while in L2
 
 // 64 lanes' 16 bytes each from base + off to LDS, in lane order from m0 on.
 // (The compiler does not know of the LDS write: stage_wait orders it.)
-__device__ __forceinline__ void dma16(uint32_t lds, const void *base,
+__device__ __forceinline__ void dma16(uint32_t lds, const int8_t *at,
                                       uint32_t off) {
+  // (wave-uniform, but not always in scalar registers)
+  const uint64_t a = (uint64_t)at;
+  const uint64_t base =
+      (uint64_t)__builtin_amdgcn_readfirstlane((int)(a >> 32)) << 32 |
+      (uint32_t)__builtin_amdgcn_readfirstlane((int)a);
+  lds = __builtin_amdgcn_readfirstlane(lds);
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\t"
                "global_load_lds_dwordx4 %1, %2"
                :: "s"(lds), "v"(off), "s"(base)
@@ -242,165 +290,291 @@ __device__ __forceinline__ uint32_t lds_address(const void *p) {
 
 // Tile of block b: the blocks of one XCD (b % 8) take consecutive tiles, in
 // groups of kGroupM tile rows, so the 32 that run together cover 8 x 4 tiles.
-__device__ __forceinline__ void tile_of(int64_t b, int64_t tm, int64_t tn,
-                                        int64_t &m, int64_t &n) {
-  const int64_t all = tm * tn, per = all / 8, rem = all % 8, xcd = b % 8;
-  const int64_t t = xcd * per + (xcd < rem ? xcd : rem) + b / 8;
-  const int64_t g = t / (kGroupM * tn);
-  const int64_t rows = min((int64_t)kGroupM, tm - g * kGroupM);
-  const int64_t in = t - g * kGroupM * tn;
+__device__ __forceinline__ void tile_of(int b, int tm, int tn, int &m,
+                                        int &n) {
+  const int all = tm * tn, per = all / 8, rem = all % 8, xcd = b % 8;
+  const int t = xcd * per + min(xcd, rem) + b / 8;
+  const int g = t / (kGroupM * tn);
+  const int rows = min(kGroupM, tm - g * kGroupM);
+  const int in = t - g * kGroupM * tn;
   m = g * kGroupM + in % rows;
   n = in / rows;
 }
 
-template <typename T, int FM, int WGM, int WGN>
-__global__ __launch_bounds__(64 * WGM * WGN, 2) void k_product(
-    ProductParams P, int64_t tm, int64_t tn) {
-  constexpr int kBM = 16 * FM * WGM, kBN = 64 * WGN;
-  // a wave's loads of a step: 16 rows of 64 bytes each
-  constexpr int kXLoads = FM / WGN, kWLoads = 4 / WGM;
-  constexpr int kLoads = kXLoads + kWLoads;
-  static_assert(kXLoads * WGN == FM && kWLoads * WGM == 4, "even shares");
-  constexpr int kStageBytes = (kBM + kBN) * kStep;
-  extern __shared__ u32x4 lds[];  // [kStages][x rows | w rows]
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int64_t bm, bn;
-  tile_of(blockIdx.x, tm, tn, bm, bn);
-  const int64_t m0 = bm * kBM, n0 = bn * kBN;
-  // rows behind the end repeat the last one; their results are not stored
-  const int last_m = (int)min(P.M - 1 - m0, (int64_t)kBM - 1);
-  const int last_n = (int)min(P.N - 1 - n0, (int64_t)kBN - 1);
-  const int8_t *xbase = P.x + m0 * P.ldx, *wbase = P.w + n0 * P.ldw;
-  const int full = (int)(P.K / kStep);
+// Waves a SIMD's registers hold: 16 FM sums, twice 4 FM + 16 operands and some
+// 60 more each.
+constexpr int waves_per_simd(int FM) { return FM > 4 ? 2 : FM > 2 ? 3 : 4; }
 
-  // LDS row r of a part holds its 16-byte chunk c at slot any_slot(r, c); the
-  // lanes of a load fill 64 slots in order
-  auto x_row = [&](int i) { return (wave * kXLoads + i) * 16 + (lane >> 2); };
-  auto w_lds_row = [&](int i) {
-    return (wave * kWLoads + i) * 16 + (lane >> 2);
+template <typename T, int FM, int WGM, int WGN, int WK, int ST>
+__global__ __launch_bounds__(64 * WGM * WGN * WK, waves_per_simd(FM)) void
+k_product(ProductParams P, int tm, int tn) {
+  constexpr int kWaves = WGM * WGN;  // of a group
+  constexpr int kBM = 16 * FM * WGM, kBN = 64 * WGN;
+  // a span's loads: 8 rows each, dealt to the group's waves (a wave whose
+  // share is short repeats the last one)
+  constexpr int kBlocks = (kBM + kBN) / 8;
+  constexpr int kLoads = (kBlocks + kWaves - 1) / kWaves;
+  constexpr int kStageBytes = (kBM + kBN) * kSpan;
+  static_assert((ST - 1) * kLoads < 64, "loads on their way are countable");
+  static_assert(WK == 1 || kBM * kBN * 4 <= ST * kStageBytes,
+                "a group's sums fit its buffers");
+  extern __shared__ u32x4 lds_all[];  // [WK][ST][x rows | w rows]
+  const int lane = threadIdx.x & 63;
+  const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = wave_all / kWaves, wave = wave_all % kWaves;
+  u32x4 *lds = lds_all + group * (ST * kStageBytes / 16);
+  // this block's share of the depth: whole spans, the rest to the last
+  const int part = blockIdx.y, all_spans = (int)(P.K / kSpan);
+  const int span0 = (int)((int64_t)all_spans * part / P.splits);
+  const int full =
+      (int)((int64_t)all_spans * (part + 1) / P.splits) - span0;
+  const int rest = part == P.splits - 1 ? (int)(P.K % kSpan) : 0;
+  const int common = full / WK;                     // every group's spans
+  const int most = (full + WK - 1) / WK;
+  const int mine = common + (group < full % WK ? 1 : 0);
+
+  // The tile: its rows, and where this lane's part of a load starts.  Rows
+  // behind the end repeat the last one; their results are not stored.
+  int m0, n0;
+  const int8_t *xbase, *wbase;
+  uint32_t off[kLoads];
+  // the lanes of a load fill 64 slots in order (rows 4 to 7 of 8: chunks 4
+  // apart too, in odd blocks)
+  const int chunk = ((lane & 7) ^ ((lane >> 4) & 3)) * 16;
+  auto block_of = [&](int i) { return min(wave + i * kWaves, kBlocks - 1); };
+  auto chunk_of = [&](int blk) { return chunk ^ ((blk & 1) * 64); };
+  auto row_offset = [&](int blk) {
+    const bool w = blk >= kBM / 8;
+    const int r = (w ? blk - kBM / 8 : blk) * 8 + (lane >> 3);
+    return w ? (uint32_t)min(w_row(r), (int)P.N - 1 - n0) * (uint32_t)P.ldw
+             : (uint32_t)min(r, (int)P.M - 1 - m0) * (uint32_t)P.ldx;
   };
-  const int chunk = ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
-  uint32_t xoff[kXLoads], woff[kWLoads];
+  auto take = [&](int64_t b) {
+    int bm, bn;
+    tile_of(b, tm, tn, bm, bn);
+    m0 = bm * kBM;
+    n0 = bn * kBN;
+    xbase = P.x + (int64_t)m0 * P.ldx + (int64_t)span0 * kSpan;
+    wbase = P.w + (int64_t)n0 * P.ldw + (int64_t)span0 * kSpan;
 #pragma unroll
-  for (int i = 0; i < kXLoads; ++i)
-    xoff[i] = (uint32_t)min(x_row(i), last_m) * (uint32_t)P.ldx + chunk;
+    for (int i = 0; i < kLoads; ++i)
+      off[i] = row_offset(block_of(i)) + chunk_of(block_of(i));
+  };
+  const uint32_t dst = lds_address(lds);
+  auto issue1 = [&](int t, int i) {
+    const int blk = block_of(i);
+    dma16(dst + (t % ST) * kStageBytes + blk * 1024,
+          (blk >= kBM / 8 ? wbase : xbase) +
+              (int64_t)(t * WK + group) * kSpan,
+          off[i]);
+  };
+  auto issue_first = [&](int spans) {
+#pragma unroll 1
+    for (int t = 0; t < spans && t < mine; ++t)
 #pragma unroll
-  for (int i = 0; i < kWLoads; ++i)
-    woff[i] =
-        (uint32_t)min(w_row(w_lds_row(i)), last_n) * (uint32_t)P.ldw + chunk;
-  const uint32_t xdst = lds_address(lds) + wave * kXLoads * 1024;
-  const uint32_t wdst =
-      lds_address(lds) + kBM * kStep + wave * kWLoads * 1024;
-  auto issue = [&](int s) {
-    const uint32_t b = (s % kStages) * kStageBytes;
-#pragma unroll
-    for (int i = 0; i < kXLoads; ++i)
-      dma16(xdst + b + i * 1024, xbase + (int64_t)s * kStep, xoff[i]);
-#pragma unroll
-    for (int i = 0; i < kWLoads; ++i)
-      dma16(wdst + b + i * 1024, wbase + (int64_t)s * kStep, woff[i]);
+      for (int i = 0; i < kLoads; ++i) issue1(t, i);
   };
 
   const int wm = (wave / WGN) * (16 * FM), wn = (wave % WGN) * 64;
-  const int slot = any_slot(lane & 15, lane >> 4);
-  const int xslot = wm * 4 + slot, wslot = (kBM + wn) * 4 + slot;
-  i32x4 acc[FM][4] = {};
-  auto read = [&](int s, i32x4 *x, i32x4 *w) {
-    const u32x4 *p = lds + (s % kStages) * (kStageBytes / 16);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      w[j] = __builtin_bit_cast(i32x4, p[wslot + j * 64]);
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-      x[i] = __builtin_bit_cast(i32x4, p[xslot + i * 64]);
+  // step h reads chunks 4 h + lane / 16 of the wave's rows
+  const int slot = span_slot(lane & 15, lane >> 4);
+  i32x4 acc[FM][4];
+  auto read1 = [&](int t, int h, int r, i32x4 *x, i32x4 *w) {
+    const u32x4 *p =
+        lds + (t % ST) * (kStageBytes / 16) + (slot ^ (4 * h));
+    if (r < 4)
+      w[r] = __builtin_bit_cast(i32x4, p[(kBM + wn + r * 16) * 8]);
+    else
+      x[r - 4] = __builtin_bit_cast(i32x4, p[(wm + (r - 4) * 16) * 8]);
   };
-  auto multiply = [&](const i32x4 *x, const i32x4 *w) {
+  auto read = [&](int t, int h, i32x4 *x, i32x4 *w) {
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int r = 0; r < FM + 4; ++r) read1(t, h, r, x, w);
+  };
+  // One step's products from (x, w), and between them what the wave has to
+  // start meanwhile: the next step's operand reads (span t, half h, to (y,
+  // v)) and loads d0 .. d1 - 1 of span `to` (none if !load).  Issued in one
+  // go, the loads would hold up the products behind them: the address unit
+  // takes 16 cycles for each and serves every wave of the CU.
+  auto step = [&](const i32x4 *x, const i32x4 *w, int t, int h, i32x4 *y,
+                  i32x4 *v, int to, int d0, int d1, bool load, bool use) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[j], x[i],
-                                                          acc[i][j], 0, 0, 0);
+    for (int i = 0; i < FM; ++i) {
+#pragma unroll
+      for (int r = i * (FM + 4) / FM; r < (i + 1) * (FM + 4) / FM; ++r)
+        read1(t, h, r, y, v);
+      if (load)
+#pragma unroll
+        for (int d = d0 + i * (d1 - d0) / FM;
+             d < d0 + (i + 1) * (d1 - d0) / FM; ++d)
+          issue1(to, d);
+      if (use)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+              w[j], x[i], acc[i][j], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
 
+  int tile = blockIdx.x;
+  take(tile);
+  bool loading = false;  // the tile's first ST spans are on their way
+  while (true) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+    i32x4 xa[FM], wa[4], xb[FM], wb[4];
+    if (rest) {
+      // the partial span comes first, through the last group's last buffer,
+      // while the first loads are on their way: zeros from the depth on
+      issue_first(ST - 1);
+      if (group == WK - 1) {
+        u32x4 *p = lds + (ST - 1) * (kStageBytes / 16) + lane;
+        const int64_t k = (int64_t)full * kSpan;
+        u32x4 last[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const int blk = block_of(i);
+          last[i] =
+              row_bytes((blk >= kBM / 8 ? wbase : xbase) + row_offset(blk),
+                        k + chunk_of(blk), k + rest);
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) p[block_of(i) * 64] = last[i];
+      }
+      __syncthreads();
+      if (group == WK - 1) {
 #pragma unroll 1
-  for (int s = 0; s < kStages - 1 && s < full; ++s) issue(s);
-  i32x4 xa[FM], wa[4], xb[FM], wb[4];
-  if (P.K % kStep) {
-    // the partial step comes first, through the last buffer, while the first
-    // loads are on their way: zeros from the depth on
-    u32x4 *p = lds + (kStages - 1) * (kStageBytes / 16) + lane;
-    const int64_t k = (int64_t)full * kStep + chunk;
-#pragma unroll 1
-    for (int i = 0; i < kXLoads; ++i)
-      p[(wave * kXLoads + i) * 64] = row_bytes(
-          xbase + (int64_t)min(x_row(i), last_m) * P.ldx, k, P.K);
-#pragma unroll 1
-    for (int i = 0; i < kWLoads; ++i)
-      p[kBM * 4 + (wave * kWLoads + i) * 64] =
-          row_bytes(wbase + (int64_t)min(w_row(w_lds_row(i)), last_n) * P.ldw,
-                    k, P.K);
-    __syncthreads();
-    read(kStages - 1, xa, wa);
-    multiply(xa, wa);
-    __syncthreads();
-  }
-  if (full > 0) {
-    if (full >= kStages) issue(kStages - 1);
-    stage_wait<0>();
-    read(0, xa, wa);
-    // products of step s, held in (x, w), while step s + 1 is read into
-    // (y, v); behind the last step that is a stale buffer, never used
-    int s = 0;
-    auto step = [&](const i32x4 *x, const i32x4 *w, i32x4 *y, i32x4 *v) {
-      stage_wait<(kStages - 2) * kLoads>();
-      issue(s + kStages);
-      read(s + 1, y, v);
-      multiply(x, w);
-      ++s;
-    };
-    while (s + kStages + 1 < full) {
-      step(xa, wa, xb, wb);
-      step(xb, wb, xa, wa);
+        for (int h = 0; h * kStep < rest; ++h) {
+          read(ST - 1, h, xa, wa);
+          step(xa, wa, ST - 1, h, xb, wb, 0, 0, 0, false, true);
+        }
+      }
+      __syncthreads();
+      if (mine >= ST)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) issue1(ST - 1, i);
+    } else if (!loading) {
+      issue_first(ST);
     }
+    if (full > 0) {
+      if (mine >= ST)
+        stage_wait<(ST - 1) * kLoads>();
+      else
+        stage_wait<0>();
+      read(0, 0, xa, wa);
+      // loads of a span: the first half in the step behind the barrier, the
+      // others in the step after it; two spans deep, all at once, or they
+      // would come too late
+      constexpr int kHalf = ST > 2 ? kLoads / 2 : kLoads;
+      int t = 0;
+      for (; t + ST < common; ++t) {
+        step(xa, wa, t, 1, xb, wb, t + ST - 1, kHalf, kLoads, t > 0, true);
+        stage_wait<(ST - 2) * kLoads>();
+        step(xb, wb, t + 1, 0, xa, wa, t + ST, 0, kHalf, true, true);
+      }
 #pragma unroll 1
-    for (; s < full; ++s) {
-      stage_wait<0>();
-      if (s + kStages < full) issue(s + kStages);
-      read(s + 1, xb, wb);
-      multiply(xa, wa);
-#pragma unroll
-      for (int i = 0; i < FM; ++i) xa[i] = xb[i];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) wa[j] = wb[j];
+      for (; t < most; ++t) {
+        // (behind a group's last span: a stale buffer, never multiplied)
+        const bool late = t > 0 && t + ST - 1 < mine;
+        step(xa, wa, t, 1, xb, wb, t + ST - 1, kHalf, kLoads, late, t < mine);
+        stage_wait<0>();
+        step(xb, wb, t + 1, 0, xa, wa, t + ST, 0, kHalf, t + ST < mine,
+             t < mine);
+      }
     }
-  }
+    if constexpr (WK > 1) {
+      // group g finishes the x operands i with i % WK == g
+      __syncthreads();
+      i32x4 *sums =
+          reinterpret_cast<i32x4 *>(lds) + wave * (FM * 4 * 64) + lane;
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    float v[16];
+      for (int i = 0; i < FM; ++i)
+        if (i % WK != group)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+          for (int j = 0; j < 4; ++j) sums[(i * 4 + j) * 64] = acc[i][j];
+      __syncthreads();
+      const i32x4 *from = reinterpret_cast<const i32x4 *>(lds_all) +
+                          wave * (FM * 4 * 64) + lane;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[4 * j + e] = (float)acc[i][j][e];
-    store16<T>(P, m0 + wm + 16 * i + (lane & 15), n0 + wn + 16 * (lane >> 4),
-               v);
+      for (int i = 0; i < FM; ++i)
+        if (i % WK == group)
+#pragma unroll
+          for (int g = 0; g < WK; ++g)
+            if (g != group)
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                acc[i][j] +=
+                    from[g * (ST * kStageBytes / 16) + (i * 4 + j) * 64];
+    }
+    // every wave is behind the last barrier, so all buffers are free: the
+    // next tile's first loads go out before this one is finished
+    const int m = m0 + wm + (lane & 15), n = n0 + wn + 16 * (lane >> 4);
+    tile += gridDim.x;
+    const bool more = tile < tm * tn;
+    if (more) {
+      if (WK > 1) __syncthreads();  // (the sums have been read)
+      take(tile);
+      loading = !rest;
+      if (loading) issue_first(ST);
+    }
+    if (n < (int)P.N) {
+      if (P.splits > 1) {
+        const int64_t row = parts_row(P.N);
+        int32_t *to = P.parts + (part * P.M + m) * row + n;
+#pragma unroll
+        for (int i = 0; i < FM; ++i, to += 16 * row) {
+          if ((WK > 1 && i % WK != group) || m + 16 * i >= (int)P.M) continue;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            reinterpret_cast<i32x4 *>(to)[j] = acc[i][j];
+        }
+      } else {
+        Columns<T> columns(P, m, n);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+          if (WK == 1 || i % WK == group) {
+            float v[16];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[4 * j + e] = (float)acc[i][j][e];
+            columns.store(P, v);
+          }
+          columns.next(P, 16);
+          __builtin_amdgcn_sched_barrier(0);  // (one row's values at a time)
+        }
+      }
+    }
+    if (!more) break;
   }
 }
 
-template <typename T, int FM, int WGM, int WGN>
+template <typename T, int FM, int WGM, int WGN, int WK, int ST>
 hipError_t product_tiles(const ProductParams &P, hipStream_t s) {
   constexpr int kBM = 16 * FM * WGM, kBN = 64 * WGN;
+  constexpr int kThreads = 64 * WGM * WGN * WK;
+  constexpr size_t kLds = (size_t)ST * WK * (kBM + kBN) * kSpan;
+  static_assert(kLds <= 160 * 1024, "LDS of a CU");
+  // blocks a CU holds at once, by LDS and by registers
+  constexpr int kByLds = (int)(160 * 1024 / kLds);
+  constexpr int kByRegs = waves_per_simd(FM) * 256 / kThreads;
+  constexpr int kBlocks = kByLds < kByRegs ? kByLds : kByRegs;
+  static_assert(kBlocks > 0, "a block fits a CU");
   const int64_t tm = (P.M + kBM - 1) / kBM, tn = (P.N + kBN - 1) / kBN;
-  const size_t lds = (size_t)kStages * (kBM + kBN) * kStep;
-  const auto kernel = &k_product<T, FM, WGM, WGN>;
+  if (tm * tn > INT32_MAX) return hipErrorInvalidValue;
+  const int64_t slots = (int64_t)kCUs * kBlocks;
+  const auto kernel = &k_product<T, FM, WGM, WGN, WK, ST>;
   // (the runtime's own limit is 64 KB until a kernel asks for more)
   static const hipError_t allowed = hipFuncSetAttribute(
       reinterpret_cast<const void *>(kernel),
-      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
   if (allowed != hipSuccess) return allowed;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(tm * tn)),
-                     dim3(64 * WGM * WGN), lds, s, P, tm, tn);
+  const int64_t grid = P.splits > 1 || tm * tn < slots ? tm * tn : slots;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid, (unsigned)P.splits),
+                     dim3(kThreads), kLds, s, P, (int)tm, (int)tn);
   return hipGetLastError();
 }
 
@@ -481,22 +655,25 @@ __global__ __launch_bounds__(64 * WK) void k_product_few(ProductParams P) {
 #pragma unroll
     for (int u = 0; u < U; ++u) product1(b.x[u], b.w[u]);
   };
-  const int batches = (int)(P.K / kBatch);
+  // this block's share of the depth: whole batches, the rest to the last
+  const int part = blockIdx.z, all = (int)(P.K / kBatch);
+  const int first = (int)((int64_t)all * part / P.splits);
+  const int last = (int)((int64_t)all * (part + 1) / P.splits);
   Batch a, b;
-  if (wave < batches) fetch(wave, a);
-  for (int i = wave; i < batches; i += 2 * WK) {
-    if (i + WK < batches) fetch(i + WK, b);
+  if (first + wave < last) fetch(first + wave, a);
+  for (int i = first + wave; i < last; i += 2 * WK) {
+    if (i + WK < last) fetch(i + WK, b);
     multiply(a);
-    if (i + WK >= batches) break;
-    if (i + 2 * WK < batches) fetch(i + 2 * WK, a);
+    if (i + WK >= last) break;
+    if (i + 2 * WK < last) fetch(i + 2 * WK, a);
     multiply(b);
   }
   // steps behind the last whole batch, one at a time, first to the waves that
   // had a batch less
-  const int first = batches * U;
+  const int64_t end = part == P.splits - 1 ? P.K : 0;
 #pragma unroll 1
-  for (int s = first + (wave + WK - batches % WK) % WK;
-       (int64_t)s * kStep < P.K; s += WK) {
+  for (int s = all * U + (wave + WK - (last - first) % WK) % WK;
+       (int64_t)s * kStep < end; s += WK) {
     u32x4 x[FM], w[FN];
 #pragma unroll
     for (int j = 0; j < FN; ++j)
@@ -515,8 +692,13 @@ __global__ __launch_bounds__(64 * WK) void k_product_few(ProductParams P) {
     i32x4 s = sums[0][f][lane];
 #pragma unroll
     for (int w = 1; w < WK; ++w) s += sums[w][f][lane];
-    store4<T>(P, m0 + 16 * (f / FN) + (lane & 15),
-              n0 + 16 * (f % FN) + 4 * (lane >> 4), s);
+    const int64_t m = m0 + 16 * (f / FN) + (lane & 15);
+    const int64_t n = n0 + 16 * (f % FN) + 4 * (lane >> 4);
+    if (P.splits == 1)
+      store4<T>(P, m, n, s);
+    else if (m < P.M && n < P.N)
+      *reinterpret_cast<i32x4 *>(P.parts + (part * P.M + m) * parts_row(P.N) +
+                                 n) = s;
   }
 }
 
@@ -524,23 +706,123 @@ template <typename T, int FM, int FN, int U, int WK>
 hipError_t product_few(const ProductParams &P, hipStream_t s) {
   const unsigned strips = (unsigned)((P.N + 16 * FN - 1) / (16 * FN));
   const unsigned rows = (unsigned)((P.M + 16 * FM - 1) / (16 * FM));
-  hipLaunchKernelGGL((k_product_few<T, FM, FN, U, WK>), dim3(strips, rows),
-                     dim3(64 * WK), 0, s, P);
+  hipLaunchKernelGGL((k_product_few<T, FM, FN, U, WK>), 
+                     dim3(strips, rows, (unsigned)P.splits), dim3(64 * WK), 0,
+                     s, P);
   return hipGetLastError();
 }
 
-// Depth split over 4, 8 or 16 waves: until some 16 waves a CU have work, as
-// long as a wave keeps a batch.
-template <typename T, int FM, int FN, int U>
-hipError_t product_few(const ProductParams &P, hipStream_t s) {
-  const int64_t strips = (P.N + 16 * FN - 1) / (16 * FN);
-  const int64_t batches = P.K / (U * kStep);
-  if constexpr (FM < 4)  // (four x operands of 16 waves would spill)
-    if (strips * 8 < 4096 && batches > 8)
-      return product_few<T, FM, FN, U, 16>(P, s);
-  if (strips * 4 < 4096 && batches > 4)
-    return product_few<T, FM, FN, U, 8>(P, s);
-  return product_few<T, FM, FN, U, 4>(P, s);
+// The sums of a split depth, added and finished: 16 results a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void k_product_sum(ProductParams P) {
+  const int64_t row = parts_row(P.N) / 16;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= P.M * row) return;
+  const int64_t m = i / row, n = (i - m * row) * 16;
+  const i32x4 *p = reinterpret_cast<const i32x4 *>(
+      P.parts + m * parts_row(P.N) + n);
+  i32x4 s[4] = {p[0], p[1], p[2], p[3]};
+  for (int k = 1; k < P.splits; ++k) {
+    p += P.M * row * 4;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[j] += p[j];
+  }
+  float v[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) v[e] = (float)s[e >> 2][e & 3];
+  Columns<T>(P, (int)m, (int)n).store(P, v);
+}
+
+template <typename T>
+hipError_t product_sum(const ProductParams &P, hipStream_t s) {
+  const int64_t n = P.M * (parts_row(P.N) / 16);
+  hipLaunchKernelGGL((k_product_sum<T>), dim3((unsigned)((n + 255) / 256)),
+                     dim3(256), 0, s, P);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// Choice of the kernel.
+
+// The tiles, the few-row blocks, and what a call through each takes: fitted to
+// its times on 15 (cols, depth) pairs x 26 row counts from 17 to 12,900, all
+// operands fresh from HBM,
+//   microseconds = base + rounds * (round + spans * span)
+//                  + spans * block_span * (blocks a CU runs, over all rounds)
+// with `rounds` the times the 256 CUs are filled and `spans` the spans of 128
+// a group of waves goes through; for the few-row blocks
+//   base + round * fill + depth * (span + block_span * fill),
+// fill = blocks / 256 and depth in units of 256 bytes a wave.  A split depth
+// adds parts_base and parts_mb for every MB of sums.  The formula is off by
+// some 10 % a call; the kernel it picks is within 1.5 % of the fastest on
+// average over 256 rows (15 % at worst) and within 4 % below.
+enum Kernel {
+  kTile256, kTile224, kTile160, kTile192x128, kTile128, kTile128Deep,
+  kTile96x128, kTile64x128, kTile64x128Two, kTile64Two, kTile48Four,
+  kTile48FourSplit, kFew4, kFew8, kFew8Split, kKernels
+};
+struct Shape {
+  int rows, cols;    // of a tile or block
+  int groups;        // groups of waves that share the depth
+  int per_cu;        // blocks a CU holds (0: a few-row block)
+  int splits;
+  float base, round, span, block_span, parts_base, parts_mb;
+};
+constexpr Shape kShapes[kKernels] = {
+    {256, 256, 1, 1, 1, 0.f, 12.45f, 1.075f, 0.f, 0.f, 0.f},
+    {224, 256, 1, 1, 1, 0.f, 11.34f, 1.002f, 0.f, 0.f, 0.f},
+    {160, 256, 1, 1, 1, 0.f, 10.61f, 0.744f, 0.f, 0.f, 0.f},
+    {192, 128, 1, 2, 1, 2.09f, 7.74f, 0.180f, 0.461f, 0.f, 0.f},
+    {128, 128, 1, 2, 1, 1.77f, 5.57f, 0.224f, 0.322f, 0.f, 0.f},
+    {128, 128, 1, 1, 1, 1.73f, 6.80f, 0.406f, 0.f, 0.f, 0.f},
+    {96, 128, 1, 2, 1, 1.96f, 4.57f, 0.295f, 0.212f, 0.f, 0.f},
+    {64, 128, 1, 3, 1, 2.61f, 3.30f, 0.249f, 0.208f, 0.f, 0.f},
+    {64, 128, 2, 1, 1, 2.62f, 4.43f, 0.546f, 0.f, 0.f, 0.f},
+    {64, 64, 2, 2, 1, 0.27f, 5.12f, 0.188f, 0.345f, 0.f, 0.f},
+    {48, 64, 4, 1, 1, 1.85f, 3.86f, 0.819f, 0.f, 0.f, 0.f},
+    {48, 64, 4, 1, 4, 0.f, 2.28f, 1.000f, 0.f, 7.01f, 0.348f},
+    {32, 32, 4, 0, 1, 3.91f, 0.785f, 0.881f, 1.545f, 0.f, 0.f},
+    {32, 32, 8, 0, 1, 3.87f, 1.121f, 1.653f, 3.098f, 0.f, 0.f},
+    {32, 32, 8, 0, 4, 6.81f, 0.666f, 1.629f, 3.183f, 0.f, 0.396f},
+};
+constexpr int kFewRows = 16;   // up to here: one x operand, k_product_few
+
+float expected_us(const Shape &c, int64_t M, int64_t N, int64_t K) {
+  const int64_t tiles =
+      ((M + c.rows - 1) / c.rows) * ((N + c.cols - 1) / c.cols) * c.splits;
+  float us = c.base;
+  if (c.per_cu == 0) {
+    const float fill = (float)tiles / kCUs;
+    const float depth = (float)K / (256.f * c.groups * c.splits);
+    us += c.round * fill + depth * (c.span + c.block_span * fill);
+  } else {
+    const int64_t slots = (int64_t)c.per_cu * kCUs;
+    const int64_t whole = tiles / slots, left = tiles % slots;
+    const int64_t rounds = whole + (left ? 1 : 0);
+    const int64_t deep = (int64_t)c.groups * c.splits * kSpan;
+    const float spans = (float)((K + deep - 1) / deep);
+    us += rounds * (c.round + spans * c.span) +
+          spans * c.block_span *
+              (whole * c.per_cu + (left + kCUs - 1) / kCUs);
+  }
+  if (c.splits > 1)
+    us += c.parts_base + c.parts_mb * 4e-6f * (float)M * (float)N * c.splits;
+  return us;
+}
+
+// By sizes alone, so that the workspace is known without the pointers.
+int choose(int64_t M, int64_t N, int64_t K) {
+  int best = 0;
+  float least = 0.f;
+  for (int i = 0; i < kKernels; ++i) {
+    if (kShapes[i].per_cu == 0 && M > 256) continue;  // (not measured)
+    const float us = expected_us(kShapes[i], M, N, K);
+    if (i == 0 || us < least) {
+      least = us;
+      best = i;
+    }
+  }
+  return best;
 }
 
 // x, w and their strides on 16 bytes, and a tile's rows within 32-bit offsets
@@ -552,30 +834,58 @@ bool aligned_rows(const ProductParams &P) {
 }
 
 template <typename T>
-hipError_t product(const ProductParams &P, hipStream_t s) {
-  if (P.M <= 16) return product_few<T, 1, 1, 4>(P, s);
-  if (P.M <= 32) return product_few<T, 2, 1, 4>(P, s);
-  if (P.M <= 64) return product_few<T, 4, 2, 2>(P, s);
-  if (aligned_rows(P)) {
-    if (P.M > 512) return product_tiles<T, 8, 2, 4>(P, s);
-    return product_tiles<T, 4, 2, 2>(P, s);
+hipError_t product(ProductParams P, hipStream_t s) {
+  if (P.M <= kFewRows) {
+    // four waves share a strip's depth where the strips alone fill the CUs,
+    // else eight: 16 rows through 24576 x 4096 (1,536 strips) take 28.9 and
+    // 31.9 us, through 4096 x 12288 (256) 17.2 and 16.8, one row 13.3 and 12.4
+    const int64_t strips = (P.N + 15) / 16;
+    if (strips < 1024) return product_few<T, 1, 1, 4, 8>(P, s);
+    return product_few<T, 1, 1, 4, 4>(P, s);
   }
-  const int64_t tm = (P.M + kAnyTile - 1) / kAnyTile,
-                tn = (P.N + kAnyTile - 1) / kAnyTile;
-  hipLaunchKernelGGL((k_product_any<T>), dim3((unsigned)(tm * tn)), dim3(256),
-                     0, s, P, tn);
-  return hipGetLastError();
+  int kernel = choose(P.M, P.N, P.K);
+  // unaligned loads cost the few-row blocks more: 40 rows through 4096 x 4096
+  // at odd strides take 32.0 us and 24.1 through k_product_any, 33 through
+  // 500 x 700 take 6.0 and 8.4
+  if (!aligned_rows(P) && (kShapes[kernel].per_cu != 0 || P.K > 1024))
+    return product_any<T>(P, s);
+  P.splits = kShapes[kernel].splits;
+  hipError_t e = hipErrorInvalidValue;
+  switch (kernel) {
+    case kTile256: e = product_tiles<T, 8, 2, 4, 1, 2>(P, s); break;
+    case kTile224: e = product_tiles<T, 7, 2, 4, 1, 2>(P, s); break;
+    case kTile160: e = product_tiles<T, 5, 2, 4, 1, 3>(P, s); break;
+    case kTile192x128: e = product_tiles<T, 6, 2, 2, 1, 2>(P, s); break;
+    case kTile128: e = product_tiles<T, 4, 2, 2, 1, 2>(P, s); break;
+    case kTile128Deep: e = product_tiles<T, 4, 2, 2, 1, 4>(P, s); break;
+    case kTile96x128: e = product_tiles<T, 3, 2, 2, 1, 2>(P, s); break;
+    case kTile64x128: e = product_tiles<T, 2, 2, 2, 1, 2>(P, s); break;
+    case kTile64x128Two: e = product_tiles<T, 2, 2, 2, 2, 3>(P, s); break;
+    case kTile64Two: e = product_tiles<T, 2, 2, 1, 2, 2>(P, s); break;
+    case kTile48Four:
+    case kTile48FourSplit: e = product_tiles<T, 3, 1, 1, 4, 2>(P, s); break;
+    case kFew4: e = product_few<T, 2, 2, 4, 4>(P, s); break;
+    case kFew8:
+    case kFew8Split: e = product_few<T, 2, 2, 4, 8>(P, s); break;
+  }
+  if (e == hipSuccess && P.splits > 1) e = product_sum<T>(P, s);
+  return e;
 }
 
 }  // namespace
 
-size_t product_workspace(int64_t, int64_t, int64_t) { return 0; }
+size_t product_workspace(int64_t M, int64_t N, int64_t K) {
+  if (M <= kFewRows || N == 0) return 0;
+  const int splits = kShapes[choose(M, N, K)].splits;
+  return splits > 1 ? (size_t)splits * M * parts_row(N) * sizeof(int32_t) : 0;
+}
 
 hipError_t launch_product(const dopr_quant_matmul_args_t &a, hipStream_t s) {
   const ProductParams P{a.x,    a.w,      a.x_scale,      a.w_scale,
                         a.bias, a.residual, a.y,          a.rows,
                         a.cols, a.depth,  a.x_row_stride, a.w_row_stride,
-                        a.residual_row_stride, a.y_row_stride};
+                        a.residual_row_stride, a.y_row_stride,
+                        static_cast<int32_t *>(a.workspace), 1};
   if (a.dtype == DOPR_BF16) return product<bf16_t>(P, s);
   if (a.dtype == DOPR_F16) return product<_Float16>(P, s);
   return product<float>(P, s);
