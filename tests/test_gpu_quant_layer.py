@@ -1,0 +1,238 @@
+"""A decoder layer with 8-bit products (pipeline.QuantLayerStep) on the GPU:
+against the float64 layer on the dequantised weights, in the layer's other
+forms (norms behind the blocks, gates, partial and interleaved rotation), and
+the prefix states it makes for the store.
+
+Bounds.  A product's input row in 8 bits is off by a uniform error of half a
+step at most, step = (largest magnitude) / 127: relative to the row's RMS
+that is (peak / RMS) / 127 / sqrt(12).  Rows of a few hundred to a few
+thousand normal values have peak / RMS = 3 to 4 (0.8 %), SiLU(gate) * up rows
+up to 12 (2.7 %).  Four such inputs feed an output (h, attention, h2, act),
+whose two blocks add to a residual of the same order: sqrt(3 * 0.8^2 + 2.7^2)
+< 3.1 % of a block, plus bf16 between the steps (0.6 %, test_gpu_layer.py).
+Relative RMS error <= 4 %; a wrong factor, norm or rotation gives 30 % and
+more.
+"""
+import numpy as np
+import pytest
+import torch
+
+import operator_refs as R
+import workloads
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+RMS_MAX = 4e-2
+
+
+def rel_rms(got, ref):
+    d = got.double() - ref
+    return (d.pow(2).mean() / ref.pow(2).mean()).sqrt().item()
+
+
+def make(hq=8, hkv=4, hidden=256, inter=512, seed=0, head_dim=128):
+    rng = np.random.default_rng(seed)
+    doc_len = np.array([0, 7, 40, 96, 130], np.int32)
+    st = workloads.custom(doc_len, rng.integers(0, 5, 14),
+                          rng.choice([1, 5, 33], 14), hq, hkv,
+                          head_dim=head_dim)
+    w = workloads.layer_weights(st, hidden, inter, DEV, seed + 21) \
+        if head_dim == 128 else None
+    return st, w
+
+
+def attention(q, k, v, pk, pv, st, doc_off):
+    """Float64 attention of each pair over [prefix; own causal keys]."""
+    out = torch.zeros_like(q)
+    cu = st.cu_seqlens
+    rep = st.n_rep
+    for p in range(st.n_pairs):
+        a, b = int(cu[p]), int(cu[p + 1])
+        d = int(st.doc_ids[p])
+        o, n = int(doc_off[d]), int(st.doc_len[d])
+        kk = torch.cat((pk[o:o + n], k[a:b])).repeat_interleave(rep, 1)
+        vv = torch.cat((pv[o:o + n], v[a:b])).repeat_interleave(rep, 1)
+        s = torch.einsum("thd,shd->hts", q[a:b], kk) * st.head_dim ** -0.5
+        t = b - a
+        mask = torch.ones(t, n + t, dtype=torch.bool, device=DEV).tril(n)
+        s = s.masked_fill(~mask, float("-inf")).softmax(-1)
+        out[a:b] = torch.einsum("hts,shd->thd", s, vv)
+    return out
+
+
+def layer64(x, w, norms, gates, prm, st, positions, freq, interleaved, factor,
+            residual_scale, pk, pv, doc_off):
+    """The layer in float64 from float64 weights."""
+    hq, hkv, d = st.n_q_heads, st.n_kv_heads, st.head_dim
+    h = R.norm(x, w["attn_norm"], 1e-6)
+    q = (h @ w["wq"].t()).view(-1, hq, d)
+    k = (h @ w["wk"].t()).view(-1, hkv, d)
+    v = (h @ w["wv"].t()).view(-1, hkv, d)
+    q, _ = R.rotary(q, positions, freq, interleaved, False, factor,
+                    prm["q_norm_w"])
+    k, _ = R.rotary(k, positions, freq, interleaved, False, factor,
+                    prm["k_norm_w"])
+    a = attention(q, k, v, pk, pv, st, doc_off).flatten(1)
+
+    def join(block, residual, norm, gate):
+        n = R.norm(block, norm, 1e-6)
+        n = n if gate is None else n * gate.double()
+        return residual_scale * residual + n
+
+    x2 = join(a @ w["wo"].t(), x, norms.get("post_attn_norm_w"),
+              gates.get("attn_gate"))
+    h2 = R.norm(x2, w["mlp_norm"], 1e-6)
+    act = R.silu_up(h2 @ w["w_gate"].t(), h2 @ w["w_up"].t())
+    return join(act @ w["w_down"].t(), x2, norms.get("post_mlp_norm_w"),
+                gates.get("mlp_gate"))
+
+
+FORMS = {
+    "plain": {},
+    "sandwich": dict(post=True, residual_scale=0.8),
+    "gated": dict(gate=True),
+    "both_chunked": dict(post=True, gate=True, residual_scale=1.25, chunk=37),
+    "partial_interleaved": dict(rotary=dict(rotary_dim=64, interleaved=True),
+                                chunk=50),
+    "scaled": dict(scaled=True),
+}
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_layer_against_float64(form):
+    from paper_2609_03311_amd import (dopr_check_status,
+                                      dopr_rotary_frequencies, pipeline)
+    f = dict(FORMS[form])
+    st, w = make()
+    hidden, inter = 256, 512
+    prm = workloads.params(st, DEV)
+    k_src, v_src, doc_off, _ = workloads.prefix_source(st, DEV, 1)
+    store = pipeline.make_store(st.doc_len, st.n_kv_heads, k_src, v_src)
+    g = torch.Generator(device=DEV).manual_seed(3)
+
+    def gain():
+        return (1 + 0.1 * torch.randn(hidden, generator=g, device=DEV)
+                ).bfloat16()
+
+    norms = {"post_attn_norm_w": gain(), "post_mlp_norm_w": gain()} \
+        if f.get("post") else {}
+    gates = {"attn_gate": 0.7 * gain(), "mlp_gate": 1.3 * gain()} \
+        if f.get("gate") else {}
+    rotary = dict(f.get("rotary", {}))
+    r = rotary.get("rotary_dim", st.head_dim)
+    freq, factor = dopr_rotary_frequencies(r, 1e6)
+    if f.get("scaled"):
+        freq, factor = dopr_rotary_frequencies(
+            r, 1e6, scaling="ramp", factor=4, original_len=64)
+        rotary.update(inv_freq=freq, attention_factor=factor)
+    x = workloads.hidden_states(st, hidden, DEV)
+    rs = f.get("residual_scale", 1.0)
+    step = pipeline.QuantLayerStep(
+        store, {**w, **norms, **gates}, n_pairs=st.n_pairs,
+        n_q_heads=st.n_q_heads, total_tokens=st.n_tokens,
+        max_tokens=int(st.seqlens.max()), hidden=hidden, intermediate=inter,
+        rotary=rotary, residual_scale=rs, chunk=f.get("chunk", 32768))
+    pos = pipeline.online_positions(st.doc_len, st.doc_ids, st.cu_seqlens)
+    ids = torch.from_numpy(st.doc_ids).to(DEV)
+    cu = torch.from_numpy(st.cu_seqlens).to(DEV)
+    y = step.run(0, ids, cu, x, pos, prm["q_norm_w"], prm["k_norm_w"])
+    assert dopr_check_status(store) == 0
+
+    def dequant(name):
+        q, s = step.w[name]
+        return q.double() * s.double()[:, None]
+
+    gu = dequant("w_gate_up")
+    w64 = {"attn_norm": w["attn_norm"], "mlp_norm": w["mlp_norm"],
+           "wq": dequant("w_q"), "wk": dequant("w_k"), "wv": dequant("w_v"),
+           "wo": dequant("w_o"), "w_gate": gu[:inter], "w_up": gu[inter:],
+           "w_down": dequant("w_down")}
+    ref = layer64(x.double(), w64, norms, gates, prm, st, pos, freq.to(DEV),
+                  rotary.get("interleaved", False), factor, rs,
+                  k_src.double(), v_src.double(), doc_off)
+    e = rel_rms(y, ref)
+    print(f"{form}: relative RMS error {e:.4f}", flush=True)
+    assert e <= RMS_MAX
+    # the same bits on a second run, over buffers that now hold the first's
+    first = y.clone()
+    step.run(0, ids, cu, x, pos, prm["q_norm_w"], prm["k_norm_w"])
+    assert torch.equal(step.y, first)
+
+
+def test_rotation_ahead_of_the_attention_is_the_attentions_own():
+    """dopr_rotary with norms, then attention without either, against the
+    attention that norms and rotates by itself: apart by the one rounding of
+    q and k to bf16 between them (2^-8 of a logit's terms, so a few 2^-8 of
+    the output rows, whose values are of order one)."""
+    from paper_2609_03311_amd import dopr_rotary, dopr_rotary_frequencies, \
+        pipeline
+    st, _ = make(seed=4)
+    prm = workloads.params(st, DEV)
+    on = workloads.online_inputs(st, DEV, 3)
+    k_src, v_src, _, _ = workloads.prefix_source(st, DEV, 1)
+    store = pipeline.make_store(st.doc_len, st.n_kv_heads, k_src, v_src)
+    step = pipeline.OnlineStep(store, n_pairs=st.n_pairs,
+                               n_q_heads=st.n_q_heads,
+                               total_tokens=st.n_tokens,
+                               max_tokens=int(st.seqlens.max()))
+    ids = torch.from_numpy(st.doc_ids).to(DEV)
+    cu = torch.from_numpy(st.cu_seqlens).to(DEV)
+    step.attention(0, ids, cu, on["q"], on["k"], on["v"], prm["q_norm_w"],
+                   prm["k_norm_w"])
+    own = step.out.float().clone()
+    pos = pipeline.online_positions(st.doc_len, st.doc_ids, st.cu_seqlens)
+    freq = dopr_rotary_frequencies(128, 1e6)[0].to(DEV)
+    q, k = torch.empty_like(on["q"]), torch.empty_like(on["k"])
+    dopr_rotary(on["q"], on["k"], pos, freq, q, k, q_norm_w=prm["q_norm_w"],
+                k_norm_w=prm["k_norm_w"])
+    step.attention(0, ids, cu, q, k, on["v"], None, None,
+                   rope_inv_freq=torch.zeros(64, device=DEV))
+    assert (step.out.float() - own).abs().max() <= 8 * 2.0 ** -8
+
+
+@pytest.mark.parametrize("interleaved,r", [(False, 128), (True, 64)])
+def test_prefix_states(interleaved, r):
+    """Keys and values for the store against float64 on the dequantised
+    weights: one product's input error each (0.8 %) and bf16."""
+    from paper_2609_03311_amd import dopr_rotary_frequencies, pipeline
+    st, w = make(seed=2)
+    store = pipeline.make_store(st.doc_len, st.n_kv_heads,
+                                *workloads.prefix_source(st, DEV, 1)[:2])
+    prm = workloads.params(st, DEV)
+    step = pipeline.QuantLayerStep(
+        store, w, n_pairs=st.n_pairs, n_q_heads=st.n_q_heads,
+        total_tokens=st.n_tokens, max_tokens=int(st.seqlens.max()),
+        hidden=256, intermediate=512,
+        rotary=dict(rotary_dim=r, interleaved=interleaved))
+    for slots in (1, 273):
+        g = torch.Generator(device=DEV).manual_seed(slots)
+        x = torch.randn(slots, 256, generator=g, device=DEV).bfloat16()
+        pos = torch.arange(slots, device=DEV, dtype=torch.int32) % 100
+        k, v = step.prefix_states(x, pos, prm["k_norm_w"])
+        h = R.norm(x, w["attn_norm"], 1e-6)
+
+        def project(name):
+            q, s = step.w[name]
+            return (h @ (q.double() * s.double()[:, None]).t()).view(
+                slots, st.n_kv_heads, 128)
+
+        freq = dopr_rotary_frequencies(r, 1e6)[0].to(DEV)
+        ref, _ = R.rotary(project("w_k"), pos, freq, interleaved,
+                          gain=prm["k_norm_w"])
+        assert rel_rms(k, ref) <= 1.5e-2
+        assert rel_rms(v, project("w_v")) <= 1.5e-2
+
+
+def test_online_positions():
+    from paper_2609_03311_amd import pipeline
+    pos = pipeline.online_positions([5, -1, 0], [0, 2, 1, 7, -3],
+                                    [0, 2, 3, 5, 6, 7])
+    assert pos.dtype == torch.int32
+    assert pos.tolist() == [5, 6, 0, 0, 1, 0, 0]
+
+
+def test_example_runs():
+    from paper_2609_03311_amd import quant_layer
+    assert quant_layer.main(["--config", "tiny", "--pairs", "20",
+                             "--steps", "2"]) <= 5e-2
