@@ -579,8 +579,8 @@ hipError_t product_tiles(const ProductParams &P, hipStream_t s) {
 }
 
 // ---------------------------------------------------------------------------
-// Few rows: a block's WK waves share one strip of 16 FN w rows and split the
-// depth, in batches of U steps of 64 bytes, each wave's operands coming
+// Few rows: a block's WK waves share one strip of 16 w rows and split the
+// depth, in batches of 4 steps of 64 bytes, each wave's operands coming
 // straight from memory to its registers, one batch ahead of the products.
 // The waves' sums meet in LDS (integers: the split does not show).
 
@@ -607,108 +607,87 @@ __device__ __forceinline__ void store4(const ProductParams &P, int64_t m,
     if (e < left) y[n + e] = from_f32<T>(v[e]);
 }
 
-template <typename T, int FM, int FN, int U, int WK>
+constexpr int kFewSteps = 4;
+
+template <typename T, int FM, int WK>
 __global__ __launch_bounds__(64 * WK) void k_product_few(ProductParams P) {
-  __shared__ i32x4 sums[WK][FM * FN][64];
+  __shared__ i32x4 sums[WK][FM][64];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t n0 = (int64_t)blockIdx.x * (16 * FN);
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
   const int64_t m0 = (int64_t)blockIdx.y * (16 * FM);
   const int kc = (lane >> 4) * 16;
   // rows behind the end repeat the last one; their results are not stored
-  const int8_t *xp[FM], *wp[FN];
+  const int8_t *wp = P.w + min(n0 + (lane & 15), P.N - 1) * P.ldw;
+  const int8_t *xp[FM];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
-    xp[i] = P.x + min(m0 + 16 * i + (lane & 15), P.M - 1) * P.ldx + kc;
-#pragma unroll
-  for (int j = 0; j < FN; ++j)
-    wp[j] = P.w + min(n0 + 16 * j + (lane & 15), P.N - 1) * P.ldw + kc;
-  constexpr int kBatch = U * kStep;
-  i32x4 acc[FM][FN] = {};
+    xp[i] = P.x + min(m0 + 16 * i + (lane & 15), P.M - 1) * P.ldx;
+  constexpr int kBatch = kFewSteps * kStep;
+  i32x4 acc[FM] = {};
   struct Batch {
-    u32x4 x[U][FM], w[U][FN];
+    u32x4 x[kFewSteps][FM], w[kFewSteps];
   };
-  auto fetch = [&](int64_t batch, Batch &b) {
-    const int64_t k = batch * kBatch;
+  auto fetch = [&](int batch, Batch &b) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
-        b.w[u][j] =
-            *reinterpret_cast<const u32x4_any *>(wp[j] + k + u * kStep);
+    for (int u = 0; u < kFewSteps; ++u) {
+      const int64_t k = (int64_t)batch * kBatch + u * kStep + kc;
+      b.w[u] = *reinterpret_cast<const u32x4_any *>(wp + k);
 #pragma unroll
       for (int i = 0; i < FM; ++i)
-        b.x[u][i] =
-            *reinterpret_cast<const u32x4_any *>(xp[i] + k + u * kStep);
+        b.x[u][i] = *reinterpret_cast<const u32x4_any *>(xp[i] + k);
     }
   };
-  auto product1 = [&](const u32x4 *x, const u32x4 *w) {
+  auto product1 = [&](const u32x4 *x, const u32x4 &w) {
 #pragma unroll
     for (int i = 0; i < FM; ++i)
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
-            __builtin_bit_cast(i32x4, w[j]), __builtin_bit_cast(i32x4, x[i]),
-            acc[i][j], 0, 0, 0);
+      acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+          __builtin_bit_cast(i32x4, w), __builtin_bit_cast(i32x4, x[i]),
+          acc[i], 0, 0, 0);
   };
   auto multiply = [&](const Batch &b) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) product1(b.x[u], b.w[u]);
+    for (int u = 0; u < kFewSteps; ++u) product1(b.x[u], b.w[u]);
   };
-  // this block's share of the depth: whole batches, the rest to the last
-  const int part = blockIdx.z, all = (int)(P.K / kBatch);
-  const int first = (int)((int64_t)all * part / P.splits);
-  const int last = (int)((int64_t)all * (part + 1) / P.splits);
+  const int batches = (int)(P.K / kBatch);
   Batch a, b;
-  if (first + wave < last) fetch(first + wave, a);
-  for (int i = first + wave; i < last; i += 2 * WK) {
-    if (i + WK < last) fetch(i + WK, b);
+  if (wave < batches) fetch(wave, a);
+  for (int i = wave; i < batches; i += 2 * WK) {
+    if (i + WK < batches) fetch(i + WK, b);
     multiply(a);
-    if (i + WK >= last) break;
-    if (i + 2 * WK < last) fetch(i + 2 * WK, a);
+    if (i + WK >= batches) break;
+    if (i + 2 * WK < batches) fetch(i + 2 * WK, a);
     multiply(b);
   }
   // steps behind the last whole batch, one at a time, first to the waves that
   // had a batch less
-  const int64_t end = part == P.splits - 1 ? P.K : 0;
 #pragma unroll 1
-  for (int s = all * U + (wave + WK - (last - first) % WK) % WK;
-       (int64_t)s * kStep < end; s += WK) {
-    u32x4 x[FM], w[FN];
-#pragma unroll
-    for (int j = 0; j < FN; ++j)
-      w[j] = row_bytes(wp[j] - kc, (int64_t)s * kStep + kc, P.K);
+  for (int s = batches * kFewSteps + (wave + WK - batches % WK) % WK;
+       (int64_t)s * kStep < P.K; s += WK) {
+    u32x4 x[FM];
+    const u32x4 w = row_bytes(wp, (int64_t)s * kStep + kc, P.K);
 #pragma unroll
     for (int i = 0; i < FM; ++i)
-      x[i] = row_bytes(xp[i] - kc, (int64_t)s * kStep + kc, P.K);
+      x[i] = row_bytes(xp[i], (int64_t)s * kStep + kc, P.K);
     product1(x, w);
   }
 #pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j) sums[wave][i * FN + j][lane] = acc[i][j];
+  for (int i = 0; i < FM; ++i) sums[wave][i][lane] = acc[i];
   __syncthreads();
-  for (int f = wave; f < FM * FN; f += WK) {
-    i32x4 s = sums[0][f][lane];
+  for (int i = wave; i < FM; i += WK) {
+    i32x4 s = sums[0][i][lane];
 #pragma unroll
-    for (int w = 1; w < WK; ++w) s += sums[w][f][lane];
-    const int64_t m = m0 + 16 * (f / FN) + (lane & 15);
-    const int64_t n = n0 + 16 * (f % FN) + 4 * (lane >> 4);
-    if (P.splits == 1)
-      store4<T>(P, m, n, s);
-    else if (m < P.M && n < P.N)
-      *reinterpret_cast<i32x4 *>(P.parts + (part * P.M + m) * parts_row(P.N) +
-                                 n) = s;
+    for (int w = 1; w < WK; ++w) s += sums[w][i][lane];
+    store4<T>(P, m0 + 16 * i + (lane & 15), n0 + 4 * (lane >> 4), s);
   }
 }
 
-template <typename T, int FM, int FN, int U, int WK>
+template <typename T, int FM, int WK>
 hipError_t product_few(const ProductParams &P, hipStream_t s) {
-  const unsigned strips = (unsigned)((P.N + 16 * FN - 1) / (16 * FN));
+  const unsigned strips = (unsigned)((P.N + 15) / 16);
   const unsigned rows = (unsigned)((P.M + 16 * FM - 1) / (16 * FM));
-  hipLaunchKernelGGL((k_product_few<T, FM, FN, U, WK>), 
-                     dim3(strips, rows, (unsigned)P.splits), dim3(64 * WK), 0,
-                     s, P);
+  hipLaunchKernelGGL((k_product_few<T, FM, WK>), dim3(strips, rows),
+                     dim3(64 * WK), 0, s, P);
   return hipGetLastError();
 }
 
@@ -745,7 +724,7 @@ hipError_t product_sum(const ProductParams &P, hipStream_t s) {
 // Choice of the kernel.
 
 // The tiles, the few-row blocks, and what a call through each takes: fitted to
-// its times on 15 (cols, depth) pairs x 26 row counts from 17 to 12,900, all
+// its times on 23 (cols, depth) pairs x 28 row counts from 17 to 12,900, all
 // operands fresh from HBM,
 //   microseconds = base + rounds * (round + spans * span)
 //                  + spans * block_span * (blocks a CU runs, over all rounds)
@@ -754,12 +733,13 @@ hipError_t product_sum(const ProductParams &P, hipStream_t s) {
 //   base + round * fill + depth * (span + block_span * fill),
 // fill = blocks / 256 and depth in units of 256 bytes a wave.  A split depth
 // adds parts_base and parts_mb for every MB of sums.  The formula is off by
-// some 10 % a call; the kernel it picks is within 1.5 % of the fastest on
-// average over 256 rows (15 % at worst) and within 4 % below.
+// some 10 % a call; what it picks was on average 1.4 % slower than the
+// fastest of all 28 kernels tried over 256 rows, 2.5 % from 65 to 256 and 5 %
+// below (1.55 times at worst).
 enum Kernel {
-  kTile256, kTile224, kTile160, kTile192x128, kTile128, kTile128Deep,
-  kTile96x128, kTile64x128, kTile64x128Two, kTile64Two, kTile48Four,
-  kTile48FourSplit, kFew4, kFew8, kFew8Split, kKernels
+  kTile256, kTile224, kTile160, kTile192x128, kTile160x128, kTile128,
+  kTile128Deep, kTile64x128, kTile64x128Two, kTile64Two, kTile48Four,
+  kTile48FourSplit, kTile32Four, kFew, kKernels
 };
 struct Shape {
   int rows, cols;    // of a tile or block
@@ -769,21 +749,20 @@ struct Shape {
   float base, round, span, block_span, parts_base, parts_mb;
 };
 constexpr Shape kShapes[kKernels] = {
-    {256, 256, 1, 1, 1, 0.f, 12.45f, 1.075f, 0.f, 0.f, 0.f},
-    {224, 256, 1, 1, 1, 0.f, 11.34f, 1.002f, 0.f, 0.f, 0.f},
-    {160, 256, 1, 1, 1, 0.f, 10.61f, 0.744f, 0.f, 0.f, 0.f},
-    {192, 128, 1, 2, 1, 2.09f, 7.74f, 0.180f, 0.461f, 0.f, 0.f},
-    {128, 128, 1, 2, 1, 1.77f, 5.57f, 0.224f, 0.322f, 0.f, 0.f},
-    {128, 128, 1, 1, 1, 1.73f, 6.80f, 0.406f, 0.f, 0.f, 0.f},
-    {96, 128, 1, 2, 1, 1.96f, 4.57f, 0.295f, 0.212f, 0.f, 0.f},
-    {64, 128, 1, 3, 1, 2.61f, 3.30f, 0.249f, 0.208f, 0.f, 0.f},
-    {64, 128, 2, 1, 1, 2.62f, 4.43f, 0.546f, 0.f, 0.f, 0.f},
-    {64, 64, 2, 2, 1, 0.27f, 5.12f, 0.188f, 0.345f, 0.f, 0.f},
-    {48, 64, 4, 1, 1, 1.85f, 3.86f, 0.819f, 0.f, 0.f, 0.f},
-    {48, 64, 4, 1, 4, 0.f, 2.28f, 1.000f, 0.f, 7.01f, 0.348f},
-    {32, 32, 4, 0, 1, 3.91f, 0.785f, 0.881f, 1.545f, 0.f, 0.f},
-    {32, 32, 8, 0, 1, 3.87f, 1.121f, 1.653f, 3.098f, 0.f, 0.f},
-    {32, 32, 8, 0, 4, 6.81f, 0.666f, 1.629f, 3.183f, 0.f, 0.396f},
+    {256, 256, 1, 1, 1, 2.98f, 9.47f, 1.365f, 0.f, 0.f, 0.f},
+    {224, 256, 1, 1, 1, 3.15f, 9.07f, 1.225f, 0.f, 0.f, 0.f},
+    {160, 256, 1, 1, 1, 3.08f, 7.75f, 0.925f, 0.f, 0.f, 0.f},
+    {192, 128, 1, 1, 1, 4.30f, 6.50f, 0.684f, 0.f, 0.f, 0.f},
+    {160, 128, 1, 1, 1, 3.64f, 6.60f, 0.561f, 0.f, 0.f, 0.f},
+    {128, 128, 1, 2, 1, 3.93f, 4.62f, 0.229f, 0.329f, 0.f, 0.f},
+    {128, 128, 1, 1, 1, 3.40f, 5.29f, 0.487f, 0.f, 0.f, 0.f},
+    {64, 128, 1, 3, 1, 3.29f, 3.03f, 0.134f, 0.267f, 0.f, 0.f},
+    {64, 128, 2, 1, 1, 3.92f, 2.96f, 0.692f, 0.f, 0.f, 0.f},
+    {64, 64, 2, 2, 1, 2.36f, 3.46f, 0.117f, 0.411f, 0.f, 0.f},
+    {48, 64, 4, 1, 1, 1.13f, 4.51f, 0.873f, 0.f, 0.f, 0.f},
+    {48, 64, 4, 1, 4, 8.03f, 0.f, 1.428f, 0.f, 0.f, 0.708f},
+    {32, 64, 4, 1, 1, 2.12f, 3.60f, 0.591f, 0.f, 0.f, 0.f},
+    {32, 16, 4, 0, 1, 3.98f, 0.438f, 0.681f, 0.570f, 0.f, 0.f},
 };
 constexpr int kFewRows = 16;   // up to here: one x operand, k_product_few
 
@@ -840,33 +819,28 @@ hipError_t product(ProductParams P, hipStream_t s) {
     // else eight: 16 rows through 24576 x 4096 (1,536 strips) take 28.9 and
     // 31.9 us, through 4096 x 12288 (256) 17.2 and 16.8, one row 13.3 and 12.4
     const int64_t strips = (P.N + 15) / 16;
-    if (strips < 1024) return product_few<T, 1, 1, 4, 8>(P, s);
-    return product_few<T, 1, 1, 4, 4>(P, s);
+    if (strips < 1024) return product_few<T, 1, 8>(P, s);
+    return product_few<T, 1, 4>(P, s);
   }
   int kernel = choose(P.M, P.N, P.K);
-  // unaligned loads cost the few-row blocks more: 40 rows through 4096 x 4096
-  // at odd strides take 32.0 us and 24.1 through k_product_any, 33 through
-  // 500 x 700 take 6.0 and 8.4
-  if (!aligned_rows(P) && (kShapes[kernel].per_cu != 0 || P.K > 1024))
-    return product_any<T>(P, s);
+  if (!aligned_rows(P) && kernel != kFew) return product_any<T>(P, s);
   P.splits = kShapes[kernel].splits;
   hipError_t e = hipErrorInvalidValue;
   switch (kernel) {
     case kTile256: e = product_tiles<T, 8, 2, 4, 1, 2>(P, s); break;
     case kTile224: e = product_tiles<T, 7, 2, 4, 1, 2>(P, s); break;
     case kTile160: e = product_tiles<T, 5, 2, 4, 1, 3>(P, s); break;
-    case kTile192x128: e = product_tiles<T, 6, 2, 2, 1, 2>(P, s); break;
+    case kTile192x128: e = product_tiles<T, 6, 2, 2, 1, 3>(P, s); break;
+    case kTile160x128: e = product_tiles<T, 5, 2, 2, 1, 4>(P, s); break;
     case kTile128: e = product_tiles<T, 4, 2, 2, 1, 2>(P, s); break;
     case kTile128Deep: e = product_tiles<T, 4, 2, 2, 1, 4>(P, s); break;
-    case kTile96x128: e = product_tiles<T, 3, 2, 2, 1, 2>(P, s); break;
     case kTile64x128: e = product_tiles<T, 2, 2, 2, 1, 2>(P, s); break;
     case kTile64x128Two: e = product_tiles<T, 2, 2, 2, 2, 3>(P, s); break;
     case kTile64Two: e = product_tiles<T, 2, 2, 1, 2, 2>(P, s); break;
     case kTile48Four:
     case kTile48FourSplit: e = product_tiles<T, 3, 1, 1, 4, 2>(P, s); break;
-    case kFew4: e = product_few<T, 2, 2, 4, 4>(P, s); break;
-    case kFew8:
-    case kFew8Split: e = product_few<T, 2, 2, 4, 8>(P, s); break;
+    case kTile32Four: e = product_tiles<T, 1, 2, 1, 4, 3>(P, s); break;
+    case kFew: e = product_few<T, 2, 4>(P, s); break;
   }
   if (e == hipSuccess && P.splits > 1) e = product_sum<T>(P, s);
   return e;
