@@ -1,7 +1,9 @@
 """Python binding of libdopr (the DoPR online scoring hot path on MI355X).
 
-Argument marshalling only: every step runs in the HIP kernels behind the C
-ABI of ``include/dopr.h``; torch provides device memory and streams.  The
+Argument marshalling only (through ctypes, or the compiled module
+``_operators`` for the calls that have to be short): every step runs in the
+HIP kernels behind the C ABI of ``include/dopr.h``; torch provides device
+memory and streams.  The
 function names are the C names.  A non-OK status raises ``DoprError``.  If
 the shared library has not been built, every call raises (there is no
 fallback path).
@@ -10,7 +12,6 @@ from __future__ import annotations
 
 import ctypes
 import os
-import struct
 from typing import Optional
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -244,13 +245,9 @@ def _ptr(t) -> Optional[int]:
 
 
 def _stream(stream) -> Optional[int]:
-    """Handle of `stream`, or of the current device's current stream."""
     if stream is None:
         import torch
-        try:  # the handle alone: no Stream object is made for it
-            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
-        except AttributeError:
-            stream = torch.cuda.current_stream()
+        stream = torch.cuda.current_stream()
     return stream.cuda_stream
 
 
@@ -590,83 +587,39 @@ def dopr_select_top_k(cu_doclens, cu_select, u, selected, *, max_doclen,
 
 
 # ---------------------------------------------------------------------------
-# Operators of a layer around its attention.  These take any strides that the
-# C ABI takes, so the wrappers check what a pointer and a size cannot show:
-# types, shapes and unit strides.
+# Operators of a layer around its attention.  Their smallest calls are a few
+# microseconds, so their tensors are checked and their arguments filled in
+# the compiled module _operators (csrc/binding.cpp); a tensor of the wrong
+# type, shape, strides or device raises ValueError before any call.
 
-_dtypes = {}
-
-
-def _dtype_code(t, what: str) -> int:
-    if not _dtypes:
-        import torch
-        _dtypes.update({torch.bfloat16: 0, torch.float16: 1,
-                        torch.float32: 2})
-    code = _dtypes.get(t.dtype)
-    if code is None:
-        raise ValueError(f"{what} must be bfloat16, float16 or float32, not "
-                         f"{t.dtype}")
-    return code
+_ops = None
 
 
-def _packer(struct_type):
-    """bytes(fields...) in the layout of a ctypes structure.  These calls are
-    a few microseconds of GPU work at their smallest, and packing is a quarter
-    of what filling a Structure costs."""
-    codes = {ctypes.c_int32: "i", ctypes.c_int64: "q", ctypes.c_void_p: "P",
-             ctypes.c_float: "f", ctypes.c_size_t: "N"}
-    fmt = "@" + "".join(codes[c] for _, c in struct_type._fields_)
-    return struct.Struct(fmt).pack
+def _compiled():
+    """The compiled calls (raises if they have not been built)."""
+    global _ops
+    if _ops is None:
+        lib()
+        import torch  # noqa: F401  (its libraries, which the module links)
+        try:
+            from . import _operators as ops
+        except ImportError as e:
+            raise RuntimeError(
+                "the module _operators is missing or stale: build it with "
+                "`python -m paper_2609_03311_amd._build` (no fallback "
+                f"exists): {e}") from e
+        _ops = ops
+    return _ops
 
 
-_pack_quantize = _packer(_QuantizeArgs)
-_pack_product = _packer(_QuantMatmulArgs)
-_pack_norm = _packer(_NormResidualArgs)
-_pack_rotary = _packer(_RotaryArgs)
-
-
-def _refuse(t, what, shape, dtype):
-    raise ValueError(
-        f"{what} must be a {dtype} GPU tensor of shape {tuple(shape)} with "
-        f"unit last stride, not {t.dtype} {tuple(t.shape)}, strides "
-        f"{t.stride()}, on {t.device}")
-
-
-def _vector(t, what, n, dtype) -> int:
-    """Address of a contiguous [n] vector of this type (0 for None)."""
-    if t is None:
-        return 0
-    if (t.dtype is not dtype or t.shape != (n,) or not t.is_cuda or
-            (n > 1 and t.stride(0) != 1)):
-        _refuse(t, what, (n,), dtype)
-    return t.data_ptr()
-
-
-def _matrix(t, what, shape, dtype):
-    """(address, row stride) of a matrix with unit column stride ((0, 0) for
-    None); a single row has no stride to speak of."""
-    if t is None:
-        return 0, 0
-    s = t.stride()
-    if (t.dtype is not dtype or t.shape != shape or not t.is_cuda or
-            (s[1] != 1 and shape[1] > 1)):
-        _refuse(t, what, shape, dtype)
-    return t.data_ptr(), s[0] if shape[0] > 1 else max(s[0], shape[1])
+def _handle(stream):
+    return None if stream is None else stream.cuda_stream
 
 
 def dopr_quantize_rows(x, q, scale, *, up=None, stream=None):
     """Rows of x [rows, width] (or SiLU(x) * up) in 8-bit integers: q int8
     [rows, width], scale fp32 [rows]."""
-    import torch
-    shape, dt = x.shape, x.dtype
-    rows, width = shape
-    _check(lib().dopr_quantize_rows(
-        _pack_quantize(_dtype_code(x, "x"), rows, width,
-                       *_matrix(x, "x", shape, dt),
-                       *_matrix(up, "up", shape, dt),
-                       *_matrix(q, "q", shape, torch.int8),
-                       _vector(scale, "scale", rows, torch.float32)),
-        _stream(stream)))
+    _check(_compiled().quantize_rows(x, q, scale, up, _handle(stream)))
 
 
 def dopr_quant_matmul_workspace(rows: int, cols: int, depth: int) -> int:
@@ -684,22 +637,8 @@ def dopr_quant_matmul(x, x_scale, w, w_scale, y, *, bias=None, residual=None,
     """y [M, N] = (x w^T) * x_scale * w_scale (+ bias) (+ residual) with x
     int8 [M, K] and w int8 [N, K]; y, bias [N] and residual [M, N] share one
     type.  y may be the residual."""
-    import torch
-    m, k = x.shape
-    n = w.shape[0]
-    dt, i8, f32 = y.dtype, torch.int8, torch.float32
-    _check(lib().dopr_quant_matmul(
-        _pack_product(_dtype_code(y, "y"), m, n, k,
-                      *_matrix(x, "x", (m, k), i8),
-                      _vector(x_scale, "x_scale", m, f32),
-                      *_matrix(w, "w", (n, k), i8),
-                      _vector(w_scale, "w_scale", n, f32),
-                      _vector(bias, "bias", n, dt),
-                      *_matrix(residual, "residual", (m, n), dt),
-                      *_matrix(y, "y", (m, n), dt),
-                      0 if workspace is None else workspace.data_ptr(),
-                      0 if workspace is None else workspace.nbytes),
-        _stream(stream)))
+    _check(_compiled().quant_matmul(x, x_scale, w, w_scale, y, bias,
+                                     residual, workspace, _handle(stream)))
 
 
 def dopr_norm_residual(x, *, residual=None, post_norm_w=None, gate=None,
@@ -709,43 +648,9 @@ def dopr_norm_residual(x, *, residual=None, post_norm_w=None, gate=None,
     z = norm(h, pre_norm_w), z also or instead in 8 bits (q int8 [rows,
     width], q_scale fp32 [rows]).  gate is [width] or [rows, width]; residual
     and h share one type, x's or fp32."""
-    import torch
-    shape, dt = x.shape, x.dtype
-    rows, width = shape
-    code = _dtype_code(x, "x")
-    # residual and h: x's type, or fp32 kept wider than it
-    rt = (residual if residual is not None else x if h is None else h).dtype
-    if rt is not dt and rt is not torch.float32:
-        raise ValueError(f"residual and h must be {dt} or float32")
-    _check(lib().dopr_norm_residual(
-        _pack_norm(code, _dtypes[rt], rows, width,
-                   *_matrix(x, "x", shape, dt),
-                   _vector(post_norm_w, "post_norm_w", width, dt),
-                   *((_vector(gate, "gate", width, dt), 0)
-                     if gate is not None and gate.dim() == 1 else
-                     _matrix(gate, "gate", shape, dt)),
-                   *_matrix(residual, "residual", shape, rt),
-                   _vector(pre_norm_w, "pre_norm_w", width, dt),
-                   residual_scale, rms_eps, *_matrix(h, "h", shape, rt),
-                   *_matrix(z, "z", shape, dt),
-                   *_matrix(q, "q", shape, torch.int8),
-                   _vector(q_scale, "q_scale", rows, torch.float32)),
-        _stream(stream)))
-
-
-def _heads(x, out, name, rows, d, dt):
-    """Both tensors' addresses and strides for [rows, heads, d]."""
-    if x is None:
-        return 0, 0, 0, 0, 0, 0
-    shape = (rows, x.shape[1], d)
-    parts = ()
-    for t, what in ((x, name), (out, name + "_out")):
-        s = t.stride()
-        if (t.dtype is not dt or t.shape != shape or not t.is_cuda or
-                (s[2] != 1 and d > 1)):
-            _refuse(t, what, shape, dt)
-        parts += (t.data_ptr(), s[0], s[1])
-    return parts
+    _check(_compiled().norm_residual(x, residual, post_norm_w, gate,
+                                      residual_scale, pre_norm_w, h, z, q,
+                                      q_scale, rms_eps, _handle(stream)))
 
 
 def dopr_rotary(q, k, positions, inv_freq, q_out, k_out, *, interleaved=False,
@@ -755,25 +660,9 @@ def dopr_rotary(q, k, positions, inv_freq, q_out, k_out, *, interleaved=False,
     D] and k [rows, Hkv, D]; either may be None.  positions int32 [rows];
     inv_freq fp32 [R/2] rotates the first R elements of a head.  Outputs may
     be the inputs."""
-    import torch
-    first = q if q is not None else k
-    if first is None:
-        raise ValueError("q and k are both None")
-    rows, _, d = first.shape
-    dt = first.dtype
-    half = inv_freq.numel()
-    _check(lib().dopr_rotary(
-        _pack_rotary(_dtype_code(first, "q"), 0 if q is None else q.shape[1],
-                     0 if k is None else k.shape[1], d, 2 * half,
-                     bool(interleaved), bool(inverse), attention_factor,
-                     rms_eps, rows,
-                     _vector(positions, "positions", rows, torch.int32),
-                     _vector(inv_freq, "inv_freq", half, torch.float32),
-                     *_heads(q, q_out, "q", rows, d, dt),
-                     *_heads(k, k_out, "k", rows, d, dt),
-                     _vector(q_norm_w, "q_norm_w", d, dt),
-                     _vector(k_norm_w, "k_norm_w", d, dt)),
-        _stream(stream)))
+    _check(_compiled().rotary(q, k, positions, inv_freq, q_out, k_out,
+                               interleaved, inverse, attention_factor,
+                               q_norm_w, k_norm_w, rms_eps, _handle(stream)))
 
 
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3, "bands": 4}

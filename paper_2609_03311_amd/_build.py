@@ -1,4 +1,5 @@
-"""Build libdopr.so (HIP, gfx950) in-tree with hipcc.
+"""Build libdopr.so (HIP, gfx950) in-tree with hipcc, and the Python
+binding's compiled module beside it with g++.
 
 Every translation unit is compiled for gfx950 only, with packed-fp32
 instruction selection disabled, then linked into one shared library next to
@@ -22,6 +23,9 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libdopr.so")
+# the compiled half of the Python binding (host code only)
+BINDING = "binding.cpp"
+BINDING_LIB = os.path.join(HERE, "_operators.so")
 TIMERS_BUILD = os.path.join(HERE, "_build", "timers")
 TIMERS_LIB = os.path.join(HERE, "libdopr_timers.so")
 SOURCES = ["api.hip", "store.hip", "group.hip", "plan.hip", "attn.hip",
@@ -64,12 +68,48 @@ def _compile(src: str, build_dir: str = BUILD, defs=()) -> str:
     return obj
 
 
+def _compile_binding() -> str:
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    obj = os.path.join(BUILD, "binding.o")
+    abi = int(torch._C._GLIBCXX_USE_CXX11_ABI)
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={abi}", "-D__HIP_PLATFORM_AMD__=1",
+           "-I", os.path.join(ROOT, "include"),
+           "-I", sysconfig.get_paths()["include"]]
+    for path in cpp_extension.include_paths():
+        cmd += ["-isystem", path]
+    cmd += ["-isystem", os.path.join(os.path.dirname(os.path.dirname(
+        os.path.realpath(hipcc()))), "include"),
+            "-c", os.path.join(CSRC, BINDING), "-o", obj]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for {BINDING}:\n{r.stderr}")
+    return obj
+
+
+def _link_binding(obj: str) -> None:
+    import torch
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    tmp = BINDING_LIB + ".tmp"
+    cmd = ["g++", "-shared", "-o", tmp, obj, "-L", HERE, "-l:libdopr.so",
+           "-L", libs, "-ltorch_python", "-ltorch_cpu", "-lc10_hip", "-lc10",
+           "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{libs}"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"link of {BINDING} failed:\n{r.stderr}")
+    os.replace(tmp, BINDING_LIB)
+
+
 def build(verbose: bool = False, timers: bool = False) -> str:
     build_dir = TIMERS_BUILD if timers else BUILD
     lib = TIMERS_LIB if timers else LIB
     defs = ("-DDOPR_PASS_TIMERS",) if timers else ()
     os.makedirs(build_dir, exist_ok=True)
     with cf.ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
+        binding = None if timers else ex.submit(_compile_binding)
         objs = list(ex.map(lambda s: _compile(s, build_dir, defs), SOURCES))
     tmp = lib + ".tmp"
     cmd = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp,
@@ -78,6 +118,8 @@ def build(verbose: bool = False, timers: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")
     os.replace(tmp, lib)
+    if binding is not None:
+        _link_binding(binding.result())
     if verbose:
         print(f"built {lib}")
     return lib
