@@ -10,9 +10,10 @@
 // and 16 rows of x as the second: lane l holds 16 consecutive bytes (depth
 // 16 * (l / 16) ..) of row l % 16 of each, and of the result column l % 16 (a
 // row of x) at rows 4 * (l / 16) .. + 3 (of w).  A wave's 64 rows of w are
-// dealt to its four operands so that a lane's 16 results of one x row are 16
-// consecutive columns of y: operand f, row i is w row
-// 16 * (i / 4) + 4 * f + i % 4.
+// dealt to its four operands so that a lane's 16 results of one x row are two
+// runs of 8 consecutive columns of y, 32 apart, and the four lanes that hold
+// an x row store 64 whole bytes of it at a time (bf16): operand f, row i is w
+// row 32 * (f / 2) + 8 * (i / 4) + 4 * (f % 2) + i % 4.
 #include <type_traits>
 
 #include "rowio.hpp"
@@ -32,84 +33,92 @@ struct ProductParams {
   int32_t splits;  // 1: y is written at once
 };
 
-// Elements between rows of the sums: stores of 16 need no bound.
+// Elements between rows of the sums: runs of 8 need no bound but their first.
 __host__ __device__ inline int64_t parts_row(int64_t N) {
-  return (N + 15) & ~(int64_t)15;
+  return (N + 7) & ~(int64_t)7;
 }
 
 // w row (of 64) behind LDS row p
 __device__ __forceinline__ int w_row(int p) {
-  return (p & ~63) + ((p & 15) >> 2) * 16 + ((p >> 4) & 3) * 4 + (p & 3);
+  return (p & ~63) + (p & 32) + ((p >> 2) & 3) * 8 + ((p >> 4) & 1) * 4 +
+         (p & 3);
+}
+// first column of a lane's two runs, among a wave's 64
+__device__ __forceinline__ int lane_column(int lane) {
+  return (lane >> 4) * 8;
+}
+constexpr int kRunApart = 32;
+
+// Finishes a lane's part of a tile: two runs of 8 columns of y, from n and n +
+// kRunApart on, in the FM rows m, m + 16, .. with own(i).  sums(i, v) gives row
+// i's integer sums, column_scales(scale) and row_scale(i) the scales.
+template <typename T, int FM, typename Columns, typename Row, typename Sums,
+          typename Own>
+__device__ __forceinline__ void finish(const ProductParams &P, int m, int n,
+                                       Columns &&column_scales,
+                                       Row &&row_scale, Sums &&sums,
+                                       Own &&own) {
+  const int left = (int)P.N - n;
+  if (left <= 0) return;
+  float scale[16];
+  column_scales(scale);
+  const T *bias = static_cast<const T *>(P.bias) + n;
+  const T *res = static_cast<const T *>(P.res) + m * P.ldr + n;
+  T *y = static_cast<T *>(P.y) + m * P.ldy + n;
+  const bool whole = left >= kRunApart + 8;
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    if (own(i) && m + 16 * i < (int)P.M) {
+      float v[16];
+      const float xs = row_scale(i);
+      sums(i, v);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = v[e] * xs * scale[e];
+      if (whole) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float *u = v + 8 * h, f[8];
+          Raw8<T> r;
+          if (P.bias) {
+            r.load(bias + kRunApart * h);
+            r.get(f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] += f[e];
+          }
+          if (P.res) {
+            r.load(res + kRunApart * h);
+            r.get(f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] += f[e];
+          }
+          store8<T>(y + kRunApart * h, 0, u);
+        }
+      } else {  // the matrix ends inside: one by one
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int c = kRunApart * (e >> 3) + (e & 7);
+          if (c < left) {
+            if (P.bias) v[e] += to_f32<T>(bias[c]);
+            if (P.res) v[e] += to_f32<T>(res[c]);
+            y[c] = from_f32<T>(v[e]);
+          }
+        }
+      }
+    }
+    y += 16 * P.ldy;
+    if (P.res) res += 16 * P.ldr;
+    __builtin_amdgcn_sched_barrier(0);  // (one row's values at a time)
+  }
 }
 
-// Finishes 16 consecutive columns of y, row by row: the columns' scales are
-// read once and the rows' addresses stepped from one to the next.
-template <typename T>
-struct Columns {
-  float scale[16];
-  const T *bias, *res;
-  T *y;
-  const float *x_scale;
-  int m, left;  // row, columns to the end of the row
-  __device__ __forceinline__ Columns(const ProductParams &P, int m0, int n)
-      : m(m0), left((int)P.N - n) {
-    const float *s = P.w_scale + n;
-    if (left >= 16) {
+// The scales of finish from memory.
+__device__ __forceinline__ void columns_from_memory(const ProductParams &P,
+                                                    int n, float *scale) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        Raw8<float> r;
-        r.load(s + 8 * h);
-        r.get(scale + 8 * h);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) scale[e] = s[min(e, left - 1)];
-    }
-    bias = static_cast<const T *>(P.bias) + n;
-    res = static_cast<const T *>(P.res) + m * P.ldr + n;
-    y = static_cast<T *>(P.y) + m * P.ldy + n;
-    x_scale = P.x_scale + m;
-  }
-  // `rows` rows further down
-  __device__ __forceinline__ void next(const ProductParams &P, int rows) {
-    m += rows;
-    x_scale += rows;
-    y += rows * P.ldy;
-    if (P.res) res += rows * P.ldr;
-  }
-  // v: the row's integer sums
-  __device__ __forceinline__ void store(const ProductParams &P, float *v) const {
-    if (m >= (int)P.M) return;
-    const float xs = *x_scale;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) v[e] = v[e] * xs * scale[e];
-    if (left >= 16) {
-      if (P.bias) add16(bias, v);
-      if (P.res) add16(res, v);
-      store8<T>(y, 0, v);
-      store8<T>(y + 8, 0, v + 8);
-      return;
-    }
-#pragma unroll
-    for (int e = 0; e < 15; ++e)
-      if (e < left) {
-        if (P.bias) v[e] += to_f32<T>(bias[e]);
-        if (P.res) v[e] += to_f32<T>(res[e]);
-        y[e] = from_f32<T>(v[e]);
-      }
-  }
-  static __device__ __forceinline__ void add16(const T *p, float *v) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float b[8];
-      Raw8<T> r;
-      r.load(p + 8 * h);
-      r.get(b);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[8 * h + e] += b[e];
-    }
-  }
-};
+  for (int e = 0; e < 16; ++e)
+    scale[e] = P.w_scale[min(n + kRunApart * (e >> 3) + (e & 7),
+                             (int)P.N - 1)];
+}
 
 // 16 bytes of a row from depth k, zeros from K on.  Nothing behind the row is
 // read: the row's last 16 bytes, shifted down.
@@ -221,19 +230,16 @@ __global__ __launch_bounds__(256, 3) void k_product_any(ProductParams P,
               wf[j], xf[i], acc[i][j], 0, 0, 0);
     }
   }
-  const int n = n0 + wn + 16 * (lane >> 4);
-  if (n >= (int)P.N) return;
-  Columns<T> columns(P, m0 + wm + (lane & 15), n);
+  const int m = m0 + wm + (lane & 15), n = n0 + wn + lane_column(lane);
+  finish<T, 2>(
+      P, m, n,
+      [&](float *scale) { columns_from_memory(P, n, scale); },
+      [&](int i) { return P.x_scale[m + 16 * i]; },
+      [&](int i, float *v) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    float v[16];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[4 * j + e] = (float)acc[i][j][e];
-    columns.store(P, v);
-    columns.next(P, 16);
-  }
+        for (int e = 0; e < 16; ++e) v[e] = (float)acc[i][e >> 2][e & 3];
+      },
+      [](int) { return true; });
 }
 
 template <typename T>
@@ -275,8 +281,17 @@ __device__ __forceinline__ void dma16(uint32_t lds, const int8_t *at,
                : "m0");
 }
 
-// At most `left` of this wave's loads are on their way, its LDS reads have
-// returned, and every wave is here.
+// 64 lanes' 4 bytes each, in the same way.
+__device__ __forceinline__ void dma4(uint32_t lds, const float *at) {
+  lds = __builtin_amdgcn_readfirstlane(lds);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\t"
+               "global_load_lds_dword %1, off"
+               :: "s"(lds), "v"(at)
+               : "m0");
+}
+
+// At most `left` of this wave's loads and stores are on their way (they
+// complete in order), its LDS reads have returned, and every wave is here.
 template <int left>
 __device__ __forceinline__ void stage_wait() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(left)
@@ -315,10 +330,14 @@ k_product(ProductParams P, int tm, int tn) {
   constexpr int kBlocks = (kBM + kBN) / 8;
   constexpr int kLoads = (kBlocks + kWaves - 1) / kWaves;
   constexpr int kStageBytes = (kBM + kBN) * kSpan;
-  static_assert((ST - 1) * kLoads < 64, "loads on their way are countable");
+  constexpr int kScaleSlots = (kBM + kBN + 63) / 64 * 64;
+  // a whole tile's stores, left on their way while the next tile starts
+  constexpr int kStores = WK == 1 ? FM * (int)sizeof(T) : 0;
+  static_assert((ST - 1) * kLoads + kStores < 64, "countable by vmcnt");
   static_assert(WK == 1 || kBM * kBN * 4 <= ST * kStageBytes,
                 "a group's sums fit its buffers");
-  extern __shared__ u32x4 lds_all[];  // [WK][ST][x rows | w rows]
+  // [WK][ST][x rows | w rows], then two tiles' scales [x rows | w rows]
+  extern __shared__ u32x4 lds_all[];
   const int lane = threadIdx.x & 63;
   const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = wave_all / kWaves, wave = wave_all % kWaves;
@@ -367,6 +386,23 @@ k_product(ProductParams P, int tm, int tn) {
           (blk >= kBM / 8 ? wbase : xbase) +
               (int64_t)(t * WK + group) * kSpan,
           off[i]);
+  };
+  // the tile's scales, to the half of theirs that its turn picks
+  float *scale_lds = reinterpret_cast<float *>(
+      lds_all + WK * ST * (kStageBytes / 16));
+  int turn = 0;
+  auto issue_scales = [&]() {
+    if (group == 0)
+#pragma unroll
+      for (int r0 = wave * 64; r0 < kBM + kBN; r0 += kWaves * 64) {
+        // (64 at a time: x and w meet inside one where BM is not 64 times
+        // something; lanes behind the last row repeat it)
+        const int r = min(r0 + lane, kBM + kBN - 1);
+        const float *at =
+            r < kBM ? P.x_scale + min(m0 + r, (int)P.M - 1)
+                    : P.w_scale + min(n0 + r - kBM, (int)P.N - 1);
+        dma4(lds_address(scale_lds + turn * kScaleSlots + r0), at);
+      }
   };
   auto issue_first = [&](int spans) {
 #pragma unroll 1
@@ -419,7 +455,9 @@ k_product(ProductParams P, int tm, int tn) {
 
   int tile = blockIdx.x;
   take(tile);
-  bool loading = false;  // the tile's first ST spans are on their way
+  issue_scales();
+  bool loading = false;  // the tile's first ST spans are on their way,
+  bool storing = false;  // and the stores of a whole tile behind them
   while (true) {
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -460,7 +498,9 @@ k_product(ProductParams P, int tm, int tn) {
       issue_first(ST);
     }
     if (full > 0) {
-      if (mine >= ST)
+      if (mine >= ST && storing)
+        stage_wait<(ST - 1) * kLoads + kStores>();
+      else if (mine >= ST)
         stage_wait<(ST - 1) * kLoads>();
       else
         stage_wait<0>();
@@ -472,7 +512,11 @@ k_product(ProductParams P, int tm, int tn) {
       int t = 0;
       for (; t + ST < common; ++t) {
         step(xa, wa, t, 1, xb, wb, t + ST - 1, kHalf, kLoads, t > 0, true);
-        stage_wait<(ST - 2) * kLoads>();
+        // (spans issued ahead of the stores need not wait for them)
+        if (storing && t < ST - 1)
+          stage_wait<(ST - 2) * kLoads + kStores>();
+        else
+          stage_wait<(ST - 2) * kLoads>();
         step(xb, wb, t + 1, 0, xa, wa, t + ST, 0, kHalf, true, true);
       }
 #pragma unroll 1
@@ -511,42 +555,49 @@ k_product(ProductParams P, int tm, int tn) {
     }
     // every wave is behind the last barrier, so all buffers are free: the
     // next tile's first loads go out before this one is finished
-    const int m = m0 + wm + (lane & 15), n = n0 + wn + 16 * (lane >> 4);
+    if (full == 0) stage_wait<0>();  // (the scales: else they came first)
+    const int m = m0 + wm + (lane & 15), n = n0 + wn + lane_column(lane);
+    const float *tile_scale = scale_lds + turn * kScaleSlots;
     tile += gridDim.x;
     const bool more = tile < tm * tn;
+    storing = kStores > 0 && P.splits == 1 && m0 + kBM <= (int)P.M &&
+              n0 + kBN <= (int)P.N;
     if (more) {
       if (WK > 1) __syncthreads();  // (the sums have been read)
       take(tile);
+      turn ^= 1;
+      issue_scales();
       loading = !rest;
       if (loading) issue_first(ST);
+      storing &= loading;
     }
-    if (n < (int)P.N) {
-      if (P.splits > 1) {
-        const int64_t row = parts_row(P.N);
-        int32_t *to = P.parts + (part * P.M + m) * row + n;
+    auto own = [&](int i) { return WK == 1 || i % WK == group; };
+    if (P.splits > 1) {
+      const int64_t row = parts_row(P.N);
+      int32_t *to = P.parts + (part * P.M + m) * row + n;
 #pragma unroll
-        for (int i = 0; i < FM; ++i, to += 16 * row) {
-          if ((WK > 1 && i % WK != group) || m + 16 * i >= (int)P.M) continue;
+      for (int i = 0; i < FM; ++i, to += 16 * row) {
+        if (!own(i) || m + 16 * i >= (int)P.M) continue;
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            reinterpret_cast<i32x4 *>(to)[j] = acc[i][j];
-        }
-      } else {
-        Columns<T> columns(P, m, n);
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-          if (WK == 1 || i % WK == group) {
-            float v[16];
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) v[4 * j + e] = (float)acc[i][j][e];
-            columns.store(P, v);
-          }
-          columns.next(P, 16);
-          __builtin_amdgcn_sched_barrier(0);  // (one row's values at a time)
-        }
+        for (int j = 0; j < 4; ++j)
+          if (n + kRunApart * (j >> 1) < (int)P.N)
+            reinterpret_cast<i32x4 *>(to)[8 * (j >> 1) + (j & 1)] = acc[i][j];
       }
+    } else {
+      finish<T, FM>(
+          P, m, n,
+          [&](float *scale) {
+            const float *s = tile_scale + kBM + wn + lane_column(lane);
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              scale[e] = s[kRunApart * (e >> 3) + (e & 7)];
+          },
+          [&](int i) { return tile_scale[wm + 16 * i + (lane & 15)]; },
+          [&](int i, float *v) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = (float)acc[i][e >> 2][e & 3];
+          },
+          own);
     }
     if (!more) break;
   }
@@ -556,7 +607,8 @@ template <typename T, int FM, int WGM, int WGN, int WK, int ST>
 hipError_t product_tiles(const ProductParams &P, hipStream_t s) {
   constexpr int kBM = 16 * FM * WGM, kBN = 64 * WGN;
   constexpr int kThreads = 64 * WGM * WGN * WK;
-  constexpr size_t kLds = (size_t)ST * WK * (kBM + kBN) * kSpan;
+  constexpr size_t kLds = (size_t)ST * WK * (kBM + kBN) * kSpan +
+                          2 * ((kBM + kBN + 63) / 64 * 64) * sizeof(float);
   static_assert(kLds <= 160 * 1024, "LDS of a CU");
   // blocks a CU holds at once, by LDS and by registers
   constexpr int kByLds = (int)(160 * 1024 / kLds);
@@ -691,30 +743,41 @@ hipError_t product_few(const ProductParams &P, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The sums of a split depth, added and finished: 16 results a thread.
+// The sums of a split depth, added and finished: 16 results a thread, the
+// columns of four threads side by side as a wave's.
 template <typename T>
 __global__ __launch_bounds__(256) void k_product_sum(ProductParams P) {
-  const int64_t row = parts_row(P.N) / 16;
+  const int row = (int)parts_row(P.N);
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= P.M * row) return;
-  const int64_t m = i / row, n = (i - m * row) * 16;
-  const i32x4 *p = reinterpret_cast<const i32x4 *>(
-      P.parts + m * parts_row(P.N) + n);
-  i32x4 s[4] = {p[0], p[1], p[2], p[3]};
-  for (int k = 1; k < P.splits; ++k) {
-    p += P.M * row * 4;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) s[j] += p[j];
+  const int per = (row + 63) / 64 * 4;
+  const int64_t m = i / per;
+  const int c = (int)(i - m * per), n = (c >> 2) * 64 + (c & 3) * 8;
+  if (m >= P.M || n >= (int)P.N) return;
+  const bool two = n + kRunApart < (int)P.N;
+  const i32x4 *p = reinterpret_cast<const i32x4 *>(P.parts + m * row + n);
+  i32x4 s[4] = {};
+  for (int k = 0; k < P.splits; ++k, p += P.M * (row / 4)) {
+    s[0] += p[0];
+    s[1] += p[1];
+    if (two) {
+      s[2] += p[8];
+      s[3] += p[9];
+    }
   }
-  float v[16];
+  finish<T, 1>(
+      P, (int)m, n,
+      [&](float *scale) { columns_from_memory(P, n, scale); },
+      [&](int) { return P.x_scale[m]; },
+      [&](int, float *v) {
 #pragma unroll
-  for (int e = 0; e < 16; ++e) v[e] = (float)s[e >> 2][e & 3];
-  Columns<T>(P, (int)m, (int)n).store(P, v);
+        for (int e = 0; e < 16; ++e) v[e] = (float)s[e >> 2][e & 3];
+      },
+      [](int) { return true; });
 }
 
 template <typename T>
 hipError_t product_sum(const ProductParams &P, hipStream_t s) {
-  const int64_t n = P.M * (parts_row(P.N) / 16);
+  const int64_t n = P.M * ((parts_row(P.N) + 63) / 64 * 4);
   hipLaunchKernelGGL((k_product_sum<T>), dim3((unsigned)((n + 255) / 256)),
                      dim3(256), 0, s, P);
   return hipGetLastError();
