@@ -631,17 +631,17 @@ hipError_t product_tiles(const ProductParams &P, hipStream_t s) {
 }
 
 // ---------------------------------------------------------------------------
-// Few rows: a block's WK waves share one strip of 16 w rows and split the
+// Few rows: a block's four waves share one strip of 16 w rows and split the
 // depth, in batches of 4 steps of 64 bytes, each wave's operands coming
 // straight from memory to its registers, one batch ahead of the products.
 // The waves' sums meet in LDS (integers: the split does not show).
 
-// 4 results of y row m from column n on.
+// 4 results of y row m from column n on (m and n inside), with the scales xs
+// and scale[0..3].
 template <typename T>
 __device__ __forceinline__ void store4(const ProductParams &P, int64_t m,
-                                       int64_t n, const i32x4 &acc) {
-  if (m >= P.M || n >= P.N) return;
-  const float xs = P.x_scale[m];
+                                       int64_t n, const i32x4 &acc, float xs,
+                                       const float *scale) {
   const T *bias = static_cast<const T *>(P.bias);
   const T *res = static_cast<const T *>(P.res) + m * P.ldr;
   T *y = static_cast<T *>(P.y) + m * P.ldy;
@@ -650,19 +650,31 @@ __device__ __forceinline__ void store4(const ProductParams &P, int64_t m,
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const int64_t c = n + min(e, left - 1);
-    v[e] = (float)acc[e] * xs * P.w_scale[c];
+    v[e] = (float)acc[e] * xs * scale[e];
     if (P.bias) v[e] += to_f32<T>(bias[c]);
     if (P.res) v[e] += to_f32<T>(res[c]);
   }
+  if (left == 4) {
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<u32x2_any *>(y + n) =
+          u32x2{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
+    else
+      *reinterpret_cast<u32x4_any *>(y + n) =
+          u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]),
+                __float_as_uint(v[2]), __float_as_uint(v[3])};
+    return;
+  }
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
+  for (int e = 0; e < 3; ++e)
     if (e < left) y[n + e] = from_f32<T>(v[e]);
 }
 
-constexpr int kFewSteps = 4;
+constexpr int kFewWaves = 4;   // 8 and 16, and batches of 2 to 8 steps,
+constexpr int kFewSteps = 4;   // measured no faster at any size
 
-template <typename T, int FM, int WK>
-__global__ __launch_bounds__(64 * WK) void k_product_few(ProductParams P) {
+template <typename T, int FM>
+__global__ __launch_bounds__(256) void k_product_few(ProductParams P) {
+  constexpr int WK = kFewWaves;
   __shared__ i32x4 sums[WK][FM][64];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -675,6 +687,13 @@ __global__ __launch_bounds__(64 * WK) void k_product_few(ProductParams P) {
 #pragma unroll
   for (int i = 0; i < FM; ++i)
     xp[i] = P.x + min(m0 + 16 * i + (lane & 15), P.M - 1) * P.ldx;
+  // wave i < FM finishes x operand i: its scales, ahead of the depth
+  static_assert(FM <= WK);
+  const int64_t m = m0 + 16 * wave + (lane & 15), n = n0 + 4 * (lane >> 4);
+  const float xs = P.x_scale[min(m, P.M - 1)];
+  float scale[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) scale[e] = P.w_scale[min(n + e, P.N - 1)];
   constexpr int kBatch = kFewSteps * kStep;
   i32x4 acc[FM] = {};
   struct Batch {
@@ -726,20 +745,20 @@ __global__ __launch_bounds__(64 * WK) void k_product_few(ProductParams P) {
 #pragma unroll
   for (int i = 0; i < FM; ++i) sums[wave][i][lane] = acc[i];
   __syncthreads();
-  for (int i = wave; i < FM; i += WK) {
-    i32x4 s = sums[0][i][lane];
+  if (wave < FM && m < P.M && n < P.N) {
+    i32x4 s = sums[0][wave][lane];
 #pragma unroll
-    for (int w = 1; w < WK; ++w) s += sums[w][i][lane];
-    store4<T>(P, m0 + 16 * i + (lane & 15), n0 + 4 * (lane >> 4), s);
+    for (int w = 1; w < WK; ++w) s += sums[w][wave][lane];
+    store4<T>(P, m, n, s, xs, scale);
   }
 }
 
-template <typename T, int FM, int WK>
+template <typename T, int FM>
 hipError_t product_few(const ProductParams &P, hipStream_t s) {
   const unsigned strips = (unsigned)((P.N + 15) / 16);
   const unsigned rows = (unsigned)((P.M + 16 * FM - 1) / (16 * FM));
-  hipLaunchKernelGGL((k_product_few<T, FM, WK>), dim3(strips, rows),
-                     dim3(64 * WK), 0, s, P);
+  hipLaunchKernelGGL((k_product_few<T, FM>), dim3(strips, rows),
+                     dim3(64 * kFewWaves), 0, s, P);
   return hipGetLastError();
 }
 
@@ -878,12 +897,13 @@ bool aligned_rows(const ProductParams &P) {
 template <typename T>
 hipError_t product(ProductParams P, hipStream_t s) {
   if (P.M <= kFewRows) {
-    // four waves share a strip's depth where the strips alone fill the CUs,
-    // else eight: 16 rows through 24576 x 4096 (1,536 strips) take 28.9 and
-    // 31.9 us, through 4096 x 12288 (256) 17.2 and 16.8, one row 13.3 and 12.4
-    const int64_t strips = (P.N + 15) / 16;
-    if (strips < 1024) return product_few<T, 1, 8>(P, s);
-    return product_few<T, 1, 4>(P, s);
+    // the loads of a whole operand cost the few-row blocks as much as w's:
+    // from 9 rows, wide and deep products go through LDS tiles instead (16
+    // rows through 6144 x 4096 10.4 and 8.4 us, through 24576 x 4096 28.7 and
+    // 25.0, but through 4096 x 12288 17.2 and 24.0, 6144 x 1024 5.0 and 5.7)
+    if (P.M > 8 && P.N >= 6144 && P.K >= 4096 && aligned_rows(P))
+      return product_tiles<T, 1, 1, 1, 4, 3>(P, s);
+    return product_few<T, 1>(P, s);
   }
   int kernel = choose(P.M, P.N, P.K);
   if (!aligned_rows(P) && kernel != kFew) return product_any<T>(P, s);
@@ -903,7 +923,7 @@ hipError_t product(ProductParams P, hipStream_t s) {
     case kTile48Four:
     case kTile48FourSplit: e = product_tiles<T, 3, 1, 1, 4, 2>(P, s); break;
     case kTile32Four: e = product_tiles<T, 1, 2, 1, 4, 3>(P, s); break;
-    case kFew: e = product_few<T, 2, 4>(P, s); break;
+    case kFew: e = product_few<T, 2>(P, s); break;
   }
   if (e == hipSuccess && P.splits > 1) e = product_sum<T>(P, s);
   return e;
