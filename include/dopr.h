@@ -496,9 +496,11 @@ dopr_status_t dopr_quantize_rows(const dopr_quantize_args_t *args,
  *   y[m, n] = (sum_k x[m, k] w[n, k]) * x_scale[m] * w_scale[n]
  *             + bias[n] + residual[m, n]
  * The integer sum is exact (32 bits).  y may be the residual (same address
- * and stride).  The bytes between a row's end and its stride are never read.
- * Rows on 16-byte addresses (x, w and both strides multiples of 16) take the
- * fast kernels.                                                            */
+ * and stride).  The bytes between a row's end and its stride are never
+ * read.  Rows on 16-byte addresses (x, w and both strides multiples of 16)
+ * are multiplied where they lie; others are first laid out again in the
+ * workspace, if there is one, else multiplied by a slower kernel (the results
+ * are the same).                                                           */
 typedef struct {
   int32_t dtype;            /* of bias, residual and y                      */
   int64_t rows;             /* M >= 0                                       */
@@ -515,13 +517,16 @@ typedef struct {
   int64_t residual_row_stride;
   void *y;                  /* dev [M, N]                                   */
   int64_t y_row_stride;
-  void *workspace;          /* dev scratch, 256-byte aligned, of at least
-                               dopr_quant_matmul_workspace() bytes (NULL
-                               where that is 0)                             */
+  void *workspace;          /* dev scratch, 256-byte aligned, or NULL: used
+                               for rows off 16-byte addresses when it holds
+                               (rows + cols) * (depth rounded up to 128)
+                               bytes                                        */
   size_t workspace_bytes;
 } dopr_quant_matmul_args_t;
 
-/* Workspace bytes for these rows, cols and depth (host arithmetic). */
+/* Workspace bytes worth giving a product of these rows, cols and depth, by
+ * sizes alone (host arithmetic): 0 up to 16 rows and where 16 divides the
+ * depth, so that rows can be expected on 16-byte addresses.                */
 dopr_status_t dopr_quant_matmul_workspace(const dopr_quant_matmul_args_t *args,
                                           size_t *bytes);
 

@@ -623,7 +623,8 @@ def dopr_quantize_rows(x, q, scale, *, up=None, stream=None):
 
 
 def dopr_quant_matmul_workspace(rows: int, cols: int, depth: int) -> int:
-    """Workspace bytes of a product (host arithmetic; 0: none is needed)."""
+    """Workspace bytes worth giving a product of these sizes (host
+    arithmetic; 0: none is used)."""
     a = _QuantMatmulArgs()
     a.rows, a.cols, a.depth = rows, cols, depth
     n = ctypes.c_size_t(0)
@@ -636,7 +637,8 @@ def dopr_quant_matmul(x, x_scale, w, w_scale, y, *, bias=None, residual=None,
                       workspace=None, stream=None):
     """y [M, N] = (x w^T) * x_scale * w_scale (+ bias) (+ residual) with x
     int8 [M, K] and w int8 [N, K]; y, bias [N] and residual [M, N] share one
-    type.  y may be the residual."""
+    type.  y may be the residual.  Rows off 16-byte addresses go faster with
+    a workspace."""
     _check(_compiled().quant_matmul(x, x_scale, w, w_scale, y, bias,
                                      residual, workspace, _handle(stream)))
 

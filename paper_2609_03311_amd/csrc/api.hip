@@ -1025,16 +1025,8 @@ dopr_status_t dopr_quant_matmul(const dopr_quant_matmul_args_t *a,
       !aligned_to(a->bias, a->dtype) || !aligned_to(a->residual, a->dtype) ||
       !aligned_to(a->y, a->dtype))
     return fail(DOPR_ERR_INVALID_ARG, "buffers must be element-aligned");
-  const size_t need = product_workspace(a->rows, a->cols, a->depth);
-  if (need > 0) {
-    if (!a->workspace || a->workspace_bytes < need)
-      return fail(DOPR_ERR_WORKSPACE,
-                  "workspace holds " +
-                      std::to_string(a->workspace ? a->workspace_bytes : 0) +
-                      " bytes, needs " + std::to_string(need));
-    if (reinterpret_cast<uintptr_t>(a->workspace) % kAlign)
-      return fail(DOPR_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-  }
+  if (a->workspace && reinterpret_cast<uintptr_t>(a->workspace) % kAlign)
+    return fail(DOPR_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
   hipError_t e = launch_product(*a, as_stream(stream));
   if (e != hipSuccess) return hip_fail(e, "product launch");
   return ok();

@@ -29,14 +29,7 @@ struct ProductParams {
   const void *bias, *res;
   void *y;
   int64_t M, N, K, ldx, ldw, ldr, ldy;
-  int32_t *parts;  // [splits][M][parts_row(N)] sums of a split depth
-  int32_t splits;  // 1: y is written at once
 };
-
-// Elements between rows of the sums: runs of 8 need no bound but their first.
-__host__ __device__ inline int64_t parts_row(int64_t N) {
-  return (N + 7) & ~(int64_t)7;
-}
 
 // w row (of 64) behind LDS row p
 __device__ __forceinline__ int w_row(int p) {
@@ -342,12 +335,7 @@ k_product(ProductParams P, int tm, int tn) {
   const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = wave_all / kWaves, wave = wave_all % kWaves;
   u32x4 *lds = lds_all + group * (ST * kStageBytes / 16);
-  // this block's share of the depth: whole spans, the rest to the last
-  const int part = blockIdx.y, all_spans = (int)(P.K / kSpan);
-  const int span0 = (int)((int64_t)all_spans * part / P.splits);
-  const int full =
-      (int)((int64_t)all_spans * (part + 1) / P.splits) - span0;
-  const int rest = part == P.splits - 1 ? (int)(P.K % kSpan) : 0;
+  const int full = (int)(P.K / kSpan), rest = (int)(P.K % kSpan);
   const int common = full / WK;                     // every group's spans
   const int most = (full + WK - 1) / WK;
   const int mine = common + (group < full % WK ? 1 : 0);
@@ -373,8 +361,8 @@ k_product(ProductParams P, int tm, int tn) {
     tile_of(b, tm, tn, bm, bn);
     m0 = bm * kBM;
     n0 = bn * kBN;
-    xbase = P.x + (int64_t)m0 * P.ldx + (int64_t)span0 * kSpan;
-    wbase = P.w + (int64_t)n0 * P.ldw + (int64_t)span0 * kSpan;
+    xbase = P.x + (int64_t)m0 * P.ldx;
+    wbase = P.w + (int64_t)n0 * P.ldw;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
       off[i] = row_offset(block_of(i)) + chunk_of(block_of(i));
@@ -560,7 +548,7 @@ k_product(ProductParams P, int tm, int tn) {
     const float *tile_scale = scale_lds + turn * kScaleSlots;
     tile += gridDim.x;
     const bool more = tile < tm * tn;
-    storing = kStores > 0 && P.splits == 1 && m0 + kBM <= (int)P.M &&
+    storing = kStores > 0 && m0 + kBM <= (int)P.M &&
               n0 + kBN <= (int)P.N;
     if (more) {
       if (WK > 1) __syncthreads();  // (the sums have been read)
@@ -572,33 +560,20 @@ k_product(ProductParams P, int tm, int tn) {
       storing &= loading;
     }
     auto own = [&](int i) { return WK == 1 || i % WK == group; };
-    if (P.splits > 1) {
-      const int64_t row = parts_row(P.N);
-      int32_t *to = P.parts + (part * P.M + m) * row + n;
+    finish<T, FM>(
+        P, m, n,
+        [&](float *scale) {
+          const float *s = tile_scale + kBM + wn + lane_column(lane);
 #pragma unroll
-      for (int i = 0; i < FM; ++i, to += 16 * row) {
-        if (!own(i) || m + 16 * i >= (int)P.M) continue;
+          for (int e = 0; e < 16; ++e)
+            scale[e] = s[kRunApart * (e >> 3) + (e & 7)];
+        },
+        [&](int i) { return tile_scale[wm + 16 * i + (lane & 15)]; },
+        [&](int i, float *v) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (n + kRunApart * (j >> 1) < (int)P.N)
-            reinterpret_cast<i32x4 *>(to)[8 * (j >> 1) + (j & 1)] = acc[i][j];
-      }
-    } else {
-      finish<T, FM>(
-          P, m, n,
-          [&](float *scale) {
-            const float *s = tile_scale + kBM + wn + lane_column(lane);
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              scale[e] = s[kRunApart * (e >> 3) + (e & 7)];
-          },
-          [&](int i) { return tile_scale[wm + 16 * i + (lane & 15)]; },
-          [&](int i, float *v) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = (float)acc[i][e >> 2][e & 3];
-          },
-          own);
-    }
+          for (int e = 0; e < 16; ++e) v[e] = (float)acc[i][e >> 2][e & 3];
+        },
+        own);
     if (!more) break;
   }
 }
@@ -624,8 +599,8 @@ hipError_t product_tiles(const ProductParams &P, hipStream_t s) {
       reinterpret_cast<const void *>(kernel),
       hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
   if (allowed != hipSuccess) return allowed;
-  const int64_t grid = P.splits > 1 || tm * tn < slots ? tm * tn : slots;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)grid, (unsigned)P.splits),
+  const int64_t grid = tm * tn < slots ? tm * tn : slots;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid),
                      dim3(kThreads), kLds, s, P, (int)tm, (int)tn);
   return hipGetLastError();
 }
@@ -762,45 +737,28 @@ hipError_t product_few(const ProductParams &P, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The sums of a split depth, added and finished: 16 results a thread, the
-// columns of four threads side by side as a wave's.
-template <typename T>
-__global__ __launch_bounds__(256) void k_product_sum(ProductParams P) {
-  const int row = (int)parts_row(P.N);
+// ---------------------------------------------------------------------------
+// Rows off 16-byte addresses, laid out again in the workspace: w behind x, rows
+// of whole spans, zeros behind the depth.
+
+struct RepackParams {
+  const int8_t *x, *w;
+  int8_t *to;
+  int64_t M, rows, K, ldx, ldw, pitch;
+};
+
+__global__ __launch_bounds__(256) void k_repack(RepackParams P) {
+  const int64_t per = P.pitch / 16;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int per = (row + 63) / 64 * 4;
-  const int64_t m = i / per;
-  const int c = (int)(i - m * per), n = (c >> 2) * 64 + (c & 3) * 8;
-  if (m >= P.M || n >= (int)P.N) return;
-  const bool two = n + kRunApart < (int)P.N;
-  const i32x4 *p = reinterpret_cast<const i32x4 *>(P.parts + m * row + n);
-  i32x4 s[4] = {};
-  for (int k = 0; k < P.splits; ++k, p += P.M * (row / 4)) {
-    s[0] += p[0];
-    s[1] += p[1];
-    if (two) {
-      s[2] += p[8];
-      s[3] += p[9];
-    }
-  }
-  finish<T, 1>(
-      P, (int)m, n,
-      [&](float *scale) { columns_from_memory(P, n, scale); },
-      [&](int) { return P.x_scale[m]; },
-      [&](int, float *v) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = (float)s[e >> 2][e & 3];
-      },
-      [](int) { return true; });
+  const int64_t r = i / per, k = (i - r * per) * 16;
+  if (r >= P.rows) return;
+  const int8_t *row = r < P.M ? P.x + r * P.ldx : P.w + (r - P.M) * P.ldw;
+  u32x4 u = {0u, 0u, 0u, 0u};
+  if (k < P.K) u = row_bytes(row, k, P.K);
+  *reinterpret_cast<u32x4 *>(P.to + r * P.pitch + k) = u;
 }
 
-template <typename T>
-hipError_t product_sum(const ProductParams &P, hipStream_t s) {
-  const int64_t n = P.M * ((parts_row(P.N) + 63) / 64 * 4);
-  hipLaunchKernelGGL((k_product_sum<T>), dim3((unsigned)((n + 255) / 256)),
-                     dim3(256), 0, s, P);
-  return hipGetLastError();
-}
+int64_t repack_pitch(int64_t K) { return (K + kSpan - 1) / kSpan * kSpan; }
 
 // ---------------------------------------------------------------------------
 // Choice of the kernel.
@@ -813,65 +771,59 @@ hipError_t product_sum(const ProductParams &P, hipStream_t s) {
 // with `rounds` the times the 256 CUs are filled and `spans` the spans of 128
 // a group of waves goes through; for the few-row blocks
 //   base + round * fill + depth * (span + block_span * fill),
-// fill = blocks / 256 and depth in units of 256 bytes a wave.  A split depth
-// adds parts_base and parts_mb for every MB of sums.  The formula is off by
-// some 10 % a call; what it picks was on average 1.4 % slower than the
-// fastest of all 28 kernels tried over 256 rows, 2.5 % from 65 to 256 and 5 %
-// below (1.55 times at worst).
+// fill = blocks / 256 and depth in units of 256 bytes a wave.  The formula is
+// off by some 10 % a call; what it picks was on average 3.4 % slower than the
+// fastest of all 21 kernels timed from 257 rows on, 2 % from 65 to 256 and
+// 4 % below (1.5 times at worst).
 enum Kernel {
-  kTile256, kTile224, kTile160, kTile192x128, kTile160x128, kTile128,
-  kTile128Deep, kTile64x128, kTile64x128Two, kTile64Two, kTile48Four,
-  kTile48FourSplit, kTile32Four, kFew, kKernels
+  kTile256, kTile160, kTile192x128, kTile160x128, kTile128, kTile128Deep,
+  kTile64x128, kTile64x128Two, kTile64Two, kTile48Four, kTile32Four,
+  kTile16Four, kFew, kKernels
 };
 struct Shape {
   int rows, cols;    // of a tile or block
   int groups;        // groups of waves that share the depth
   int per_cu;        // blocks a CU holds (0: a few-row block)
-  int splits;
-  float base, round, span, block_span, parts_base, parts_mb;
+  float base, round, span, block_span;
 };
 constexpr Shape kShapes[kKernels] = {
-    {256, 256, 1, 1, 1, 2.98f, 9.47f, 1.365f, 0.f, 0.f, 0.f},
-    {224, 256, 1, 1, 1, 3.15f, 9.07f, 1.225f, 0.f, 0.f, 0.f},
-    {160, 256, 1, 1, 1, 3.08f, 7.75f, 0.925f, 0.f, 0.f, 0.f},
-    {192, 128, 1, 1, 1, 4.30f, 6.50f, 0.684f, 0.f, 0.f, 0.f},
-    {160, 128, 1, 1, 1, 3.64f, 6.60f, 0.561f, 0.f, 0.f, 0.f},
-    {128, 128, 1, 2, 1, 3.93f, 4.62f, 0.229f, 0.329f, 0.f, 0.f},
-    {128, 128, 1, 1, 1, 3.40f, 5.29f, 0.487f, 0.f, 0.f, 0.f},
-    {64, 128, 1, 3, 1, 3.29f, 3.03f, 0.134f, 0.267f, 0.f, 0.f},
-    {64, 128, 2, 1, 1, 3.92f, 2.96f, 0.692f, 0.f, 0.f, 0.f},
-    {64, 64, 2, 2, 1, 2.36f, 3.46f, 0.117f, 0.411f, 0.f, 0.f},
-    {48, 64, 4, 1, 1, 1.13f, 4.51f, 0.873f, 0.f, 0.f, 0.f},
-    {48, 64, 4, 1, 4, 8.03f, 0.f, 1.428f, 0.f, 0.f, 0.708f},
-    {32, 64, 4, 1, 1, 2.12f, 3.60f, 0.591f, 0.f, 0.f, 0.f},
-    {32, 16, 4, 0, 1, 3.98f, 0.438f, 0.681f, 0.570f, 0.f, 0.f},
+    {256, 256, 1, 1, 3.14f, 8.44f, 1.350f, 0.f},
+    {160, 256, 1, 1, 3.98f, 6.55f, 0.955f, 0.f},
+    {192, 128, 1, 1, 3.95f, 4.98f, 0.708f, 0.f},
+    {160, 128, 1, 1, 4.36f, 4.89f, 0.562f, 0.f},
+    {128, 128, 1, 2, 4.15f, 3.89f, 0.173f, 0.340f},
+    {128, 128, 1, 1, 3.96f, 3.97f, 0.480f, 0.f},
+    {64, 128, 1, 3, 4.28f, 2.93f, 0.185f, 0.218f},
+    {64, 128, 2, 1, 4.81f, 2.56f, 0.660f, 0.f},
+    {64, 64, 2, 2, 2.57f, 2.96f, 0.138f, 0.399f},
+    {48, 64, 4, 1, 1.84f, 3.45f, 0.883f, 0.f},
+    {32, 64, 4, 1, 2.60f, 3.01f, 0.579f, 0.f},
+    {16, 64, 4, 1, 0.51f, 3.92f, 0.513f, 0.f},
+    {32, 16, 4, 0, 3.53f, 0.301f, 0.712f, 0.636f},
 };
 constexpr int kFewRows = 16;   // up to here: one x operand, k_product_few
 
 float expected_us(const Shape &c, int64_t M, int64_t N, int64_t K) {
   const int64_t tiles =
-      ((M + c.rows - 1) / c.rows) * ((N + c.cols - 1) / c.cols) * c.splits;
+      ((M + c.rows - 1) / c.rows) * ((N + c.cols - 1) / c.cols);
   float us = c.base;
   if (c.per_cu == 0) {
     const float fill = (float)tiles / kCUs;
-    const float depth = (float)K / (256.f * c.groups * c.splits);
+    const float depth = (float)K / (256.f * c.groups);
     us += c.round * fill + depth * (c.span + c.block_span * fill);
   } else {
     const int64_t slots = (int64_t)c.per_cu * kCUs;
     const int64_t whole = tiles / slots, left = tiles % slots;
     const int64_t rounds = whole + (left ? 1 : 0);
-    const int64_t deep = (int64_t)c.groups * c.splits * kSpan;
+    const int64_t deep = (int64_t)c.groups * kSpan;
     const float spans = (float)((K + deep - 1) / deep);
     us += rounds * (c.round + spans * c.span) +
           spans * c.block_span *
               (whole * c.per_cu + (left + kCUs - 1) / kCUs);
   }
-  if (c.splits > 1)
-    us += c.parts_base + c.parts_mb * 4e-6f * (float)M * (float)N * c.splits;
   return us;
 }
 
-// By sizes alone, so that the workspace is known without the pointers.
 int choose(int64_t M, int64_t N, int64_t K) {
   int best = 0;
   float least = 0.f;
@@ -895,7 +847,28 @@ bool aligned_rows(const ProductParams &P) {
 }
 
 template <typename T>
-hipError_t product(ProductParams P, hipStream_t s) {
+hipError_t product_by_size(const ProductParams &P, hipStream_t s) {
+  switch (choose(P.M, P.N, P.K)) {
+    case kTile256: return product_tiles<T, 8, 2, 4, 1, 2>(P, s);
+    case kTile160: return product_tiles<T, 5, 2, 4, 1, 3>(P, s);
+    case kTile192x128: return product_tiles<T, 6, 2, 2, 1, 3>(P, s);
+    case kTile160x128: return product_tiles<T, 5, 2, 2, 1, 4>(P, s);
+    case kTile128: return product_tiles<T, 4, 2, 2, 1, 2>(P, s);
+    case kTile128Deep: return product_tiles<T, 4, 2, 2, 1, 4>(P, s);
+    case kTile64x128: return product_tiles<T, 2, 2, 2, 1, 2>(P, s);
+    case kTile64x128Two: return product_tiles<T, 2, 2, 2, 2, 3>(P, s);
+    case kTile64Two: return product_tiles<T, 2, 2, 1, 2, 2>(P, s);
+    case kTile48Four: return product_tiles<T, 3, 1, 1, 4, 2>(P, s);
+    case kTile32Four: return product_tiles<T, 1, 2, 1, 4, 3>(P, s);
+    case kTile16Four: return product_tiles<T, 1, 1, 1, 4, 3>(P, s);
+    case kFew: return product_few<T, 2>(P, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+template <typename T>
+hipError_t product(ProductParams P, void *workspace, size_t bytes,
+                   hipStream_t s) {
   if (P.M <= kFewRows) {
     // the loads of a whole operand cost the few-row blocks as much as w's:
     // from 9 rows, wide and deep products go through LDS tiles instead (16
@@ -905,47 +878,40 @@ hipError_t product(ProductParams P, hipStream_t s) {
       return product_tiles<T, 1, 1, 1, 4, 3>(P, s);
     return product_few<T, 1>(P, s);
   }
-  int kernel = choose(P.M, P.N, P.K);
-  if (!aligned_rows(P) && kernel != kFew) return product_any<T>(P, s);
-  P.splits = kShapes[kernel].splits;
-  hipError_t e = hipErrorInvalidValue;
-  switch (kernel) {
-    case kTile256: e = product_tiles<T, 8, 2, 4, 1, 2>(P, s); break;
-    case kTile224: e = product_tiles<T, 7, 2, 4, 1, 2>(P, s); break;
-    case kTile160: e = product_tiles<T, 5, 2, 4, 1, 3>(P, s); break;
-    case kTile192x128: e = product_tiles<T, 6, 2, 2, 1, 3>(P, s); break;
-    case kTile160x128: e = product_tiles<T, 5, 2, 2, 1, 4>(P, s); break;
-    case kTile128: e = product_tiles<T, 4, 2, 2, 1, 2>(P, s); break;
-    case kTile128Deep: e = product_tiles<T, 4, 2, 2, 1, 4>(P, s); break;
-    case kTile64x128: e = product_tiles<T, 2, 2, 2, 1, 2>(P, s); break;
-    case kTile64x128Two: e = product_tiles<T, 2, 2, 2, 2, 3>(P, s); break;
-    case kTile64Two: e = product_tiles<T, 2, 2, 1, 2, 2>(P, s); break;
-    case kTile48Four:
-    case kTile48FourSplit: e = product_tiles<T, 3, 1, 1, 4, 2>(P, s); break;
-    case kTile32Four: e = product_tiles<T, 1, 2, 1, 4, 3>(P, s); break;
-    case kFew: e = product_few<T, 2>(P, s); break;
+  if (!aligned_rows(P)) {
+    RepackParams R{P.x,   P.w, static_cast<int8_t *>(workspace), P.M,
+                   P.M + P.N, P.K, P.ldx, P.ldw, repack_pitch(P.K)};
+    if (!workspace || bytes < (size_t)(R.rows * R.pitch) || P.K == 0)
+      return product_any<T>(P, s);
+    const int64_t n = R.rows * (R.pitch / 16);
+    hipLaunchKernelGGL(k_repack, dim3((unsigned)((n + 255) / 256)), dim3(256),
+                       0, s, R);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    P.x = R.to;
+    P.w = R.to + P.M * R.pitch;
+    P.ldx = P.ldw = P.K = R.pitch;
   }
-  if (e == hipSuccess && P.splits > 1) e = product_sum<T>(P, s);
-  return e;
+  return product_by_size<T>(P, s);
 }
 
 }  // namespace
 
+// Rows of a depth that 16 does not divide can hardly lie on 16-byte addresses.
 size_t product_workspace(int64_t M, int64_t N, int64_t K) {
-  if (M <= kFewRows || N == 0) return 0;
-  const int splits = kShapes[choose(M, N, K)].splits;
-  return splits > 1 ? (size_t)splits * M * parts_row(N) * sizeof(int32_t) : 0;
+  return M <= kFewRows || N == 0 || K % 16 == 0
+             ? 0
+             : (size_t)((M + N) * repack_pitch(K));
 }
 
 hipError_t launch_product(const dopr_quant_matmul_args_t &a, hipStream_t s) {
   const ProductParams P{a.x,    a.w,      a.x_scale,      a.w_scale,
                         a.bias, a.residual, a.y,          a.rows,
                         a.cols, a.depth,  a.x_row_stride, a.w_row_stride,
-                        a.residual_row_stride, a.y_row_stride,
-                        static_cast<int32_t *>(a.workspace), 1};
-  if (a.dtype == DOPR_BF16) return product<bf16_t>(P, s);
-  if (a.dtype == DOPR_F16) return product<_Float16>(P, s);
-  return product<float>(P, s);
+                        a.residual_row_stride, a.y_row_stride};
+  if (a.dtype == DOPR_BF16) return product<bf16_t>(P, a.workspace, a.workspace_bytes, s);
+  if (a.dtype == DOPR_F16) return product<_Float16>(P, a.workspace, a.workspace_bytes, s);
+  return product<float>(P, a.workspace, a.workspace_bytes, s);
 }
 
 }  // namespace dopr

@@ -209,6 +209,33 @@ def test_product_unaligned(m, n, k):
                 bias=True)
 
 
+@pytest.mark.parametrize("m,n,k", [(17, 33, 129), (70, 129, 1023),
+                                   (300, 520, 64), (1021, 515, 2501)])
+def test_product_of_rows_laid_out_again(m, n, k):
+    """Rows off 16-byte addresses: the same bits with a workspace (laid out
+    again), with one too small and without (multiplied as they lie)."""
+    D = _D()
+    g = gen(m)
+    x = Guarded(m, k, torch.int8, gap=1, offset=1)
+    w = Guarded(n, k, torch.int8, gap=3, offset=5)
+    x.set(int8(g, m, k))
+    w.set(int8(g, n, k))
+    xs, ws = torch.rand(m, device=DEV), torch.rand(n, device=DEV)
+    need = (m + n) * -(-k // 128) * 128
+    out = []
+    for size in (None, need - 1, need, need + 1000):
+        y = Guarded(m, n, torch.float32)
+        wsp = None if size is None else torch.full(
+            (size,), 0x5a, dtype=torch.uint8, device=DEV)
+        D.dopr_quant_matmul(x.view, xs, w.view, ws, y.view, workspace=wsp)
+        y.check()
+        out.append(y.view)
+        if size == need - 1:
+            assert (wsp == 0x5a).all()
+    R.assert_close(out[0], *R.product(x.view, xs, w.view, ws))
+    assert all(torch.equal(o, out[0]) for o in out[1:])
+
+
 def test_product_empty_depth_and_extremes():
     """Depth 0 leaves bias and residual; -128 and full depth stay exact."""
     D = _D()

@@ -199,25 +199,18 @@ def test_empty_calls_and_null_args():
     assert e.value.status == UNSUPPORTED
 
 
-def test_workspace_is_required_where_asked_for():
-    """A product that needs a workspace refuses none and a short one."""
+def test_product_workspace():
+    """Sizes (both operands' rows at a pitch of whole spans of 128 bytes,
+    none up to 16 rows or where 16 divides the depth) and its alignment."""
     D = _D()
-    L = D.lib()
-    sizes = [(m, n, k) for m in (1, 16, 64, 129, 512, 4096)
-             for n in (64, 1024, 4096) for k in (64, 4096, 12288)]
-    for m, n, k in sizes:
-        need = D.dopr_quant_matmul_workspace(m, n, k)
-        if need == 0:
-            continue
-        a = _fields(D._QuantMatmulArgs, **{
-            **MATMUL, "rows": m, "cols": n, "depth": k, "x_row_stride": k,
-            "w_row_stride": k, "y_row_stride": n})
-        assert L.dopr_quant_matmul(ctypes.byref(a), None) == WORKSPACE
-        a.workspace, a.workspace_bytes = 256, need - 1
-        assert L.dopr_quant_matmul(ctypes.byref(a), None) == WORKSPACE
-        assert str(need) in D.dopr_last_error()
-        a.workspace, a.workspace_bytes = 128, need
-        assert L.dopr_quant_matmul(ctypes.byref(a), None) == INVALID
+    for m, n, k in ((1, 64, 100), (16, 64, 100), (129, 64, 4096),
+                    (17, 0, 100), (17, 64, 0)):
+        assert D.dopr_quant_matmul_workspace(m, n, k) == 0, (m, n, k)
+    assert D.dopr_quant_matmul_workspace(17, 64, 100) == 81 * 128
+    assert D.dopr_quant_matmul_workspace(1021, 2563, 2501) == 3584 * 2560
+    _refused(D, "dopr_quant_matmul", D._QuantMatmulArgs, MATMUL,
+             dict(workspace=128, workspace_bytes=4096), INVALID,
+             "256-byte aligned")
 
 
 def test_wrappers_refuse_wrong_tensors():
