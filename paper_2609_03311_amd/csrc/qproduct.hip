@@ -84,7 +84,7 @@ __device__ __forceinline__ void finish(const ProductParams &P, int m, int n,
 #pragma unroll
             for (int e = 0; e < 8; ++e) u[e] += f[e];
           }
-          store8<T>(y + kRunApart * h, 0, u);
+          store8<T, true>(y + kRunApart * h, 0, u);
         }
       } else {  // the matrix ends inside: one by one
 #pragma unroll

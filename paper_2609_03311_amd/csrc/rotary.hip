@@ -41,57 +41,63 @@ struct RotaryParams {
   float factor, sign, eps;
 };
 
-// A unit's two runs of 8 elements, of which [lo, n) are its own.
+// A unit's two runs of 8 elements, of which [lo, n) are its own (lo = 8: none).
+// The units' first runs lie side by side, and so do their second ones: a wave
+// loads and stores whole lines.
 struct Unit {
   int pa, pb, lo_a, lo_b, n_a, n_b;
-  int pair;  // first pair, or -1: passes through
+  bool rotated;
+  int pair_a, pair_b;  // first pairs, when rotated: of the first four of the
+                       // unit's 8 and of the others
 };
 
-// SMALL: runs are cut at their ends (element loads); else the last run of a
-// part moves back to end with it and keeps its own tail.
+// SMALL: runs are cut at their part's end (element loads); else the last run
+// of a part moves back to end with it and keeps its own tail.
 template <bool INTER, bool SMALL>
 __device__ __forceinline__ Unit unit_of(int u, int pair_units, int D, int R) {
   Unit k;
   k.n_a = k.n_b = 8;
-  const int half = R / 2;
-  if (u < pair_units) {
-    int i0 = 8 * u, lo = 0;
-    if (!SMALL && i0 + 8 > half) {
-      lo = i0 + 8 - half;
+  k.lo_a = k.lo_b = 0;
+  k.rotated = u < pair_units;
+  if (k.rotated && !INTER) {
+    const int half = R / 2;
+    int i0 = 8 * u;
+    if (SMALL) {
+      k.n_a = k.n_b = min(8, half - i0);
+    } else if (i0 + 8 > half) {
+      k.lo_a = k.lo_b = i0 + 8 - half;
       i0 = half - 8;
     }
-    k.pair = i0;
-    if (INTER) {
-      k.pa = 2 * i0;
-      k.pb = 2 * i0 + 8;
-      k.lo_a = min(2 * lo, 8);
-      k.lo_b = max(2 * lo - 8, 0);
-      if (SMALL) {
-        k.n_a = min(8, R - k.pa);
-        k.n_b = max(0, min(8, R - k.pb));
-      }
-    } else {
-      k.pa = i0;
-      k.pb = i0 + half;
-      k.lo_a = k.lo_b = lo;
-      if (SMALL) k.n_a = k.n_b = min(8, half - i0);
-    }
-  } else {
-    int c = R + 16 * (u - pair_units), lo = 0;
-    if (!SMALL && c + 16 > D) {
-      lo = c + 16 - D;
-      c = D - 16;
-    }
-    k.pair = -1;
-    k.pa = c;
-    k.pb = c + 8;
-    k.lo_a = min(lo, 8);
-    k.lo_b = max(lo - 8, 0);
-    if (SMALL) {
-      k.n_a = max(0, min(8, D - k.pa));
-      k.n_b = max(0, min(8, D - k.pb));
-    }
+    k.pa = i0;
+    k.pb = i0 + half;
+    k.pair_a = i0;
+    k.pair_b = i0 + 4;
+    return k;
   }
+  // runs of 8 elements of [from, to): unit j takes the runs j and j + units
+  const int from = k.rotated ? 0 : R, to = k.rotated ? R : D;
+  const int j = k.rotated ? u : u - pair_units;
+  const int runs = (to - from + 7) / 8, units = (runs + 1) / 2;
+  auto run = [&](int r, int &p, int &lo, int &n) {
+    p = from + 8 * r;
+    if (r >= runs) {  // an odd number of runs: no second one here
+      p = from;
+      lo = 8;
+      n = SMALL ? 0 : 8;
+    } else if (SMALL) {
+      n = min(8, to - p);
+    } else if (p + 8 > to) {
+      lo = p + 8 - to;
+      p = to - 8;
+    }
+    // (a run past a part's end starts in front of `to`; with to < 8 only in
+    // SMALL, which cuts it)
+  };
+  run(j, k.pa, k.lo_a, k.n_a);
+  run(j + units, k.pb, k.lo_b, k.n_b);
+  if (!SMALL && k.lo_b == 8) k.pb = k.pa;  // (any run of this head)
+  k.pair_a = k.pa / 2;
+  k.pair_b = k.pb / 2;
   return k;
 }
 
@@ -159,9 +165,9 @@ __global__ __launch_bounds__(64 * kRotaryWaves) void k_rotary(RotaryParams P) {
   float c[8], s[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    // (pairs behind a small part's end belong to no element)
-    const int i = k.pair + e;
-    const bool in = k.pair >= 0 && i < P.R / 2;
+    // (pairs behind a part's end belong to no element)
+    const int i = e < 4 ? k.pair_a + e : k.pair_b + e - 4;
+    const bool in = k.rotated && i < P.R / 2;
     const float2 t = table[wave][in ? i : 0];
     c[e] = in ? t.x : 1.f;
     s[e] = in ? t.y : 0.f;
@@ -215,7 +221,7 @@ __global__ __launch_bounds__(64 * kRotaryWaves) void k_rotary(RotaryParams P) {
           }
         }
       }
-      if (k.pair >= 0) {
+      if (k.rotated) {
         float a[8], b2[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -283,8 +289,10 @@ hipError_t launch_rotary(const dopr_rotary_args_t &a, hipStream_t s) {
   P.factor = a.attention_factor;
   P.sign = a.inverse ? -1.f : 1.f;
   P.eps = a.rms_eps;
-  const int rest = a.head_dim - a.rotary_dim;
-  const bool small = a.rotary_dim < 16 || (rest > 0 && rest < 16);
+  // (runs of 8 elements that end with their part have to fit in it, or, those
+  // behind the rotated part, in the head)
+  const bool small = a.rotary_dim < (a.interleaved ? 8 : 16) ||
+                     (a.rotary_dim < a.head_dim && a.head_dim < 8);
   // few tokens: a token's head groups go to several waves (each forms the
   // rotations again) until about eight waves a SIMD are there
   const int groups = (P.n_heads + (64 >> P.group_log2) - 1) /

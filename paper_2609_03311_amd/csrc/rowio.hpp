@@ -130,21 +130,30 @@ struct Chunk {
   }
 };
 
-// Elements lo..7 of f to p[lo..7].
-template <typename T>
+// Elements lo..7 of f to p[lo..7].  STREAM: past the caches' order of use,
+// for stores of whole lines that nothing reads soon.
+template <bool STREAM, typename V, typename P>
+__device__ __forceinline__ void put(const V &v, P *p) {
+  if constexpr (STREAM)
+    __builtin_nontemporal_store(v, p);
+  else
+    *p = v;
+}
+
+template <typename T, bool STREAM = false>
 __device__ __forceinline__ void store8(T *p, int lo, const float *f) {
   if (lo == 0) {
     if constexpr (sizeof(T) == 2) {
       const u32x4 u = {pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]),
                        pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7])};
-      *reinterpret_cast<u32x4_any *>(p) = u;
+      put<STREAM>(u, reinterpret_cast<u32x4_any *>(p));
     } else {
       const u32x4 u = {__float_as_uint(f[0]), __float_as_uint(f[1]),
                        __float_as_uint(f[2]), __float_as_uint(f[3])};
       const u32x4 v = {__float_as_uint(f[4]), __float_as_uint(f[5]),
                        __float_as_uint(f[6]), __float_as_uint(f[7])};
-      *reinterpret_cast<u32x4_any *>(p) = u;
-      *reinterpret_cast<u32x4_any *>(p + 4) = v;
+      put<STREAM>(u, reinterpret_cast<u32x4_any *>(p));
+      put<STREAM>(v, reinterpret_cast<u32x4_any *>(p + 4));
     }
   } else if (lo < 8) {
 #pragma unroll

@@ -254,7 +254,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm_residual(
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const Chunk k((v * TPR + t) * 8, W);
-      store8<R>(p + k.c, k.lo, f[v]);
+      store8<R, true>(p + k.c, k.lo, f[v]);
     }
   }
   if (!P.z && !P.q) return;
@@ -264,7 +264,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm_residual(
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const Chunk k((v * TPR + t) * 8, W);
-      store8<T>(p + k.c, k.lo, f[v]);
+      store8<T, true>(p + k.c, k.lo, f[v]);
     }
   }
   if (P.q) {
