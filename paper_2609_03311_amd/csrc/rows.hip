@@ -17,15 +17,15 @@ namespace {
 // Rows of at most this many elements belong to one wave (four rows a block).
 constexpr int kWaveRow = 2048;
 
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float *part) {
+template <int TPR, typename S>
+__device__ __forceinline__ S row_sum(S v, S *part) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
   if constexpr (TPR > 64) {
     __syncthreads();  // the parts of an earlier reduction have been read
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = 0.f;
+    v = 0;
 #pragma unroll
     for (int w = 0; w < TPR / 64; ++w) v += part[w];
   }
@@ -35,17 +35,18 @@ __device__ __forceinline__ float row_sum(float v, float *part) {
 // Largest |v| as its bit pattern: unsigned order puts infinities above every
 // finite value and NaN above those, where a float maximum would drop NaN.
 template <int TPR>
-__device__ __forceinline__ uint32_t row_max_bits(uint32_t v, float *part) {
+__device__ __forceinline__ uint32_t row_max_bits(uint32_t v,
+                                                 uint32_t *part) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1)
     v = max(v, (uint32_t)__shfl_xor((int)v, off, 64));
   if constexpr (TPR > 64) {
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = __uint_as_float(v);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
     v = 0;
 #pragma unroll
-    for (int w = 0; w < TPR / 64; ++w) v = max(v, __float_as_uint(part[w]));
+    for (int w = 0; w < TPR / 64; ++w) v = max(v, part[w]);
   }
   return v;
 }
@@ -103,7 +104,7 @@ template <typename T, int TPR, int NV, bool UP>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_quantize_rows(
     QuantizeParams P) {
   constexpr int kRows = TPR > 64 ? 1 : 4;
-  __shared__ float part[TPR / 64];
+  __shared__ uint32_t part[TPR / 64];
   const int t = TPR > 64 ? threadIdx.x : threadIdx.x & 63;
   const int64_t r = (int64_t)blockIdx.x * kRows +
                     (TPR > 64 ? 0 : threadIdx.x >> 6);
@@ -125,11 +126,19 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_quantize_rows(
     if constexpr (UP) {
       float g[8];
       ru[v].get(g);
-      // SiLU(x) * up; the reciprocal is good to one unit in the last place
+      // SiLU(x) * up.  16-bit inputs: the hardware's exponential and
+      // reciprocal, a few units in fp32's last place, 2^-13 of an input's own.
+      // fp32 inputs: both to the last place, as a caller who keeps 32 bits
+      // expects.  Either way HBM is the bound (12,900 x 12,288: 5.5 and 5.1
+      // TB/s).
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        f[v][e] = f[v][e] * __builtin_amdgcn_rcpf(1.0f + __expf(-f[v][e])) *
-                  g[e];
+      for (int e = 0; e < 8; ++e) {
+        const float a = f[v][e];
+        if constexpr (sizeof(T) == 4)
+          f[v][e] = a / (1.0f + expf(-a)) * g[e];
+        else
+          f[v][e] = a * __builtin_amdgcn_rcpf(1.0f + __expf(-a)) * g[e];
+      }
     }
     // (a chunk's dropped elements are elements of the same row)
 #pragma unroll
@@ -165,7 +174,10 @@ template <typename T, typename R, int TPR, int NV>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm_residual(
     NormParams P) {
   constexpr int kRows = TPR > 64 ? 1 : 4;
-  __shared__ float part[TPR / 64];
+  // fp32 activations: sums in 64 bits, so that a row's factor is the nearest
+  // fp32 to the exact one and its 8-bit form does not turn on the order
+  using Sum = std::conditional_t<sizeof(T) == 4, double, float>;
+  __shared__ Sum part[TPR / 64];
   const int t = TPR > 64 ? threadIdx.x : threadIdx.x & 63;
   const int64_t r = (int64_t)blockIdx.x * kRows +
                     (TPR > 64 ? 0 : threadIdx.x >> 6);
@@ -201,30 +213,29 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm_residual(
 #pragma unroll
     for (int v = 0; v < NV; ++v)
       rw[v].load(w + Chunk((v * TPR + t) * 8, W).c);
-    float ss = 0.f;
+    auto squares = [&]() {
+      Sum ss = 0;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      Chunk((v * TPR + t) * 8, W).mask(f[v]);
+      for (int v = 0; v < NV; ++v)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(f[v][e], f[v][e], ss);
-    }
-    ss = row_sum<TPR>(ss, part);
-    float eps = P.eps;
-    if (ss == __builtin_inff()) {
+        for (int e = 0; e < 8; ++e)
+          ss = fma((Sum)f[v][e], (Sum)f[v][e], ss);
+      return (float)(row_sum<TPR>(ss, part) / (Sum)W);
+    };
+#pragma unroll
+    for (int v = 0; v < NV; ++v) Chunk((v * TPR + t) * 8, W).mask(f[v]);
+    float mean = squares(), eps = P.eps;
+    if (mean == __builtin_inff()) {
       // squares past fp32's range (values over 2^55 or so; the whole row
       // takes this turn together): the same with the row 2^80 times smaller
-      ss = 0.f;
       eps *= 0x1p-80f * 0x1p-80f;
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          f[v][e] *= 0x1p-80f;
-          ss = fmaf(f[v][e], f[v][e], ss);
-        }
-      ss = row_sum<TPR>(ss, part);
+        for (int e = 0; e < 8; ++e) f[v][e] *= 0x1p-80f;
+      mean = squares();
     }
-    const float inv = 1.0f / sqrtf(ss / (float)W + eps);
+    const float inv = 1.0f / sqrtf(mean + eps);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       rw[v].get(g);
@@ -276,7 +287,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm_residual(
       for (int e = 0; e < 8; ++e)
         m = max(m, __float_as_uint(f[v][e]) & 0x7fffffffu);
     }
-    m = row_max_bits<TPR>(m, part);
+    m = row_max_bits<TPR>(m, reinterpret_cast<uint32_t *>(part));
     float scale, inv;
     row_scale(m, scale, inv);
     int8_t *q = P.q + r * P.ldq;
