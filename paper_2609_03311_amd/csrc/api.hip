@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "internal.hpp"
+#include "operators.hpp"
 
 using namespace dopr;
 

@@ -576,15 +576,6 @@ hipError_t launch_salience_chunk(const SalienceParams &p, int32_t n_docs,
                                  int hr, int pm, hipStream_t s);
 hipError_t launch_topk(const TopkParams &p, int32_t n_docs, hipStream_t s);
 
-// Operators around the attention (rows.hip, qproduct.hip, rotary.hip); the
-// arguments have been checked.
-hipError_t launch_quantize_rows(const dopr_quantize_args_t &a, hipStream_t s);
-hipError_t launch_norm_residual(const dopr_norm_residual_args_t &a,
-                                hipStream_t s);
-size_t product_workspace(int64_t rows, int64_t cols, int64_t depth);
-hipError_t launch_product(const dopr_quant_matmul_args_t &a, hipStream_t s);
-hipError_t launch_rotary(const dopr_rotary_args_t &a, hipStream_t s);
-
 // Record a deferred error code in a status word (first error wins).
 __device__ inline void raise_status(int32_t *status, int32_t code) {
   atomicCAS(status, 0, code);

@@ -2,9 +2,9 @@
 // qproduct.hip): loads and stores of 8 elements at any element alignment, in
 // fp32.
 #pragma once
-#include <hip/hip_runtime.h>
+#include <cstdint>
 
-#include "internal.hpp"
+#include "operators.hpp"
 
 namespace dopr {
 

@@ -37,6 +37,8 @@ SOURCE_SETS = {
     "attention": KERNEL_SOURCES,
     "salience": ("csrc/salience.hip", "csrc/internal.hpp"),
     "store": ("csrc/store.hip", "csrc/internal.hpp"),
+    "operators": ("csrc/rows.hip", "csrc/qproduct.hip", "csrc/rotary.hip",
+                  "csrc/rowio.hpp"),
     "layer": ("csrc/layer.hip", "csrc/group.hip", "csrc/score.hip")
     + KERNEL_SOURCES,
 }
