@@ -84,7 +84,7 @@ __device__ __forceinline__ void finish(const ProductParams &P, int m, int n,
 #pragma unroll
             for (int e = 0; e < 8; ++e) u[e] += f[e];
           }
-          store8<T, true>(y + kRunApart * h, 0, u);
+          store8<T, true>(y + kRunApart * h, u);
         }
       } else {  // the matrix ends inside: one by one
 #pragma unroll
@@ -614,7 +614,7 @@ hipError_t product_tiles(const ProductParams &P, hipStream_t s) {
 // 4 results of y row m from column n on (m and n inside), with the scales xs
 // and scale[0..3].
 template <typename T>
-__device__ __forceinline__ void store4(const ProductParams &P, int64_t m,
+__device__ __forceinline__ void finish4(const ProductParams &P, int64_t m,
                                        int64_t n, const i32x4 &acc, float xs,
                                        const float *scale) {
   const T *bias = static_cast<const T *>(P.bias);
@@ -630,13 +630,7 @@ __device__ __forceinline__ void store4(const ProductParams &P, int64_t m,
     if (P.res) v[e] += to_f32<T>(res[c]);
   }
   if (left == 4) {
-    if constexpr (sizeof(T) == 2)
-      *reinterpret_cast<u32x2_any *>(y + n) =
-          u32x2{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
-    else
-      *reinterpret_cast<u32x4_any *>(y + n) =
-          u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]),
-                __float_as_uint(v[2]), __float_as_uint(v[3])};
+    store4<T>(y + n, v);
     return;
   }
 #pragma unroll
@@ -724,7 +718,7 @@ __global__ __launch_bounds__(256) void k_product_few(ProductParams P) {
     i32x4 s = sums[0][wave][lane];
 #pragma unroll
     for (int w = 1; w < WK; ++w) s += sums[w][wave][lane];
-    store4<T>(P, m, n, s, xs, scale);
+    finish4<T>(P, m, n, s, xs, scale);
   }
 }
 

@@ -129,7 +129,7 @@ struct Run {
       for (int e = 0; e < 8; ++e)
         if (e < n) p[e] = from_f32<T>(g[e]);
     } else {
-      store8<T>(p, lo, g);
+      store_part<T, 8>(p, lo, 8, g);
     }
   }
 };

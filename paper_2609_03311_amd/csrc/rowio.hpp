@@ -20,6 +20,7 @@ typedef _Float16 f16x2v __attribute__((ext_vector_type(2)));
 // address happens to be aligned
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
 typedef u32x4 u32x4_any __attribute__((aligned(1)));
 typedef u32x2 u32x2_any __attribute__((aligned(1)));
 
@@ -83,55 +84,80 @@ __device__ __forceinline__ uint32_t pack2<_Float16>(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, f16x2v));
 }
 
-// 8 elements as they lie in memory
-template <typename T>
-struct Raw8 {
+// E elements as they lie in memory: one load of up to 16 bytes, two for 8 of
+// fp32
+template <typename T, int E>
+struct Raw {
+  static_assert(E == 8 && sizeof(T) == 2, "other forms below");
   u32x4 u;
   __device__ __forceinline__ void load(const T *p) {
     u = *reinterpret_cast<const u32x4_any *>(p);
   }
   __device__ __forceinline__ void get(float *f) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2<T>(u[i], f[2 * i], f[2 * i + 1]);
+  }
+};
+template <typename T>
+struct Raw<T, 4> {
+  u32x2 u;
+  __device__ __forceinline__ void load(const T *p) {
+    u = *reinterpret_cast<const u32x2_any *>(p);
+  }
+  __device__ __forceinline__ void get(float *f) const {
     unpack2<T>(u.x, f[0], f[1]);
     unpack2<T>(u.y, f[2], f[3]);
-    unpack2<T>(u.z, f[4], f[5]);
-    unpack2<T>(u.w, f[6], f[7]);
   }
 };
 template <>
-struct Raw8<float> {
-  u32x4 u, v;
+struct Raw<float, 4> {
+  u32x4 u;
   __device__ __forceinline__ void load(const float *p) {
     u = *reinterpret_cast<const u32x4_any *>(p);
-    v = *reinterpret_cast<const u32x4_any *>(p + 4);
   }
   __device__ __forceinline__ void get(float *f) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[i] = __uint_as_float(u[i]);
-      f[4 + i] = __uint_as_float(v[i]);
-    }
+    for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(u[i]);
   }
 };
+template <>
+struct Raw<float, 8> {
+  Raw<float, 4> a, b;
+  __device__ __forceinline__ void load(const float *p) {
+    a.load(p);
+    b.load(p + 4);
+  }
+  __device__ __forceinline__ void get(float *f) const {
+    a.get(f);
+    b.get(f + 4);
+  }
+};
+template <typename T>
+using Raw8 = Raw<T, 8>;
 
-// The 8 elements of a row of `width` that start at c0, as one load that stays
-// inside the row: chunks behind the end read the row's first elements and
-// keep none, the row's last partial chunk reads the last 8 and keeps those
-// from `lo` on.  `width` is at least 8.
+// The E elements of a row of `width` that start at c0, as one load that stays
+// inside the row: chunks outside it read the row's first elements and keep
+// none; a chunk that starts in front of the row (c0 < 0) reads the first E and
+// keeps those below `hi`, one that ends behind it reads the last E and keeps
+// those from `lo` on.  `width` is at least E.
+template <int E>
 struct Chunk {
-  int c, lo;
+  int c, lo, hi;
   __device__ __forceinline__ Chunk(int c0, int width) {
     const int n = width - c0;
-    c = n >= 8 ? c0 : n > 0 ? width - 8 : 0;
-    lo = n >= 8 ? 0 : n > 0 ? 8 - n : 8;
+    c = n > 0 ? max(min(c0, width - E), 0) : 0;
+    lo = n >= E ? 0 : n > 0 ? E - n : E;
+    hi = c0 >= 0 ? E : c0 > -E ? E + c0 : 0;
   }
+  __device__ __forceinline__ bool whole() const { return lo == 0 && hi == E; }
   __device__ __forceinline__ void mask(float *f) const {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = e >= lo ? f[e] : 0.f;
+    for (int e = 0; e < E; ++e) f[e] = e >= lo && e < hi ? f[e] : 0.f;
   }
 };
 
-// Elements lo..7 of f to p[lo..7].  STREAM: past the caches' order of use,
-// for stores of whole lines that nothing reads soon.
+// STREAM: past the caches' order of use, for stores of whole lines that
+// nothing reads soon.
 template <bool STREAM, typename V, typename P>
 __device__ __forceinline__ void put(const V &v, P *p) {
   if constexpr (STREAM)
@@ -141,25 +167,43 @@ __device__ __forceinline__ void put(const V &v, P *p) {
 }
 
 template <typename T, bool STREAM = false>
-__device__ __forceinline__ void store8(T *p, int lo, const float *f) {
-  if (lo == 0) {
-    if constexpr (sizeof(T) == 2) {
-      const u32x4 u = {pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]),
-                       pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7])};
-      put<STREAM>(u, reinterpret_cast<u32x4_any *>(p));
-    } else {
-      const u32x4 u = {__float_as_uint(f[0]), __float_as_uint(f[1]),
-                       __float_as_uint(f[2]), __float_as_uint(f[3])};
-      const u32x4 v = {__float_as_uint(f[4]), __float_as_uint(f[5]),
-                       __float_as_uint(f[6]), __float_as_uint(f[7])};
-      put<STREAM>(u, reinterpret_cast<u32x4_any *>(p));
-      put<STREAM>(v, reinterpret_cast<u32x4_any *>(p + 4));
-    }
-  } else if (lo < 8) {
-#pragma unroll
-    for (int e = 1; e < 8; ++e)
-      if (e >= lo) p[e] = from_f32<T>(f[e]);
+__device__ __forceinline__ void store4(T *p, const float *f) {
+  if constexpr (sizeof(T) == 2) {
+    const u32x2 u = {pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3])};
+    put<STREAM>(u, reinterpret_cast<u32x2_any *>(p));
+  } else {
+    const u32x4 u = {__float_as_uint(f[0]), __float_as_uint(f[1]),
+                     __float_as_uint(f[2]), __float_as_uint(f[3])};
+    put<STREAM>(u, reinterpret_cast<u32x4_any *>(p));
   }
+}
+
+template <typename T, bool STREAM = false>
+__device__ __forceinline__ void store8(T *p, const float *f) {
+  if constexpr (sizeof(T) == 2) {
+    const u32x4 u = {pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]),
+                     pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7])};
+    put<STREAM>(u, reinterpret_cast<u32x4_any *>(p));
+  } else {
+    store4<T, STREAM>(p, f);
+    store4<T, STREAM>(p + 4, f + 4);
+  }
+}
+
+// Elements lo..hi-1 of E to p[lo..hi-1].
+template <typename T, int E, bool STREAM = false>
+__device__ __forceinline__ void store_part(T *p, int lo, int hi,
+                                           const float *f) {
+  if (lo == 0 && hi == E) {
+    if constexpr (E == 8)
+      store8<T, STREAM>(p, f);
+    else
+      store4<T, STREAM>(p, f);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (e >= lo && e < hi) p[e] = from_f32<T>(f[e]);
 }
 
 }  // namespace dopr

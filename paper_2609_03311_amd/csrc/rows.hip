@@ -2,8 +2,8 @@
 // memory each: rows in 8-bit integers (k_quantize_rows) and the norms around a
 // gated, scaled residual (k_norm_residual).
 //
-// A row is held in registers by TPR threads (a wave, or a whole block), 8
-// elements of NV chunks each, so that its sums and its largest magnitude are
+// A row is held in registers by TPR threads (a wave, or a whole block), 8 NV
+// elements each, so that its sums and its largest magnitude are
 // known before its first output is written and nothing is read twice.  Both
 // kernels are bound by HBM: a row's arithmetic is some ten vector
 // instructions per 8 elements.
@@ -13,9 +13,6 @@
 
 namespace dopr {
 namespace {
-
-// Rows of at most this many elements belong to one wave (four rows a block).
-constexpr int kWaveRow = 2048;
 
 template <int TPR, typename S>
 __device__ __forceinline__ S row_sum(S v, S *part) {
@@ -77,20 +74,31 @@ __device__ __forceinline__ void row_scale(uint32_t bits, float &scale,
   inv = 127.f / a;
 }
 
-__device__ __forceinline__ void store_int8(int8_t *p, int lo, const float *f,
-                                           float inv) {
-  if (lo >= 8) return;
+template <int E>
+__device__ __forceinline__ void store_int8(int8_t *p, const Chunk<E> &k,
+                                           const float *f, float inv) {
   // inf * 0 and NaN * 0 are NaN: a row that is not finite stores zeros
-  const u32x2 u = inv == 0.f ? u32x2{0u, 0u}
-                             : u32x2{pack_int8(f, inv), pack_int8(f + 4, inv)};
-  if (lo == 0) {
-    *reinterpret_cast<u32x2_any *>(p) = u;
+  uint32_t u[E / 4];
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i)
+    u[i] = inv == 0.f ? 0u : pack_int8(f + 4 * i, inv);
+  if (k.whole()) {
+    if constexpr (E == 8)
+      *reinterpret_cast<u32x2_any *>(p) = u32x2{u[0], u[1]};
+    else
+      *reinterpret_cast<u32_any *>(p) = u[0];
     return;
   }
 #pragma unroll
-  for (int e = 1; e < 8; ++e)
-    if (e >= lo) p[e] = (int8_t)(u[e >> 2] >> (8 * (e & 3)));
+  for (int e = 0; e < E; ++e)
+    if (e >= k.lo && e < k.hi) p[e] = (int8_t)(u[e >> 2] >> (8 * (e & 3)));
 }
+
+// Elements of a lane's chunk: 16 bytes of the widest type, so that a wave's
+// loads and stores are whole lines (with 32 bytes a lane, half of each
+// line is the next instruction's: norms of 12,900 x 4096 around an fp32 residual
+// 108 us, with 16 97).
+constexpr int chunk_of(int bytes) { return 16 / bytes; }
 
 struct QuantizeParams {
   const void *x, *up;
@@ -101,9 +109,10 @@ struct QuantizeParams {
 };
 
 template <typename T, int TPR, int NV, bool UP>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_quantize_rows(
+__global__ __launch_bounds__(TPR > 64 ? TPR : 256) void k_quantize_rows(
     QuantizeParams P) {
   constexpr int kRows = TPR > 64 ? 1 : 4;
+  constexpr int E = chunk_of(sizeof(T)), NC = NV * 8 / E;
   __shared__ uint32_t part[TPR / 64];
   const int t = TPR > 64 ? threadIdx.x : threadIdx.x & 63;
   const int64_t r = (int64_t)blockIdx.x * kRows +
@@ -111,20 +120,20 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_quantize_rows(
   if (r >= P.rows) return;  // one wave per row here: no barrier is missed
   const T *x = static_cast<const T *>(P.x) + r * P.ldx;
   const T *up = static_cast<const T *>(P.up) + r * P.ldu;
-  Raw8<T> rx[NV], ru[NV];
+  Raw<T, E> rx[NC], ru[NC];
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const Chunk k((v * TPR + t) * 8, P.width);
+  for (int v = 0; v < NC; ++v) {
+    const Chunk<E> k((v * TPR + t) * E, P.width);
     rx[v].load(x + k.c);
     if constexpr (UP) ru[v].load(up + k.c);
   }
-  float f[NV][8];
+  float f[NC][E];
   uint32_t m = 0;
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
+  for (int v = 0; v < NC; ++v) {
     rx[v].get(f[v]);
     if constexpr (UP) {
-      float g[8];
+      float g[E];
       ru[v].get(g);
       // SiLU(x) * up.  16-bit inputs: the hardware's exponential and
       // reciprocal, a few units in fp32's last place, 2^-13 of an input's own.
@@ -132,7 +141,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_quantize_rows(
       // expects.  Either way HBM is the bound (12,900 x 12,288: 5.5 and 5.1
       // TB/s).
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < E; ++e) {
         const float a = f[v][e];
         if constexpr (sizeof(T) == 4)
           f[v][e] = a / (1.0f + expf(-a)) * g[e];
@@ -142,7 +151,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_quantize_rows(
     }
     // (a chunk's dropped elements are elements of the same row)
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < E; ++e)
       m = max(m, __float_as_uint(f[v][e]) & 0x7fffffffu);
   }
   m = row_max_bits<TPR>(m, part);
@@ -150,9 +159,9 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_quantize_rows(
   row_scale(m, scale, inv);
   int8_t *q = P.q + r * P.ldq;
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const Chunk k((v * TPR + t) * 8, P.width);
-    store_int8(q + k.c, k.lo, f[v], inv);
+  for (int v = 0; v < NC; ++v) {
+    const Chunk<E> k((v * TPR + t) * E, P.width);
+    store_int8(q + k.c, k, f[v], inv);
   }
   if (t == 0) P.scale[r] = scale;
 }
@@ -168,12 +177,23 @@ struct NormParams {
   int64_t rows, ldx, ldg, ldr, ldh, ldz, ldq;
   int32_t width;
   float residual_scale, eps;
+  // Chunks start on the output's lines, not at the row's start, so that no
+  // line is written in two parts by two waves: rows of 9001 64 -> 55 us.
+  bool lines;
 };
 
+// Elements between p and the 64-element line of its buffer that it lies in.
+template <typename T>
+__device__ __forceinline__ int line_offset(const T *p) {
+  return (int)(reinterpret_cast<uintptr_t>(p) / sizeof(T)) & 63;
+}
+
 template <typename T, typename R, int TPR, int NV>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm_residual(
+__global__ __launch_bounds__(TPR > 64 ? TPR : 256) void k_norm_residual(
     NormParams P) {
   constexpr int kRows = TPR > 64 ? 1 : 4;
+  constexpr int E = chunk_of(sizeof(T) > sizeof(R) ? sizeof(T) : sizeof(R));
+  constexpr int NC = NV * 8 / E;
   // fp32 activations: sums in 64 bits, so that a row's factor is the nearest
   // fp32 to the exact one and its 8-bit form does not turn on the order
   using Sum = std::conditional_t<sizeof(T) == 4, double, float>;
@@ -183,89 +203,93 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm_residual(
                     (TPR > 64 ? 0 : threadIdx.x >> 6);
   if (r >= P.rows) return;
   const int W = P.width;
+  const int shift =
+      P.lines ? P.h ? line_offset(static_cast<const R *>(P.h) + r * P.ldh)
+                    : line_offset(static_cast<const T *>(P.z) + r * P.ldz)
+              : 0;
   // everything the row reads is on its way before the first sum is waited for
   const T *x = static_cast<const T *>(P.x) + r * P.ldx;
-  Raw8<T> rx[NV], rg[NV];
-  Raw8<R> rr[NV];
+  Raw<T, E> rx[NC], rg[NC];
+  Raw<R, E> rr[NC];
 #pragma unroll
-  for (int v = 0; v < NV; ++v)
-    rx[v].load(x + Chunk((v * TPR + t) * 8, W).c);
+  for (int v = 0; v < NC; ++v)
+    rx[v].load(x + Chunk<E>((v * TPR + t) * E - shift, W).c);
   if (P.res) {
     const R *p = static_cast<const R *>(P.res) + r * P.ldr;
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-      rr[v].load(p + Chunk((v * TPR + t) * 8, W).c);
+    for (int v = 0; v < NC; ++v)
+      rr[v].load(p + Chunk<E>((v * TPR + t) * E - shift, W).c);
   }
   if (P.gate) {
     const T *p = static_cast<const T *>(P.gate) + r * P.ldg;
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-      rg[v].load(p + Chunk((v * TPR + t) * 8, W).c);
+    for (int v = 0; v < NC; ++v)
+      rg[v].load(p + Chunk<E>((v * TPR + t) * E - shift, W).c);
   }
-  float f[NV][8];
-  float g[8];
+  float f[NC][E];
+  float g[E];
 #pragma unroll
-  for (int v = 0; v < NV; ++v) rx[v].get(f[v]);
+  for (int v = 0; v < NC; ++v) rx[v].get(f[v]);
   // f = RMSNorm(f) * gain
   auto norm = [&](const void *gain) {
     const T *w = static_cast<const T *>(gain);
-    Raw8<T> rw[NV];
+    Raw<T, E> rw[NC];
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-      rw[v].load(w + Chunk((v * TPR + t) * 8, W).c);
+    for (int v = 0; v < NC; ++v)
+      rw[v].load(w + Chunk<E>((v * TPR + t) * E - shift, W).c);
     auto squares = [&]() {
       Sum ss = 0;
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
+      for (int v = 0; v < NC; ++v)
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < E; ++e)
           ss = fma((Sum)f[v][e], (Sum)f[v][e], ss);
       return (float)(row_sum<TPR>(ss, part) / (Sum)W);
     };
 #pragma unroll
-    for (int v = 0; v < NV; ++v) Chunk((v * TPR + t) * 8, W).mask(f[v]);
+    for (int v = 0; v < NC; ++v) Chunk<E>((v * TPR + t) * E - shift, W).mask(f[v]);
     float mean = squares(), eps = P.eps;
     if (mean == __builtin_inff()) {
       // squares past fp32's range (values over 2^55 or so; the whole row
       // takes this turn together): the same with the row 2^80 times smaller
       eps *= 0x1p-80f * 0x1p-80f;
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
+      for (int v = 0; v < NC; ++v)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[v][e] *= 0x1p-80f;
+        for (int e = 0; e < E; ++e) f[v][e] *= 0x1p-80f;
       mean = squares();
     }
     const float inv = 1.0f / sqrtf(mean + eps);
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
+    for (int v = 0; v < NC; ++v) {
       rw[v].get(g);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[v][e] = f[v][e] * inv * g[e];
+      for (int e = 0; e < E; ++e) f[v][e] = f[v][e] * inv * g[e];
     }
   };
   if (P.post_w) norm(P.post_w);
   if (P.gate) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
+    for (int v = 0; v < NC; ++v) {
       rg[v].get(g);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[v][e] *= g[e];
+      for (int e = 0; e < E; ++e) f[v][e] *= g[e];
     }
   }
   if (P.res) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
+    for (int v = 0; v < NC; ++v) {
       rr[v].get(g);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[v][e] += P.residual_scale * g[e];
+      for (int e = 0; e < E; ++e) f[v][e] += P.residual_scale * g[e];
     }
   }
   if (P.h) {
     R *p = static_cast<R *>(P.h) + r * P.ldh;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const Chunk k((v * TPR + t) * 8, W);
-      store8<R, true>(p + k.c, k.lo, f[v]);
+    for (int v = 0; v < NC; ++v) {
+      const Chunk<E> k((v * TPR + t) * E - shift, W);
+      store_part<R, E, true>(p + k.c, k.lo, k.hi, f[v]);
     }
   }
   if (!P.z && !P.q) return;
@@ -273,18 +297,18 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm_residual(
   if (P.z) {
     T *p = static_cast<T *>(P.z) + r * P.ldz;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const Chunk k((v * TPR + t) * 8, W);
-      store8<T, true>(p + k.c, k.lo, f[v]);
+    for (int v = 0; v < NC; ++v) {
+      const Chunk<E> k((v * TPR + t) * E - shift, W);
+      store_part<T, E, true>(p + k.c, k.lo, k.hi, f[v]);
     }
   }
   if (P.q) {
     uint32_t m = 0;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      Chunk((v * TPR + t) * 8, W).mask(f[v]);
+    for (int v = 0; v < NC; ++v) {
+      Chunk<E>((v * TPR + t) * E - shift, W).mask(f[v]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
+      for (int e = 0; e < E; ++e)
         m = max(m, __float_as_uint(f[v][e]) & 0x7fffffffu);
     }
     m = row_max_bits<TPR>(m, reinterpret_cast<uint32_t *>(part));
@@ -292,15 +316,22 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm_residual(
     row_scale(m, scale, inv);
     int8_t *q = P.q + r * P.ldq;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const Chunk k((v * TPR + t) * 8, W);
-      store_int8(q + k.c, k.lo, f[v], inv);
+    for (int v = 0; v < NC; ++v) {
+      const Chunk<E> k((v * TPR + t) * E - shift, W);
+      store_int8(q + k.c, k, f[v], inv);
     }
     if (t == 0) P.q_scale[r] = scale;
   }
 }
 
-// The instance that holds a row of `width`: f(threads per row, chunks).
+constexpr int64_t kMostWidth = 65536;
+
+// The instance that holds a row of `width`: f(threads per row, chunks of 8).
+// Rows of a wave need no barrier, but hold few loads in flight once their
+// registers keep waves out; idle lanes cost their loads.  20,011 x 2561, fp16
+// around an fp32 residual: 135, 127, 137 us at (64, 6), (128, 3), (256, 2);
+// 12,900 x 4096, bf16: 64, 61, 60 at (64, 8), (128, 4), (256, 2); 5000 x 9001:
+// 54 at (256, 5), 55 at (512, 3).
 template <typename F>
 hipError_t by_width(int64_t width, F f) {
   using std::integral_constant;
@@ -309,9 +340,14 @@ hipError_t by_width(int64_t width, F f) {
     return f(integral_constant<int, tpr>{}, integral_constant<int, nv>{});
   DOPR_ROW(64, 1)
   DOPR_ROW(64, 2)
+  DOPR_ROW(64, 3)
   DOPR_ROW(64, 4)
+  DOPR_ROW(128, 3)
   DOPR_ROW(256, 2)
+  DOPR_ROW(256, 3)
   DOPR_ROW(256, 4)
+  DOPR_ROW(256, 5)
+  DOPR_ROW(512, 3)
   DOPR_ROW(512, 4)
   DOPR_ROW(1024, 4)
   DOPR_ROW(1024, 8)
@@ -322,7 +358,7 @@ hipError_t by_width(int64_t width, F f) {
 template <int TPR>
 void row_grid(int64_t rows, dim3 &grid, dim3 &block) {
   grid = dim3((unsigned)(TPR > 64 ? rows : (rows + 3) / 4));
-  block = dim3(TPR > 256 ? TPR : 256);
+  block = dim3(TPR > 64 ? TPR : 256);
 }
 
 template <typename T>
@@ -342,7 +378,7 @@ hipError_t quantize(const QuantizeParams &P, hipStream_t s) {
 
 template <typename T, typename R>
 hipError_t norm(const NormParams &P, hipStream_t s) {
-  return by_width(P.width, [&](auto tpr, auto nv) {
+  return by_width(P.width + (P.lines ? 63 : 0), [&](auto tpr, auto nv) {
     dim3 grid, block;
     row_grid<tpr.value>(P.rows, grid, block);
     hipLaunchKernelGGL((k_norm_residual<T, R, tpr.value, nv.value>), grid,
@@ -370,6 +406,12 @@ hipError_t launch_quantize_rows(const dopr_quantize_args_t &a, hipStream_t s) {
 
 hipError_t launch_norm_residual(const dopr_norm_residual_args_t &a,
                                 hipStream_t s) {
+  const bool wide = a.residual_dtype == DOPR_F32;
+  const uintptr_t size = (a.h ? wide : a.dtype == DOPR_F32) ? 4 : 2;
+  const uintptr_t out = reinterpret_cast<uintptr_t>(a.h ? a.h : a.z);
+  const uintptr_t pitch = size * (a.h ? a.h_row_stride : a.z_row_stride);
+  const bool lines =
+      out && (out | pitch) % 128 != 0 && a.width + 63 <= kMostWidth;
   const NormParams P{a.x,
                      a.post_norm_w,
                      a.gate,
@@ -388,8 +430,8 @@ hipError_t launch_norm_residual(const dopr_norm_residual_args_t &a,
                      a.q_row_stride,
                      (int32_t)a.width,
                      a.residual_scale,
-                     a.rms_eps};
-  const bool wide = a.residual_dtype == DOPR_F32;
+                     a.rms_eps,
+                     lines};
   if (a.dtype == DOPR_BF16)
     return wide ? norm<bf16_t, float>(P, s) : norm<bf16_t, bf16_t>(P, s);
   if (a.dtype == DOPR_F16)
