@@ -7,7 +7,9 @@
 // once, then every head uses them.  A lane holds 8 pairs (16 elements) of a
 // head, so a rotation never leaves the lane, in-place calls are safe, and a
 // head's sum of squares is a butterfly over the 1 to 64 lanes of that head.
-// Bound by HBM: each head is read and written once.
+// Bound by HBM: each head is read and written once (32,768 tokens, 40 heads of
+// 128 in bf16: 115 us, 5.8 TB/s, with the norm 118, interleaved 120; half of
+// each head interleaved, out of a fused q, k, v buffer, 120).
 //
 // The angle's whole turns are dropped in 64 bits (four operations per pair
 // and token): in 32 bits the product of a position and a frequency is off by
@@ -36,9 +38,12 @@ struct RotaryParams {
   int32_t n_q, n_heads;      // query heads, all heads
   int32_t D, R;
   int32_t group_log2;        // lanes per head
-  int32_t pair_units, units; // 16-element units of a head: rotated, all
+  int32_t pair_units, units; // 16-element units of a head: rotated (where
+                             // they lie apart), all
   int32_t splits;            // waves that share a token's heads
   float factor, sign, eps;
+  bool whole;    // every lane's elements are its own
+  bool stream;   // stores past the caches' order of use
 };
 
 // A unit's two runs of 8 elements, of which [lo, n) are its own (lo = 8: none).
@@ -46,13 +51,15 @@ struct RotaryParams {
 // loads and stores whole lines.
 struct Unit {
   int pa, pb, lo_a, lo_b, n_a, n_b;
-  bool rotated;
-  int pair_a, pair_b;  // first pairs, when rotated: of the first four of the
-                       // unit's 8 and of the others
+  bool rotated;        // some of its elements turn
+  int pair_a, pair_b;  // first pairs: of the first four of the unit's 8 and of
+                       // the others
 };
 
 // SMALL: runs are cut at their part's end (element loads); else the last run
-// of a part moves back to end with it and keeps its own tail.
+// of a part moves back to end with it and keeps its own tail.  Rotate-half
+// layouts deal out the rotated part (pairs of runs R / 2 apart) and the rest of
+// a head apart; interleaved ones, whose pairs lie inside a run, the whole head.
 template <bool INTER, bool SMALL>
 __device__ __forceinline__ Unit unit_of(int u, int pair_units, int D, int R) {
   Unit k;
@@ -74,10 +81,10 @@ __device__ __forceinline__ Unit unit_of(int u, int pair_units, int D, int R) {
     k.pair_b = i0 + 4;
     return k;
   }
-  // runs of 8 elements of [from, to): unit j takes the runs j and j + units
-  const int from = k.rotated ? 0 : R, to = k.rotated ? R : D;
-  const int j = k.rotated ? u : u - pair_units;
-  const int runs = (to - from + 7) / 8, units = (runs + 1) / 2;
+  // runs of 8 elements of [from, D): unit j takes the runs j and j + units
+  const int from = INTER ? 0 : R;
+  const int j = INTER ? u : u - pair_units;
+  const int runs = (D - from + 7) / 8, units = (runs + 1) / 2;
   auto run = [&](int r, int &p, int &lo, int &n) {
     p = from + 8 * r;
     if (r >= runs) {  // an odd number of runs: no second one here
@@ -85,19 +92,20 @@ __device__ __forceinline__ Unit unit_of(int u, int pair_units, int D, int R) {
       lo = 8;
       n = SMALL ? 0 : 8;
     } else if (SMALL) {
-      n = min(8, to - p);
-    } else if (p + 8 > to) {
-      lo = p + 8 - to;
-      p = to - 8;
+      n = min(8, D - p);
+    } else if (p + 8 > D) {
+      lo = p + 8 - D;
+      p = D - 8;
     }
-    // (a run past a part's end starts in front of `to`; with to < 8 only in
-    // SMALL, which cuts it)
+    // (a run past the end starts in front of D; D < 8 only in SMALL, which
+    // cuts it)
   };
   run(j, k.pa, k.lo_a, k.n_a);
   run(j + units, k.pb, k.lo_b, k.n_b);
   if (!SMALL && k.lo_b == 8) k.pb = k.pa;  // (any run of this head)
   k.pair_a = k.pa / 2;
   k.pair_b = k.pb / 2;
+  k.rotated = INTER && k.pa < R;
   return k;
 }
 
@@ -123,21 +131,25 @@ struct Run {
     }
   }
   static __device__ __forceinline__ void store(T *p, int lo, int n,
-                                               const float *g) {
+                                               const float *g, bool stream) {
     if constexpr (SMALL) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         if (e < n) p[e] = from_f32<T>(g[e]);
     } else {
-      store_part<T, 8>(p, lo, 8, g);
+      if (stream)
+        store_part<T, 8, true>(p, lo, 8, g);
+      else
+        store_part<T, 8>(p, lo, 8, g);
     }
   }
 };
 
-template <typename T, bool INTER, bool SMALL>
-__global__ __launch_bounds__(64 * kRotaryWaves) void k_rotary(RotaryParams P) {
+template <typename T, bool INTER, bool SMALL, bool NORM>
+__global__ __launch_bounds__(64 * kRotaryWaves, 3) void k_rotary(RotaryParams P) {
   __shared__ float2 table[kRotaryWaves][256];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t item = (int64_t)blockIdx.x * kRotaryWaves + wave;
   if (item >= P.items) return;  // no block barrier below
   const int64_t tok = item / P.splits;
@@ -163,15 +175,25 @@ __global__ __launch_bounds__(64 * kRotaryWaves) void k_rotary(RotaryParams P) {
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   float c[8], s[8];
+  uint32_t turns = 0;  // pairs that turn
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    // (pairs behind a part's end belong to no element)
+    // (pairs behind a part's end belong to no element, or to none that turns)
     const int i = e < 4 ? k.pair_a + e : k.pair_b + e - 4;
     const bool in = k.rotated && i < P.R / 2;
     const float2 t = table[wave][in ? i : 0];
-    c[e] = in ? t.x : 1.f;
-    s[e] = in ? t.y : 0.f;
+    c[e] = t.x;
+    s[e] = t.y;
+    turns |= in ? 1u << e : 0u;
   }
+
+  // the token's heads, as if they all were q's or k's
+  const T *q_in = static_cast<const T *>(P.q.x) + tok * P.q.row;
+  const T *k_in = static_cast<const T *>(P.k.x) + tok * P.k.row -
+                  P.n_q * P.k.head;
+  T *q_out = static_cast<T *>(P.q.out) + tok * P.q.out_row;
+  T *k_out = static_cast<T *>(P.k.out) + tok * P.k.out_row -
+             P.n_q * P.k.out_head;
 
   for (int h0 = split * per_wave; h0 < P.n_heads; h0 += step * kRotaryBatch) {
     Run<T, SMALL> ra[kRotaryBatch], rb[kRotaryBatch];
@@ -179,9 +201,7 @@ __global__ __launch_bounds__(64 * kRotaryWaves) void k_rotary(RotaryParams P) {
     for (int b = 0; b < kRotaryBatch; ++b) {
       const int h = min(h0 + b * step + sub, P.n_heads - 1);
       const bool is_k = h >= P.n_q;
-      const RotaryHeads &H = is_k ? P.k : P.q;
-      const T *x = static_cast<const T *>(H.x) + tok * H.row +
-                   (int64_t)(is_k ? h - P.n_q : h) * H.head;
+      const T *x = (is_k ? k_in : q_in) + h * (is_k ? P.k.head : P.q.head);
       ra[b].load(x + k.pa, k.n_a);
       rb[b].load(x + k.pb, k.n_b);
     }
@@ -191,23 +211,32 @@ __global__ __launch_bounds__(64 * kRotaryWaves) void k_rotary(RotaryParams P) {
       if (h0 + b * step >= P.n_heads) break;
       const int h = min(hr, P.n_heads - 1);
       const bool is_k = h >= P.n_q;
-      const RotaryHeads &H = is_k ? P.k : P.q;
       float fa[8], fb[8];
       ra[b].get(fa);
       rb[b].get(fb);
-      if (P.q.norm_w || P.k.norm_w) {
+      if constexpr (NORM) {
         float ss = 0.f;
+        if (P.whole) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float a = e >= k.lo_a && u == u_raw ? fa[e] : 0.f;
-          const float b2 = e >= k.lo_b && u == u_raw ? fb[e] : 0.f;
-          ss = fmaf(a, a, fmaf(b2, b2, ss));
+          for (int e = 0; e < 8; ++e)
+            ss = fmaf(fa[e], fa[e], fmaf(fb[e], fb[e], ss));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float a = e >= k.lo_a && u == u_raw ? fa[e] : 0.f;
+            const float b2 = e >= k.lo_b && u == u_raw ? fb[e] : 0.f;
+            ss = fmaf(a, a, fmaf(b2, b2, ss));
+          }
         }
         for (int off = (1 << P.group_log2) >> 1; off > 0; off >>= 1)
           ss += __shfl_xor(ss, off, 64);
-        if (H.norm_w) {
-          const float inv = 1.0f / sqrtf(ss / (float)P.D + P.eps);
-          const T *w = static_cast<const T *>(H.norm_w);
+        // (the hardware's square root is off by a unit of fp32's last place,
+        // 2^-15 of a 16-bit output's)
+        const float mean = ss / (float)P.D + P.eps;
+        const float inv =
+            sizeof(T) == 2 ? __builtin_amdgcn_rsqf(mean) : 1.0f / sqrtf(mean);
+        const T *w = static_cast<const T *>(is_k ? P.k.norm_w : P.q.norm_w);
+        if (w) {
           Run<T, SMALL> wa, wb;
           wa.load(w + k.pa, k.n_a);
           wb.load(w + k.pb, k.n_b);
@@ -230,8 +259,10 @@ __global__ __launch_bounds__(64 * kRotaryWaves) void k_rotary(RotaryParams P) {
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float x0 = a[e] * c[e] - b2[e] * s[e];
-          const float x1 = b2[e] * c[e] + a[e] * s[e];
+          // (selected, not turned by zero: 0 times an infinity is NaN)
+          const bool in = !INTER || (turns >> e & 1);
+          const float x0 = in ? a[e] * c[e] - b2[e] * s[e] : a[e];
+          const float x1 = in ? b2[e] * c[e] + a[e] * s[e] : b2[e];
           if (INTER) {
             (e < 4 ? fa[2 * e] : fb[2 * e - 8]) = x0;
             (e < 4 ? fa[2 * e + 1] : fb[2 * e - 7]) = x1;
@@ -242,31 +273,32 @@ __global__ __launch_bounds__(64 * kRotaryWaves) void k_rotary(RotaryParams P) {
         }
       }
       if (hr < P.n_heads && u == u_raw) {
-        T *o = static_cast<T *>(H.out) + tok * H.out_row +
-               (int64_t)(is_k ? h - P.n_q : h) * H.out_head;
-        Run<T, SMALL>::store(o + k.pa, k.lo_a, k.n_a, fa);
-        Run<T, SMALL>::store(o + k.pb, k.lo_b, k.n_b, fb);
+        T *o = (is_k ? k_out : q_out) +
+               h * (is_k ? P.k.out_head : P.q.out_head);
+        Run<T, SMALL>::store(o + k.pa, k.lo_a, k.n_a, fa, P.stream);
+        Run<T, SMALL>::store(o + k.pb, k.lo_b, k.n_b, fb, P.stream);
       }
     }
   }
 }
 
-template <typename T, bool INTER>
-void launch(const RotaryParams &P, bool small, hipStream_t s) {
+template <typename T, bool INTER, bool SMALL>
+void launch(const RotaryParams &P, hipStream_t s) {
   const dim3 grid((unsigned)((P.items + kRotaryWaves - 1) / kRotaryWaves));
   const dim3 block(64 * kRotaryWaves);
-  if (small)
-    hipLaunchKernelGGL((k_rotary<T, INTER, true>), grid, block, 0, s, P);
+  if (P.q.norm_w || P.k.norm_w)
+    hipLaunchKernelGGL((k_rotary<T, INTER, SMALL, true>), grid, block, 0, s, P);
   else
-    hipLaunchKernelGGL((k_rotary<T, INTER, false>), grid, block, 0, s, P);
+    hipLaunchKernelGGL((k_rotary<T, INTER, SMALL, false>), grid, block, 0, s,
+                       P);
 }
 
 template <typename T>
 void launch(const RotaryParams &P, bool inter, bool small, hipStream_t s) {
   if (inter)
-    launch<T, true>(P, small, s);
+    small ? launch<T, true, true>(P, s) : launch<T, true, false>(P, s);
   else
-    launch<T, false>(P, small, s);
+    small ? launch<T, false, true>(P, s) : launch<T, false, false>(P, s);
 }
 
 }  // namespace
@@ -284,15 +316,25 @@ hipError_t launch_rotary(const dopr_rotary_args_t &a, hipStream_t s) {
   P.D = a.head_dim;
   P.R = a.rotary_dim;
   P.pair_units = (a.rotary_dim / 2 + 7) / 8;
-  P.units = P.pair_units + (a.head_dim - a.rotary_dim + 15) / 16;
+  P.units = a.interleaved
+                ? (a.head_dim + 15) / 16
+                : P.pair_units + (a.head_dim - a.rotary_dim + 15) / 16;
   while ((1 << P.group_log2) < P.units) ++P.group_log2;
   P.factor = a.attention_factor;
   P.sign = a.inverse ? -1.f : 1.f;
   P.eps = a.rms_eps;
+  P.whole = (a.interleaved || a.rotary_dim % 16 == 0) &&
+            (a.interleaved || (a.head_dim - a.rotary_dim) % 16 == 0) &&
+            a.head_dim % 16 == 0 && P.units == 1 << P.group_log2;
+  // Streamed where every store of a wave fills lines (32,768 tokens, 40 heads
+  // of 128: 118 us, else 125); in rotate-half layouts of part of a head, two
+  // stores fill one (half of each head turned: 138 us streamed, else 130).
+  P.stream = a.interleaved || a.rotary_dim == a.head_dim;
   // (runs of 8 elements that end with their part have to fit in it, or, those
-  // behind the rotated part, in the head)
-  const bool small = a.rotary_dim < (a.interleaved ? 8 : 16) ||
-                     (a.rotary_dim < a.head_dim && a.head_dim < 8);
+  // behind the rotated part, in the head; a run that moves back to end with an
+  // odd head would split its pairs)
+  const bool small = a.interleaved ? a.head_dim < 8 || a.head_dim % 2
+                                   : a.rotary_dim < 16;
   // few tokens: a token's head groups go to several waves (each forms the
   // rotations again) until about eight waves a SIMD are there
   const int groups = (P.n_heads + (64 >> P.group_log2) - 1) /

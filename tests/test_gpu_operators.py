@@ -507,6 +507,27 @@ def test_rotary_far_positions():
     R.assert_close(out, *R.rotary(x, pos, freq.to(DEV)), fp32=2.0 ** -20)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,r", [(128, 64), (128, 60), (67, 66), (65, 10),
+                                 (24, 18), (9, 2)])
+def test_rotary_leaves_the_rest_as_it_is(d, r, interleaved):
+    """Elements behind the rotated part keep their bits, next to turning ones
+    and with infinities among them; the turning ones stay finite."""
+    D = _D()
+    x = randn(gen(d + r), 7, 3, d)
+    x[:, 1, r:] = float("inf")
+    x[:, 2, r:] = -0.0
+    out = torch.empty_like(x)
+    pos = torch.arange(7, device=DEV, dtype=torch.int32)
+    freq = D.dopr_rotary_frequencies(r, 1e4)[0].to(DEV)
+    D.dopr_rotary(x, None, pos, freq, out, None, interleaved=interleaved)
+    assert torch.equal(out[..., r:].view(torch.int32),
+                       x[..., r:].view(torch.int32))
+    R.assert_close(out[..., :r], *[v[..., :r] for v in R.rotary(
+        torch.cat((x[..., :r], torch.zeros_like(x[..., r:])), -1), pos, freq,
+        interleaved)])
+
+
 def test_rotary_inverse_undoes_it():
     D = _D()
     x = randn(gen(2), 50, 4, 64)
