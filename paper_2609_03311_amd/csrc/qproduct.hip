@@ -768,10 +768,12 @@ int64_t repack_pitch(int64_t K) { return (K + kSpan - 1) / kSpan * kSpan; }
 // fill = blocks / 256 and depth in units of 256 bytes a wave.  The formula is
 // off by some 10 % a call; what it picks was on average 3.4 % slower than the
 // fastest of all 21 kernels timed from 257 rows on, 2 % from 65 to 256 and
-// 4 % below (1.5 times at worst).
+// 4 % below (1.5 times at worst).  The 224 and 192 row tiles are fitted to nine
+// sizes beside the 256 row ones, whose last round they fill better (9001 x 6144
+// x 2560 138 -> 129 us by 224, 9001 x 2560 x 9728 198 -> 171 by 192).
 enum Kernel {
-  kTile256, kTile160, kTile192x128, kTile160x128, kTile128, kTile128Deep,
-  kTile64x128, kTile64x128Two, kTile64Two, kTile48Four, kTile32Four,
+  kTile256, kTile224, kTile192, kTile160, kTile192x128, kTile160x128,
+  kTile128, kTile128Deep, kTile64x128, kTile64x128Two, kTile64Two, kTile48Four, kTile32Four,
   kTile16Four, kFew, kKernels
 };
 struct Shape {
@@ -782,6 +784,8 @@ struct Shape {
 };
 constexpr Shape kShapes[kKernels] = {
     {256, 256, 1, 1, 3.14f, 8.44f, 1.350f, 0.f},
+    {224, 256, 1, 1, 3.40f, 7.04f, 1.278f, 0.f},
+    {192, 256, 1, 1, 3.40f, 5.79f, 1.151f, 0.f},
     {160, 256, 1, 1, 3.98f, 6.55f, 0.955f, 0.f},
     {192, 128, 1, 1, 3.95f, 4.98f, 0.708f, 0.f},
     {160, 128, 1, 1, 4.36f, 4.89f, 0.562f, 0.f},
@@ -844,6 +848,8 @@ template <typename T>
 hipError_t product_by_size(const ProductParams &P, hipStream_t s) {
   switch (choose(P.M, P.N, P.K)) {
     case kTile256: return product_tiles<T, 8, 2, 4, 1, 2>(P, s);
+    case kTile224: return product_tiles<T, 7, 2, 4, 1, 2>(P, s);
+    case kTile192: return product_tiles<T, 6, 2, 4, 1, 2>(P, s);
     case kTile160: return product_tiles<T, 5, 2, 4, 1, 3>(P, s);
     case kTile192x128: return product_tiles<T, 6, 2, 2, 1, 3>(P, s);
     case kTile160x128: return product_tiles<T, 5, 2, 2, 1, 4>(P, s);
