@@ -345,6 +345,7 @@ k_product(ProductParams P, int tm, int tn) {
   int m0, n0;
   const int8_t *xbase, *wbase;
   uint32_t off[kLoads];
+  int turned = 0;  // the span that the depth starts with
   // the lanes of a load fill 64 slots in order (rows 4 to 7 of 8: chunks 4
   // apart too, in odd blocks)
   const int chunk = ((lane & 7) ^ ((lane >> 4) & 3)) * 16;
@@ -361,6 +362,11 @@ k_product(ProductParams P, int tm, int tn) {
     tile_of(b, tm, tn, bm, bn);
     m0 = bm * kBM;
     n0 = bn * kBN;
+    // Rows a multiple of 4096 bytes apart put equal depths on the same memory
+    // channels.  A single row of tiles shares nothing but x, so every tile can
+    // start elsewhere (129 x 24576 x 4096 31.7 -> 28.7 us, x 32768 38.8 ->
+    // 33.1); tiles that share w stay in step.
+    if (tm == 1 && full > 0) turned = bn % full;
     xbase = P.x + (int64_t)m0 * P.ldx;
     wbase = P.w + (int64_t)n0 * P.ldw;
 #pragma unroll
@@ -370,9 +376,11 @@ k_product(ProductParams P, int tm, int tn) {
   const uint32_t dst = lds_address(lds);
   auto issue1 = [&](int t, int i) {
     const int blk = block_of(i);
+    int span = t * WK + group + turned;
+    span -= span >= full ? full : 0;
     dma16(dst + (t % ST) * kStageBytes + blk * 1024,
           (blk >= kBM / 8 ? wbase : xbase) +
-              (int64_t)(t * WK + group) * kSpan,
+              (int64_t)span * kSpan,
           off[i]);
   };
   // the tile's scales, to the half of theirs that its turn picks
@@ -690,13 +698,22 @@ __global__ __launch_bounds__(256) void k_product_few(ProductParams P) {
     for (int u = 0; u < kFewSteps; ++u) product1(b.x[u], b.w[u]);
   };
   const int batches = (int)(P.K / kBatch);
+  // blocks start at different depths, those of an XCD (every 8th) one batch
+  // apart: rows 4096 bytes apart put equal depths on the same memory channels
+  // (1 x 24576 x 4096 23.5 -> 19.1 us, 5.3 TB/s, x 6144 8.0 -> 6.9)
+  const int turned =
+      batches > 0 ? (int)(blockIdx.x / 8 % (unsigned)batches) : 0;
+  auto next = [&](int i, Batch &to) {
+    i += turned;
+    fetch(i >= batches ? i - batches : i, to);
+  };
   Batch a, b;
-  if (wave < batches) fetch(wave, a);
+  if (wave < batches) next(wave, a);
   for (int i = wave; i < batches; i += 2 * WK) {
-    if (i + WK < batches) fetch(i + WK, b);
+    if (i + WK < batches) next(i + WK, b);
     multiply(a);
     if (i + WK >= batches) break;
-    if (i + 2 * WK < batches) fetch(i + 2 * WK, a);
+    if (i + 2 * WK < batches) next(i + 2 * WK, a);
     multiply(b);
   }
   // steps behind the last whole batch, one at a time, first to the waves that
