@@ -208,6 +208,10 @@ void heads(PyObject *x, PyObject *out, const char *what, const char *out_what,
   const int64_t h = t.dim() == 3 ? t.size(1) : -1;
   expect(x, what, type, {rows, h, d});
   const at::Tensor &u = expect(out, out_what, type, {rows, h, d});
+  if (h > INT32_MAX || d > INT32_MAX) {
+    PyErr_Format(PyExc_ValueError, "%s has too many heads or elements", what);
+    throw Refused{};
+  }
   n = (int32_t)h;
   p = t.data_ptr();
   row = t.stride(0);

@@ -302,8 +302,12 @@ class QuantLayerStep:
     def prefix_states(self, x, positions, k_norm_w, stream=None):
         """Keys and values of this layer for prefix inputs x [slots, W] at
         `positions` (int32 [slots]): bf16 [slots, Hkv, D] each, the keys
-        normed and rotated, as dopr_store_put takes them."""
+        normed and rotated, as dopr_store_put takes them.  With a stream, they
+        and the scratch in between are allocated on it."""
         import torch
+        if stream is not None and stream != torch.cuda.current_stream():
+            with torch.cuda.stream(stream):
+                return self.prefix_states(x, positions, k_norm_w)
         n, d, hk = x.shape[0], self.store.head_dim, self.store.n_kv_heads
         x8 = self._int8(n, self.hidden, x.device)[:, :self.hidden]
         scale = torch.empty(n, dtype=torch.float32, device=x.device)

@@ -31,6 +31,11 @@ def rel_rms(got, ref):
     return (d.pow(2).mean() / ref.pow(2).mean()).sqrt().item()
 
 
+def randn_bf16(*shape, seed=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return torch.randn(shape, generator=g, device=DEV).bfloat16()
+
+
 def make(hq=8, hkv=4, hidden=256, inter=512, seed=0, head_dim=128):
     rng = np.random.default_rng(seed)
     doc_len = np.array([0, 7, 40, 96, 130], np.int32)
@@ -222,6 +227,32 @@ def test_prefix_states(interleaved, r):
                           gain=prm["k_norm_w"])
         assert rel_rms(k, ref) <= 1.5e-2
         assert rel_rms(v, project("w_v")) <= 1.5e-2
+
+
+def test_prefix_states_on_another_stream():
+    """The same bits, with outputs and scratch in that stream's memory: the
+    current stream's next allocations are not written by pending kernels."""
+    from paper_2609_03311_amd import pipeline
+    st, w = make(seed=4)
+    store = pipeline.make_store(st.doc_len, st.n_kv_heads,
+                                *workloads.prefix_source(st, DEV, 1)[:2])
+    prm = workloads.params(st, DEV)
+    step = pipeline.QuantLayerStep(
+        store, w, n_pairs=st.n_pairs, n_q_heads=st.n_q_heads,
+        total_tokens=st.n_tokens, max_tokens=int(st.seqlens.max()),
+        hidden=256, intermediate=512)
+    x = randn_bf16(4000, 256)
+    pos = torch.arange(4000, device=DEV, dtype=torch.int32)
+    want = step.prefix_states(x, pos, prm["k_norm_w"])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = step.prefix_states(x, pos, prm["k_norm_w"], stream=side)
+    for _ in range(4):  # sizes of the call's scratch, on the current stream
+        torch.empty((4000, 256), dtype=torch.int8, device=DEV).fill_(77)
+        torch.empty(4000, device=DEV).fill_(1e9)
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
 
 
 def test_online_positions():
