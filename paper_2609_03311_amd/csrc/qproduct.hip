@@ -10,10 +10,11 @@
 // and 16 rows of x as the second: lane l holds 16 consecutive bytes (depth
 // 16 * (l / 16) ..) of row l % 16 of each, and of the result column l % 16 (a
 // row of x) at rows 4 * (l / 16) .. + 3 (of w).  A wave's 64 rows of w are
-// dealt to its four operands so that a lane's 16 results of one x row are two
-// runs of 8 consecutive columns of y, 32 apart, and the four lanes that hold
-// an x row store 64 whole bytes of it at a time (bf16): operand f, row i is w
-// row 32 * (f / 2) + 8 * (i / 4) + 4 * (f % 2) + i % 4.
+// dealt to its four operands so that the four lanes that hold an x row store 64
+// whole bytes of it at a time: with outputs of 16 bits a lane's 16 results of
+// one x row are two runs of 8 consecutive columns of y, 32 apart (operand f,
+// row i is w row 32 * (f / 2) + 8 * (i / 4) + 4 * (f % 2) + i % 4), with fp32
+// four runs of 4, 16 apart (w row 16 f + i).
 #include <type_traits>
 
 #include "rowio.hpp"
@@ -31,20 +32,32 @@ struct ProductParams {
   int64_t M, N, K, ldx, ldw, ldr, ldy;
 };
 
-// w row (of 64) behind LDS row p
-__device__ __forceinline__ int w_row(int p) {
-  return (p & ~63) + (p & 32) + ((p >> 2) & 3) * 8 + ((p >> 4) & 1) * 4 +
-         (p & 3);
-}
-// first column of a lane's two runs, among a wave's 64
-__device__ __forceinline__ int lane_column(int lane) {
-  return (lane >> 4) * 8;
-}
-constexpr int kRunApart = 32;
+// The runs of columns of y that a lane's 16 results make up in an x row.
+template <typename T>
+struct Runs {
+  static constexpr int kLength = 16 / (int)sizeof(T);  // 16 bytes
+  static constexpr int kApart = 4 * kLength;           // of four lanes: 64
+  static constexpr int kCount = 16 / kLength;
+  // a run's first column in the first run's place, among a wave's 64
+  static __device__ __forceinline__ int column(int lane) {
+    return (lane >> 4) * kLength;
+  }
+  // result e's column behind it
+  static __device__ __forceinline__ constexpr int of(int e) {
+    return kApart * (e / kLength) + e % kLength;
+  }
+  // w row (of 64) behind LDS row p
+  static __device__ __forceinline__ int w_row(int p) {
+    if constexpr (kLength == 4)
+      return p;
+    else
+      return (p & ~31) + ((p >> 2) & 3) * 8 + ((p >> 4) & 1) * 4 + (p & 3);
+  }
+};
 
-// Finishes a lane's part of a tile: two runs of 8 columns of y, from n and n +
-// kRunApart on, in the FM rows m, m + 16, .. with own(i).  sums(i, v) gives row
-// i's integer sums, column_scales(scale) and row_scale(i) the scales.
+// Finishes a lane's part of a tile: its runs of columns of y, the first from n
+// on, in the FM rows m, m + 16, .. with own(i).  sums(i, v) gives row i's
+// integer sums, column_scales(scale) and row_scale(i) the scales.
 template <typename T, int FM, typename Columns, typename Row, typename Sums,
           typename Own>
 __device__ __forceinline__ void finish(const ProductParams &P, int m, int n,
@@ -58,59 +71,80 @@ __device__ __forceinline__ void finish(const ProductParams &P, int m, int n,
   const T *bias = static_cast<const T *>(P.bias) + n;
   const T *res = static_cast<const T *>(P.res) + m * P.ldr + n;
   T *y = static_cast<T *>(P.y) + m * P.ldy + n;
-  const bool whole = left >= kRunApart + 8;
+  using R = Runs<T>;
+  constexpr int L = R::kLength;
+  const bool whole = left > R::of(15);
+  Raw<T, L> add[R::kCount];
+  if (P.bias && whole)
+#pragma unroll
+    for (int h = 0; h < R::kCount; ++h) add[h].load(bias + R::kApart * h);
+  float plus[16] = {};
+  if (P.bias && whole)
+#pragma unroll
+    for (int h = 0; h < R::kCount; ++h) add[h].get(plus + L * h);
+  // a row's residual is asked for ahead of the stores of the row before it,
+  // which it would otherwise wait for (loads and stores complete in order)
+  auto ask = [&](int i) {
+    if (P.res && whole && own(i) && m + 16 * i < (int)P.M)
+#pragma unroll
+      for (int h = 0; h < R::kCount; ++h)
+        add[h].load(res + 16 * i * P.ldr + R::kApart * h);
+  };
+  ask(0);
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
-    if (own(i) && m + 16 * i < (int)P.M) {
-      float v[16];
+    const bool mine = own(i) && m + 16 * i < (int)P.M;
+    float v[16];
+    if (mine) {
       const float xs = row_scale(i);
       sums(i, v);
 #pragma unroll
       for (int e = 0; e < 16; ++e) v[e] = v[e] * xs * scale[e];
+      if (P.bias)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] += plus[e];
+      if (P.res && whole) {
+        float f[16];
+#pragma unroll
+        for (int h = 0; h < R::kCount; ++h) add[h].get(f + L * h);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] += f[e];
+      }
+    }
+    if (i + 1 < FM) ask(i + 1);
+    if (mine) {
       if (whole) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float *u = v + 8 * h, f[8];
-          Raw8<T> r;
-          if (P.bias) {
-            r.load(bias + kRunApart * h);
-            r.get(f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) u[e] += f[e];
-          }
-          if (P.res) {
-            r.load(res + kRunApart * h);
-            r.get(f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) u[e] += f[e];
-          }
-          store8<T, true>(y + kRunApart * h, u);
+        for (int h = 0; h < R::kCount; ++h) {
+          if constexpr (L == 8)
+            store8<T, true>(y + R::kApart * h, v + L * h);
+          else
+            store4<T, true>(y + R::kApart * h, v + L * h);
         }
       } else {  // the matrix ends inside: one by one
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int c = kRunApart * (e >> 3) + (e & 7);
+          const int c = R::of(e);
           if (c < left) {
             if (P.bias) v[e] += to_f32<T>(bias[c]);
-            if (P.res) v[e] += to_f32<T>(res[c]);
+            if (P.res) v[e] += to_f32<T>(res[16 * i * P.ldr + c]);
             y[c] = from_f32<T>(v[e]);
           }
         }
       }
     }
     y += 16 * P.ldy;
-    if (P.res) res += 16 * P.ldr;
     __builtin_amdgcn_sched_barrier(0);  // (one row's values at a time)
   }
 }
 
 // The scales of finish from memory.
+template <typename T>
 __device__ __forceinline__ void columns_from_memory(const ProductParams &P,
                                                     int n, float *scale) {
 #pragma unroll
   for (int e = 0; e < 16; ++e)
-    scale[e] = P.w_scale[min(n + kRunApart * (e >> 3) + (e & 7),
-                             (int)P.N - 1)];
+    scale[e] = P.w_scale[min(n + Runs<T>::of(e), (int)P.N - 1)];
 }
 
 // 16 bytes of a row from depth k, zeros from K on.  Nothing behind the row is
@@ -176,8 +210,8 @@ __global__ __launch_bounds__(256, 3) void k_product_any(ProductParams P,
     // rows behind the end repeat the last one; their results are not stored
     at[i] = r < kAnyM
                 ? P.x + (int64_t)min(m0 + r, (int)P.M - 1) * P.ldx
-                : P.w + (int64_t)min(n0 + w_row(r - kAnyM), (int)P.N - 1) *
-                            P.ldw;
+                : P.w + (int64_t)min(n0 + Runs<T>::w_row(r - kAnyM),
+                                     (int)P.N - 1) * P.ldw;
     slot[i] = span_slot(r, tid & 7);
   }
   u32x4 next[kLoads];
@@ -223,10 +257,10 @@ __global__ __launch_bounds__(256, 3) void k_product_any(ProductParams P,
               wf[j], xf[i], acc[i][j], 0, 0, 0);
     }
   }
-  const int m = m0 + wm + (lane & 15), n = n0 + wn + lane_column(lane);
+  const int m = m0 + wm + (lane & 15), n = n0 + wn + Runs<T>::column(lane);
   finish<T, 2>(
       P, m, n,
-      [&](float *scale) { columns_from_memory(P, n, scale); },
+      [&](float *scale) { columns_from_memory<T>(P, n, scale); },
       [&](int i) { return P.x_scale[m + 16 * i]; },
       [&](int i, float *v) {
 #pragma unroll
@@ -354,7 +388,8 @@ k_product(ProductParams P, int tm, int tn) {
   auto row_offset = [&](int blk) {
     const bool w = blk >= kBM / 8;
     const int r = (w ? blk - kBM / 8 : blk) * 8 + (lane >> 3);
-    return w ? (uint32_t)min(w_row(r), (int)P.N - 1 - n0) * (uint32_t)P.ldw
+    return w ? (uint32_t)min(Runs<T>::w_row(r), (int)P.N - 1 - n0) *
+                   (uint32_t)P.ldw
              : (uint32_t)min(r, (int)P.M - 1 - m0) * (uint32_t)P.ldx;
   };
   auto take = [&](int64_t b) {
@@ -552,7 +587,7 @@ k_product(ProductParams P, int tm, int tn) {
     // every wave is behind the last barrier, so all buffers are free: the
     // next tile's first loads go out before this one is finished
     if (full == 0) stage_wait<0>();  // (the scales: else they came first)
-    const int m = m0 + wm + (lane & 15), n = n0 + wn + lane_column(lane);
+    const int m = m0 + wm + (lane & 15), n = n0 + wn + Runs<T>::column(lane);
     const float *tile_scale = scale_lds + turn * kScaleSlots;
     tile += gridDim.x;
     const bool more = tile < tm * tn;
@@ -571,10 +606,10 @@ k_product(ProductParams P, int tm, int tn) {
     finish<T, FM>(
         P, m, n,
         [&](float *scale) {
-          const float *s = tile_scale + kBM + wn + lane_column(lane);
+          const float *s = tile_scale + kBM + wn + Runs<T>::column(lane);
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            scale[e] = s[kRunApart * (e >> 3) + (e & 7)];
+            scale[e] = s[Runs<T>::of(e)];
         },
         [&](int i) { return tile_scale[wm + 16 * i + (lane & 15)]; },
         [&](int i, float *v) {
