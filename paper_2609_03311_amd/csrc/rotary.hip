@@ -230,11 +230,16 @@ __global__ __launch_bounds__(64 * kRotaryWaves, 3) void k_rotary(RotaryParams P)
         }
         for (int off = (1 << P.group_log2) >> 1; off > 0; off >>= 1)
           ss += __shfl_xor(ss, off, 64);
-        // (the hardware's square root is off by a unit of fp32's last place,
-        // 2^-15 of a 16-bit output's)
+        // 16-bit outputs: the hardware's 1 / sqrt, off by a unit of fp32's last
+        // place, 2^-15 of theirs (it takes subnormals for 0: small means are
+        // scaled)
         const float mean = ss / (float)P.D + P.eps;
+        const bool small = mean < 0x1p-64f;
         const float inv =
-            sizeof(T) == 2 ? __builtin_amdgcn_rsqf(mean) : 1.0f / sqrtf(mean);
+            sizeof(T) == 2
+                ? __builtin_amdgcn_rsqf(small ? mean * 0x1p64f : mean) *
+                      (small ? 0x1p32f : 1.f)
+                : 1.0f / sqrtf(mean);
         const T *w = static_cast<const T *>(is_k ? P.k.norm_w : P.q.norm_w);
         if (w) {
           Run<T, SMALL> wa, wb;

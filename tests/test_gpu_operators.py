@@ -528,6 +528,23 @@ def test_rotary_leaves_the_rest_as_it_is(d, r, interleaved):
         interleaved)])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rotary_norm_of_tiny_heads(dtype):
+    """Without an epsilon, heads whose mean square is subnormal in fp32 are
+    normed like any other."""
+    D = _D()
+    scale = 2.0 ** -18 if dtype == torch.float16 else 2.0 ** -66
+    x = randn(gen(8), 5, 4, 128, dtype=dtype, scale=scale)
+    pos = torch.arange(5, device=DEV, dtype=torch.int32)
+    freq = D.dopr_rotary_frequencies(128, 1e4)[0].to(DEV)
+    w = torch.ones(128, dtype=dtype, device=DEV)
+    out = torch.empty_like(x)
+    D.dopr_rotary(x, None, pos, freq, out, None, q_norm_w=w, rms_eps=0.0)
+    # subnormal squares keep 2^-149 each: 128 of them, of a mean of 2^-132
+    R.assert_close(out, *R.rotary(x, pos, freq, gain=w, eps=0.0),
+                   fp32=2.0 ** -15 + 2.0 ** -16)
+
+
 def test_rotary_inverse_undoes_it():
     D = _D()
     x = randn(gen(2), 50, 4, 64)
