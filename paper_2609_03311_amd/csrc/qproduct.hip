@@ -815,23 +815,23 @@ int64_t repack_pitch(int64_t K) { return (K + kSpan - 1) / kSpan * kSpan; }
 // Choice of the kernel.
 
 // The tiles, the few-row blocks, and what a call through each takes: fitted to
-// its times on 23 (cols, depth) pairs x 28 row counts from 17 to 12,900, all
-// operands fresh from HBM,
+// its times on 18 (cols, depth) pairs x up to 22 row counts from 17 to 12,900
+// (bf16 outputs, operands mostly fresh from HBM), then moved to what picks the
+// fastest most often,
 //   microseconds = base + rounds * (round + spans * span)
 //                  + spans * block_span * (blocks a CU runs, over all rounds)
 // with `rounds` the times the 256 CUs are filled and `spans` the spans of 128
 // a group of waves goes through; for the few-row blocks
 //   base + round * fill + depth * (span + block_span * fill),
-// fill = blocks / 256 and depth in units of 256 bytes a wave.  The formula is
-// off by some 10 % a call; what it picks was on average 3.4 % slower than the
-// fastest of all 21 kernels timed from 257 rows on, 2 % from 65 to 256 and
-// 4 % below (1.5 times at worst).  The 224 and 192 row tiles are fitted to nine
-// sizes beside the 256 row ones, whose last round they fill better (9001 x 6144
-// x 2560 138 -> 129 us by 224, 9001 x 2560 x 9728 198 -> 171 by 192).
+// fill = blocks / 256 and depth in units of 256 bytes a wave.  What it picks was
+// on average 1.1 % slower than the fastest kernel from 65 rows on (1.3 times at
+// worst) and 3.7 % below (1.5 times).  The 224 and 192 row tiles fill rounds that
+// leave the 256 row ones idle (9001 x 6144 x 2560 138 -> 129 us by 224, 9001 x
+// 2560 x 9728 198 -> 171 by 192).
 enum Kernel {
   kTile256, kTile224, kTile192, kTile160, kTile192x128, kTile160x128,
-  kTile128, kTile128Deep, kTile64x128, kTile64x128Two, kTile64Two, kTile48Four, kTile32Four,
-  kTile16Four, kFew, kKernels
+  kTile128, kTile128Deep, kTile64x128, kTile64x128Two, kTile64Two,
+  kTile48Four, kTile32Four, kTile16Four, kFew, kKernels
 };
 struct Shape {
   int rows, cols;    // of a tile or block
@@ -840,21 +840,21 @@ struct Shape {
   float base, round, span, block_span;
 };
 constexpr Shape kShapes[kKernels] = {
-    {256, 256, 1, 1, 3.14f, 8.44f, 1.350f, 0.f},
-    {224, 256, 1, 1, 3.40f, 7.04f, 1.278f, 0.f},
-    {192, 256, 1, 1, 3.40f, 5.79f, 1.151f, 0.f},
-    {160, 256, 1, 1, 3.98f, 6.55f, 0.955f, 0.f},
-    {192, 128, 1, 1, 3.95f, 4.98f, 0.708f, 0.f},
-    {160, 128, 1, 1, 4.36f, 4.89f, 0.562f, 0.f},
-    {128, 128, 1, 2, 4.15f, 3.89f, 0.173f, 0.340f},
-    {128, 128, 1, 1, 3.96f, 3.97f, 0.480f, 0.f},
-    {64, 128, 1, 3, 4.28f, 2.93f, 0.185f, 0.218f},
-    {64, 128, 2, 1, 4.81f, 2.56f, 0.660f, 0.f},
-    {64, 64, 2, 2, 2.57f, 2.96f, 0.138f, 0.399f},
-    {48, 64, 4, 1, 1.84f, 3.45f, 0.883f, 0.f},
-    {32, 64, 4, 1, 2.60f, 3.01f, 0.579f, 0.f},
-    {16, 64, 4, 1, 0.51f, 3.92f, 0.513f, 0.f},
-    {32, 16, 4, 0, 3.53f, 0.301f, 0.712f, 0.636f},
+    {256, 256, 1, 1, 0.17f, 7.26f, 1.138f, 0.000f},
+    {224, 256, 1, 1, 0.37f, 8.44f, 1.068f, 0.000f},
+    {192, 256, 1, 1, 0.00f, 5.79f, 1.035f, 0.000f},
+    {160, 256, 1, 1, 0.34f, 7.82f, 0.739f, 0.000f},
+    {192, 128, 1, 1, 1.29f, 6.02f, 0.703f, 0.000f},
+    {160, 128, 1, 1, 1.73f, 5.27f, 0.577f, 0.000f},
+    {128, 128, 1, 2, 1.91f, 3.73f, 0.389f, 0.262f},
+    {128, 128, 1, 1, 1.58f, 4.89f, 0.499f, 0.000f},
+    {64, 128, 1, 3, 2.84f, 2.86f, 0.215f, 0.241f},
+    {64, 128, 2, 1, 1.91f, 5.31f, 0.602f, 0.000f},
+    {64, 64, 2, 2, 2.43f, 1.86f, 0.383f, 0.182f},
+    {48, 64, 4, 1, 1.44f, 3.54f, 0.907f, 0.000f},
+    {32, 64, 4, 1, 1.78f, 2.54f, 0.611f, 0.000f},
+    {16, 64, 4, 1, 0.57f, 3.54f, 0.475f, 0.000f},
+    {32, 16, 4, 0, 2.35f, 0.16f, 0.694f, 0.798f},
 };
 constexpr int kFewRows = 16;   // up to here: one x operand, k_product_few
 
