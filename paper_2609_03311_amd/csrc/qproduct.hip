@@ -30,6 +30,10 @@ struct ProductParams {
   const void *bias, *res;
   void *y;
   int64_t M, N, K, ldx, ldw, ldr, ldy;
+  // y's rows lie on 64 bytes: four lanes' stores fill a piece of memory, so they
+  // go past the caches' order of use.  Off them, two waves' stores meet in a
+  // piece, in L2 (10,014 x 14,985 x 3968 to bf16 609 -> 537 us).
+  bool stream;
 };
 
 // The runs of columns of y that a lane's 16 results make up in an x row.
@@ -58,12 +62,12 @@ struct Runs {
 // Finishes a lane's part of a tile: its runs of columns of y, the first from n
 // on, in the FM rows m, m + 16, .. with own(i).  sums(i, v) gives row i's
 // integer sums, column_scales(scale) and row_scale(i) the scales.
-template <typename T, int FM, typename Columns, typename Row, typename Sums,
-          typename Own>
-__device__ __forceinline__ void finish(const ProductParams &P, int m, int n,
-                                       Columns &&column_scales,
-                                       Row &&row_scale, Sums &&sums,
-                                       Own &&own) {
+template <typename T, int FM, bool STREAM, typename Columns, typename Row,
+          typename Sums, typename Own>
+__device__ __forceinline__ void finish_rows(const ProductParams &P, int m,
+                                            int n, Columns &&column_scales,
+                                            Row &&row_scale, Sums &&sums,
+                                            Own &&own) {
   const int left = (int)P.N - n;
   if (left <= 0) return;
   float scale[16];
@@ -116,10 +120,8 @@ __device__ __forceinline__ void finish(const ProductParams &P, int m, int n,
       if (whole) {
 #pragma unroll
         for (int h = 0; h < R::kCount; ++h) {
-          if constexpr (L == 8)
-            store8<T, true>(y + R::kApart * h, v + L * h);
-          else
-            store4<T, true>(y + R::kApart * h, v + L * h);
+          T *to = y + R::kApart * h;
+          store_part<T, L, STREAM>(to, 0, L, v + L * h);
         }
       } else {  // the matrix ends inside: one by one
 #pragma unroll
@@ -136,6 +138,19 @@ __device__ __forceinline__ void finish(const ProductParams &P, int m, int n,
     y += 16 * P.ldy;
     __builtin_amdgcn_sched_barrier(0);  // (one row's values at a time)
   }
+}
+
+template <typename T, int FM, typename Columns, typename Row, typename Sums,
+          typename Own>
+__device__ __forceinline__ void finish(const ProductParams &P, int m, int n,
+                                       Columns &&column_scales,
+                                       Row &&row_scale, Sums &&sums,
+                                       Own &&own) {
+  // (apart: one loop with both kinds of store was slower than either)
+  if (P.stream)
+    finish_rows<T, FM, true>(P, m, n, column_scales, row_scale, sums, own);
+  else
+    finish_rows<T, FM, false>(P, m, n, column_scales, row_scale, sums, own);
 }
 
 // The scales of finish from memory.
@@ -291,7 +306,7 @@ hipError_t product_any(const ProductParams &P, hipStream_t s) {
 // there, and the loads of ST spans later follow it.
 
 // Measured: 12,900 x 24576 x 4096 1040 us, 2.5 POP/s, the matrix cores busy for
-// 62 % of the cycles and the rest of the time behind the next span's loads (two
+// 64 % of the cycles and the rest of the time behind the next span's loads (two
 // spans fill the LDS); 129 x 24576 x 4096 28 us, bound by L2, through which every
 // tile reads all of x beside its part of w.
 
@@ -961,11 +976,18 @@ size_t product_workspace(int64_t M, int64_t N, int64_t K) {
              : (size_t)((M + N) * repack_pitch(K));
 }
 
+static bool whole_pieces(const dopr_quant_matmul_args_t &a) {
+  const int64_t size = a.dtype == DOPR_F32 ? 4 : 2;
+  return (reinterpret_cast<uintptr_t>(a.y) |
+          (uintptr_t)(a.y_row_stride * size)) % 64 == 0;
+}
+
 hipError_t launch_product(const dopr_quant_matmul_args_t &a, hipStream_t s) {
   const ProductParams P{a.x,    a.w,      a.x_scale,      a.w_scale,
                         a.bias, a.residual, a.y,          a.rows,
                         a.cols, a.depth,  a.x_row_stride, a.w_row_stride,
-                        a.residual_row_stride, a.y_row_stride};
+                        a.residual_row_stride, a.y_row_stride,
+                        whole_pieces(a)};
   if (a.dtype == DOPR_BF16) return product<bf16_t>(P, a.workspace, a.workspace_bytes, s);
   if (a.dtype == DOPR_F16) return product<_Float16>(P, a.workspace, a.workspace_bytes, s);
   return product<float>(P, a.workspace, a.workspace_bytes, s);
