@@ -306,7 +306,7 @@ hipError_t product_any(const ProductParams &P, hipStream_t s) {
 // there, and the loads of ST spans later follow it.
 
 // Measured: 12,900 x 24576 x 4096 1040 us, 2.5 POP/s, the matrix cores busy for
-// 64 % of the cycles and the rest of the time behind the next span's loads (two
+// 63 % of the cycles and the rest of the time behind the next span's loads (two
 // spans fill the LDS); 129 x 24576 x 4096 28 us, bound by L2, through which every
 // tile reads all of x beside its part of w.
 

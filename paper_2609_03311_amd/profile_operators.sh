@@ -4,8 +4,7 @@
 # tokens; the bf16 layer runs beside it for comparison):
 #   quant_layer_qwen3_8b_kernel_stats.txt   time of every kernel
 #   k_product_qwen3_8b_pmc.txt              shader counters of the products
-# Raw output stays in gpurun_out/prof_operators/; the summaries are written to
-# gpurun_out/summaries/.
+# Raw output stays under $out, the summaries are written to $sum.
 # usage: bash paper_2609_03311_amd/profile_operators.sh
 set -o pipefail
 R=$(cd "$(dirname "$0")/.." && pwd)
