@@ -944,8 +944,8 @@ hipError_t product(ProductParams P, void *workspace, size_t bytes,
   if (P.M <= kFewRows) {
     // the loads of a whole operand cost the few-row blocks as much as w's:
     // from 9 rows, wide and deep products go through LDS tiles instead (16
-    // rows through 6144 x 4096 10.4 and 8.4 us, through 24576 x 4096 28.7 and
-    // 25.0, but through 4096 x 12288 17.2 and 24.0, 6144 x 1024 5.0 and 5.7)
+    // rows through 6144 x 4096 9.4 and 7.5 us, through 24576 x 4096 26.2 and
+    // 24.3, but through 4096 x 12288 12.9 and 14.2)
     if (P.M > 8 && P.N >= 6144 && P.K >= 4096 && aligned_rows(P))
       return product_tiles<T, 1, 1, 1, 4, 3>(P, s);
     return product_few<T, 1>(P, s);
