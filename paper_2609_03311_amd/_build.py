@@ -41,7 +41,9 @@ ARCH = "gfx950"
 
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
-    "-Wall", "-Wno-unused-function",
+    # (output of compilations that succeed is not shown: what must not pass
+    # is an error)
+    "-Wall", "-Wno-unused-function", "-Werror=align-mismatch",
     # results must not depend on which template instance or inlining
     # context the compiler fuses multiply-adds in: fuse only where written
     "-ffp-contract=off",

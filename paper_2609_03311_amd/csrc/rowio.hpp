@@ -156,34 +156,42 @@ struct Chunk {
   }
 };
 
-// STREAM: past the caches' order of use, for stores of whole lines that
-// nothing reads soon.
-template <bool STREAM, typename V, typename P>
-__device__ __forceinline__ void put(const V &v, P *p) {
+// 16 and 8 bytes to any byte.  (The places keep their types: passed on as a
+// template's pointer they would be taken to lie on their size.)  STREAM: past
+// the caches' order of use, for stores of whole lines that nothing reads soon.
+template <bool STREAM>
+__device__ __forceinline__ void put(u32x4 v, void *p) {
+  u32x4_any *to = static_cast<u32x4_any *>(p);
   if constexpr (STREAM)
-    __builtin_nontemporal_store(v, p);
+    __builtin_nontemporal_store(v, to);
   else
-    *p = v;
+    *to = v;
+}
+template <bool STREAM>
+__device__ __forceinline__ void put(u32x2 v, void *p) {
+  u32x2_any *to = static_cast<u32x2_any *>(p);
+  if constexpr (STREAM)
+    __builtin_nontemporal_store(v, to);
+  else
+    *to = v;
 }
 
 template <typename T, bool STREAM = false>
 __device__ __forceinline__ void store4(T *p, const float *f) {
-  if constexpr (sizeof(T) == 2) {
-    const u32x2 u = {pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3])};
-    put<STREAM>(u, reinterpret_cast<u32x2_any *>(p));
-  } else {
-    const u32x4 u = {__float_as_uint(f[0]), __float_as_uint(f[1]),
-                     __float_as_uint(f[2]), __float_as_uint(f[3])};
-    put<STREAM>(u, reinterpret_cast<u32x4_any *>(p));
-  }
+  if constexpr (sizeof(T) == 2)
+    put<STREAM>(u32x2{pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3])}, p);
+  else
+    put<STREAM>(u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]),
+                      __float_as_uint(f[2]), __float_as_uint(f[3])},
+                p);
 }
 
 template <typename T, bool STREAM = false>
 __device__ __forceinline__ void store8(T *p, const float *f) {
   if constexpr (sizeof(T) == 2) {
-    const u32x4 u = {pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]),
-                     pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7])};
-    put<STREAM>(u, reinterpret_cast<u32x4_any *>(p));
+    put<STREAM>(u32x4{pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]),
+                      pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7])},
+                p);
   } else {
     store4<T, STREAM>(p, f);
     store4<T, STREAM>(p + 4, f + 4);
