@@ -15,6 +15,7 @@
 // one x row are two runs of 8 consecutive columns of y, 32 apart (operand f,
 // row i is w row 32 * (f / 2) + 8 * (i / 4) + 4 * (f % 2) + i % 4), with fp32
 // four runs of 4, 16 apart (w row 16 f + i).
+#include <atomic>
 #include <type_traits>
 
 #include "rowio.hpp"
@@ -641,6 +642,21 @@ k_product(ProductParams P, int tm, int tn) {
   }
 }
 
+// Lets a kernel have so much dynamic LDS on the current device (64 KB until it
+// asks for more); `devices` holds those that have granted it, by bits.
+hipError_t allow_lds(const void *kernel, size_t bytes,
+                     std::atomic<uint64_t> &devices) {
+  int device = 0;
+  hipError_t e = hipGetDevice(&device);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = device < 64 ? 1ull << device : 0;  // (others: each call)
+  if (devices.load() & bit) return hipSuccess;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
+                          (int)bytes);
+  if (e == hipSuccess) devices.fetch_or(bit);
+  return e;
+}
+
 template <typename T, int FM, int WGM, int WGN, int WK, int ST>
 hipError_t product_tiles(const ProductParams &P, hipStream_t s) {
   constexpr int kBM = 16 * FM * WGM, kBN = 64 * WGN;
@@ -657,11 +673,10 @@ hipError_t product_tiles(const ProductParams &P, hipStream_t s) {
   if (tm * tn > INT32_MAX) return hipErrorInvalidValue;
   const int64_t slots = (int64_t)kCUs * kBlocks;
   const auto kernel = &k_product<T, FM, WGM, WGN, WK, ST>;
-  // (the runtime's own limit is 64 KB until a kernel asks for more)
-  static const hipError_t allowed = hipFuncSetAttribute(
-      reinterpret_cast<const void *>(kernel),
-      hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
-  if (allowed != hipSuccess) return allowed;
+  static std::atomic<uint64_t> devices{0};
+  const hipError_t e =
+      allow_lds(reinterpret_cast<const void *>(kernel), kLds, devices);
+  if (e != hipSuccess) return e;
   const int64_t grid = tm * tn < slots ? tm * tn : slots;
   hipLaunchKernelGGL(kernel, dim3((unsigned)grid),
                      dim3(kThreads), kLds, s, P, (int)tm, (int)tn);
