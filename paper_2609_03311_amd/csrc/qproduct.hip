@@ -285,13 +285,28 @@ __global__ __launch_bounds__(256, 3) void k_product_any(ProductParams P,
       [](int) { return true; });
 }
 
+// P's rows m .. m + n - 1.
+template <typename T>
+ProductParams rows_of(const ProductParams &P, int64_t m, int64_t n) {
+  ProductParams S = P;
+  S.M = n;
+  S.x = ahead(P.x, m * P.ldx);
+  S.x_scale = P.x_scale + m;
+  S.res = ahead(P.res, m * P.ldr * (int)sizeof(T));
+  S.y = ahead(P.y, m * P.ldy * (int)sizeof(T));
+  return S;
+}
+
 template <typename T>
 hipError_t product_any(const ProductParams &P, hipStream_t s) {
-  const int64_t tm = (P.M + kAnyM - 1) / kAnyM, tn = (P.N + kAnyN - 1) / kAnyN;
-  if (tm * tn > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((k_product_any<T>), dim3((unsigned)(tm * tn)), dim3(256),
-                     0, s, P, (int)tn);
-  return hipGetLastError();
+  const int64_t tn = (P.N + kAnyN - 1) / kAnyN;
+  const int64_t most = std::max<int64_t>(a_launch(256) / tn, 1) * kAnyM;
+  return in_slices(P.M, most, [&](int64_t m, int64_t n) {
+    const int64_t tm = (n + kAnyM - 1) / kAnyM;
+    hipLaunchKernelGGL((k_product_any<T>), dim3((unsigned)(tm * tn)),
+                       dim3(256), 0, s, rows_of<T>(P, m, n), (int)tn);
+    return hipGetLastError();
+  });
 }
 
 // ---------------------------------------------------------------------------
@@ -809,13 +824,29 @@ __global__ __launch_bounds__(256) void k_product_few(ProductParams P) {
   }
 }
 
+// P's columns n .. n + count - 1.
+template <typename T>
+ProductParams columns_of(const ProductParams &P, int64_t n, int64_t count) {
+  ProductParams S = P;
+  S.N = count;
+  S.w = ahead(P.w, n * P.ldw);
+  S.w_scale = P.w_scale + n;
+  S.bias = ahead(P.bias, n * (int)sizeof(T));
+  S.res = ahead(P.res, n * (int)sizeof(T));
+  S.y = ahead(P.y, n * (int)sizeof(T));
+  return S;
+}
+
 template <typename T, int FM>
 hipError_t product_few(const ProductParams &P, hipStream_t s) {
-  const unsigned strips = (unsigned)((P.N + 15) / 16);
+  constexpr int kThreads = 64 * kFewWaves;
   const unsigned rows = (unsigned)((P.M + 16 * FM - 1) / (16 * FM));
-  hipLaunchKernelGGL((k_product_few<T, FM>), dim3(strips, rows),
-                     dim3(64 * kFewWaves), 0, s, P);
-  return hipGetLastError();
+  return in_slices(P.N, 16 * a_launch(kThreads), [&](int64_t n, int64_t count) {
+    hipLaunchKernelGGL((k_product_few<T, FM>),
+                       dim3((unsigned)((count + 15) / 16), rows),
+                       dim3(kThreads), 0, s, columns_of<T>(P, n, count));
+    return hipGetLastError();
+  });
 }
 
 // ---------------------------------------------------------------------------
@@ -826,17 +857,30 @@ struct RepackParams {
   const int8_t *x, *w;
   int8_t *to;
   int64_t M, rows, K, ldx, ldw, pitch;
+  int64_t first;  // row that the launch begins with
 };
 
 __global__ __launch_bounds__(256) void k_repack(RepackParams P) {
   const int64_t per = P.pitch / 16;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t r = i / per, k = (i - r * per) * 16;
+  const int64_t in = i / per, k = (i - in * per) * 16;
+  const int64_t r = P.first + in;
   if (r >= P.rows) return;
   const int8_t *row = r < P.M ? P.x + r * P.ldx : P.w + (r - P.M) * P.ldw;
   u32x4 u = {0u, 0u, 0u, 0u};
   if (k < P.K) u = row_bytes(row, k, P.K);
   *reinterpret_cast<u32x4 *>(P.to + r * P.pitch + k) = u;
+}
+
+hipError_t repack(const RepackParams &R, hipStream_t s) {
+  const int64_t per = R.pitch / 16;
+  return in_slices(R.rows, a_launch(per), [&](int64_t r, int64_t n) {
+    RepackParams S = R;
+    S.first = r;
+    hipLaunchKernelGGL(k_repack, dim3((unsigned)((n * per + 255) / 256)),
+                       dim3(256), 0, s, S);
+    return hipGetLastError();
+  });
 }
 
 int64_t repack_pitch(int64_t K) { return (K + kSpan - 1) / kSpan * kSpan; }
@@ -967,13 +1011,10 @@ hipError_t product(ProductParams P, void *workspace, size_t bytes,
   }
   if (!aligned_rows(P)) {
     RepackParams R{P.x,   P.w, static_cast<int8_t *>(workspace), P.M,
-                   P.M + P.N, P.K, P.ldx, P.ldw, repack_pitch(P.K)};
+                   P.M + P.N, P.K, P.ldx, P.ldw, repack_pitch(P.K), 0};
     if (!workspace || bytes < (size_t)(R.rows * R.pitch) || P.K == 0)
       return product_any<T>(P, s);
-    const int64_t n = R.rows * (R.pitch / 16);
-    hipLaunchKernelGGL(k_repack, dim3((unsigned)((n + 255) / 256)), dim3(256),
-                       0, s, R);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = repack(R, s);
     if (e != hipSuccess) return e;
     P.x = R.to;
     P.w = R.to + P.M * R.pitch;

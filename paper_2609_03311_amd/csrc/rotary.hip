@@ -288,7 +288,7 @@ __global__ __launch_bounds__(64 * kRotaryWaves, 3) void k_rotary(RotaryParams P)
 }
 
 template <typename T, bool INTER, bool SMALL>
-void launch(const RotaryParams &P, hipStream_t s) {
+void launch1(const RotaryParams &P, hipStream_t s) {
   const dim3 grid((unsigned)((P.items + kRotaryWaves - 1) / kRotaryWaves));
   const dim3 block(64 * kRotaryWaves);
   if (P.q.norm_w || P.k.norm_w)
@@ -299,11 +299,27 @@ void launch(const RotaryParams &P, hipStream_t s) {
 }
 
 template <typename T>
-void launch(const RotaryParams &P, bool inter, bool small, hipStream_t s) {
-  if (inter)
-    small ? launch<T, true, true>(P, s) : launch<T, true, false>(P, s);
-  else
-    small ? launch<T, false, true>(P, s) : launch<T, false, false>(P, s);
+hipError_t launch(const RotaryParams &P, int64_t tokens, bool inter, bool small,
+                  hipStream_t s) {
+  auto from = [](const RotaryHeads &h, int64_t token) {
+    RotaryHeads f = h;
+    f.x = ahead(h.x, token * h.row * (int)sizeof(T));
+    f.out = ahead(h.out, token * h.out_row * (int)sizeof(T));
+    return f;
+  };
+  // (many tokens: one wave each)
+  return in_slices(tokens, a_launch(64 * P.splits), [&](int64_t t, int64_t n) {
+    RotaryParams S = P;
+    S.q = from(P.q, t);
+    S.k = from(P.k, t);
+    S.positions = P.positions + t;
+    S.items = n * P.splits;
+    if (inter)
+      small ? launch1<T, true, true>(S, s) : launch1<T, true, false>(S, s);
+    else
+      small ? launch1<T, false, true>(S, s) : launch1<T, false, false>(S, s);
+    return hipGetLastError();
+  });
 }
 
 }  // namespace
@@ -347,14 +363,11 @@ hipError_t launch_rotary(const dopr_rotary_args_t &a, hipStream_t s) {
   P.splits = 1;
   while (P.splits < groups && a.rows * P.splits < 8192) P.splits *= 2;
   if (P.splits > groups) P.splits = groups;
-  P.items = a.rows * P.splits;
   if (a.dtype == DOPR_BF16)
-    launch<bf16_t>(P, a.interleaved, small, s);
-  else if (a.dtype == DOPR_F16)
-    launch<_Float16>(P, a.interleaved, small, s);
-  else
-    launch<float>(P, a.interleaved, small, s);
-  return hipGetLastError();
+    return launch<bf16_t>(P, a.rows, a.interleaved, small, s);
+  if (a.dtype == DOPR_F16)
+    return launch<_Float16>(P, a.rows, a.interleaved, small, s);
+  return launch<float>(P, a.rows, a.interleaved, small, s);
 }
 
 }  // namespace dopr

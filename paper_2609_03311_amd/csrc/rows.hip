@@ -365,26 +365,45 @@ void row_grid(int64_t rows, dim3 &grid, dim3 &block) {
 template <typename T>
 hipError_t quantize(const QuantizeParams &P, hipStream_t s) {
   return by_width(P.width, [&](auto tpr, auto nv) {
-    dim3 grid, block;
-    row_grid<tpr.value>(P.rows, grid, block);
-    if (P.up)
-      hipLaunchKernelGGL((k_quantize_rows<T, tpr.value, nv.value, true>), grid,
-                         block, 0, s, P);
-    else
-      hipLaunchKernelGGL((k_quantize_rows<T, tpr.value, nv.value, false>),
-                         grid, block, 0, s, P);
-    return hipGetLastError();
+    return in_slices(P.rows, a_launch(tpr.value), [&](int64_t r, int64_t n) {
+      QuantizeParams S = P;
+      S.rows = n;
+      S.x = ahead(P.x, r * P.ldx * (int)sizeof(T));
+      S.up = ahead(P.up, r * P.ldu * (int)sizeof(T));
+      S.q = ahead(P.q, r * P.ldq);
+      S.scale = P.scale + r;
+      dim3 grid, block;
+      row_grid<tpr.value>(n, grid, block);
+      if (P.up)
+        hipLaunchKernelGGL((k_quantize_rows<T, tpr.value, nv.value, true>),
+                           grid, block, 0, s, S);
+      else
+        hipLaunchKernelGGL((k_quantize_rows<T, tpr.value, nv.value, false>),
+                           grid, block, 0, s, S);
+      return hipGetLastError();
+    });
   });
 }
 
 template <typename T, typename R>
 hipError_t norm(const NormParams &P, hipStream_t s) {
   return by_width(P.width + (P.lines ? 63 : 0), [&](auto tpr, auto nv) {
-    dim3 grid, block;
-    row_grid<tpr.value>(P.rows, grid, block);
-    hipLaunchKernelGGL((k_norm_residual<T, R, tpr.value, nv.value>), grid,
-                       block, 0, s, P);
-    return hipGetLastError();
+    return in_slices(P.rows, a_launch(tpr.value), [&](int64_t r, int64_t n) {
+      NormParams S = P;
+      S.rows = n;
+      S.x = ahead(P.x, r * P.ldx * (int)sizeof(T));
+      S.gate = ahead(P.gate, r * P.ldg * (int)sizeof(T));
+      S.res = ahead(P.res, r * P.ldr * (int)sizeof(R));
+      S.h = ahead(P.h, r * P.ldh * (int)sizeof(R));
+      S.z = ahead(P.z, r * P.ldz * (int)sizeof(T));
+      S.q = ahead(P.q, r * P.ldq);
+      S.q_scale = ahead(P.q_scale, r * (int)sizeof(float));
+      dim3 grid, block;
+      row_grid<tpr.value>(n, grid, block);
+      hipLaunchKernelGGL((k_norm_residual<T, R, tpr.value, nv.value>), grid,
+                         block, 0, s, S);
+      return hipGetLastError();
+    });
   });
 }
 

@@ -44,3 +44,77 @@ def test_dynamic_lds_is_asked_for_on_every_device():
     assert [len(g["launches"]) for g in got] == [1, 1, 0, 1, 1, 1, 1, 1]
     assert got[2]["status"] != 0 and "product launch" in got[2]["error"]
     assert all(g["status"] == 0 for i, g in enumerate(got) if i != 2)
+
+
+MANY = 1 << 31
+
+
+def rows_call(rows, width):
+    return ["dopr_quantize_rows", "_QuantizeArgs",
+            dict(dtype=1, rows=rows, width=width, x=256, x_row_stride=width,
+                 q=256, q_row_stride=width, scale=256)]
+
+
+def norm_call(rows, width):
+    return ["dopr_norm_residual", "_NormResidualArgs",
+            dict(dtype=0, residual_dtype=2, rows=rows, width=width, x=256,
+                 x_row_stride=width, residual_scale=1.0, rms_eps=1e-6, h=256,
+                 h_row_stride=width, z=256, z_row_stride=width)]
+
+
+def rotary_call(rows, heads, dim):
+    pitch = heads * dim
+    return ["dopr_rotary", "_RotaryArgs",
+            dict(dtype=0, n_q_heads=heads, n_kv_heads=0, head_dim=dim,
+                 rotary_dim=dim, attention_factor=1.0, rms_eps=1e-6,
+                 rows=rows, positions=256, inv_freq=256, q=256,
+                 q_row_stride=pitch, q_head_stride=dim, q_out=256,
+                 q_out_row_stride=pitch, q_out_head_stride=dim)]
+
+
+# (call, items, items a block takes): every row, token, strip of 16 columns,
+# tile or piece of 16 bytes belongs to one block
+LARGE = [
+    (rows_call(MANY - 1, 8), MANY - 1, 4),
+    (rows_call((1 << 26) - 4, 8), (1 << 26) - 4, 4),
+    (rows_call(1 << 26, 2048), 1 << 26, 4),
+    (rows_call(1 << 25, 4096), 1 << 25, 1),
+    (rows_call(1 << 23, 65536), 1 << 23, 1),
+    (norm_call(MANY - 1, 8), MANY - 1, 4),
+    (norm_call(1 << 24, 4096), 1 << 24, 1),
+    (norm_call((1 << 22) + 1, 65000), (1 << 22) + 1, 1),
+    (rotary_call(MANY - 1, 1, 64), MANY - 1, 4),
+    (rotary_call((1 << 26) + 3, 3, 512), (1 << 26) + 3, 4),
+    (product(1, MANY - 1025, 16), -(-(MANY - 1025) // 16), 1),
+    (product(16, 1 << 28, 1), 1 << 24, 1),
+    (product(MANY - 1025, 1, 1, x_row_stride=1), -(-(MANY - 1025) // 64), 1),
+    (product(17, MANY - 1025, 1, x_row_stride=1, w_row_stride=1),
+     -(-(MANY - 1025) // 128), 1),
+    (product(1 << 29, 65, 1, x_row_stride=1, w_row_stride=1,
+             workspace=256, workspace_bytes=(1 << 29) * 128 + 65 * 128),
+     (1 << 32) + 520, 256),
+]
+
+
+def test_launches_of_many_rows_fit():
+    """Sizes whose rows ask for 2^32 threads and more come as several
+    launches (one has fewer), every row, token or column in one of them;
+    tiles that a block takes in turn need no more than fill the GPU."""
+    for (_, items, per), got in zip(LARGE, launches([c for c, _, _ in LARGE])):
+        assert got["status"] == 0, got["error"]
+        run = [k for k in got["launches"] if not k["kernel"].startswith(
+            "k_product<")]
+        for k in got["launches"]:
+            assert k["gx"] * k["bx"] < 1 << 32 and k["gy"] * k["gz"] < 1 << 16
+        blocks = sum(k["gx"] for k in run)
+        least = -(-items // per)
+        assert least <= blocks < least + len(run), (got, items)
+
+
+def test_ordinary_calls_are_one_launch():
+    for call in (rows_call(12900, 12288), norm_call(20011, 2561),
+                 rotary_call(32768, 40, 128), product(1, 6144, 4096),
+                 product(12900, 24576, 4096),
+                 product(600, 520, 777, x_row_stride=777)):
+        got, = launches([call])
+        assert got["status"] == 0 and len(got["launches"]) == 1
