@@ -497,10 +497,10 @@ dopr_status_t dopr_quantize_rows(const dopr_quantize_args_t *args,
  *             + bias[n] + residual[m, n]
  * The integer sum is exact (32 bits).  y may be the residual (same address
  * and stride).  The bytes between a row's end and its stride are never
- * read.  Rows on 16-byte addresses (x, w and both strides multiples of 16)
- * are multiplied where they lie; others are first laid out again in the
- * workspace, if there is one, else multiplied by a slower kernel (the results
- * are the same).                                                           */
+ * read.  Rows on 16-byte addresses (x, w and both strides multiples of 16,
+ * the strides under 2^22) are multiplied where they lie; others are first
+ * laid out again in the workspace, if there is one, else multiplied by a
+ * slower kernel (the results are the same).                                */
 typedef struct {
   int32_t dtype;            /* of bias, residual and y                      */
   int64_t rows;             /* M >= 0                                       */
@@ -524,9 +524,11 @@ typedef struct {
   size_t workspace_bytes;
 } dopr_quant_matmul_args_t;
 
-/* Workspace bytes worth giving a product of these rows, cols and depth, by
- * sizes alone (host arithmetic): 0 up to 16 rows and where 16 divides the
- * depth, so that rows can be expected on 16-byte addresses.                */
+/* Workspace bytes worth giving a product (host arithmetic): 0 up to 16 rows,
+ * and where the rows lie on 16-byte addresses.  It goes by rows, cols and
+ * depth, and by x, w and their strides where they are set: a stride of 0
+ * stands for rows back to back, a NULL x or w for an aligned one.  Strides of
+ * 2^22 bytes and more count as off 16-byte addresses.                      */
 dopr_status_t dopr_quant_matmul_workspace(const dopr_quant_matmul_args_t *args,
                                           size_t *bytes);
 

@@ -622,11 +622,17 @@ def dopr_quantize_rows(x, q, scale, *, up=None, stream=None):
     _check(_compiled().quantize_rows(x, q, scale, up, _handle(stream)))
 
 
-def dopr_quant_matmul_workspace(rows: int, cols: int, depth: int) -> int:
+def dopr_quant_matmul_workspace(rows: int, cols: int, depth: int, *, x=None,
+                                w=None) -> int:
     """Workspace bytes worth giving a product of these sizes (host
-    arithmetic; 0: none is used)."""
+    arithmetic; 0: none is used).  x [rows, depth] and w [cols, depth], where
+    given, say how their rows lie; else they are taken to be back to back."""
     a = _QuantMatmulArgs()
     a.rows, a.cols, a.depth = rows, cols, depth
+    if x is not None:
+        a.x, a.x_row_stride = x.data_ptr(), x.stride(0)
+    if w is not None:
+        a.w, a.w_row_stride = w.data_ptr(), w.stride(0)
     n = ctypes.c_size_t(0)
     _check(lib().dopr_quant_matmul_workspace(ctypes.byref(a),
                                              ctypes.byref(n)))

@@ -1004,7 +1004,7 @@ dopr_status_t dopr_quant_matmul_workspace(const dopr_quant_matmul_args_t *a,
   if (!bytes) return fail(DOPR_ERR_INVALID_ARG, "bytes is NULL");
   dopr_status_t s = check_product(a);
   if (s != DOPR_OK) return s;
-  *bytes = product_workspace(a->rows, a->cols, a->depth);
+  *bytes = product_workspace(*a);
   return ok();
 }
 

@@ -968,11 +968,14 @@ int choose(int64_t M, int64_t N, int64_t K) {
 }
 
 // x, w and their strides on 16 bytes, and a tile's rows within 32-bit offsets
+bool aligned_rows(const void *x, const void *w, int64_t ldx, int64_t ldw) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x) |
+                      reinterpret_cast<uintptr_t>(w) | (uintptr_t)ldx |
+                      (uintptr_t)ldw;
+  return a % 16 == 0 && ldx < (1 << 22) && ldw < (1 << 22);
+}
 bool aligned_rows(const ProductParams &P) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(P.x) |
-                      reinterpret_cast<uintptr_t>(P.w) | (uintptr_t)P.ldx |
-                      (uintptr_t)P.ldw;
-  return a % 16 == 0 && P.ldx < (1 << 22) && P.ldw < (1 << 22);
+  return aligned_rows(P.x, P.w, P.ldx, P.ldw);
 }
 
 template <typename T>
@@ -1025,11 +1028,13 @@ hipError_t product(ProductParams P, void *workspace, size_t bytes,
 
 }  // namespace
 
-// Rows of a depth that 16 does not divide can hardly lie on 16-byte addresses.
-size_t product_workspace(int64_t M, int64_t N, int64_t K) {
-  return M <= kFewRows || N == 0 || K % 16 == 0
-             ? 0
-             : (size_t)((M + N) * repack_pitch(K));
+// Strides that are not set: rows back to back.
+size_t product_workspace(const dopr_quant_matmul_args_t &a) {
+  if (a.rows <= kFewRows || a.cols == 0 || a.depth == 0 ||
+      aligned_rows(a.x, a.w, a.x_row_stride ? a.x_row_stride : a.depth,
+                   a.w_row_stride ? a.w_row_stride : a.depth))
+    return 0;
+  return (size_t)((a.rows + a.cols) * repack_pitch(a.depth));
 }
 
 static bool whole_pieces(const dopr_quant_matmul_args_t &a) {

@@ -118,3 +118,69 @@ def test_ordinary_calls_are_one_launch():
                  product(600, 520, 777, x_row_stride=777)):
         got, = launches([call])
         assert got["status"] == 0 and len(got["launches"]) == 1
+
+
+@pytest.mark.parametrize("how,needs", [
+    (dict(), False),                                   # sizes alone
+    (dict(x=256, w=512, x_row_stride=4096, w_row_stride=4096), False),
+    (dict(x=257), True),
+    (dict(w=264), True),
+    (dict(x_row_stride=4100), True),
+    (dict(w_row_stride=4104), True),
+    (dict(w_row_stride=1 << 22), True),                # past 32-bit offsets
+    (dict(depth=4090), True),
+    (dict(depth=4090, x_row_stride=4096), True),       # w's back to back
+    (dict(depth=4090, x_row_stride=4096, w_row_stride=4112), False),
+    (dict(depth=0, x=257), False),
+    (dict(rows=16, x=257), False),
+    (dict(cols=0, x=257), False),
+])
+def test_workspace_is_asked_for_where_it_is_used(how, needs):
+    """The bytes asked for are those a call with such rows uses: with them
+    rows are laid out again, without any they are multiplied as they lie, and
+    where none are asked for neither happens."""
+    import ctypes
+
+    import paper_2609_03311_amd as D
+    a = D._QuantMatmulArgs()
+    fields = dict(rows=200, cols=300, depth=4096) | how
+    for k, v in fields.items():
+        setattr(a, k, v)
+    n = ctypes.c_size_t(7)
+    assert D.lib().dopr_quant_matmul_workspace(
+        ctypes.byref(a), ctypes.byref(n)) == 0
+    rows = (fields["rows"] + fields["cols"]) * 4096
+    assert n.value == (rows if needs else 0)
+    if fields["depth"] == 0 or fields["cols"] == 0:
+        return
+    k = fields["depth"]
+    call = product(**fields | dict(x_row_stride=how.get("x_row_stride", k),
+                                   w_row_stride=how.get("w_row_stride", k)))
+    call[2] |= dict(x=how.get("x", 256), w=how.get("w", 256))
+    with_it = [call[0], call[1],
+               call[2] | dict(workspace=256, workspace_bytes=n.value)]
+    names = [[k["kernel"] for k in g["launches"]]
+             for g in launches([call, with_it])]
+    if needs:
+        assert names[0] == ["k_product_any<bf16_t>"]
+        assert names[1][0] == "k_repack" and len(names[1]) == 2
+    else:
+        assert names[0] == names[1] and "any" not in names[0][0]
+
+
+def test_workspace_by_tensors():
+    import torch
+
+    import paper_2609_03311_amd as D
+    x = torch.zeros(200, 4112, dtype=torch.int8)
+    w = torch.zeros(300, 4096, dtype=torch.int8)
+    size = 500 * 4096
+    assert x.data_ptr() % 16 == w.data_ptr() % 16 == 0
+    assert D.dopr_quant_matmul_workspace(200, 300, 4096) == 0
+    assert D.dopr_quant_matmul_workspace(200, 300, 4096, x=x[:, 1:4097],
+                                         w=w) == size
+    assert D.dopr_quant_matmul_workspace(200, 300, 4080, x=x[:, :4080],
+                                         w=w[:, :4080]) == 0
+    assert D.dopr_quant_matmul_workspace(200, 300, 4090) == size
+    assert D.dopr_quant_matmul_workspace(200, 300, 4090, x=x[:, :4090],
+                                         w=w[:, :4090]) == 0
