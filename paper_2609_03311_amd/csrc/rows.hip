@@ -250,14 +250,17 @@ __global__ __launch_bounds__(TPR > 64 ? TPR : 256) void k_norm_residual(
 #pragma unroll
     for (int v = 0; v < NC; ++v) Chunk<E>((v * TPR + t) * E - shift, W).mask(f[v]);
     float mean = squares(), eps = P.eps;
-    if (mean == __builtin_inff()) {
-      // squares past fp32's range (values over 2^55 or so; the whole row
-      // takes this turn together): the same with the row 2^80 times smaller
-      eps *= 0x1p-80f * 0x1p-80f;
+    const bool large = mean == __builtin_inff();
+    if (large || mean + eps < 0x1p-100f) {
+      // squares out of fp32's range (values over 2^55 or so, or, with next to
+      // no epsilon, all under 2^-42; the whole row takes this turn together):
+      // the same with the row 2^80 times smaller, or 2^100 times larger
+      const float by = large ? 0x1p-80f : 0x1p100f;
+      eps = eps * by * by;
 #pragma unroll
       for (int v = 0; v < NC; ++v)
 #pragma unroll
-        for (int e = 0; e < E; ++e) f[v][e] *= 0x1p-80f;
+        for (int e = 0; e < E; ++e) f[v][e] *= by;
       mean = squares();
     }
     const float inv = 1.0f / sqrtf(mean + eps);

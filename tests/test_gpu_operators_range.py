@@ -1,0 +1,70 @@
+"""Norms of rows and heads whose squares leave fp32's range (GPU), against the
+64-bit form.  The bounds are those of operator_refs.py."""
+import pytest
+import torch
+
+import operator_refs as R
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+
+
+def _D():
+    import paper_2609_03311_amd as D
+    return D
+
+
+def randn(seed, *shape, dtype):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return torch.randn(shape, generator=g, device=DEV).to(dtype)
+
+
+def of_size(v, exponents):
+    """Row i of v times 2^exponents[i], exact but for subnormal results."""
+    e = torch.tensor(exponents, dtype=torch.float64, device=DEV)
+    e = e.view(-1, *[1] * (v.dim() - 1))
+    return (v.double() * torch.exp2(e)).to(v.dtype)
+
+
+# 16-bit floats hold little of this range
+EXPONENTS = {torch.bfloat16: [-125, -100, -80, -76, -74, -60, -51, -49, -40,
+                              0, 50, 60, 64, 100, 125],
+             torch.float16: [-22, -14, -10, 0, 10, 13],
+             torch.float32: [-145, -126, -110, -80, -75, -60, -51, -49, -40,
+                             0, 50, 60, 64, 100, 125]}
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-36, 1e-6])
+@pytest.mark.parametrize("width", [64, 1030, 4096, 20000])
+@pytest.mark.parametrize("dtype", list(EXPONENTS))
+def test_norm_of_rows_of_any_size(dtype, width, eps):
+    """Both norms, in front of and behind the join."""
+    D = _D()
+    e = EXPONENTS[dtype]
+    x = of_size(randn(width, len(e), width, dtype=dtype), e)
+    w = (1 + 0.1 * randn(1, width, dtype=torch.float32)).to(dtype)
+    z = torch.empty_like(x)
+    D.dopr_norm_residual(x, pre_norm_w=w, z=z, rms_eps=eps)
+    R.assert_close(z, R.norm(x, w, eps))
+    h = torch.empty_like(x)
+    D.dopr_norm_residual(x, post_norm_w=w, h=h, rms_eps=eps)
+    R.assert_close(h, R.norm(x, w, eps))
+    q = torch.empty(x.shape, dtype=torch.int8, device=DEV)
+    s = torch.empty(len(e), device=DEV)
+    D.dopr_norm_residual(x, pre_norm_w=w, q=q, q_scale=s, rms_eps=eps)
+    R.assert_int8_rows(q, s, R.norm(x, w, eps))
+
+
+def test_norm_of_zeros_without_an_epsilon():
+    """0 / 0 by the formula, as with infinities and NaN."""
+    D = _D()
+    x = torch.zeros(3, 64, device=DEV)
+    x[1] = 1e-30
+    x[2, 3] = float("inf")
+    z = torch.empty_like(x)
+    D.dopr_norm_residual(x, pre_norm_w=torch.ones(64, device=DEV), z=z,
+                         rms_eps=0.0)
+    assert torch.isnan(z[0]).all()
+    R.assert_close(z[1], torch.ones(64, dtype=torch.float64, device=DEV))
+    assert torch.isnan(z[2, 3]) and (z[2, 4:] == 0).all()
