@@ -581,8 +581,7 @@ dopr_status_t dopr_norm_residual(const dopr_norm_residual_args_t *args,
  *   attention_factor * (a cos t - b sin t, b cos t + a sin t)
  * (`inverse`: t -> -t); x[R ..] passes through.  With a norm gain, the
  * head's RMSNorm over all of head_dim, times the gain, comes first
- * (dopr_prefix_attn's order; its sum of squares is fp32, so values stay below
- * 2^60).  A prefix attention of heads that are already
+ * (dopr_prefix_attn's order).  A prefix attention of heads that are already
  * normed and rotated takes both gains NULL and rope_inv_freq all zero.
  * Outputs may be the inputs (same addresses and strides); other overlaps
  * are not allowed.  Heads lie head_stride apart, so a head-major layout or

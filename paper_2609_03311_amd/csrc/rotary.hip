@@ -15,6 +15,8 @@
 // and token): in 32 bits the product of a position and a frequency is off by
 // up to 2^-25 of itself, at position 2^17 0.004 rad, more than a bf16
 // rounding.
+#include <type_traits>
+
 #include "rowio.hpp"
 
 namespace dopr {
@@ -145,8 +147,20 @@ struct Run {
   }
 };
 
+// What a run's values are held in behind its load: wide, or f itself.
+template <typename V>
+__device__ __forceinline__ auto &values(V (&wide)[8], float (&f)[8]) {
+  if constexpr (std::is_same_v<V, float>)
+    return f;
+  else
+    return wide;
+}
+
 template <typename T, bool INTER, bool SMALL, bool NORM>
 __global__ __launch_bounds__(64 * kRotaryWaves, 3) void k_rotary(RotaryParams P) {
+  // fp32 heads are normed and turned in 64 bits, so that what is rounded in
+  // between does not show next to the output's own rounding (subnormals too)
+  using Value = std::conditional_t<NORM && sizeof(T) == 4, double, float>;
   __shared__ float2 table[kRotaryWaves][256];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -214,33 +228,57 @@ __global__ __launch_bounds__(64 * kRotaryWaves, 3) void k_rotary(RotaryParams P)
       float fa[8], fb[8];
       ra[b].get(fa);
       rb[b].get(fb);
+      Value wide_a[8], wide_b[8];
+      auto &va = values(wide_a, fa);
+      auto &vb = values(wide_b, fb);
       if constexpr (NORM) {
-        float ss = 0.f;
-        if (P.whole) {
+        auto mean_square = [&]() {
+          float ss = 0.f;
+          if (P.whole) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            ss = fmaf(fa[e], fa[e], fmaf(fb[e], fb[e], ss));
-        } else {
+            for (int e = 0; e < 8; ++e)
+              ss = fmaf(fa[e], fa[e], fmaf(fb[e], fb[e], ss));
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float a = e >= k.lo_a && u == u_raw ? fa[e] : 0.f;
+              const float b2 = e >= k.lo_b && u == u_raw ? fb[e] : 0.f;
+              ss = fmaf(a, a, fmaf(b2, b2, ss));
+            }
+          }
+          for (int off = (1 << P.group_log2) >> 1; off > 0; off >>= 1)
+            ss += __shfl_xor(ss, off, 64);
+          return ss / (float)P.D;
+        };
+        float mean = mean_square(), eps = P.eps;
+        const bool large = mean == __builtin_inff();
+        const bool small = mean + eps < 0x1p-100f;
+        const T *w = static_cast<const T *>(is_k ? P.k.norm_w : P.q.norm_w);
+        if (__any(w && (large || small))) {
+          // squares out of fp32's range (values over 2^59 or so, or, with next
+          // to no epsilon, all under 2^-45): the same with those heads 2^80
+          // times smaller, or 2^100 times larger
+          const float by =
+              !w ? 1.f : large ? 0x1p-80f : small ? 0x1p100f : 1.f;
+          eps = eps * by * by;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float a = e >= k.lo_a && u == u_raw ? fa[e] : 0.f;
-            const float b2 = e >= k.lo_b && u == u_raw ? fb[e] : 0.f;
-            ss = fmaf(a, a, fmaf(b2, b2, ss));
+            fa[e] *= by;
+            fb[e] *= by;
+          }
+          mean = mean_square();
+        }
+        // 16-bit outputs: the hardware's 1 / sqrt, off by a unit of fp32's last
+        // place, 2^-15 of theirs (no subnormals come here, which it takes for 0)
+        const float inv = sizeof(T) == 2 ? __builtin_amdgcn_rsqf(mean + eps)
+                                         : 1.0f / sqrtf(mean + eps);
+        if constexpr (sizeof(Value) == 8) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            va[e] = fa[e];
+            vb[e] = fb[e];
           }
         }
-        for (int off = (1 << P.group_log2) >> 1; off > 0; off >>= 1)
-          ss += __shfl_xor(ss, off, 64);
-        // 16-bit outputs: the hardware's 1 / sqrt, off by a unit of fp32's last
-        // place, 2^-15 of theirs (it takes subnormals for 0: small means are
-        // scaled)
-        const float mean = ss / (float)P.D + P.eps;
-        const bool small = mean < 0x1p-64f;
-        const float inv =
-            sizeof(T) == 2
-                ? __builtin_amdgcn_rsqf(small ? mean * 0x1p64f : mean) *
-                      (small ? 0x1p32f : 1.f)
-                : 1.0f / sqrtf(mean);
-        const T *w = static_cast<const T *>(is_k ? P.k.norm_w : P.q.norm_w);
         if (w) {
           Run<T, SMALL> wa, wb;
           wa.load(w + k.pa, k.n_a);
@@ -250,31 +288,38 @@ __global__ __launch_bounds__(64 * kRotaryWaves, 3) void k_rotary(RotaryParams P)
           wb.get(gb);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            fa[e] = fa[e] * inv * ga[e];
-            fb[e] = fb[e] * inv * gb[e];
+            va[e] = (Value)fa[e] * inv * ga[e];
+            vb[e] = (Value)fb[e] * inv * gb[e];
           }
         }
       }
       if (k.rotated) {
-        float a[8], b2[8];
+        Value a[8], b2[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          a[e] = INTER ? (e < 4 ? fa[2 * e] : fb[2 * e - 8]) : fa[e];
-          b2[e] = INTER ? (e < 4 ? fa[2 * e + 1] : fb[2 * e - 7]) : fb[e];
+          a[e] = INTER ? (e < 4 ? va[2 * e] : vb[2 * e - 8]) : va[e];
+          b2[e] = INTER ? (e < 4 ? va[2 * e + 1] : vb[2 * e - 7]) : vb[e];
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           // (selected, not turned by zero: 0 times an infinity is NaN)
           const bool in = !INTER || (turns >> e & 1);
-          const float x0 = in ? a[e] * c[e] - b2[e] * s[e] : a[e];
-          const float x1 = in ? b2[e] * c[e] + a[e] * s[e] : b2[e];
+          const Value x0 = in ? a[e] * c[e] - b2[e] * s[e] : a[e];
+          const Value x1 = in ? b2[e] * c[e] + a[e] * s[e] : b2[e];
           if (INTER) {
-            (e < 4 ? fa[2 * e] : fb[2 * e - 8]) = x0;
-            (e < 4 ? fa[2 * e + 1] : fb[2 * e - 7]) = x1;
+            (e < 4 ? va[2 * e] : vb[2 * e - 8]) = x0;
+            (e < 4 ? va[2 * e + 1] : vb[2 * e - 7]) = x1;
           } else {
-            fa[e] = x0;
-            fb[e] = x1;
+            va[e] = x0;
+            vb[e] = x1;
           }
+        }
+      }
+      if constexpr (sizeof(Value) == 8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          fa[e] = (float)va[e];
+          fb[e] = (float)vb[e];
         }
       }
       if (hr < P.n_heads && u == u_raw) {

@@ -68,3 +68,31 @@ def test_norm_of_zeros_without_an_epsilon():
     assert torch.isnan(z[0]).all()
     R.assert_close(z[1], torch.ones(64, dtype=torch.float64, device=DEV))
     assert torch.isnan(z[2, 3]) and (z[2, 4:] == 0).all()
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-36, 1e-6])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,r", [(2, 2), (64, 64), (96, 40), (128, 128),
+                                 (512, 128)])
+@pytest.mark.parametrize("dtype", list(EXPONENTS))
+def test_rotary_norm_of_heads_of_any_size(dtype, d, r, interleaved, eps):
+    """Heads of every size side by side in a wave, some of q's and some of
+    k's, the latter also without a gain."""
+    D = _D()
+    e = EXPONENTS[dtype]
+    x = of_size(randn(d, len(e), 5, d, dtype=dtype), e).transpose(0, 1)
+    q, k = x[:, :-3], x[:, -3:]
+    pos = torch.arange(5, device=DEV, dtype=torch.int32)
+    freq = D.dopr_rotary_frequencies(r, 1e4)[0].to(DEV)
+    w = (1 + 0.1 * randn(1, d, dtype=torch.float32)).to(dtype)
+    for gain in (w, None):
+        qo, ko = torch.empty_like(q), torch.empty_like(k)
+        D.dopr_rotary(q, k, pos, freq, qo, ko, interleaved=interleaved,
+                      q_norm_w=w, k_norm_w=gain, rms_eps=eps)
+        R.assert_close(qo, *R.rotary(q, pos, freq, interleaved, gain=w,
+                                     eps=eps))
+        # (without a gain sums of values next to the type's end may pass it)
+        want, mag = R.rotary(k, pos, freq, interleaved, gain=gain, eps=eps)
+        fine = mag < torch.finfo(dtype).max
+        want, mag = want * fine, torch.where(fine, mag, 0)
+        R.assert_close(torch.where(fine, ko, 0), want, mag)
