@@ -114,6 +114,12 @@ float real(PyObject *o) {
   return (float)v;
 }
 
+int32_t flag(PyObject *o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Refused{};  // (an error of the object's own)
+  return v;
+}
+
 PyObject *quantize_rows(PyObject *const *a) {
   dopr_quantize_args_t s{};
   const at::Tensor &x = tensor(a[0], "x");
@@ -225,6 +231,8 @@ PyObject *rotary(PyObject *const *a) {
   // q, k, positions, inv_freq, q_out, k_out, interleaved, inverse,
   // attention_factor, q_norm_w, k_norm_w, rms_eps, stream
   dopr_rotary_args_t s{};
+  s.interleaved = flag(a[6]);
+  s.inverse = flag(a[7]);
   if (a[0] == Py_None && a[1] == Py_None) {
     PyErr_SetString(PyExc_ValueError, "q and k are both None");
     throw Refused{};
@@ -249,8 +257,6 @@ PyObject *rotary(PyObject *const *a) {
   const int64_t half = tensor(a[3], "inv_freq").numel();
   vector(a[3], "inv_freq", ScalarType::Float, half, s.inv_freq);
   s.rotary_dim = (int32_t)(2 * half);
-  s.interleaved = PyObject_IsTrue(a[6]);
-  s.inverse = PyObject_IsTrue(a[7]);
   s.attention_factor = real(a[8]);
   vector(a[9], "q_norm_w", t, s.head_dim, s.q_norm_w);
   vector(a[10], "k_norm_w", t, s.head_dim, s.k_norm_w);

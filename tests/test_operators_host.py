@@ -184,3 +184,17 @@ def test_workspace_by_tensors():
     assert D.dopr_quant_matmul_workspace(200, 300, 4090) == size
     assert D.dopr_quant_matmul_workspace(200, 300, 4090, x=x[:, :4090],
                                          w=w[:, :4090]) == 0
+
+
+def test_flags_without_a_truth_value_are_refused():
+    import numpy as np
+    import torch
+
+    import paper_2609_03311_amd as D
+    x = torch.zeros(4, 2, 64)
+    f = torch.zeros(32)
+    p = torch.zeros(4, dtype=torch.int32)
+    for flag in ("interleaved", "inverse"):
+        with pytest.raises(ValueError, match="ambiguous"):
+            D.dopr_rotary(x, None, p, f, x, None,
+                          **{flag: np.array([True, False])})
