@@ -42,6 +42,14 @@ const char *record_take(void) {
   return record;
 }
 
+const char *record_kernels(void) {
+  for (size_t i = 0; i < n_kernels; ++i) {
+    put(kernels[i].name);
+    put("\n");
+  }
+  return record_take();
+}
+
 /* for the library */
 int hipGetDevice(int *d) {
   *d = device;

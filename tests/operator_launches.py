@@ -38,12 +38,21 @@ def demangled(name):
     return re.sub(r"dopr::|\(anonymous namespace\)::", "", short)
 
 
-def launches(calls):
+def _run(calls):
     r = subprocess.run([sys.executable, os.path.abspath(__file__),
                         recorder()], input=json.dumps(calls), cwd=ROOT,
                        capture_output=True, text=True)
     assert r.returncode == 0, r.stderr[-3000:]
-    out = json.loads(r.stdout.splitlines()[-1])
+    return json.loads(r.stdout.splitlines()[-1])
+
+
+def kernels():
+    """The names of the library's kernels."""
+    return {demangled(name) for name in _run(None).split() if "dopr" in name}
+
+
+def launches(calls):
+    out = _run(calls)
     for call in out:
         lines = [line.split() for line in call.pop("record").splitlines()]
         call["launches"] = [
@@ -61,8 +70,12 @@ def _child(path):
     sys.path.insert(0, ROOT)
     import paper_2609_03311_amd as D
     L = D.lib()
-    out = []
-    for name, struct, fields, *more in json.load(sys.stdin):
+    R.record_kernels.restype = ctypes.c_char_p
+    calls, out = json.load(sys.stdin), []
+    if calls is None:
+        print(json.dumps(R.record_kernels().decode()))
+        return
+    for name, struct, fields, *more in calls:
         env = more[0] if more else {}
         R.record_device(env.get("device", 0))
         R.record_refuse(int(env.get("refuse", False)))

@@ -4,7 +4,7 @@ import subprocess
 
 import pytest
 
-from operator_launches import launches
+from operator_launches import kernels, launches
 from paper_2609_03311_amd import _build
 
 
@@ -198,3 +198,50 @@ def test_flags_without_a_truth_value_are_refused():
         with pytest.raises(ValueError, match="ambiguous"):
             D.dopr_rotary(x, None, p, f, x, None,
                           **{flag: np.array([True, False])})
+
+
+def product_way(call, got):
+    """How a call of rows on 16-byte addresses runs: its kernel, how many
+    tiles a block takes (3: more than two), whether the depth ends in a
+    partial span, and whether it is shorter than the spans in flight."""
+    k, = got["launches"]
+    name = k["kernel"]
+    if not name.startswith("k_product<"):
+        return name, 1, False, False
+    fm, wgm, wgn, wk, st = map(int, name[:-1].split(",")[1:])
+    a = call[2]
+    tiles = -(-a["rows"] // (16 * fm * wgm)) * -(-a["cols"] // (64 * wgn))
+    return (name, min(-(-tiles // k["gx"]), 3), a["depth"] % 128 > 0,
+            a["depth"] // 128 // wk < st)
+
+
+def test_gpu_tests_reach_every_way_a_product_runs():
+    """Whatever way random sizes take is taken by one of the sizes that the
+    GPU tests compare bit for bit: costs that are fitted anew may pick other
+    kernels, and then more sizes have to be listed."""
+    import math
+    import random
+
+    from product_sizes import SIZES
+    calls = [product(*size) for size in SIZES]
+    covered = {product_way(c, g) for c, g in zip(calls, launches(calls))}
+    rng = random.Random(5)
+
+    def size(lo, hi):
+        return int(math.exp(rng.uniform(math.log(lo), math.log(hi))))
+
+    sizes = [(size(1, 9000), size(32, 60000), size(20, 9000))
+             for _ in range(8000)]
+    calls = [product(m, n, k if i % 2 else -(-k // 128) * 128)
+             for i, (m, n, k) in enumerate(sizes) if m * n < 9e7]
+    missed = {}
+    for c, g in zip(calls, launches(calls)):
+        missed.setdefault(product_way(c, g), c[2])
+    missed = {w: [c[k] for k in ("rows", "cols", "depth")]
+              for w, c in missed.items() if w not in covered}
+    assert not missed
+    # and every kernel that is compiled for such rows
+    names = {w[0] for w in covered}
+    compiled = {n for n in kernels() if n.startswith("k_product") and
+                "<bf16_t" in n and "any" not in n}
+    assert names == compiled
