@@ -462,10 +462,11 @@ dopr_status_t dopr_select_top_k(const dopr_salience_args_t *args,
  * forwarded as prefix inputs and their keys and values kept).
  *
  * Activations are bf16, fp16 or fp32 (`dtype`); sums, norms and scales are
- * fp32, and every output is rounded once, to nearest even.  Strides are in
- * elements; rows may start at any element-aligned address and lie any
- * distance of at least their length apart.  Everything is asynchronous on
- * `stream`, and outputs do not vary from run to run.                       */
+ * held in fp32 or wider, and what comes out is rounded to its type, to nearest
+ * even, behind that arithmetic.  Strides are in elements; rows may start at
+ * any element-aligned address and lie any distance of at least their length
+ * apart.  Everything is asynchronous on `stream`, and outputs do not vary
+ * from run to run.                                                         */
 typedef enum { DOPR_BF16 = 0, DOPR_F16 = 1, DOPR_F32 = 2 } dopr_dtype_t;
 
 /* Rows in 8-bit integers: v = x, or SiLU(x) * up when `up` is given; with
@@ -495,7 +496,8 @@ dopr_status_t dopr_quantize_rows(const dopr_quantize_args_t *args,
  * the stored-weight convention (w is [out, in]):
  *   y[m, n] = (sum_k x[m, k] w[n, k]) * x_scale[m] * w_scale[n]
  *             + bias[n] + residual[m, n]
- * The integer sum is exact (32 bits).  y may be the residual (same address
+ * The integer sum is exact (32 bits); it goes to fp32, where the two scales,
+ * bias and residual follow in this order.  y may be the residual (same address
  * and stride).  The bytes between a row's end and its stride are never
  * read.  Rows on 16-byte addresses (x, w and both strides multiples of 16,
  * the strides under 2^22) are multiplied where they lie; others are first
@@ -622,7 +624,10 @@ dopr_status_t dopr_rotary(const dopr_rotary_args_t *args, void *stream);
  *   DOPR_ROPE_RAMP    w_i (g_i + (1 - g_i) / s), g_i = 1 for pairs that turn
  *                     at least turns_high times within original_len, 0 for
  *                     at most turns_low, linear in the pair's index between
- *                     the two (real-valued) indices where the turns are met
+ *                     the two (real-valued) indices where the turns are met.
+ *                     Implementations that round these two outward to whole
+ *                     indices have other frequencies in between: a model that
+ *                     was trained with such ones brings its own inv_freq
  *   DOPR_ROPE_BANDS   the same with g_i linear in the number of turns
  * *attention_factor receives 0.1 ln s + 1 for RAMP with s > 1, else 1.
  * Host arithmetic in 64 bits; inv_freq is a HOST array of R/2 floats.      */

@@ -3,8 +3,10 @@
 //   y[m][n] = (sum_k x[m][k] w[n][k]) * x_scale[m] * w_scale[n]
 //             (+ bias[n]) (+ residual[m][n])
 // The sum is exact in 32-bit integers (depth <= 131071 keeps 128^2 * depth
-// below 2^31), so it does not depend on the order or the split of the depth;
-// the rest is fp32, rounded once.
+// below 2^31), so it does not depend on the order or the split of the depth.
+// The rest is fp32: the sum's conversion (exact up to 2^24), the two scales, bias
+// and residual in this order, each rounded to fp32 (five roundings, 5 * 2^-24 of
+// the magnitudes that are added), then the output's own rounding.
 //
 // Matrix cores: v_mfma_i32_16x16x64_i8 with 16 rows of w as the first operand
 // and 16 rows of x as the second: lane l holds 16 consecutive bytes (depth
@@ -323,8 +325,10 @@ hipError_t product_any(const ProductParams &P, hipStream_t s) {
 
 // Measured: 12,900 x 24576 x 4096 1040 us, 2.5 POP/s, the matrix cores busy for
 // 63 % of the cycles and the rest of the time behind the next span's loads (two
-// spans fill the LDS); 129 x 24576 x 4096 28 us, bound by L2, through which every
-// tile reads all of x beside its part of w.
+// spans fill the LDS); 129 x 24576 x 4096 28 us on 192 of the CUs, with neither
+// HBM (3.8 TB/s) nor the matrix cores (busy for a quarter of the cycles) at its
+// rate.  L2, through which every tile reads all of x beside its part of w, hands
+// out 219 MB, 7.8 TB/s, half of it hits; what bounds that size is open.
 
 constexpr int kGroupM = 8;  // tile rows that share w tiles while in L2
 
@@ -379,8 +383,12 @@ __device__ __forceinline__ void tile_of(int b, int tm, int tn, int &m,
   n = in / rows;
 }
 
-// Waves a SIMD's registers hold: 16 FM sums, twice 4 FM + 16 operands and some
-// 60 more each.
+// Waves a SIMD's registers are shared out to: 16 FM sums, twice 4 FM + 16
+// operands and some 60 more each.  That is over the share of the largest and the
+// smallest tiles, and instances that LDS holds to one block a CU get no more than
+// others.  What does not fit goes to scratch, none of it in the steady depth
+// loop: 24 registers and less (FM 8: 1, FM 7: 16), 39 in 64 x 128 tiles of two
+// groups (48 with fp32 outputs).
 constexpr int waves_per_simd(int FM) { return FM > 4 ? 2 : FM > 2 ? 3 : 4; }
 
 template <typename T, int FM, int WGM, int WGN, int WK, int ST>
@@ -888,11 +896,12 @@ int64_t repack_pitch(int64_t K) { return (K + kSpan - 1) / kSpan * kSpan; }
 // ---------------------------------------------------------------------------
 // Choice of the kernel.
 
-// The tiles, the few-row blocks, and what a call through each takes: fitted to
-// its times on 18 (cols, depth) pairs x up to 22 row counts from 17 to 12,900
-// (bf16 outputs, operands mostly fresh from HBM), then moved to what picks the
-// fastest most often,
-//   microseconds = base + rounds * (round + spans * span)
+// The tiles, the few-row blocks, and a cost by which a call picks one: fitted to
+// the times of each on 18 (cols, depth) pairs x up to 22 row counts from 17 to
+// 12,900 (bf16 outputs, operands mostly fresh from HBM), then moved to what picks
+// the fastest most often.  So costs are near microseconds but no forecast (the
+// largest product measured, 1040 us, costs 874):
+//   cost = base + rounds * (round + spans * span)
 //                  + spans * block_span * (blocks a CU runs, over all rounds)
 // with `rounds` the times the 256 CUs are filled and `spans` the spans of 128
 // a group of waves goes through; for the few-row blocks
@@ -1007,7 +1016,8 @@ hipError_t product(ProductParams P, void *workspace, size_t bytes,
     // the loads of a whole operand cost the few-row blocks as much as w's:
     // from 9 rows, wide and deep products go through LDS tiles instead (16
     // rows through 6144 x 4096 9.4 and 7.5 us, through 24576 x 4096 26.2 and
-    // 24.3, but through 4096 x 12288 12.9 and 14.2)
+    // 24.3, but through 4096 x 12288 12.9 and 14.2: three sizes, of which the
+    // first stands for the edge)
     if (P.M > 8 && P.N >= 6144 && P.K >= 4096 && aligned_rows(P))
       return product_tiles<T, 1, 1, 1, 4, 3>(P, s);
     return product_few<T, 1>(P, s);

@@ -14,7 +14,8 @@
 // The angle's whole turns are dropped in 64 bits (four operations per pair
 // and token): in 32 bits the product of a position and a frequency is off by
 // up to 2^-25 of itself, at position 2^17 0.004 rad, more than a bf16
-// rounding.
+// rounding.  Normed fp32 heads are turned in 64 bits too (244 us for the above,
+// 5.5 TB/s).
 #include <type_traits>
 
 #include "rowio.hpp"

@@ -2,12 +2,16 @@
 // memory each: rows in 8-bit integers (k_quantize_rows) and the norms around a
 // gated, scaled residual (k_norm_residual).
 //
-// A row is held in registers by TPR threads (a wave, or a whole block), 8 NV
-// elements each, so that its sums and its largest magnitude are
-// known before its first output is written and nothing is read twice.  Both
-// kernels are bound by HBM: a row's arithmetic is some ten vector
-// instructions per 8 elements (residual sum and norm of 12,900 x 4096 in bf16:
-// 71 us, 6.0 TB/s).
+// A row is held by TPR threads (a wave, or a whole block), 8 NV elements each, so
+// that its sums and its largest magnitude are known before its first output is
+// written and no input is read twice.  Up to a width of 16,384 it is held in
+// registers, and both kernels are bound by HBM: a row's arithmetic is some ten
+// vector instructions per 8 elements (residual sum and norm of 12,900 x 4096 in
+// bf16: 71 us, 6.0 TB/s; of 4000 x 16,384 92 us, 5.7 TB/s).  Wider rows of norms
+// do not fit the 128 registers a lane of 1,024 threads: 30 to 106 a lane go
+// through scratch where the residual is fp32, from 32,769 on 177 to 491 in every
+// type (2000 x 32,768 in bf16 97 us, 5.4 TB/s, around an fp32 residual 159 us,
+// 5.0, in fp32 254 us, 4.1; 1000 x 65,536 195, 368 and 510 us, 2.7 to 2.1 TB/s).
 #include <type_traits>
 
 #include "rowio.hpp"
@@ -137,7 +141,9 @@ __global__ __launch_bounds__(TPR > 64 ? TPR : 256) void k_quantize_rows(
       float g[E];
       ru[v].get(g);
       // SiLU(x) * up.  16-bit inputs: the hardware's exponential and
-      // reciprocal, a few units in fp32's last place, 2^-13 of an input's own.
+      // reciprocal, off by 3 + |x| units of fp32's last place at most (the
+      // exponential's argument is rounded), 2^-18 at |x| = 20, where an 8-bit
+      // step is 2^-7; x under -89 counts as 0.
       // fp32 inputs: both to the last place, as a caller who keeps 32 bits
       // expects.  Either way HBM is the bound (12,900 x 12,288 in bf16:
       // 140 us, 5.7 TB/s).
@@ -195,8 +201,9 @@ __global__ __launch_bounds__(TPR > 64 ? TPR : 256) void k_norm_residual(
   constexpr int kRows = TPR > 64 ? 1 : 4;
   constexpr int E = chunk_of(sizeof(T) > sizeof(R) ? sizeof(T) : sizeof(R));
   constexpr int NC = NV * 8 / E;
-  // fp32 activations: sums in 64 bits, so that a row's factor is the nearest
-  // fp32 to the exact one and its 8-bit form does not turn on the order
+  // fp32 activations: sums in 64 bits, so that a row's factor does not turn on
+  // their order; it is then within 2 units of fp32's last place of the exact
+  // one (the mean, the epsilon, the root and the reciprocal round)
   using Sum = std::conditional_t<sizeof(T) == 4, double, float>;
   __shared__ Sum part[TPR / 64];
   const int t = TPR > 64 ? threadIdx.x : threadIdx.x & 63;

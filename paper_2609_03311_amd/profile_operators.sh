@@ -4,6 +4,8 @@
 # tokens; the bf16 layer runs beside it for comparison):
 #   quant_layer_qwen3_8b_kernel_stats.txt   time of every kernel
 #   k_product_qwen3_8b_pmc.txt              shader counters of the products
+# and from one pair (129 tokens) through it:
+#   k_product_one_pair_pmc.txt              shader and L2 counters of the products
 # Raw output stays under $out, the summaries are written to $sum.
 # usage: bash paper_2609_03311_amd/profile_operators.sh
 set -o pipefail
@@ -12,24 +14,28 @@ out=$R/gpurun_out/prof_operators
 sum=$R/gpurun_out/summaries
 mkdir -p "$out" "$sum"
 me="bash paper_2609_03311_amd/profile_operators.sh"
-run="-m paper_2609_03311_amd.quant_layer --config qwen3_8b --pairs 100 --steps 3"
+layer="-m paper_2609_03311_amd.quant_layer --config qwen3_8b --steps 3 --pairs"
+run="$layer 100" run1="$layer 1"
 pm() { python3 -c "import sys; sys.path.insert(0, '$R'); from paper_2609_03311_amd import profiling as p; print(p.PMC_PASSES[$1])"; }
 export TMPDIR=/tmp PYTHONPATH=$R
 cd /tmp
 
-step() {  # name, rocprofv3 options...
-  local name=$1
-  shift
+step() {  # name, what to run, rocprofv3 options...
+  local name=$1 what=$2
+  shift 2
   echo "== $name" && timeout -k 10 -s KILL 200 rocprofv3 "$@" -d "$out/$name" \
-    -o run --output-format csv -- python3 $run > "$out/$name.log" 2>&1
+    -o run --output-format csv -- python3 $what > "$out/$name.log" 2>&1
   local rc=$?
   tail -1 "$out/$name.log" | cut -c1-160
   return $rc
 }
 
-step stats --kernel-trace --stats &&
-  step pmc_a --pmc $(pm 0) &&
-  step pmc_b --pmc $(pm 1) || exit $?
+step stats "$run" --kernel-trace --stats &&
+  step pmc_a "$run" --pmc $(pm 0) &&
+  step pmc_b "$run" --pmc $(pm 1) &&
+  step one_a "$run1" --pmc $(pm 0) &&
+  step one_b "$run1" --pmc $(pm 1) &&
+  step one_c "$run1" --pmc $(pm 2) || exit $?
 
 P="python3 -m paper_2609_03311_amd.profiling"
 cd "$R" &&
@@ -38,4 +44,7 @@ cd "$R" &&
     > "$sum/quant_layer_qwen3_8b_kernel_stats.txt" &&
   $P pmc "$out/pmc_a" "$out/pmc_b" --sources operators --kernel "k_product<" \
     --command "$me (rocprofv3 --pmc <PMC_PASSES[0]>, then <PMC_PASSES[1]> -- python3 $run)" \
-    > "$sum/k_product_qwen3_8b_pmc.txt"
+    > "$sum/k_product_qwen3_8b_pmc.txt" &&
+  $P pmc "$out/one_a" "$out/one_b" "$out/one_c" --sources operators --kernel "k_product<" \
+    --command "$me (rocprofv3 --pmc <PMC_PASSES[0]>, [1], [2] -- python3 $run1)" \
+    > "$sum/k_product_one_pair_pmc.txt"

@@ -175,6 +175,8 @@ PMC_PASSES = (
     "SQ_WAIT_ANY SQ_WAIT_INST_ANY SQ_WAIT_INST_LDS SQ_ACTIVE_INST_ANY "
     "SQ_ACTIVE_INST_LDS SQ_LDS_BANK_CONFLICT SQ_LDS_IDX_ACTIVE "
     "SQ_ACTIVE_INST_VMEM GRBM_GUI_ACTIVE",
+    # L2: requests of 128 bytes, and those it passes on to memory
+    "TCC_REQ_sum TCC_HIT_sum TCC_MISS_sum TCC_EA0_RDREQ_sum",
 )
 
 
