@@ -121,6 +121,75 @@ dopr_status_t dopr_store_put(dopr_store_t st, int32_t layer, int64_t n,
 
 dopr_status_t dopr_store_destroy(dopr_store_t st);
 
+/* Stores of 4 bits a value.  A store has a format, and every call that takes a
+ * store takes one of either (dopr_store_put and dopr_gather_prefix included,
+ * whose k and v stay bf16; dopr_store_copy_docs wants both of one format).
+ *   DOPR_STORE_BF16  the states as they are put (dopr_store_create)
+ *   DOPR_STORE_FP4   17 bytes for 32 values, about a quarter of the bytes: a
+ *                    block of 32 values holds a power of two, the smallest 2^e
+ *                    with 7 * 2^e >= the block's largest magnitude (e in
+ *                    -125 .. 125), and for each value a 4-bit float c (0, 0.5,
+ *                    1, 1.5, 2, 3, 4, 6 and their negatives), the nearest to
+ *                    value / 2^e, ties to the even code, at most 6.
+ *                    A key's block is the 32 dims 64 j + 16 i + 8 h + e of one
+ *                    (j, h), i < 4, e < 8, of one slot; a value's block is one
+ *                    dim of 32 slots (32 s .. 32 s + 31 of the document, fewer
+ *                    at its end).  No value is off by more than 2^e (beyond
+ *                    7 * 2^125, by more).  A block with a value that is not
+ *                    finite reads as NaN.
+ * What is held are bf16 values, and a call on a 4-bit store computes what it
+ * computes on a bf16 store that holds those values: the same bits wherever the
+ * same kernels run (not the pairs of one token, see dopr_prefix_attn).  */
+typedef enum { DOPR_STORE_BF16 = 0, DOPR_STORE_FP4 = 1 } dopr_store_format_t;
+
+/* dopr_store_bytes and dopr_store_create for a format.  *payload_bytes of a
+ * 4-bit store: codes and exponents of the documents' slots; its pool holds
+ * whole chunks of 32 slots.                                                */
+dopr_status_t dopr_store_bytes_as(const dopr_store_desc_t *desc,
+                                  int32_t format, size_t *pool_bytes,
+                                  size_t *payload_bytes);
+dopr_status_t dopr_store_create_as(const dopr_store_desc_t *desc,
+                                   int32_t format, void *pool,
+                                   size_t pool_bytes, void *stream,
+                                   dopr_store_t *out);
+
+/* dopr_store_put of keys as a projection leaves them: for slot j of document
+ * doc_ids[i], source row r = src_cu_slots[i] + j,
+ *   k' = RoPE_pos(RMSNorm(k[r]) * k_norm_w)     (no norm without k_norm_w)
+ *   pos = positions[r], or j when positions is NULL
+ * the rotation being dopr_rotary's (rotary_dim, interleaved, inv_freq,
+ * attention_factor).  k' is formed in 64 bits and rounded to bf16, v is rounded
+ * to bf16, and both go into the store, of either format, as dopr_store_put
+ * would put them.  Rows and heads lie any distance apart (k and v may be parts
+ * of one buffer).  A document whose rows do not lie in [0, rows), whose slot
+ * count differs from L_d, or that is out of range or not resident, is skipped
+ * and reported by dopr_check_status as DOC_RANGE.  A call names a document
+ * once.                                                                    */
+typedef struct {
+  int32_t layer;
+  int32_t dtype;            /* of k, v and k_norm_w (dopr_dtype_t: bf16, fp16
+                               or fp32)                                     */
+  int64_t n;                /* documents, >= 0                              */
+  int64_t rows;             /* of k, v and positions                        */
+  const int32_t *doc_ids;   /* dev int32 [n]                                */
+  const int64_t *src_cu_slots; /* dev int64 [n+1]                           */
+  const void *k;            /* dev [rows, Hkv, D]                           */
+  int64_t k_row_stride, k_head_stride; /* elements, >= 0                    */
+  const void *v;            /* dev [rows, Hkv, D]                           */
+  int64_t v_row_stride, v_head_stride;
+  const void *k_norm_w;     /* dev [D] or NULL                              */
+  const int32_t *positions; /* dev int32 [rows] or NULL                     */
+  const float *inv_freq;    /* dev fp32 [rotary_dim / 2]                    */
+  int32_t rotary_dim;       /* even, 2 .. D                                 */
+  int32_t interleaved;      /* 0 or 1                                       */
+  float attention_factor;   /* finite                                       */
+  float rms_eps;            /* finite, >= 0                                 */
+} dopr_put_rotary_args_t;
+
+dopr_status_t dopr_store_put_rotary(dopr_store_t st,
+                                    const dopr_put_rotary_args_t *args,
+                                    void *stream);
+
 /* Carry documents over from one store to another (store maintenance: the
  * prefix states are built once per document offline and kept for reuse,
  * Sec. 3.3-3.4, so a collection that grows or shrinks is served by a new

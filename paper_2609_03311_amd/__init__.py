@@ -25,6 +25,9 @@ DOPR_ERR_WORKSPACE = -4
 DOPR_ERR_HIP = -5
 DOPR_ERR_SEQLEN = -6
 
+DOPR_STORE_BF16 = 0
+DOPR_STORE_FP4 = 1
+
 
 class DoprError(RuntimeError):
     def __init__(self, status: int, msg: str):
@@ -155,11 +158,35 @@ class _RotaryArgs(ctypes.Structure):
                 ("q_norm_w", ctypes.c_void_p), ("k_norm_w", ctypes.c_void_p)]
 
 
+class _PutRotaryArgs(ctypes.Structure):
+    _fields_ = [("layer", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("n", ctypes.c_int64), ("rows", ctypes.c_int64),
+                ("doc_ids", ctypes.c_void_p),
+                ("src_cu_slots", ctypes.c_void_p), ("k", ctypes.c_void_p),
+                ("k_row_stride", ctypes.c_int64),
+                ("k_head_stride", ctypes.c_int64), ("v", ctypes.c_void_p),
+                ("v_row_stride", ctypes.c_int64),
+                ("v_head_stride", ctypes.c_int64),
+                ("k_norm_w", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("inv_freq", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32),
+                ("attention_factor", ctypes.c_float),
+                ("rms_eps", ctypes.c_float)]
+
+
 EXPORTS = {
     "dopr_store_bytes": ([ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p],
                          ctypes.c_int),
     "dopr_store_create": ([ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
                            ctypes.c_void_p, ctypes.c_void_p], ctypes.c_int),
+    "dopr_store_bytes_as": ([ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
+                             ctypes.c_void_p], ctypes.c_int),
+    "dopr_store_create_as": ([ctypes.c_void_p, ctypes.c_int32,
+                              ctypes.c_void_p, ctypes.c_size_t,
+                              ctypes.c_void_p, ctypes.c_void_p],
+                             ctypes.c_int),
+    "dopr_store_put_rotary": ([ctypes.c_void_p, ctypes.c_void_p,
+                               ctypes.c_void_p], ctypes.c_int),
     "dopr_store_put": ([ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                         ctypes.c_void_p, ctypes.c_void_p], ctypes.c_int),
@@ -260,22 +287,30 @@ def _desc(n_layers, n_kv_heads, head_dim, doc_len):
 
 
 def dopr_store_bytes(n_layers: int, n_kv_heads: int, head_dim: int,
-                     doc_len):
+                     doc_len, format: int = DOPR_STORE_BF16):
     """Returns (pool_bytes, payload_bytes) for a store (host arithmetic)."""
     d, keep = _desc(n_layers, n_kv_heads, head_dim, doc_len)
     pool = ctypes.c_size_t(0)
     payload = ctypes.c_size_t(0)
-    _check(lib().dopr_store_bytes(ctypes.byref(d), ctypes.byref(pool),
-                                  ctypes.byref(payload)))
+    _check(lib().dopr_store_bytes_as(ctypes.byref(d), int(format),
+                                     ctypes.byref(pool),
+                                     ctypes.byref(payload)))
     return pool.value, payload.value
+
+
+def dopr_store_bytes_as(n_layers: int, n_kv_heads: int, head_dim: int,
+                        doc_len, format: int):
+    """dopr_store_bytes of a format."""
+    return dopr_store_bytes(n_layers, n_kv_heads, head_dim, doc_len, format)
 
 
 class Store:
     """Handle of a prefix store laid out in a caller-owned device pool."""
 
     def __init__(self, handle, pool, n_layers, n_kv_heads, doc_len,
-                 head_dim=128):
+                 head_dim=128, format=DOPR_STORE_BF16):
         self.handle = handle
+        self.format = format  # DOPR_STORE_BF16 or DOPR_STORE_FP4
         self.pool = pool  # keeps the device memory alive
         self.n_layers = n_layers
         self.n_kv_heads = n_kv_heads
@@ -295,21 +330,33 @@ class Store:
 
 
 def dopr_store_create(n_layers: int, n_kv_heads: int, head_dim: int,
-                      doc_len, pool=None, stream=None, device=None) -> Store:
+                      doc_len, pool=None, stream=None, device=None,
+                      format: int = DOPR_STORE_BF16) -> Store:
     """Create a store.  `pool` is a uint8 CUDA tensor of at least
-    dopr_store_bytes(...)[0] bytes; allocated with torch if omitted."""
+    dopr_store_bytes(...)[0] bytes; allocated with torch if omitted.
+    `format`: DOPR_STORE_BF16 or DOPR_STORE_FP4 (states held in 4 bits)."""
     import torch
-    pool_bytes, _ = dopr_store_bytes(n_layers, n_kv_heads, head_dim, doc_len)
+    pool_bytes, _ = dopr_store_bytes(n_layers, n_kv_heads, head_dim, doc_len,
+                                     format)
     if pool is None:
         pool = torch.empty(max(pool_bytes, 256), dtype=torch.uint8,
                            device=device or "cuda")
     d, keep = _desc(n_layers, n_kv_heads, head_dim, doc_len)
     h = ctypes.c_void_p(0)
-    _check(lib().dopr_store_create(ctypes.byref(d), pool.data_ptr(),
-                                   pool.numel() * pool.element_size(),
-                                   _stream(stream), ctypes.byref(h)))
+    _check(lib().dopr_store_create_as(ctypes.byref(d), int(format),
+                                      pool.data_ptr(),
+                                      pool.numel() * pool.element_size(),
+                                      _stream(stream), ctypes.byref(h)))
     return Store(h.value, pool, n_layers, n_kv_heads, keep.copy(),
-                 head_dim=head_dim)
+                 head_dim=head_dim, format=int(format))
+
+
+def dopr_store_create_as(n_layers: int, n_kv_heads: int, head_dim: int,
+                         doc_len, format: int, pool=None, stream=None,
+                         device=None) -> Store:
+    """dopr_store_create of a format."""
+    return dopr_store_create(n_layers, n_kv_heads, head_dim, doc_len, pool,
+                             stream, device, format)
 
 
 def dopr_store_put(store: Store, layer: int, doc_ids, src_cu_slots, k_src,
@@ -317,6 +364,62 @@ def dopr_store_put(store: Store, layer: int, doc_ids, src_cu_slots, k_src,
     _check(lib().dopr_store_put(store.handle, layer, doc_ids.numel(),
                                 _ptr(doc_ids), _ptr(src_cu_slots),
                                 _ptr(k_src), _ptr(v_src), _stream(stream)))
+
+
+def _put_heads(name, t, store, rows):
+    """(row, head) strides of k or v [rows, Hkv, D]."""
+    if t.dim() != 3 or tuple(t.shape) != (rows, store.n_kv_heads,
+                                          store.head_dim):
+        raise ValueError(f"{name} must be [rows, {store.n_kv_heads}, "
+                         f"{store.head_dim}], the rows of k")
+    if t.stride(2) != 1:
+        raise ValueError(f"{name} must have elements back to back")
+    return t.stride(0), t.stride(1)
+
+
+def dopr_store_put_rotary(store: Store, layer: int, doc_ids, src_cu_slots, k,
+                          v, inv_freq, *, positions=None, k_norm_w=None,
+                          interleaved=False, attention_factor=1.0,
+                          rms_eps=1e-6, stream=None):
+    """dopr_store_put of keys as a projection leaves them: k [rows, Hkv, D]
+    (bf16, fp16 or fp32) after an optional RMSNorm (k_norm_w [D]) turned to
+    `positions` int32 [rows] (None: each document's slots 0, 1, ..), and v
+    alike, rows and heads at any stride.  inv_freq fp32 [R/2] rotates the
+    first R elements of a head."""
+    import torch
+    kinds = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+    if k.dtype not in kinds:
+        raise ValueError("k must be bfloat16, float16 or float32")
+    rows = k.shape[0]
+    k_row, k_head = _put_heads("k", k, store, rows)
+    v_row, v_head = _put_heads("v", v, store, rows)
+    if v.dtype != k.dtype:
+        raise ValueError("v must have k's type")
+    n = doc_ids.numel()
+    for name, t, dtype, shape in (
+            ("doc_ids", doc_ids, torch.int32, (n,)),
+            ("src_cu_slots", src_cu_slots, torch.int64, (n + 1,)),
+            ("positions", positions, torch.int32, (rows,)),
+            ("k_norm_w", k_norm_w, k.dtype, (store.head_dim,)),
+            ("inv_freq", inv_freq, torch.float32, (inv_freq.numel(),)),
+            ("k", k, k.dtype, None), ("v", v, k.dtype, None)):
+        if t is None:
+            continue
+        if t.dtype != dtype:
+            raise ValueError(f"{name} must be {dtype}")
+        if shape is not None and (tuple(t.shape) != shape
+                                  or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous, of shape {shape}")
+        if t.device != store.pool.device:
+            raise ValueError(f"{name} must be on the store's device")
+    a = _PutRotaryArgs(int(layer), kinds[k.dtype], n, rows, _ptr(doc_ids),
+                       _ptr(src_cu_slots), _ptr(k), k_row, k_head, _ptr(v),
+                       v_row, v_head, _ptr(k_norm_w), _ptr(positions),
+                       _ptr(inv_freq), 2 * inv_freq.numel(),
+                       int(bool(interleaved)), float(attention_factor),
+                       float(rms_eps))
+    _check(lib().dopr_store_put_rotary(store.handle, ctypes.byref(a),
+                                       _stream(stream)))
 
 
 def dopr_store_destroy(store: Store):

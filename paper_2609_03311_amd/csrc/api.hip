@@ -43,6 +43,15 @@ bool aligned16(const void *p) {
   return (reinterpret_cast<uintptr_t>(p) & 15) == 0;
 }
 
+bool is_dtype(int32_t t) {
+  return t == DOPR_BF16 || t == DOPR_F16 || t == DOPR_F32;
+}
+
+bool aligned_to(const void *p, int32_t dtype) {
+  const uintptr_t e = dtype == DOPR_F32 ? 4 : 2;
+  return reinterpret_cast<uintptr_t>(p) % e == 0;
+}
+
 hipStream_t as_stream(void *s) { return static_cast<hipStream_t>(s); }
 
 struct StoreLayout {
@@ -52,9 +61,12 @@ struct StoreLayout {
 };
 
 // Offsets of the pool sections; optionally the per-document block offsets.
-dopr_status_t layout_store(const dopr_store_desc_t *d, StoreLayout *lay,
-                           std::vector<int64_t> *doc_off) {
+dopr_status_t layout_store(const dopr_store_desc_t *d, int32_t format,
+                           StoreLayout *lay, std::vector<int64_t> *doc_off) {
   if (!d) return fail(DOPR_ERR_INVALID_ARG, "desc is NULL");
+  if (format != DOPR_STORE_BF16 && format != DOPR_STORE_FP4)
+    return fail(DOPR_ERR_INVALID_ARG, "unknown store format");
+  const bool fp4 = format == DOPR_STORE_FP4;
   if (d->n_docs < 0 || d->n_docs > INT32_MAX)
     return fail(DOPR_ERR_INVALID_ARG, "n_docs must be in [0, 2^31)");
   if (d->n_docs > 0 && !d->doc_len)
@@ -85,8 +97,14 @@ dopr_status_t layout_store(const dopr_store_desc_t *d, StoreLayout *lay,
     if (L < 0) continue;
     if (doc_off) (*doc_off)[i] = elems;
     elems += (int64_t)d->n_layers *
-             layer_block_elems(L, d->n_kv_heads, d->head_dim);
-    canon += (size_t)L * d->n_layers * d->n_kv_heads * d->head_dim * 2 * 2;
+             layer_block_elems(L, d->n_kv_heads, d->head_dim, fp4);
+    // (4 bits a value, and a byte for 32 values of a key, for up to 32 slots
+    // of a value's dim)
+    const size_t per_head =
+        fp4 ? ((size_t)L + (size_t)L / 32 + (((size_t)L + 31) / 32)) *
+                  d->head_dim
+            : (size_t)L * d->head_dim * 2 * 2;
+    canon += per_head * d->n_layers * d->n_kv_heads;
     if (L > max_len) max_len = L;
   }
   lay->total = off + sizeof(uint16_t) * (size_t)elems;
@@ -115,7 +133,7 @@ int32_t default_rows_per_item(int32_t variant, bool score_only,
 // token.
 bool uses_pass_kernel(int32_t variant, const dopr_store *st, int64_t rows) {
   if (variant != 0 && variant != 5) return variant == 8;
-  return st->head_dim != 64 || rows > kPassRows ||
+  return st->fp4 || st->head_dim != 64 || rows > kPassRows ||
          st->max_len <= kOneTileSlots;
 }
 
@@ -129,7 +147,7 @@ bool uses_pass_kernel(int32_t variant, const dopr_store *st, int64_t rows) {
 bool pass_kernel_holds(const dopr_store *st, int32_t n_rep) {
   const int64_t D = st->head_dim;
   return n_rep < (1 << 15) &&
-         2 * D * (int64_t)pad8(st->max_len) <= UINT32_MAX &&
+         (st->fp4 || 2 * D * (int64_t)pad8(st->max_len) <= UINT32_MAX) &&
          st->n_kv_heads * D < (1 << 25);
 }
 
@@ -244,9 +262,15 @@ const char *dopr_last_error(void) { return g_last_error.c_str(); }
 
 dopr_status_t dopr_store_bytes(const dopr_store_desc_t *desc,
                                size_t *pool_bytes, size_t *payload_bytes) {
+  return dopr_store_bytes_as(desc, DOPR_STORE_BF16, pool_bytes, payload_bytes);
+}
+
+dopr_status_t dopr_store_bytes_as(const dopr_store_desc_t *desc,
+                                  int32_t format, size_t *pool_bytes,
+                                  size_t *payload_bytes) {
   if (!pool_bytes) return fail(DOPR_ERR_INVALID_ARG, "pool_bytes is NULL");
   StoreLayout lay;
-  dopr_status_t s = layout_store(desc, &lay, nullptr);
+  dopr_status_t s = layout_store(desc, format, &lay, nullptr);
   if (s != DOPR_OK) return s;
   *pool_bytes = lay.total;
   if (payload_bytes) *payload_bytes = lay.payload_canonical;
@@ -256,11 +280,19 @@ dopr_status_t dopr_store_bytes(const dopr_store_desc_t *desc,
 dopr_status_t dopr_store_create(const dopr_store_desc_t *desc, void *pool,
                                 size_t pool_bytes, void *stream,
                                 dopr_store_t *out) {
+  return dopr_store_create_as(desc, DOPR_STORE_BF16, pool, pool_bytes, stream,
+                              out);
+}
+
+dopr_status_t dopr_store_create_as(const dopr_store_desc_t *desc,
+                                   int32_t format, void *pool,
+                                   size_t pool_bytes, void *stream,
+                                   dopr_store_t *out) {
   if (!out) return fail(DOPR_ERR_INVALID_ARG, "out is NULL");
   *out = nullptr;
   StoreLayout lay;
   std::vector<int64_t> doc_off;
-  dopr_status_t s = layout_store(desc, &lay, &doc_off);
+  dopr_status_t s = layout_store(desc, format, &lay, &doc_off);
   if (s != DOPR_OK) return s;
   if (!pool) return fail(DOPR_ERR_INVALID_ARG, "pool is NULL");
   if (reinterpret_cast<uintptr_t>(pool) % kAlign)
@@ -288,6 +320,7 @@ dopr_status_t dopr_store_create(const dopr_store_desc_t *desc, void *pool,
   st->d_payload = reinterpret_cast<uint16_t *>(base + lay.payload_off);
   st->max_len = lay.max_len;
   st->device = dev;
+  st->fp4 = format == DOPR_STORE_FP4;
   hipStream_t hs = as_stream(stream);
   e = hipMemsetAsync(st->d_status, 0, sizeof(int32_t) * kStatusWords, hs);
   if (e == hipSuccess && desc->n_docs > 0)
@@ -327,11 +360,68 @@ dopr_status_t dopr_store_put(dopr_store_t st, int32_t layer, int64_t n,
     return fail(DOPR_ERR_INVALID_ARG, "k_src/v_src must be 16-byte aligned");
   dopr_status_t s = check_device(st);
   if (s != DOPR_OK) return s;
-  hipError_t e = launch_store_put(*st, layer, n, doc_ids, src_cu_slots,
-                                  static_cast<const uint16_t *>(k_src),
-                                  static_cast<const uint16_t *>(v_src),
-                                  as_stream(stream));
+  hipError_t e;
+  if (st->fp4) {
+    const int64_t D = st->head_dim, row = st->n_kv_heads * D;
+    dopr_put_rotary_args_t a{};
+    a.layer = layer;
+    a.dtype = DOPR_BF16;
+    a.n = n;
+    a.rows = INT64_MAX;
+    a.doc_ids = doc_ids;
+    a.src_cu_slots = src_cu_slots;
+    a.k = k_src;
+    a.v = v_src;
+    a.k_row_stride = a.v_row_stride = row;
+    a.k_head_stride = a.v_head_stride = D;
+    e = launch_put_states(*st, a, as_stream(stream));
+  } else {
+    e = launch_store_put(*st, layer, n, doc_ids, src_cu_slots,
+                         static_cast<const uint16_t *>(k_src),
+                         static_cast<const uint16_t *>(v_src),
+                         as_stream(stream));
+  }
   if (e != hipSuccess) return hip_fail(e, "store_put launch");
+  return ok();
+}
+
+dopr_status_t dopr_store_put_rotary(dopr_store_t st,
+                                    const dopr_put_rotary_args_t *a,
+                                    void *stream) {
+  if (!st) return fail(DOPR_ERR_INVALID_ARG, "store is NULL");
+  if (!a) return fail(DOPR_ERR_INVALID_ARG, "args is NULL");
+  if (a->layer < 0 || a->layer >= st->n_layers)
+    return fail(DOPR_ERR_INVALID_ARG, "layer out of range");
+  if (!is_dtype(a->dtype)) return fail(DOPR_ERR_INVALID_ARG, "unknown dtype");
+  if (a->n < 0 || a->n > INT32_MAX)
+    return fail(DOPR_ERR_INVALID_ARG, "bad n");
+  if (a->rows < 0) return fail(DOPR_ERR_INVALID_ARG, "rows < 0");
+  if (a->rotary_dim < 2 || a->rotary_dim % 2 || a->rotary_dim > st->head_dim)
+    return fail(DOPR_ERR_INVALID_ARG,
+                "rotary_dim must be even, in [2, head_dim]");
+  if (a->interleaved & ~1)
+    return fail(DOPR_ERR_INVALID_ARG, "interleaved is 0 or 1");
+  if (!std::isfinite(a->attention_factor))
+    return fail(DOPR_ERR_INVALID_ARG, "attention_factor must be finite");
+  if (!(a->rms_eps >= 0.f) || !std::isfinite(a->rms_eps))
+    return fail(DOPR_ERR_INVALID_ARG, "rms_eps must be finite and >= 0");
+  if (a->k_row_stride < 0 || a->k_head_stride < 0 || a->v_row_stride < 0 ||
+      a->v_head_stride < 0)
+    return fail(DOPR_ERR_INVALID_ARG, "strides must be >= 0");
+  if (a->n == 0) return ok();
+  if (!a->doc_ids || !a->src_cu_slots || !a->inv_freq || !a->k || !a->v)
+    return fail(DOPR_ERR_INVALID_ARG, "NULL buffer");
+  if (!aligned_to(a->k, a->dtype) || !aligned_to(a->v, a->dtype) ||
+      !aligned_to(a->k_norm_w, a->dtype) ||
+      !aligned_to(a->positions, DOPR_F32) ||
+      !aligned_to(a->inv_freq, DOPR_F32) ||
+      !aligned_to(a->doc_ids, DOPR_F32) ||
+      reinterpret_cast<uintptr_t>(a->src_cu_slots) % 8)
+    return fail(DOPR_ERR_INVALID_ARG, "buffers must be element-aligned");
+  dopr_status_t s = check_device(st);
+  if (s != DOPR_OK) return s;
+  const hipError_t e = launch_put_states(*st, *a, as_stream(stream));
+  if (e != hipSuccess) return hip_fail(e, "store_put_rotary launch");
   return ok();
 }
 
@@ -342,6 +432,8 @@ dopr_status_t dopr_store_copy_docs(dopr_store_t dst, dopr_store_t src,
       dst->n_kv_heads != src->n_kv_heads || dst->head_dim != src->head_dim)
     return fail(DOPR_ERR_INVALID_ARG,
                 "stores differ in n_docs, n_layers, n_kv_heads or head_dim");
+  if (dst->fp4 != src->fp4)
+    return fail(DOPR_ERR_INVALID_ARG, "stores differ in format");
   if (dst->pool < src->pool + src->pool_bytes &&
       src->pool < dst->pool + dst->pool_bytes)
     return fail(DOPR_ERR_INVALID_ARG, "store pools overlap");
@@ -752,10 +844,10 @@ dopr_status_t dopr_gather_prefix(dopr_store_t st, int32_t layer, int32_t n,
     return fail(DOPR_ERR_INVALID_ARG, "k_out/v_out must be 16-byte aligned");
   dopr_status_t s = check_device(st);
   if (s != DOPR_OK) return s;
-  hipError_t e = launch_gather(*st, layer, n, doc_ids, out_cu_slots,
-                               static_cast<uint16_t *>(k_out),
-                               static_cast<uint16_t *>(v_out),
-                               as_stream(stream));
+  const auto launch = st->fp4 ? launch_gather_fp4 : launch_gather;
+  hipError_t e = launch(*st, layer, n, doc_ids, out_cu_slots,
+                        static_cast<uint16_t *>(k_out),
+                        static_cast<uint16_t *>(v_out), as_stream(stream));
   if (e != hipSuccess) return hip_fail(e, "gather launch");
   return ok();
 }
@@ -937,15 +1029,6 @@ namespace {
 
 constexpr int64_t kMaxRowWidth = 65536;   // a row held by 1,024 threads
 constexpr int64_t kMaxDepth = 131071;     // 128^2 * depth < 2^31
-
-bool is_dtype(int32_t t) {
-  return t == DOPR_BF16 || t == DOPR_F16 || t == DOPR_F32;
-}
-
-bool aligned_to(const void *p, int32_t dtype) {
-  const uintptr_t e = dtype == DOPR_F32 ? 4 : 2;
-  return reinterpret_cast<uintptr_t>(p) % e == 0;
-}
 
 dopr_status_t check_rows(int32_t dtype, int64_t rows, int64_t width) {
   if (!is_dtype(dtype)) return fail(DOPR_ERR_INVALID_ARG, "unknown dtype");

@@ -60,7 +60,7 @@ namespace {
 // SMX fixed, so every loop below is straight-line code over one set of
 // accumulators.  Returns whether some row of this wave left the range the
 // fast modes guarantee (the unit is then recomputed in SAFE mode).
-template <int WAVES, int NQB, int SMX, bool SCORE, int D, int NCHK>
+template <int WAVES, int NQB, int SMX, bool SCORE, int D, int NCHK, bool FP4>
 __device__ __forceinline__ bool run_unit(const AttnParams &P,
                                          Smem<D, NCHK> &sm, const Frag<D> &fo,
                                          int g, int row0, int row1, int L,
@@ -139,7 +139,11 @@ __device__ __forceinline__ bool run_unit(const AttnParams &P,
       const int n = L - seg0 < PSEG ? L - seg0 : PSEG;
       if (!resident) {
         __syncthreads();
-        stage_prefix<WAVES, D, NCHK>(Kp, VTp, L, seg0, n, sm);
+        if constexpr (FP4)
+          stage_prefix_fp4<WAVES, D, NCHK>(
+              reinterpret_cast<const char *>(Kp), seg0, n, sm);
+        else
+          stage_prefix<WAVES, D, NCHK>(Kp, VTp, L, seg0, n, sm);
       }
       wait_vmem();
       __syncthreads();
@@ -285,7 +289,8 @@ constexpr int waves_per_simd(int waves, int d, int nchk) {
   return (waves / 4) * ((nchk + 2) * 2 * KC * d * 2 <= 81920 ? 2 : 1);
 }
 
-template <int WAVES, int NQB, bool SAFE, bool SCORE, int D, int NCHK>
+// FP4: on a 4-bit store.
+template <int WAVES, int NQB, bool SAFE, bool SCORE, int D, int NCHK, bool FP4>
 __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(
     waves_per_simd(WAVES, D, NCHK),
     waves_per_simd(WAVES, D, NCHK)))) void k_prefix_attn(AttnParams P) {
@@ -324,9 +329,18 @@ __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(
     const int doc = P.group_doc[it.x];
     const int L = P.doc_len[doc], Lp = pad8(L);
     const int64_t blk = P.doc_off[doc];
-    const uint16_t *Kp = P.payload + k_offset(blk, L, P.Hkv, P.layer, g, D);
+    const uint16_t *Kp =
+        P.payload + (FP4 ? fp4_offset(blk, L, P.Hkv, P.layer, g, D)
+                         : k_offset(blk, L, P.Hkv, P.layer, g, D));
     const uint16_t *VTp =
-        P.payload + vt_offset(blk, L, P.Hkv, P.layer, g, D);
+        P.payload + vt_offset(blk, L, P.Hkv, P.layer, g, D);  // (bf16 only)
+    auto stage = [&]() {
+      if constexpr (FP4)
+        stage_prefix_fp4<WAVES, D, NCHK>(reinterpret_cast<const char *>(Kp), 0,
+                                         L, sm);
+      else
+        stage_prefix<WAVES, D, NCHK>(Kp, VTp, L, 0, L, sm);
+    };
     // every logit of this unit lies in [-B, B] (log2 units).  Without
     // QK-norm no bound is known (kown = 0, so B = 0): the unit runs the
     // no-reference mode anyway, and a row whose normaliser leaves the range
@@ -339,9 +353,8 @@ __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(
     const bool resident = n_seg <= 1;
     if (!SAFE) {
       if (B <= kNoRefBound) {
-        if (resident && L > 0)
-          stage_prefix<WAVES, D, NCHK>(Kp, VTp, L, 0, L, sm);
-        wave_bad = run_unit<WAVES, NQB, 0, SCORE, D, NCHK>(
+        if (resident && L > 0) stage();
+        wave_bad = run_unit<WAVES, NQB, 0, SCORE, D, NCHK, FP4>(
                        P, sm, fo, g, row0, row1, L, Lp, Kp, VTp, B) ||
                    P.flag_all;
       }
@@ -358,12 +371,11 @@ __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(
       }
       __syncthreads();
     } else {
-      if (resident && L > 0)
-        stage_prefix<WAVES, D, NCHK>(Kp, VTp, L, 0, L, sm);
+      if (resident && L > 0) stage();
       // (self-check mode sends every unit to the exact mode)
       bool exact = !unscored || P.flag_all;
       if (!exact) {
-        wave_bad = run_unit<WAVES, NQB, 1, SCORE, D, NCHK>(
+        wave_bad = run_unit<WAVES, NQB, 1, SCORE, D, NCHK, FP4>(
             P, sm, fo, g, row0, row1, L, Lp, Kp, VTp, B);
         __syncthreads();
         if (lane == 0) sm.words()[1 + wave] = wave_bad;
@@ -372,8 +384,8 @@ __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(
         __syncthreads();
       }
       if (exact)
-        run_unit<WAVES, NQB, 2, SCORE, D, NCHK>(P, sm, fo, g, row0, row1, L,
-                                                Lp, Kp, VTp, B);
+        run_unit<WAVES, NQB, 2, SCORE, D, NCHK, FP4>(P, sm, fo, g, row0, row1,
+                                                     L, Lp, Kp, VTp, B);
       __syncthreads();  // every wave is done with this item's LDS
     }
   }
@@ -575,7 +587,7 @@ __device__ __forceinline__ void pv_regs(floatx16 *S, const bf16x8 *vf,
         vf[f], pb[0][f & 1], acc[0].o[f >> 1], 0, 0, 0);
 }
 
-template <int D>
+template <int D, bool FP4>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(
     2, 2))) void k_score_rows(AttnParams P) {
   __shared__ __attribute__((aligned(16))) uint16_t sov[4][D * KC];
@@ -605,9 +617,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(
     const int doc = P.group_doc[it.x];
     const int L = P.doc_len[doc], Lp = pad8(L);
     const int64_t blk = P.doc_off[doc];
-    const uint16_t *Kp = P.payload + k_offset(blk, L, P.Hkv, P.layer, g, D);
+    const uint16_t *Kp =
+        P.payload + (FP4 ? fp4_offset(blk, L, P.Hkv, P.layer, g, D)
+                         : k_offset(blk, L, P.Hkv, P.layer, g, D));
     const uint16_t *VTp =
-        P.payload + vt_offset(blk, L, P.Hkv, P.layer, g, D);
+        P.payload + vt_offset(blk, L, P.Hkv, P.layer, g, D);  // (bf16 only)
     const float kbound = fmaxf(
         P.kown[0], P.kmax[((int64_t)doc * P.n_layers + P.layer) * P.Hkv + g]);
     const float B = P.c * P.kown[1] * kbound * 1.001f;
@@ -650,7 +664,38 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(
       // V^T granules past the stored columns are zero
       // (at D = 128 the V^T fragments are gathered after the QK products,
       // so the K fragments' registers are free again: fewer spills)
-      for (int c0 = 0; c0 < L; c0 += KC) {
+      if constexpr (FP4) {
+        // (a 4-bit store's chunks lie in operand order: the next chunk's codes
+        // are asked for before this one's products)
+        const char *chunk = reinterpret_cast<const char *>(Kp);
+        Fp4Raw<D> kr, vr;
+        if (L > 0) {
+          fp4_load_k<D>(chunk, lt_, kr);
+          fp4_load_v<D>(chunk, lt_, vr);
+        }
+        for (int c0 = 0; c0 < L; c0 += KC) {
+          const Fp4Raw<D> k0 = kr, v0 = vr;
+          if (c0 + KC < L) {
+            chunk += fp4_chunk_bytes(D);
+            fp4_load_k<D>(chunk, lt_, kr);
+            fp4_load_v<D>(chunk, lt_, vr);
+          }
+          floatx16 S[1];
+          bf16x8 kf[D / 16], vf[D / 16];
+#pragma unroll
+          for (int s = 0; s < D / 16; ++s) kf[s] = fp4_k<D>(k0, s);
+          qk_regs<D>(kf, qf, S);
+#pragma unroll
+          for (int f = 0; f < D / 16; ++f) vf[f] = fp4_v<D>(v0, f);
+          if (c0 + KC <= L) {
+            pv_regs<0, D>(S, vf, acc, hf, nullptr);
+          } else {
+            const int lim[1] = {L - c0 - 1};
+            pv_regs<1, D>(S, vf, acc, hf, lim);
+          }
+        }
+      }
+      for (int c0 = 0; !FP4 && c0 < L; c0 += KC) {
         floatx16 S[1];
         bf16x8 kf[D / 16], vf[D / 16];
         const int krow = c0 + prow < L ? c0 + prow : L - 1;
@@ -800,7 +845,7 @@ __global__ __launch_bounds__(256) void k_queue_all(const int64_t *totals,
 }
 
 template <int WAVES, int NQB, bool SAFE, bool SCORE, int D,
-          int NCHK = big_chunks(D)>
+          int NCHK = big_chunks(D), bool FP4 = false>
 hipError_t launch_variant(const AttnParams &p, hipStream_t s, int max_grid) {
   int dev = 0, n_cu = 0, per_cu = 0;
   hipError_t e = hipGetDevice(&dev);
@@ -808,7 +853,7 @@ hipError_t launch_variant(const AttnParams &p, hipStream_t s, int max_grid) {
   e = hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, dev);
   if (e != hipSuccess) return e;
   e = hipOccupancyMaxActiveBlocksPerMultiprocessor(
-      &per_cu, k_prefix_attn<WAVES, NQB, SAFE, SCORE, D, NCHK>, WAVES * 64,
+      &per_cu, k_prefix_attn<WAVES, NQB, SAFE, SCORE, D, NCHK, FP4>, WAVES * 64,
       0);
   if (e != hipSuccess) return e;
   if (per_cu < 1) per_cu = 1;
@@ -817,61 +862,68 @@ hipError_t launch_variant(const AttnParams &p, hipStream_t s, int max_grid) {
   unsigned grid = (unsigned)(n_cu * per_cu);
   grid = (grid + 7) / 8 * 8;
   if (max_grid > 0 && grid > (unsigned)max_grid) grid = (unsigned)max_grid;
-  hipLaunchKernelGGL((k_prefix_attn<WAVES, NQB, SAFE, SCORE, D, NCHK>),
+  hipLaunchKernelGGL((k_prefix_attn<WAVES, NQB, SAFE, SCORE, D, NCHK, FP4>),
                      dim3(grid), dim3(WAVES * 64), 0, s, p);
   return hipGetLastError();
 }
 
 // One-wave-per-unit score kernel: a persistent grid of 4-wave blocks, as
 // many as fit (two per CU), a multiple of 8 so block b serves queue b % 8.
-template <int D>
+template <int D, bool FP4>
 hipError_t launch_score_rows(const AttnParams &p, hipStream_t s) {
   int dev = 0, n_cu = 0, per_cu = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
   e = hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, dev);
   if (e != hipSuccess) return e;
-  e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, k_score_rows<D>,
+  e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, k_score_rows<D, FP4>,
                                                    256, 0);
   if (e != hipSuccess) return e;
   if (per_cu < 1) per_cu = 1;
   const unsigned grid = (unsigned)((n_cu * per_cu + 7) / 8 * 8);
-  hipLaunchKernelGGL(k_score_rows<D>, dim3(grid), dim3(256), 0, s, p);
+  hipLaunchKernelGGL((k_score_rows<D, FP4>), dim3(grid), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
 // The fast pass in tile shape shape_v (1, 2, 3, 6; 7 the one-wave-per-unit
 // score kernel; 4 queues every unit for the exact pass instead), then the
 // exact pass over the queued units.
-template <int D>
+// On a 4-bit store the block-wide shape is 6.
+template <int D, bool FP4>
 hipError_t launch_passes(const AttnParams &p, int shape_v, bool score,
                          hipStream_t s) {
   hipError_t e;
+  if (FP4 && shape_v < 4) shape_v = 6;
+  constexpr int SMALL = small_chunks(D), BIG = big_chunks(D);
   switch (shape_v) {
-    case 8: e = launch_stream(D, p, s); break;
-    case 7: e = launch_score_rows<D>(p, s); break;
-    case 1: e = launch_variant<4, 2, false, false, D>(p, s, 0); break;
-    case 3: e = launch_variant<4, 1, false, false, D>(p, s, 0); break;
+    case 8: e = launch_stream(D, FP4, p, s); break;
+    case 7: e = launch_score_rows<D, FP4>(p, s); break;
     case 6:
-      e = score ? launch_variant<4, 1, false, true, D, small_chunks(D)>(p, s, 0)
-                : launch_variant<4, 1, false, false, D, small_chunks(D)>(p, s,
-                                                                         0);
+      e = score ? launch_variant<4, 1, false, true, D, SMALL, FP4>(p, s, 0)
+                : launch_variant<4, 1, false, false, D, SMALL, FP4>(p, s, 0);
       break;
     case 4:
       hipLaunchKernelGGL(k_queue_all, dim3(256), dim3(256), 0, s, p.totals,
                          p.items_cap, p.Hkv, p.counters, p.fix);
       e = hipGetLastError();
       break;
-    default:  // 2
-      e = score ? launch_variant<8, 1, false, true, D>(p, s, 0)
-                : launch_variant<8, 1, false, false, D>(p, s, 0);
+    default:
+      if constexpr (FP4)
+        e = hipErrorInvalidValue;  // (none of these)
+      else if (shape_v == 1)
+        e = launch_variant<4, 2, false, false, D>(p, s, 0);
+      else if (shape_v == 3)
+        e = launch_variant<4, 1, false, false, D>(p, s, 0);
+      else  // 2
+        e = score ? launch_variant<8, 1, false, true, D>(p, s, 0)
+                  : launch_variant<8, 1, false, false, D>(p, s, 0);
       break;
   }
   if (e != hipSuccess) return e;
   // Work units the fast pass flagged or left unscored (normally none) are
   // computed here; in exact mode that is every unit.
-  return score ? launch_variant<4, 1, true, true, D>(p, s, 0)
-               : launch_variant<4, 1, true, false, D>(p, s, 0);
+  return score ? launch_variant<4, 1, true, true, D, BIG, FP4>(p, s, 0)
+               : launch_variant<4, 1, true, false, D, BIG, FP4>(p, s, 0);
 }
 
 }  // namespace
@@ -954,8 +1006,12 @@ hipError_t launch_attention(const AttnCall &c, const Plan &pl,
     e = launch_khat(D, khat_params(c, pl), a->n_pairs, s);
     if (e != hipSuccess) return e;
   }
-  e = D == 128 ? launch_passes<128>(p, shape_v, score, s)
-               : launch_passes<64>(p, shape_v, score, s);
+  if (D == 128)
+    e = st.fp4 ? launch_passes<128, true>(p, shape_v, score, s)
+               : launch_passes<128, false>(p, shape_v, score, s);
+  else
+    e = st.fp4 ? launch_passes<64, true>(p, shape_v, score, s)
+               : launch_passes<64, false>(p, shape_v, score, s);
   if (e != hipSuccess) return e;
   if (a->timing_end) {
     e = hipEventRecord(static_cast<hipEvent_t>(a->timing_end), s);

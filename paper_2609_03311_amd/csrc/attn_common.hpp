@@ -7,6 +7,7 @@
 
 #include <cmath>
 
+#include "fp4.hpp"
 #include "internal.hpp"
 
 namespace dopr {
@@ -67,8 +68,8 @@ struct KhatParams {
 hipError_t launch_khat(int D, const KhatParams &kp, int32_t n_pairs,
                        hipStream_t s);
 KhatParams khat_params(const AttnCall &c, const Plan &pl);
-// stream.hip: the pass kernel (head size D).
-hipError_t launch_stream(int D, const AttnParams &p, hipStream_t s);
+// stream.hip: the pass kernel (head size D; fp4: on a 4-bit store).
+hipError_t launch_stream(int D, bool fp4, const AttnParams &p, hipStream_t s);
 
 namespace {
 
@@ -478,6 +479,49 @@ __device__ __forceinline__ void stage_prefix(const uint16_t *Kp,
     else
       *reinterpret_cast<uint4 *>(pv + b * 512 + lane * 8) =
           make_uint4(0, 0, 0, 0);
+  }
+}
+
+// The same from a 4-bit store's chunks (seg0 a multiple of 32): each wave takes
+// a part of a chunk's K or V codes, 16 bytes a lane, and writes the four
+// fragments they stand for where the products read them.  Slots past the
+// document's end are stored as zeros.
+template <int WAVES, int D, int NCHK>
+__device__ __forceinline__ void stage_prefix_fp4(const char *chunks, int seg0,
+                                                 int n, Smem<D, NCHK> &sm) {
+  constexpr int PARTS = D / 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lq = lane & 31, hf = lane >> 5, row = perm32(lq);
+  const char *from = chunks + (int64_t)(seg0 / KC) * fp4_chunk_bytes(D);
+  const int tasks = ((n + KC - 1) / KC) * 2 * PARTS;
+  for (int t = wave; t < tasks; t += WAVES) {
+    const int ck = t / (2 * PARTS), h = t % (2 * PARTS);
+    const int j = h % PARTS;
+    const char *c = from + (int64_t)ck * fp4_chunk_bytes(D);
+    if (h < PARTS) {
+      const fp4_u32x4 w = *reinterpret_cast<const fp4_u32x4 *>(
+          c + 1024 * j + 16 * lane);
+      const float scale = fp4_scale(
+          *reinterpret_cast<const uint8_t *>(c + 32 * D + lane * PARTS + j));
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<bf16x8 *>(
+            sm.pk[ck] + kc_off<D>(row, 2 * (4 * j + i) + hf)) =
+            fp4_fragment(w[i], scale);
+    } else {
+      const fp4_u32x4 w = *reinterpret_cast<const fp4_u32x4 *>(
+          c + 16 * D + 1024 * j + 16 * lane);
+      const char *x = c + 33 * D + lq * (D / 32) + 2 * j;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float scale =
+            fp4_scale(*reinterpret_cast<const uint8_t *>(x + (i >> 1)));
+        *reinterpret_cast<bf16x8 *>(
+            sm.pv[ck] + vc_off(32 * (2 * j + (i >> 1)) + row,
+                               2 * hf + (i & 1))) =
+            fp4_fragment(w[i], scale);
+      }
+    }
   }
 }
 

@@ -74,6 +74,10 @@ enum StatusSlot { kStatusFirstError = 0, kStatusWords = 64 };
 //   Vt [D][Lp]  at  blk + l*Hkv*D*(L+Lp) + Hkv*L*D + g*D*Lp
 // with Lp = L rounded up to 8 (V is stored transposed so the PV contraction
 // over keys reads 16-byte runs; the pad columns are zero).
+//
+// A 4-bit store (DOPR_STORE_FP4) holds a slice, layer l and kv head g, as
+// chunks of 32 slots in a row, at  blk + (l*Hkv + g) * 17*D*ceil(L/32), each
+// 34*D bytes: codes of K, codes of V, exponents of K, exponents of V (fp4.hpp).
 struct StoreView {
   const int32_t *doc_len;  // [n_docs], -1 = not resident
   const int64_t *doc_off;  // [n_docs], element offset of the doc block
@@ -81,22 +85,35 @@ struct StoreView {
   uint16_t *payload;
   int64_t n_docs;
   int32_t n_layers, n_kv_heads, head_dim;
+  int32_t fp4;             // DOPR_STORE_FP4
 };
 
+// Elements (of 2 bytes) of a document's slices of one layer; of one slice of
+// a 4-bit store.
+__host__ __device__ inline int64_t fp4_slice_elems(int32_t L, int32_t D) {
+  return ((int64_t)L + 31) / 32 * 17 * D;
+}
 __host__ __device__ inline int64_t layer_block_elems(int32_t L, int32_t hkv,
-                                                     int32_t D) {
-  return (int64_t)hkv * D * ((int64_t)L + pad8(L));
+                                                     int32_t D, bool fp4) {
+  return fp4 ? hkv * fp4_slice_elems(L, D)
+             : (int64_t)hkv * D * ((int64_t)L + pad8(L));
+}
+__host__ __device__ inline int64_t fp4_offset(int64_t blk, int32_t L,
+                                              int32_t hkv, int32_t layer,
+                                              int32_t g, int32_t D) {
+  return blk + ((int64_t)layer * hkv + g) * fp4_slice_elems(L, D);
 }
 __host__ __device__ inline int64_t k_offset(int64_t blk, int32_t L, int32_t hkv,
                                             int32_t layer, int32_t g,
                                             int32_t D) {
-  return blk + layer * layer_block_elems(L, hkv, D) + (int64_t)g * L * D;
+  return blk + layer * layer_block_elems(L, hkv, D, false) +
+         (int64_t)g * L * D;
 }
 __host__ __device__ inline int64_t vt_offset(int64_t blk, int32_t L,
                                              int32_t hkv, int32_t layer,
                                              int32_t g, int32_t D) {
-  return blk + layer * layer_block_elems(L, hkv, D) + (int64_t)hkv * L * D +
-         (int64_t)g * D * pad8(L);
+  return blk + layer * layer_block_elems(L, hkv, D, false) +
+         (int64_t)hkv * L * D + (int64_t)g * D * pad8(L);
 }
 
 }  // namespace dopr
@@ -113,9 +130,10 @@ struct dopr_store {
   uint16_t *d_payload;
   int32_t max_len;  // largest L over resident documents
   int device;
+  int32_t fp4;      // DOPR_STORE_FP4
   dopr::StoreView view() const {
     return {d_len, d_off, d_kmax, d_payload, n_docs, n_layers, n_kv_heads,
-            head_dim};
+            head_dim, fp4};
   }
 };
 
@@ -178,7 +196,8 @@ struct PassUnit {
   int32_t rows;      // rows (at most 128) | first row's head in the group << 8
   int32_t s;         // first sorted pair; sign bit: over the logit bound
   int32_t L;         // prefix slots
-  int32_t k[2];      // the document's K slice (this layer and head)
+  int32_t k[2];      // the document's K slice (this layer and head), or, in
+                     // a 4-bit store, its chunks
   int32_t vt[2];     // its V^T slice
   int32_t own_k[2];  // k^ of the first pair's first token (this head)
   int32_t own_v[2];  // its v
@@ -409,8 +428,13 @@ __device__ inline void write_unit(const Plan &pl, const StoreView &sv,
   r.u.rows = (over ? 1 : it.z - it.y) | (it.y - r.u.u0 * ua.n_rep) << 8;
   r.u.s = over ? it.w | INT32_MIN : it.w;
   r.u.L = over ? 0 : L;
-  put(r.u.k, sv.payload + k_offset(blk, L, sv.n_kv_heads, ua.layer, g, D));
-  put(r.u.vt, sv.payload + vt_offset(blk, L, sv.n_kv_heads, ua.layer, g, D));
+  if (sv.fp4) {
+    put(r.u.k, sv.payload + fp4_offset(blk, L, sv.n_kv_heads, ua.layer, g, D));
+    put(r.u.vt, sv.payload);  // (not read)
+  } else {
+    put(r.u.k, sv.payload + k_offset(blk, L, sv.n_kv_heads, ua.layer, g, D));
+    put(r.u.vt, sv.payload + vt_offset(blk, L, sv.n_kv_heads, ua.layer, g, D));
+  }
   put(r.u.own_k, pl.kh + (g * ua.ntok + sp.x) * D);
   put(r.u.own_v, ua.v + ((int64_t)sp.x * sv.n_kv_heads + g) * D);
   r.u.tok0 = sp.x;
@@ -473,6 +497,13 @@ hipError_t launch_gather(const dopr_store &st, int32_t layer, int32_t n,
                          uint16_t *k, uint16_t *v, hipStream_t s);
 hipError_t launch_store_copy(const dopr_store &dst, const dopr_store &src,
                              hipStream_t s);
+// states.hip: states into a store of either format, keys normed and rotated on
+// the way (rotary_dim 0: as they are), and out of a 4-bit one.
+hipError_t launch_put_states(const dopr_store &st,
+                             const dopr_put_rotary_args_t &a, hipStream_t s);
+hipError_t launch_gather_fp4(const dopr_store &st, int32_t layer, int32_t n,
+                             const int32_t *doc_ids, const int64_t *out_cu,
+                             uint16_t *k, uint16_t *v, hipStream_t s);
 
 struct AttnCall {
   const dopr_store *st;

@@ -151,7 +151,7 @@ __global__ __launch_bounds__(kThreads) void k_store_copy(StoreView dst,
     }
     const int64_t n16 =
         (int64_t)dst.n_layers *
-        layer_block_elems(L, dst.n_kv_heads, dst.head_dim) / 8;
+        layer_block_elems(L, dst.n_kv_heads, dst.head_dim, dst.fp4) / 8;
     const uint4 *s = reinterpret_cast<const uint4 *>(src.payload +
                                                      src.doc_off[d]);
     uint4 *t = reinterpret_cast<uint4 *>(dst.payload + dst.doc_off[d]);

@@ -222,6 +222,45 @@ __device__ __forceinline__ void attend_slot(const uint16_t *slot, bool two,
   }
 }
 
+// n 32-key chunks of a 4-bit store in LDS (KC keys of them all but the last
+// full): a fragment is made of four bytes of codes and its block's scale where
+// the products take it, so that LDS hands out a quarter of the bytes.  The
+// chunk's order, operands and sums are those of a bf16 store that holds the
+// same values, bit for bit.
+template <int D>
+__device__ __forceinline__ void attend_fp4(const uint16_t *slot, int n,
+                                           int lane, const bf16x8 (*qf)[D / 16],
+                                           Acc<D> *acc, int hf, int lim) {
+  const char *chunk = reinterpret_cast<const char *>(slot);
+  Fp4Raw<D> kr, vr;
+  fp4_load_k<D>(chunk, lane, kr);
+  for (int c = 0; c < n; ++c) {
+    fp4_load_v<D>(chunk, lane, vr);
+    floatx16 S[1];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) S[0][i] = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+      S[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp4_k<D>(kr, s), qf[0][s],
+                                                     S[0], 0, 0, 0);
+    chunk += fp4_chunk_bytes(D);
+    // (the next chunk's codes arrive under this one's softmax)
+    if (c + 1 < n) fp4_load_k<D>(chunk, lane, kr);
+    if (lim < KC - 1) {  // (wave-uniform: every row sees the whole prefix)
+      const int li = lim - 16 * hf;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) S[0][i] = i <= li ? S[0][i] : -INFINITY;
+    }
+    lim -= KC;
+    bf16x8 pb[1][2];
+    softmax_part<0, 1, 0, D>(S, acc, hf, 0.f, nullptr, pb);
+#pragma unroll
+    for (int f = 0; f < D / 16; ++f)
+      acc[0].o[f >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          fp4_v<D>(vr, f), pb[0][f & 1], acc[0].o[f >> 1], 0, 0, 0);
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Pass kernel (full layer).  A work unit is a pass of at most 128 stacked
 // rows of one document for one kv head: one 32-row tile for each of a
@@ -333,7 +372,8 @@ struct Feed {
 // with T tokens, or (tok0 < 0) of a prefix of T slots.
 struct Batch {
   int tok0, T, k0;
-  int two, last;  // two chunks; the unit's last batch
+  int two, last;  // two chunks (a 4-bit prefix: chunks but one); the unit's
+                  // last batch
 };
 
 // A lane's place in the loads of a chunk, for the first of its wave's KB 1 KB
@@ -377,7 +417,7 @@ __device__ __forceinline__ void feed_own(Feed &f, const FeedLane &l, int tok0,
 }
 
 // First segment of a unit.
-template <int D>
+template <int D, bool FP4>
 __device__ __forceinline__ void feed_unit(Feed &f, const FeedLane &l,
                                           const PassUnit &u, int n_rep,
                                           int stride) {
@@ -398,22 +438,64 @@ __device__ __forceinline__ void feed_unit(Feed &f, const FeedLane &l,
     f.jmax = u.L - 1;
     f.tok0 = -1;
     f.T = u.L;
-    f.vo = 2 * (l.d * Lp + l.key);
-    f.vo2 = 2 * ((l.d + 16) * Lp + (l.key ^ 16));
+    if constexpr (!FP4) {
+      f.vo = 2 * (l.d * Lp + l.key);
+      f.vo2 = 2 * ((l.d + 16) * Lp + (l.key ^ 16));
+    }
   } else {
     feed_own<D>(f, l, f.otok, f.oT, f.ojmax, stride);
+  }
+}
+
+// Chunks of a 4-bit store that fit in a buffer of two bf16 chunks.
+template <int D>
+constexpr int kFp4Batch = 2 * 2 * KC * D * 2 / fp4_chunk_bytes(D);
+
+// The segment that follows the one whose last batch `b` is.
+template <int D>
+__device__ __forceinline__ void feed_next(Feed &f, const FeedLane &l, Batch &b,
+                                          int stride) {
+  if (f.tok0 < 0) {
+    feed_own<D>(f, l, f.otok, f.oT, f.ojmax, stride);
+  } else if (f.next.z < f.row1) {
+    // the next pair starts inside the unit: all of its keys are seen
+    ++f.s;
+    feed_own<D>(f, l, f.next.x, f.next.y, f.next.y - 1, stride);
+    f.next = cld(args_here()->spair, f.s + 1);
+  } else {
+    b.last = 1;
   }
 }
 
 // Issue the direct loads of the next batch into the buffer at LDS address
 // `lds` (wave w takes the 1 KB blocks w * KB .. of each chunk's K and V) and
 // go on to the next segment at a segment's end.
-template <int D>
+template <int D, bool FP4>
 __device__ __forceinline__ Batch feed_batch(Feed &f, const FeedLane &l,
                                             uint32_t lds, int stride) {
   constexpr int KB = KC * D * 2 / 1024 / 4;  // 1 KB blocks per wave
   constexpr uint32_t VOFF = KC * D * 2;      // V's place in a chunk
   Batch b{f.tok0, f.T, f.k0, f.jmax - f.k0 >= KC, 0};
+  if (FP4 && f.tok0 < 0) {
+    // up to seven chunks, as they lie: 1 KB blocks, every fourth of them this
+    // wave's, the last one's lanes past the end on its last 16 bytes
+    const int left = (unsigned)(f.T - f.k0 + KC - 1) / KC;
+    const int n = left <= kFp4Batch<D> ? left
+                  : left >= 2 * kFp4Batch<D> ? kFp4Batch<D> : (left + 1) / 2;
+    const uint32_t bytes = n * fp4_chunk_bytes(D);
+    const int wave = rfl(threadIdx.x >> 6);
+    uint32_t at = lds + wave * (1 - KB) * 1024;
+    const uint32_t mine = 16 * (threadIdx.x & 63);
+    for (uint32_t o = wave * 1024; o < bytes; o += 4096, at += 4096) {
+      const uint32_t x = o + mine;
+      dma_base(at, f.ka, x < bytes - 16 ? x : bytes - 16);
+    }
+    b.two = n - 1;
+    f.ka += n * (fp4_chunk_bytes(D) / 2);
+    f.k0 += n * KC;
+    if (f.k0 > f.jmax) feed_next<D>(f, l, b, stride);
+    return b;
+  }
   const int n = f.T - f.k0;
   if (n >= 2 * KC && b.two) {
     dma_chunk<D, VOFF>(lds, f.ka, l.kofs, l.kofs2, f.va, f.vo, f.vo2);
@@ -449,22 +531,12 @@ __device__ __forceinline__ Batch feed_batch(Feed &f, const FeedLane &l,
   f.ka += 2 * KC * D;
   f.va += 2 * f.vstep;
   f.k0 += 2 * KC;
-  if (f.k0 > f.jmax) {
-    if (f.tok0 < 0) {
-      feed_own<D>(f, l, f.otok, f.oT, f.ojmax, stride);
-    } else if (f.next.z < f.row1) {
-      // the next pair starts inside the unit: all of its keys are seen
-      ++f.s;
-      feed_own<D>(f, l, f.next.x, f.next.y, f.next.y - 1, stride);
-      f.next = cld(args_here()->spair, f.s + 1);
-    } else {
-      b.last = 1;
-    }
-  }
+  if (f.k0 > f.jmax) feed_next<D>(f, l, b, stride);
   return b;
 }
 
-template <int D, int GROUP>
+// FP4: on a 4-bit store.
+template <int D, int GROUP, bool FP4>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(
     D == 64 ? 3 : 2, D == 64 ? 3 : 2))) void k_pass_attn(AttnParams P0) {
   constexpr int GW = D / 16 / GROUP;
@@ -529,9 +601,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(
     asked = 1;
   };
   Feed f{};
-  feed_unit<D>(f, fl, nx, n_rep, stride);
+  feed_unit<D, FP4>(f, fl, nx, n_rep, stride);
   // the batch on its way, into buffer `buf`
-  Batch nb = feed_batch<D>(f, fl, ring, stride);
+  Batch nb = feed_batch<D, FP4>(f, fl, ring, stride);
   int buf = 0;
   ask_rows();
 
@@ -581,15 +653,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(
       const uint16_t *at = sm.batch[buf][0];
       buf ^= 1;
       // the next batch: this unit's, or the first of the next one
-      if (b.last && nw >= 0) feed_unit<D>(f, fl, nx, n_rep, stride);
+      if (b.last && nw >= 0) feed_unit<D, FP4>(f, fl, nx, n_rep, stride);
       if (!b.last || nw >= 0)
-        nb = feed_batch<D>(f, fl, ring + buf * BUF, stride);
+        nb = feed_batch<D, FP4>(f, fl, ring + buf * BUF, stride);
       PT_MARK(kPtFeed);
       const int own = b.tok0 >= 0;
       const int jr = tokq - b.tok0;
       int lim = b.T - 1 - b.k0;
       if (own) lim = (unsigned)jr < (unsigned)b.T ? jr - b.k0 : -1;
-      if (__any(valid && lim >= 0))
+      if (FP4 && !own) {
+        if (__any(valid))
+          attend_fp4<D>(at, b.two + 1, lane, qf, acc, hf, lim);
+      } else if (__any(valid && lim >= 0))
         attend_slot<D>(at, b.two && __any(valid && lim >= KC), own, vaddr, ex,
                        fo, qf, acc, hf, lim);
       PT_MARK(own ? kPtOwn : kPtPrefix);
@@ -665,28 +740,29 @@ extern "C" int dopr_pass_phase_read(unsigned long long *out, int reset) {
 #endif
 
 namespace {
-template <int D>
+template <int D, bool FP4>
 hipError_t launch_pass(const AttnParams &p, unsigned grid, hipStream_t s) {
   // (the lanes that share a token: see q_fragments_any)
-  if ((p.n_rep & 3) == 0)
-    hipLaunchKernelGGL((k_pass_attn<D, 4>), dim3(grid), dim3(256), 0, s, p);
-  else if ((p.n_rep & 1) == 0)
-    hipLaunchKernelGGL((k_pass_attn<D, 2>), dim3(grid), dim3(256), 0, s, p);
-  else
-    hipLaunchKernelGGL((k_pass_attn<D, 1>), dim3(grid), dim3(256), 0, s, p);
+  const auto kernel = (p.n_rep & 3) == 0   ? k_pass_attn<D, 4, FP4>
+                      : (p.n_rep & 1) == 0 ? k_pass_attn<D, 2, FP4>
+                                           : k_pass_attn<D, 1, FP4>;
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 }  // namespace
 
-hipError_t launch_stream(int D, const AttnParams &p, hipStream_t s) {
+hipError_t launch_stream(int D, bool fp4, const AttnParams &p, hipStream_t s) {
   int dev = 0, n_cu = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
   e = hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, dev);
   if (e != hipSuccess) return e;
   const unsigned grid = (unsigned)((n_cu + 7) / 8 * 8);
-  return D == 128 ? launch_pass<128>(p, 2 * grid, s)
-                  : launch_pass<64>(p, 3 * grid, s);
+  if (D == 128)
+    return fp4 ? launch_pass<128, true>(p, 2 * grid, s)
+               : launch_pass<128, false>(p, 2 * grid, s);
+  return fp4 ? launch_pass<64, true>(p, 3 * grid, s)
+             : launch_pass<64, false>(p, 3 * grid, s);
 }
 
 }  // namespace dopr

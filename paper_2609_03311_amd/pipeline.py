@@ -8,7 +8,8 @@ from __future__ import annotations
 
 import numpy as np
 
-from . import (dopr_decoder_layer, dopr_decoder_layer_workspace,
+from . import (DOPR_STORE_BF16, dopr_decoder_layer,
+               dopr_decoder_layer_workspace,
                dopr_norm_residual, dopr_prefix_attn, dopr_prefix_attn_score,
                dopr_prefix_attn_score_workspace, dopr_prefix_attn_workspace,
                dopr_quant_matmul, dopr_quant_matmul_workspace,
@@ -20,14 +21,16 @@ HEAD_DIM = 128
 
 
 def make_store(doc_len, n_kv_heads, k_src, v_src, *, n_layers=1, layer=0,
-               device="cuda", stream=None):
-    """Create a store for `doc_len` and fill `layer` from canonical prefix
-    states k_src/v_src [slots, Hkv, D] (bf16, device; D = 128 or 64) holding
-    the resident documents' slots in ascending doc-id order."""
+               device="cuda", stream=None, format=DOPR_STORE_BF16):
+    """Create a store (of bf16 states, or DOPR_STORE_FP4) for `doc_len` and
+    fill `layer` from canonical prefix states k_src/v_src [slots, Hkv, D]
+    (bf16, device; D = 128 or 64) holding the resident documents' slots in
+    ascending doc-id order."""
     import torch
     doc_len = np.ascontiguousarray(doc_len, np.int32)
     store = dopr_store_create(n_layers, n_kv_heads, int(k_src.shape[-1]),
-                              doc_len, device=device, stream=stream)
+                              doc_len, device=device, stream=stream,
+                              format=format)
     res = np.nonzero(doc_len >= 0)[0].astype(np.int32)
     if res.size:
         cu = np.zeros(res.size + 1, np.int64)

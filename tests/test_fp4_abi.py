@@ -1,0 +1,143 @@
+"""The 4-bit prefix store on the CPU: sizes, struct layout, refusals and
+launches."""
+import ctypes
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+from store_calls import store_calls
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+INVALID, UNSUPPORTED, WORKSPACE = -1, -2, -4
+
+
+def _D():
+    import paper_2609_03311_amd as D
+    D.lib()
+    return D
+
+
+def test_store_bytes_closed_form():
+    D = _D()
+    rng = np.random.default_rng(0)
+    for layers, hkv, d in [(1, 8, 128), (36, 8, 128), (3, 2, 64)]:
+        lens = rng.integers(-1, 300, 500).astype(np.int32)
+        pool, payload = D.dopr_store_bytes(layers, hkv, d, lens,
+                                           D.DOPR_STORE_FP4)
+        n = lens[lens >= 0].astype(np.int64)
+        chunks = -(-n // 32)
+        # half a byte a value of K and V, a byte for 32 dims of a key and for
+        # a chunk's slots of a value's dim
+        assert payload == layers * hkv * d * (n + n // 32 + chunks).sum()
+        index = (12 + 4 * layers * hkv) * len(lens)
+        held = 34 * d * chunks.sum() * layers * hkv
+        assert held + index <= pool <= held + index + 5 * 256
+        assert (pool, payload) == D.dopr_store_bytes_as(layers, hkv, d, lens,
+                                                        D.DOPR_STORE_FP4)
+        assert D.dopr_store_bytes_as(layers, hkv, d, lens,
+                                     D.DOPR_STORE_BF16) == \
+            D.dopr_store_bytes(layers, hkv, d, lens)
+
+
+def test_store_refusals():
+    D = _D()
+    for fmt in (-1, 2):
+        with pytest.raises(D.DoprError) as e:
+            D.dopr_store_bytes(1, 8, 128, [4], fmt)
+        assert e.value.status == INVALID and "format" in str(e.value)
+    with pytest.raises(D.DoprError) as e:
+        D.dopr_store_bytes(1, 8, 96, [4], D.DOPR_STORE_FP4)
+    assert e.value.status == UNSUPPORTED
+    L = D.lib()
+    desc, _keep = D._desc(1, 8, 128, [4])
+    h = ctypes.c_void_p(0)
+    pool, _ = D.dopr_store_bytes(1, 8, 128, [4], D.DOPR_STORE_FP4)
+    for at, size, code in ((None, pool, INVALID), (128, pool, INVALID),
+                           (256, pool - 1, WORKSPACE)):
+        assert L.dopr_store_create_as(ctypes.byref(desc), 1, at, size, None,
+                                      ctypes.byref(h)) == code
+    assert L.dopr_store_create_as(ctypes.byref(desc), 7, 256, pool, None,
+                                  ctypes.byref(h)) == INVALID
+    assert L.dopr_store_put_rotary(None, None, None) == INVALID
+
+
+def test_struct_layout_matches_header(tmp_path):
+    D = _D()
+    py, cname = D._PutRotaryArgs, "dopr_put_rotary_args_t"
+    lines = ['#include <stdio.h>', '#include <stddef.h>', '#include "dopr.h"',
+             "int main(void) {", f'printf("%zu\\n", sizeof({cname}));']
+    lines += [f'printf("%zu\\n", offsetof({cname}, {f}));'
+              for f, _ in py._fields_]
+    probe = tmp_path / "probe.c"
+    probe.write_text("\n".join(lines + ["return 0; }"]))
+    exe = tmp_path / "probe"
+    subprocess.run(["gcc", "-std=c11", "-I", os.path.join(ROOT, "include"),
+                    str(probe), "-o", str(exe)], check=True)
+    out = subprocess.run([str(exe)], capture_output=True, text=True,
+                         check=True).stdout.split()
+    assert [int(x) for x in out] == [ctypes.sizeof(py)] + [
+        getattr(py, f).offset for f, _ in py._fields_]
+
+
+PUT = dict(layer=0, dtype=0, n=2, rows=100, doc_ids=256, src_cu_slots=256,
+           k=256, k_row_stride=256, k_head_stride=128, v=256,
+           v_row_stride=256, v_head_stride=128, inv_freq=256, rotary_dim=128,
+           attention_factor=1.0, rms_eps=1e-6)
+
+
+def _put(**more):
+    return ["dopr_store_put_rotary", "_PutRotaryArgs", PUT | more]
+
+
+def test_put_rotary_refusals():
+    bad = [(dict(layer=2), "layer"), (dict(layer=-1), "layer"),
+           (dict(dtype=3), "dtype"), (dict(n=-1), "bad n"),
+           (dict(n=1 << 31), "bad n"), (dict(rows=-1), "rows"),
+           (dict(rotary_dim=0), "rotary_dim"),
+           (dict(rotary_dim=7), "rotary_dim"),
+           (dict(rotary_dim=130), "rotary_dim"),
+           (dict(interleaved=2), "interleaved"),
+           (dict(attention_factor=float("inf")), "attention_factor"),
+           (dict(rms_eps=-1.0), "rms_eps"),
+           (dict(rms_eps=float("nan")), "rms_eps"),
+           (dict(k_row_stride=-1), "strides"),
+           (dict(v_head_stride=-1), "strides"), (dict(k=None), "NULL"),
+           (dict(v=None), "NULL"), (dict(doc_ids=None), "NULL"),
+           (dict(src_cu_slots=None), "NULL"), (dict(inv_freq=None), "NULL"),
+           (dict(k=257), "aligned"), (dict(dtype=2, v=258), "aligned"),
+           (dict(k_norm_w=255), "aligned"), (dict(positions=258), "aligned"),
+           (dict(inv_freq=258), "aligned"),
+           (dict(src_cu_slots=260), "aligned")]
+    for fmt in (0, 1):
+        got = store_calls((2, 2, 128, [5, 6], fmt),
+                          [_put(**b) for b, _ in bad])
+        for (b, text), g in zip(bad, got):
+            assert g["status"] == INVALID and not g["launches"], b
+            assert text in g["error"], (b, g)
+
+
+def test_put_launches():
+    got = store_calls((1, 2, 64, [40, 300], 1), [
+        _put(n=0, rotary_dim=64), _put(rotary_dim=64),
+        _put(n=(1 << 23) + 5, rotary_dim=64),
+        ["dopr_store_put", None, [0, 1, 256, 256, 256, 256]],
+        ["dopr_gather_prefix", None, [0, 1, 256, 256, 256, 256]],
+        ["dopr_gather_prefix", None, [0, (1 << 24) + 1, 256, 256, 256, 256]],
+    ])
+    assert all(g["status"] == 0 for g in got)
+    names = [[x["kernel"].split("<")[0] for x in g["launches"]] for g in got]
+    assert names[0] == []
+    # ten chunks of the longest document in blocks of their own, their key
+    # bounds cleared in front
+    assert names[1] == ["k_put_clear", "k_put_states"]
+    assert (got[1]["launches"][1]["gx"], got[1]["launches"][1]["gy"]) == \
+        (2, 10)
+    # (the last slice's five documents' chunks again)
+    assert names[2] == ["k_put_states"] * 2 + ["k_put_clear", "k_put_states"]
+    assert names[3] == ["k_put_clear", "k_put_states"]
+    assert names[4] == ["k_gather_fp4"] and names[5] == ["k_gather_fp4"] * 3
+    for g in got:
+        for x in g["launches"]:
+            assert x["gx"] * x["bx"] < 1 << 32 and x["gy"] <= 65535

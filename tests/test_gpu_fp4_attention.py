@@ -1,0 +1,203 @@
+"""Prefix attention, last-layer scoring and the decoder layer over a 4-bit
+store: bit for bit what a bf16 store of the held values gives."""
+import numpy as np
+import pytest
+import torch
+
+import fp4_refs
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+
+
+def _D():
+    import paper_2609_03311_amd as D
+    return D
+
+
+def _cu(lens):
+    out = np.zeros(len(lens) + 1, np.int64)
+    np.cumsum(lens, out=out[1:])
+    return out
+
+
+class Batch:
+    """A 4-bit store and a bf16 store that hold the same values, and a batch
+    of pairs."""
+
+    def __init__(self, lens, docs, tokens, hq, hkv, d, *, norm=True, seed=0,
+                 key_scale=1.0, gain=1.0):
+        D = _D()
+        gen = torch.Generator().manual_seed(seed)
+
+        def randn(*shape):
+            return torch.randn(shape, generator=gen)
+
+        res = [i for i, n in enumerate(lens) if n >= 0]
+        cu = _cu([lens[i] for i in res])
+        rows = int(cu[-1])
+        k = (randn(rows, hkv, d) * key_scale).to(torch.bfloat16)
+        v = randn(rows, hkv, d).to(torch.bfloat16)
+        ids = torch.tensor(res, dtype=torch.int32, device=DEV)
+        self.stores = []
+        for fmt, (a, b) in ((D.DOPR_STORE_FP4, (k, v)),
+                            (D.DOPR_STORE_BF16, fp4_refs.held(k, v, cu))):
+            st = D.dopr_store_create(1, hkv, d, np.asarray(lens, np.int32),
+                                     format=fmt)
+            if rows:
+                D.dopr_store_put(st, 0, ids, torch.from_numpy(cu).to(DEV),
+                                 a.to(DEV), b.to(DEV))
+            self.stores.append(st)
+        self.n = len(tokens)
+        tcu = _cu(tokens)
+        self.total, self.most = int(tcu[-1]), max(tokens)
+        self.doc_ids = torch.tensor(docs, dtype=torch.int32, device=DEV)
+        self.tcu = torch.from_numpy(tcu).to(DEV, torch.int32)
+        self.q = randn(self.total, hq, d).to(DEV, torch.bfloat16)
+        self.k = randn(self.total, hkv, d).to(DEV, torch.bfloat16)
+        self.v = randn(self.total, hkv, d).to(DEV, torch.bfloat16)
+        self.qw = self.kw = None
+        if norm:
+            self.qw, self.kw = ((gain * (1 + 0.1 * randn(d))).to(
+                DEV, torch.bfloat16) for _ in range(2))
+        self.freq = (1e6 ** (-torch.arange(0, d, 2) / d)).to(DEV)
+        self.head = [randn(hq * d).to(DEV, torch.bfloat16)
+                     for _ in range(1)]
+        self.w_head = (randn(2, hq * d) * (hq * d) ** -0.5).to(
+            DEV, torch.bfloat16)
+        self.hq, self.d = hq, d
+
+    def _args(self, out, lse):
+        return dict(max_tokens=self.most, lse=lse, total_tokens=self.total,
+                    rope_inv_freq=self.freq)
+
+    def attention(self, st, variant=0, noalloc=False):
+        D = _D()
+        out = torch.full((self.total, self.hq, self.d), 3.0,
+                         dtype=torch.bfloat16, device=DEV)
+        lse = torch.full((self.total, self.hq), 3.0, device=DEV)
+        kw = dict(self._args(out, lse), kernel_variant=variant)
+        if noalloc:
+            D.dopr_prefix_attn_noalloc(st, 0, self.doc_ids, self.tcu, self.q,
+                                       self.k, self.v, self.qw, self.kw, out,
+                                       **kw)
+        else:
+            need = D.dopr_prefix_attn_workspace(
+                st, n_pairs=self.n, n_q_heads=self.hq, max_tokens=self.most,
+                total_tokens=self.total, kernel_variant=variant)
+            ws = torch.empty(max(need, 256), dtype=torch.uint8, device=DEV)
+            D.dopr_prefix_attn(st, 0, self.doc_ids, self.tcu, self.q, self.k,
+                               self.v, self.qw, self.kw, out, ws, **kw)
+        return out, lse
+
+    def scored(self, st, variant=0):
+        D = _D()
+        out = torch.full((self.n, self.hq, self.d), 3.0,
+                         dtype=torch.bfloat16, device=DEV)
+        lse = torch.full((self.n, self.hq), 3.0, device=DEV)
+        score = torch.full((self.n,), 3.0, device=DEV)
+        need = D.dopr_prefix_attn_score_workspace(
+            st, n_pairs=self.n, n_q_heads=self.hq, max_tokens=self.most,
+            total_tokens=self.total, kernel_variant=variant)
+        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=DEV)
+        D.dopr_prefix_attn_score(st, 0, self.doc_ids, self.tcu, self.q,
+                                 self.k, self.v, self.qw, self.kw, out, ws,
+                                 self.head[0], self.w_head, score,
+                                 kernel_variant=variant,
+                                 **self._args(out, lse))
+        return out, lse, score
+
+
+def _same(a, b):
+    for x, y in zip(a, b):
+        x, y = x.cpu().contiguous(), y.cpu().contiguous()
+        kind = torch.int16 if x.dtype == torch.bfloat16 else torch.int32
+        assert torch.equal(x.view(kind), y.view(kind))
+
+
+SHAPES = [
+    # lens, docs, tokens, q heads, kv heads
+    ([5], [0], [2], 4, 4),
+    ([0, 33], [0, 1, 1], [3, 40, 70], 8, 2),
+    ([256], [0], [129], 32, 8),
+    ([1, 31, 32, 224, 225, 255, 257, 448, 449, 700], list(range(10)),
+     [7, 33, 2, 5, 64, 3, 20, 2, 9, 40], 6, 2),
+    ([90, -1, 300, 12], [0, 2, 1, 3, 2, 9, 0, 2, 2, 2],
+     [17, 31, 5, 2, 66, 4, 33, 2, 100, 9], 15, 3),
+    ([300, 4100, 40], [1, 0, 1, 2], [5, 33, 2, 64], 8, 1),
+]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_attention_is_the_bf16_stores(d, norm, shape):
+    b = Batch(*SHAPES[shape], d, norm=norm, seed=shape)
+    want = b.attention(b.stores[1], 8)
+    for variant in (0, 8, 6, 2, 1, 3):
+        _same(b.attention(b.stores[0], variant), want)
+    _same(b.attention(b.stores[0], noalloc=True), want)
+    for variant in (4, 5):
+        _same(b.attention(b.stores[0], variant),
+              b.attention(b.stores[1], variant))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_scores_are_the_bf16_stores(d, norm, shape):
+    b = Batch(*SHAPES[shape], d, norm=norm, seed=shape)
+    want = b.scored(b.stores[1])
+    for variant in (0, 6, 5):
+        _same(b.scored(b.stores[0], variant), b.scored(b.stores[1], variant))
+    _same(b.scored(b.stores[0]), want)
+
+
+@pytest.mark.parametrize("scale,gain", [(30.0, 1.0), (1.0, 6.0)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_units_over_the_logit_bound(d, scale, gain):
+    """Keys, or gains, that leave the range of the reference-free softmax: the
+    exact pass reads the 4-bit chunks."""
+    b = Batch([300, 40, 64], [0, 1, 2, 0], [40, 3, 9, 66], 8, 2, d, seed=3,
+              key_scale=scale, gain=gain)
+    for variant in (0, 6):
+        _same(b.attention(b.stores[0], variant),
+              b.attention(b.stores[1], variant))
+    _same(b.scored(b.stores[0]), b.scored(b.stores[1]))
+
+
+def test_more_pairs_than_one_block_plans():
+    rng = np.random.default_rng(5)
+    docs = rng.integers(0, 200, 9000).tolist()
+    lens = rng.integers(0, 80, 200).tolist()
+    tokens = rng.integers(2, 5, 9000).tolist()
+    b = Batch(lens, docs, tokens, 4, 2, 64, seed=5)
+    _same(b.attention(b.stores[0]), b.attention(b.stores[1]))
+    _same(b.scored(b.stores[0]), b.scored(b.stores[1]))
+
+
+def test_decoder_layer():
+    D = _D()
+    lens, docs, tokens = [40, 100], [1, 0, 1], [5, 33, 17]
+    b = Batch(lens, docs, tokens, 4, 2, 128, seed=7)
+    W, I = 256, 512
+    gen = torch.Generator().manual_seed(8)
+    shapes = {"attn_norm_w": (W,), "w_q": (512, W), "w_k": (256, W),
+              "w_v": (256, W), "w_o": (W, 512), "mlp_norm_w": (W,),
+              "w_gate": (I, W), "w_up": (I, W), "w_down": (W, I)}
+    weights = {n: (torch.randn(s, generator=gen) * s[-1] ** -0.5).to(
+        DEV, torch.bfloat16) for n, s in shapes.items()}
+    x = torch.randn((b.total, W), generator=gen).to(DEV, torch.bfloat16)
+    ys = []
+    for st in b.stores:
+        need = D.dopr_decoder_layer_workspace(
+            st, weights, n_pairs=b.n, n_q_heads=4, max_tokens=b.most,
+            total_tokens=b.total, hidden=W, intermediate=I)
+        ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+        y = torch.empty_like(x)
+        D.dopr_decoder_layer(st, 0, b.doc_ids, b.tcu, x, y, weights, b.qw,
+                             b.kw, ws, n_q_heads=4, max_tokens=b.most,
+                             hidden=W, intermediate=I)
+        ys.append(y)
+    _same([ys[0]], [ys[1]])
