@@ -231,6 +231,21 @@ dopr_status_t check_attn(const dopr_store *st, const dopr_attn_args_t *a,
   return DOPR_OK;
 }
 
+// Whether a call is one of pairs of a single token that token.hip serves.
+bool is_token_call(const dopr_store *st, const dopr_attn_args_t *a) {
+  return st->fp4 && a->kernel_variant == 0 && a->max_tokens == 1 &&
+         a->total_tokens == a->n_pairs;
+}
+
+// Workspace bytes of a full call: its plan (also where none is made, as grouping
+// takes the same buffer), or what takes the plan's place.
+size_t attn_bytes(const dopr_store *st, const dopr_attn_args_t *a,
+                  const PlanShape &shape) {
+  const size_t plan = plan_bytes(shape);
+  if (!is_token_call(st, a) || a->n_pairs == 0) return plan;
+  return std::max(plan, token_bytes(*st, a->n_pairs, shape.n_rep));
+}
+
 dopr_status_t check_device(const dopr_store *st) {
   int dev = -1;
   hipError_t e = hipGetDevice(&dev);
@@ -459,7 +474,7 @@ dopr_status_t dopr_prefix_attn_workspace(dopr_store_t st,
   int32_t n_rep = 0;
   dopr_status_t s = check_attn(st, args, &shape, &n_rep);
   if (s != DOPR_OK) return s;
-  *bytes = plan_bytes(shape);
+  *bytes = attn_bytes(st, args, shape);
   return ok();
 }
 
@@ -525,6 +540,21 @@ dopr_status_t noalloc_shape(const dopr_attn_args_t *a, PlanShape *shape) {
   return DOPR_OK;
 }
 
+// The launches of a checked call.
+dopr_status_t launch_call(const AttnCall &call, void *ws,
+                          const PlanShape &shape, hipStream_t hs) {
+  hipError_t e;
+  if (!call.head && is_token_call(call.st, call.a)) {
+    e = launch_token(call, ws, hs);
+  } else {
+    const Plan plan = plan_carve(ws, shape);
+    e = launch_plan(call, plan, shape, hs);
+    if (e != hipSuccess) return hip_fail(e, "scheduler launch");
+    e = launch_attention(call, plan, shape, hs);
+  }
+  return e == hipSuccess ? DOPR_OK : hip_fail(e, "attention launch");
+}
+
 // The attention call in both modes: every online row (head == NULL) or the
 // score token's rows with the fused score head.  no_alloc: the plan goes to
 // the library's scratch array instead of the caller's workspace; the
@@ -574,7 +604,9 @@ dopr_status_t run_attention(dopr_store_t st, int32_t layer,
       return fail(DOPR_ERR_INVALID_ARG,
                   "head norm_w and w_head must be 16-byte aligned");
   }
-  const size_t need = plan_bytes(shape);
+  const bool token = !score && is_token_call(st, a);
+  const size_t need = token ? token_bytes(*st, a->n_pairs, n_rep)
+                            : plan_bytes(shape);
   void *ws = a->workspace;
   if (no_alloc) {
     if (need > kNoAllocScratchBytes) return noalloc_too_large(need);
@@ -592,14 +624,9 @@ dopr_status_t run_attention(dopr_store_t st, int32_t layer,
     s = scratch_ptr(st->device, &ws);
     if (s != DOPR_OK) return s;
   }
-  const Plan plan = plan_carve(ws, shape);
-  AttnCall call{st, layer, a, n_rep, head};
-  hipStream_t hs = as_stream(stream);
-  hipError_t e = launch_plan(call, plan, shape, hs);
-  if (e != hipSuccess) return hip_fail(e, "scheduler launch");
-  e = launch_attention(call, plan, shape, hs);
-  if (e != hipSuccess) return hip_fail(e, "attention launch");
-  return ok();
+  const AttnCall call{st, layer, a, n_rep, head};
+  s = launch_call(call, ws, shape, as_stream(stream));
+  return s == DOPR_OK ? ok() : s;
 }
 
 }  // namespace
@@ -664,8 +691,9 @@ dopr_status_t check_layer(dopr_store_t st, const dopr_attn_args_t *b,
   return DOPR_OK;
 }
 
-size_t layer_bytes(const LayerShape &ls, const PlanShape &shape) {
-  return layer_carve(nullptr, ls).bytes + plan_bytes(shape);
+size_t layer_bytes(const LayerShape &ls, const dopr_store *st,
+                   const dopr_attn_args_t *b, const PlanShape &shape) {
+  return layer_carve(nullptr, ls).bytes + attn_bytes(st, b, shape);
 }
 
 }  // namespace
@@ -682,7 +710,7 @@ dopr_status_t dopr_decoder_layer_workspace(dopr_store_t st,
   int32_t n_rep = 0;
   dopr_status_t s = check_layer(st, batch, lw, &ls, &shape, &n_rep);
   if (s != DOPR_OK) return s;
-  *bytes = layer_bytes(ls, shape);
+  *bytes = layer_bytes(ls, st, batch, shape);
   return ok();
 }
 
@@ -712,7 +740,7 @@ dopr_status_t dopr_decoder_layer(dopr_store_t st, int32_t layer,
                   "weights, x and y must be 16-byte aligned");
   if (reinterpret_cast<uintptr_t>(b->workspace) % kAlign)
     return fail(DOPR_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-  const size_t need = layer_bytes(ls, shape);
+  const size_t need = layer_bytes(ls, st, b, shape);
   if (b->workspace_bytes < need)
     return fail(DOPR_ERR_WORKSPACE,
                 "workspace holds " + std::to_string(b->workspace_bytes) +
@@ -726,8 +754,7 @@ dopr_status_t dopr_decoder_layer(dopr_store_t st, int32_t layer,
   a.v = w.v;
   a.out = w.att;
   a.workspace = w.plan;
-  a.workspace_bytes = plan_bytes(shape);
-  const Plan plan = plan_carve(w.plan, shape);
+  a.workspace_bytes = attn_bytes(st, b, shape);
   AttnCall call{st, layer, &a, n_rep};
   hipStream_t hs = as_stream(stream);
   int g = launch_layer_pre(ls, l, w, b->rms_eps, hs);
@@ -735,10 +762,8 @@ dopr_status_t dopr_decoder_layer(dopr_store_t st, int32_t layer,
     return g < 0 ? hip_fail(hipGetLastError(), "layer launch")
                  : fail(DOPR_ERR_HIP, std::string("hipBLASLt: ") +
                                           gemm_status_str(g));
-  hipError_t e = launch_plan(call, plan, shape, hs);
-  if (e != hipSuccess) return hip_fail(e, "scheduler launch");
-  e = launch_attention(call, plan, shape, hs);
-  if (e != hipSuccess) return hip_fail(e, "attention launch");
+  s = launch_call(call, w.plan, shape, hs);
+  if (s != DOPR_OK) return s;
   g = launch_layer_post(ls, l, w, b->rms_eps, hs);
   if (g != 0)
     return g < 0 ? hip_fail(hipGetLastError(), "layer launch")

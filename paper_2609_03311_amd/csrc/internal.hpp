@@ -526,6 +526,10 @@ inline UnitArgs unit_args(const AttnCall &c) {
   return {c.layer, c.n_rep, c.a->softmax_scale * 1.4426950408889634f,
           c.a->total_tokens, static_cast<const uint16_t *>(c.a->v)};
 }
+// token.hip: pairs of one token over a 4-bit store, without a plan, and the
+// workspace it takes.
+size_t token_bytes(const dopr_store &st, int64_t pairs, int32_t n_rep);
+hipError_t launch_token(const AttnCall &c, void *workspace, hipStream_t s);
 hipError_t launch_plan(const AttnCall &c, const Plan &plan,
                        const PlanShape &shape, hipStream_t s);
 hipError_t launch_attention(const AttnCall &c, const Plan &plan,

@@ -1,0 +1,456 @@
+// token.hip -- prefix attention of pairs of one token over a 4-bit store
+// (k_token_fp4), the form that serving a token at a time takes.
+//
+// A pair has n_rep rows a kv head, one own key (its own), and a prefix to
+// read: bound by HBM, 17/16 bytes a slot and dim of K and V.  No plan: a block
+// takes one (pair, kv head), finds its document, forms q^ and k^ and the own
+// key's logit itself, and its four waves take the document's 32-slot chunks in
+// turn, codes straight from memory into operand registers, the next chunk's
+// asked for before the present one's products.  Each wave keeps its own sums;
+// they meet in LDS.  Where pairs are few and prefixes long, several blocks
+// share a (pair, kv head) and leave their sums to k_token_join.
+//
+// The softmax has no running maximum where |q^| |k| bounds the logits (exact
+// norms of this pair's rows; kmax of the document's keys), and an exact one
+// elsewhere, in the same launch.  q^ enters the products as two bf16 parts (16
+// bits of mantissa): the matrix cores have room, and the keys are exact.
+#include <cmath>
+
+#include "attn_common.hpp"
+#include "operators.hpp"
+
+namespace dopr {
+namespace {
+
+constexpr int kTokenWaves = 4;
+
+struct TokenParams {
+  StoreView sv;
+  const uint16_t *q, *k, *v, *qw, *kw;  // (no gains: no norm)
+  const int32_t *doc_ids, *cu;
+  const float *inv_freq;
+  int32_t *status;
+  uint16_t *out;
+  float *lse;
+  float *part;  // [pair, kv head, split][n_rep][D + 2]: O, m, l
+  double log_theta;
+  int64_t p0, n_pairs, total_tokens;  // first pair of this launch; all pairs
+  float eps, c;
+  int32_t Hq, n_rep, layer, splits;
+};
+
+// Whether pair p has one token, and which.
+__device__ __forceinline__ bool one_token(const TokenParams &P, int64_t p,
+                                          int64_t &t0) {
+  t0 = P.cu[p];
+  return t0 >= 0 && P.cu[p + 1] == t0 + 1 && t0 < P.total_tokens;
+}
+__device__ __forceinline__ bool has_document(const TokenParams &P, int32_t d) {
+  return d >= 0 && (int64_t)d < P.sv.n_docs && P.sv.doc_len[d] >= 0;
+}
+
+__device__ __forceinline__ void store_out(uint16_t *to, const float *o,
+                                          float inv) {
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const bf16x2 h = {(__bf16)(o[2 * i] * inv), (__bf16)(o[2 * i + 1] * inv)};
+    w[i] = __builtin_bit_cast(uint32_t, h);
+  }
+  *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+}
+
+// RT: rows of a tile, at most 32.
+template <int D, int RT>
+struct TokenSm {
+  float o[kTokenWaves][RT][D];  // the waves' sums
+  float m[kTokenWaves][RT], l[kTokenWaves][RT];
+  float q[RT][D];   // c q^
+  float k[D];       // k^ of the own key
+  float2 rope[D / 2];
+  float norm2[RT + 1];  // of the rows of q, and of k
+  float own[RT];        // logits of the own key
+};
+
+// Chunks c, c + step, .. < end: O and the normaliser of this wave's share.
+// (kr, vr: chunk c's codes, on their way or there.)
+template <int SMX, int D>
+__device__ __forceinline__ void token_chunks(const char *slice, int c, int end,
+                                             int step, int L, int lane,
+                                             const bf16x8 (*qh)[D / 16],
+                                             const bf16x8 *ql, Fp4Raw<D> &kr,
+                                             Fp4Raw<D> &vr, Acc<D> *acc) {
+  const int hf = lane >> 5;
+  for (; c < end; c += step) {
+    const Fp4Raw<D> k0 = kr, v0 = vr;
+    if (c + step < end) {
+      const char *next = slice + (int64_t)(c + step) * fp4_chunk_bytes(D);
+      fp4_load_k<D>(next, lane, kr);
+      fp4_load_v<D>(next, lane, vr);
+    }
+    floatx16 S[1];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) S[0][i] = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      const bf16x8 kf = fp4_k<D>(k0, s);
+      S[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qh[0][s], S[0], 0, 0,
+                                                     0);
+      S[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, ql[s], S[0], 0, 0, 0);
+    }
+    const int lim = L - 1 - c * KC;
+    if (lim < KC - 1) {
+      const int li = lim - 16 * hf;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) S[0][i] = i <= li ? S[0][i] : -INFINITY;
+    }
+    bf16x8 pb[1][2];
+    softmax_part<0, 1, SMX, D>(S, acc, hf, 0.f, nullptr, pb);
+#pragma unroll
+    for (int f = 0; f < D / 16; ++f)
+      acc[0].o[f >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          fp4_v<D>(v0, f), pb[0][f & 1], acc[0].o[f >> 1], 0, 0, 0);
+  }
+}
+
+template <int D, int RT>
+__global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
+    amdgpu_waves_per_eu(2, 2))) void k_token_fp4(TokenParams P) {
+  constexpr int G = D / 8;  // lanes a row, eight dims each
+  __shared__ __attribute__((aligned(16))) TokenSm<D, RT> sm;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lq = lane & 31, hf = lane >> 5;
+  const int hkv = P.sv.n_kv_heads;
+  const int g = blockIdx.x % hkv;
+  const unsigned rest = blockIdx.x / hkv;
+  const int split = rest % P.splits;
+  const int64_t p = P.p0 + rest / P.splits;
+  int64_t tok;
+  const bool well = one_token(P, p, tok);
+  const int32_t doc = P.doc_ids[p];
+  if (tid == 0 && g == 0 && split == 0 &&
+      (!well || (p == 0 && P.cu[0] != 0) ||
+       (p == P.n_pairs - 1 && P.cu[P.n_pairs] != P.total_tokens)))
+    raise_status(P.status, DOPR_ERR_SEQLEN);
+  if (!well) return;  // (the whole block)
+  const int64_t row0 = tok * P.Hq + g * P.n_rep;
+  if (!has_document(P, doc)) {
+    if (split == 0) {
+      if (tid == 0 && g == 0) raise_status(P.status, DOPR_ERR_DOC_RANGE);
+      for (int e = tid; e < P.n_rep * G; e += 64 * kTokenWaves)
+        reinterpret_cast<uint4 *>(P.out + row0 * D)[e] =
+            make_uint4(0, 0, 0, 0);
+      if (P.lse)
+        for (int e = tid; e < P.n_rep; e += 64 * kTokenWaves)
+          P.lse[row0 + e] = -INFINITY;
+    }
+    return;
+  }
+  const int L = P.sv.doc_len[doc];
+  const char *slice = reinterpret_cast<const char *>(
+      P.sv.payload +
+      fp4_offset(P.sv.doc_off[doc], L, hkv, P.layer, g, D));
+  const float kmax =
+      P.sv.kmax[((int64_t)doc * P.sv.n_layers + P.layer) * hkv + g];
+  const int n_chunks = (L + KC - 1) / KC;
+  const int per = (n_chunks + P.splits - 1) / P.splits;
+  const int begin = min(split * per, n_chunks),
+            end = min(begin + per, n_chunks);
+  const int first = begin + wave;
+
+  for (int r0 = 0; r0 < P.n_rep; r0 += RT) {
+    const int rows = min(RT, P.n_rep - r0);
+    Fp4Raw<D> kr{}, vr{};
+    if (first < end) {
+      const char *chunk = slice + (int64_t)first * fp4_chunk_bytes(D);
+      fp4_load_k<D>(chunk, lane, kr);
+      fp4_load_v<D>(chunk, lane, vr);
+    }
+    // c q^ of the rows and k^, G lanes a row; row `rows` is the own key
+    const int gc = tid % G;
+    auto row_of = [&](int rr) {
+      return rr < rows ? P.q + (row0 + r0 + rr) * D
+                       : P.k + (tok * hkv + g) * D;
+    };
+    uint4 raw = make_uint4(0, 0, 0, 0);
+    if (tid / G <= rows)
+      raw = *reinterpret_cast<const uint4 *>(row_of(tid / G) + 8 * gc);
+    if (r0 == 0 && tid < D / 2) {
+      const double freq = P.inv_freq
+                              ? (double)P.inv_freq[tid]
+                              : exp(-(double)tid / (D / 2) * P.log_theta);
+      double sn, cs;
+      sincos((double)L * freq, &sn, &cs);
+      sm.rope[tid] = make_float2((float)cs, (float)sn);
+    }
+    __syncthreads();
+    for (int rr = tid / G; rr <= rows; rr += 64 * kTokenWaves / G) {
+      if (rr != tid / G)
+        raw = *reinterpret_cast<const uint4 *>(row_of(rr) + 8 * gc);
+      float x[8], y[8];
+      unpack8(raw, x);
+      const uint16_t *w = rr < rows ? P.qw : P.kw;
+      if (w) {
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+#pragma unroll
+        for (int off = 1; off < G; off <<= 1) ss += __shfl_xor(ss, off, 64);
+        const float inv = 1.0f / sqrtf(ss * (1.0f / D) + P.eps);
+        float gain[8];
+        unpack8(*reinterpret_cast<const uint4 *>(w + 8 * gc), gain);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * gain[e];
+      }
+      // (the partner of dim i is i +- D/2)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = __shfl_xor(x[e], G / 2, 64);
+      const float sign = gc < G / 2 ? -1.f : 1.f, by = rr < rows ? P.c : 1.f;
+      float n2 = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float2 t = sm.rope[(8 * gc + e) % (D / 2)];
+        x[e] = by * fmaf(x[e], t.x, sign * y[e] * t.y);
+        n2 = fmaf(x[e], x[e], n2);
+      }
+#pragma unroll
+      for (int off = 1; off < G; off <<= 1) n2 += __shfl_xor(n2, off, 64);
+      if (gc == 0) sm.norm2[rr < rows ? rr : RT] = n2;
+      float4 *to = reinterpret_cast<float4 *>(
+          (rr < rows ? sm.q[rr] : sm.k) + 8 * gc);
+      to[0] = make_float4(x[0], x[1], x[2], x[3]);
+      to[1] = make_float4(x[4], x[5], x[6], x[7]);
+    }
+    __syncthreads();
+    float top = 0.f;
+    bool bounded = true;
+    for (int rr = 0; rr < rows; ++rr) top = fmaxf(top, sm.norm2[rr]);
+    for (int rr = tid / G; rr < rows; rr += 64 * kTokenWaves / G) {
+      float dot = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        dot = fmaf(sm.q[rr][8 * gc + e], sm.k[8 * gc + e], dot);
+#pragma unroll
+      for (int off = 1; off < G; off <<= 1) dot += __shfl_xor(dot, off, 64);
+      if (gc == 0) sm.own[rr] = dot;
+    }
+    // every logit (log2 units) lies in [-bound, bound]; NaN is not bounded
+    const float bound =
+        sqrtf(top) * fmaxf(kmax, sqrtf(sm.norm2[RT])) * 1.001f;
+    bounded = bound <= kNoRefBound;
+
+    bf16x8 qh[1][D / 16], ql[D / 16];
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      float x[8];
+      const float4 *from = reinterpret_cast<const float4 *>(
+          &sm.q[lq < rows ? lq : 0][16 * s + 8 * hf]);
+      const float4 a = from[0], b = from[1];
+      x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
+      x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+      qh[0][s] = to_bf16x8(x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] -= (float)qh[0][s][e];
+      ql[s] = to_bf16x8(x);
+    }
+    Acc<D> acc[1];
+    acc[0].m = bounded ? 0.f : -INFINITY;
+    acc[0].l = 0.f;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[0].o[db][i] = 0.f;
+    if (bounded)
+      token_chunks<0, D>(slice, first, end, kTokenWaves, L, lane, qh, ql, kr,
+                         vr, acc);
+    else
+      token_chunks<2, D>(slice, first, end, kTokenWaves, L, lane, qh, ql, kr,
+                         vr, acc);
+
+    // the waves' sums meet
+    const float lt = acc[0].l + __shfl_xor(acc[0].l, 32, 64);
+    if (lq < rows) {
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<float4 *>(
+              &sm.o[wave][lq][32 * db + 16 * hf + i]) =
+              make_float4(acc[0].o[db][i], acc[0].o[db][i + 1],
+                          acc[0].o[db][i + 2], acc[0].o[db][i + 3]);
+      if (hf == 0) {
+        sm.m[wave][lq] = acc[0].m;
+        sm.l[wave][lq] = lt;
+      }
+    }
+    __syncthreads();
+    for (int e = tid; e < rows * (D / 4); e += 64 * kTokenWaves) {
+      const int rr = e / (D / 4), d = 4 * (e % (D / 4));
+      const float own = split == 0 ? sm.own[rr] : -INFINITY;
+      float M = 0.f;
+      if (!bounded) {
+        M = own;
+#pragma unroll
+        for (int w = 0; w < kTokenWaves; ++w) M = fmaxf(M, sm.m[w][rr]);
+      }
+      // (nothing seen, M = -inf: all weights are zero)
+      const float ref = M == -INFINITY ? 0.f : M;
+      float l = __builtin_amdgcn_exp2f(own - ref);
+      float o[4] = {0.f, 0.f, 0.f, 0.f};
+      if (split == 0) {
+        const uint2 u = *reinterpret_cast<const uint2 *>(
+            P.v + (tok * hkv + g) * D + d);
+        o[0] = l * __uint_as_float(u.x << 16);
+        o[1] = l * __uint_as_float(u.x & 0xffff0000u);
+        o[2] = l * __uint_as_float(u.y << 16);
+        o[3] = l * __uint_as_float(u.y & 0xffff0000u);
+      }
+#pragma unroll
+      for (int w = 0; w < kTokenWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(sm.m[w][rr] - ref);
+        const float4 x = *reinterpret_cast<const float4 *>(&sm.o[w][rr][d]);
+        l = fmaf(f, sm.l[w][rr], l);
+        o[0] = fmaf(f, x.x, o[0]);
+        o[1] = fmaf(f, x.y, o[1]);
+        o[2] = fmaf(f, x.z, o[2]);
+        o[3] = fmaf(f, x.w, o[3]);
+      }
+      if (P.splits == 1) {
+        store_out(P.out + (row0 + r0 + rr) * D + d, o, 1.0f / l);
+        if (P.lse && d == 0)
+          P.lse[row0 + r0 + rr] = (ref + __log2f(l)) * kLn2;
+      } else {
+        float *to = P.part +
+                    (((p - P.p0) * hkv + g) * P.splits + split) * P.n_rep *
+                        (int64_t)(D + 2) +
+                    (r0 + rr) * (D + 2);
+        // (rows of D + 2: two 8-byte halves)
+        *reinterpret_cast<float2 *>(to + d) = make_float2(o[0], o[1]);
+        *reinterpret_cast<float2 *>(to + d + 2) = make_float2(o[2], o[3]);
+        if (d == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(M, l);
+      }
+    }
+    __syncthreads();  // (the next tile writes where this one was read)
+  }
+}
+
+// The sums of a (pair, kv head)'s blocks, one block for each.
+template <int D>
+__global__ __launch_bounds__(128) void k_token_join(TokenParams P) {
+  const int hkv = P.sv.n_kv_heads;
+  const int g = blockIdx.x % hkv;
+  const int64_t p = P.p0 + blockIdx.x / hkv;
+  int64_t tok;
+  if (!one_token(P, p, tok) || !has_document(P, P.doc_ids[p])) return;
+  const int64_t row0 = tok * P.Hq + g * P.n_rep;
+  const int64_t step = (int64_t)P.n_rep * (D + 2);
+  const float *from = P.part + ((p - P.p0) * hkv + g) * P.splits * step;
+  for (int e = threadIdx.x; e < P.n_rep * (D / 2); e += 128) {
+    const int rr = e / (D / 2), d = 2 * (e % (D / 2));
+    const float *x = from + (int64_t)rr * (D + 2);
+    float M = -INFINITY;
+    for (int s = 0; s < P.splits; ++s) M = fmaxf(M, x[s * step + D]);
+    // (a wave's block without keys has m = 0 or -inf, and no weight)
+    const float ref = M == -INFINITY ? 0.f : M;
+    float l = 0.f, o0 = 0.f, o1 = 0.f;
+    for (int s = 0; s < P.splits; ++s) {
+      const float2 ml = *reinterpret_cast<const float2 *>(x + s * step + D);
+      const float2 o = *reinterpret_cast<const float2 *>(x + s * step + d);
+      const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+      l = fmaf(f, ml.y, l);
+      o0 = fmaf(f, o.x, o0);
+      o1 = fmaf(f, o.y, o1);
+    }
+    const float inv = 1.0f / l;
+    const bf16x2 h = {(__bf16)(o0 * inv), (__bf16)(o1 * inv)};
+    *reinterpret_cast<uint32_t *>(P.out + (row0 + rr) * D + d) =
+        __builtin_bit_cast(uint32_t, h);
+    if (P.lse && d == 0) P.lse[row0 + rr] = (ref + __log2f(l)) * kLn2;
+  }
+}
+
+template <int D>
+hipError_t launch_token1(const TokenParams &P, int64_t pairs, hipStream_t s) {
+  const int hkv = P.sv.n_kv_heads;
+  return in_slices(
+      pairs, a_launch((int64_t)64 * kTokenWaves * hkv * P.splits),
+      [&](int64_t at, int64_t n) {
+        TokenParams S = P;
+        S.p0 = P.p0 + at;
+        const dim3 grid((unsigned)(n * hkv * P.splits));
+        const auto kernel =
+            P.n_rep <= 8 ? k_token_fp4<D, 8> : k_token_fp4<D, 32>;
+        hipLaunchKernelGGL(kernel, grid, dim3(64 * kTokenWaves), 0, s, S);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess || P.splits == 1) return e;
+        hipLaunchKernelGGL(k_token_join<D>, dim3((unsigned)(n * hkv)),
+                           dim3(128), 0, s, S);
+        return hipGetLastError();
+      });
+}
+
+}  // namespace
+
+namespace {
+
+// Blocks that share a (pair, kv head): until some 1,024 blocks are there, of at
+// least two chunks a wave of the longest document, and within 32 MB (half of
+// the no-alloc call's scratch).
+int32_t token_splits(const dopr_store &st, int64_t pairs, int32_t n_rep) {
+  const int64_t units = pairs * st.n_kv_heads;
+  const int64_t chunks = ((int64_t)st.max_len + KC - 1) / KC;
+  const int64_t want = (1024 + units - 1) / units;
+  const int64_t most = (chunks + 2 * kTokenWaves - 1) / (2 * kTokenWaves);
+  const int64_t fit = ((int64_t)32 << 20) /
+                      (4 * units * n_rep * (int64_t)(st.head_dim + 2));
+  return (int32_t)std::max<int64_t>(1, std::min({want, most, fit}));
+}
+
+}  // namespace
+
+size_t token_bytes(const dopr_store &st, int64_t pairs, int32_t n_rep) {
+  const int64_t splits = token_splits(st, pairs, n_rep);
+  return splits == 1 ? 0
+                     : sizeof(float) * (size_t)(pairs * st.n_kv_heads) *
+                           splits * n_rep * (st.head_dim + 2);
+}
+
+hipError_t launch_token(const AttnCall &c, void *workspace, hipStream_t s) {
+  const dopr_attn_args_t *a = c.a;
+  const dopr_store &st = *c.st;
+  TokenParams P{};
+  P.sv = st.view();
+  P.q = static_cast<const uint16_t *>(a->q);
+  P.k = static_cast<const uint16_t *>(a->k);
+  P.v = static_cast<const uint16_t *>(a->v);
+  P.qw = static_cast<const uint16_t *>(a->q_norm_w);
+  P.kw = static_cast<const uint16_t *>(a->k_norm_w);
+  P.doc_ids = a->doc_ids;
+  P.cu = a->cu_seqlens;
+  P.inv_freq = a->rope_inv_freq;
+  P.status = st.d_status;
+  P.out = static_cast<uint16_t *>(a->out);
+  P.lse = a->lse;
+  P.part = static_cast<float *>(workspace);
+  P.log_theta = std::log((double)a->rope_theta);
+  P.n_pairs = a->n_pairs;
+  P.total_tokens = a->total_tokens;
+  P.eps = a->rms_eps;
+  P.c = a->softmax_scale * 1.4426950408889634f;
+  P.Hq = a->n_q_heads;
+  P.n_rep = c.n_rep;
+  P.layer = c.layer;
+  P.splits = token_splits(st, a->n_pairs, c.n_rep);
+  hipError_t e = hipSuccess;
+  if (a->timing_begin)
+    e = hipEventRecord(static_cast<hipEvent_t>(a->timing_begin), s);
+  if (e == hipSuccess)
+    e = st.head_dim == 128 ? launch_token1<128>(P, a->n_pairs, s)
+                           : launch_token1<64>(P, a->n_pairs, s);
+  if (e == hipSuccess && a->timing_end)
+    e = hipEventRecord(static_cast<hipEvent_t>(a->timing_end), s);
+  return e;
+}
+
+}  // namespace dopr
