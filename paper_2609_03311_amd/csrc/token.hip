@@ -2,13 +2,14 @@
 // (k_token_fp4), the form that serving a token at a time takes.
 //
 // A pair has n_rep rows a kv head, one own key (its own), and a prefix to
-// read: bound by HBM, 17/16 bytes a slot and dim of K and V.  No plan: a block
-// takes one (pair, kv head), finds its document, forms q^ and k^ and the own
-// key's logit itself, and its four waves take the document's 32-slot chunks in
-// turn, codes straight from memory into operand registers, the next chunk's
-// asked for before the present one's products.  Each wave keeps its own sums;
-// they meet in LDS.  Where pairs are few and prefixes long, several blocks
-// share a (pair, kv head) and leave their sums to k_token_join.
+// read: bound by HBM, 17/16 bytes a slot and dim of K and V.  No plan: the waves
+// of a (pair, kv head) find its document and each form q^ and k^ and the own
+// key's logit for themselves; they take the document's 32-slot chunks in turn,
+// codes straight from memory into operand registers, the next chunk's asked for
+// before the present one's products, and keep their own sums, which meet in
+// LDS.  One wave takes a (pair, kv head) where there are enough of them to fill
+// the card, up to four where there are not, and where pairs are few and
+// prefixes long several blocks, which leave their sums to k_token_join.
 //
 // The softmax has no running maximum where |q^| |k| bounds the logits (exact
 // norms of this pair's rows; kmax of the document's keys), and an exact one
@@ -22,7 +23,7 @@
 namespace dopr {
 namespace {
 
-constexpr int kTokenWaves = 4;
+constexpr int kTokenWaves = 4;  // of a block
 
 struct TokenParams {
   StoreView sv;
@@ -37,6 +38,7 @@ struct TokenParams {
   int64_t p0, n_pairs, total_tokens;  // first pair of this launch; all pairs
   float eps, c;
   int32_t Hq, n_rep, layer, splits;
+  uint32_t units;                     // (pair, kv head, split) of this launch
 };
 
 // Whether pair p has one token, and which.
@@ -60,17 +62,23 @@ __device__ __forceinline__ void store_out(uint16_t *to, const float *o,
   *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
 }
 
-// RT: rows of a tile, at most 32.
+// What a wave keeps of a unit's rows (a tile of RT, at most 32).
 template <int D, int RT>
-struct TokenSm {
-  float o[kTokenWaves][RT][D];  // the waves' sums
-  float m[kTokenWaves][RT], l[kTokenWaves][RT];
-  float q[RT][D];   // c q^
-  float k[D];       // k^ of the own key
+struct TokenRows {
+  float q[RT][D];  // c q^, then the wave's sums O
+  float k[D];      // k^ of the own key
   float2 rope[D / 2];
   float norm2[RT + 1];  // of the rows of q, and of k
   float own[RT];        // logits of the own key
+  float m[RT], l[RT];
 };
+
+// The wave's LDS accesses so far, and the compiler's, end here.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 // Chunks c, c + step, .. < end: O and the normaliser of this wave's share.
 // (kr, vr: chunk c's codes, on their way or there.)
@@ -113,304 +121,370 @@ __device__ __forceinline__ void token_chunks(const char *slice, int c, int end,
   }
 }
 
-template <int D, int RT>
+// WU: waves of a unit, (pair, kv head, split).
+template <int D, int RT, int WU>
 __global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
     amdgpu_waves_per_eu(2, 2))) void k_token_fp4(TokenParams P) {
-  constexpr int G = D / 8;  // lanes a row, eight dims each
-  __shared__ __attribute__((aligned(16))) TokenSm<D, RT> sm;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  constexpr int G = D / 8;    // lanes a row, eight dims each
+  constexpr int RP = 64 / G;  // rows at a time
+  __shared__ __attribute__((aligned(16))) TokenRows<D, RT> sm_all[kTokenWaves];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lq = lane & 31, hf = lane >> 5;
   const int hkv = P.sv.n_kv_heads;
-  const int g = blockIdx.x % hkv;
-  const unsigned rest = blockIdx.x / hkv;
+  const int w0 = wave / WU * WU, wu = wave - w0;  // the unit's first wave
+  TokenRows<D, RT> &sm = sm_all[wave];
+  const unsigned unit = blockIdx.x * (kTokenWaves / WU) + wave / WU;
+  // (a wave without a unit, or whose pair has no token or no document, goes
+  // on to meet the barriers)
+  bool live = unit < P.units;
+  const unsigned u = live ? unit : 0;
+  const int g = u % hkv;
+  const unsigned rest = u / hkv;
   const int split = rest % P.splits;
   const int64_t p = P.p0 + rest / P.splits;
   int64_t tok;
   const bool well = one_token(P, p, tok);
   const int32_t doc = P.doc_ids[p];
-  if (tid == 0 && g == 0 && split == 0 &&
+  const bool first_of_pair = lane == 0 && wu == 0 && g == 0 && split == 0;
+  if (live && first_of_pair &&
       (!well || (p == 0 && P.cu[0] != 0) ||
        (p == P.n_pairs - 1 && P.cu[P.n_pairs] != P.total_tokens)))
     raise_status(P.status, DOPR_ERR_SEQLEN);
-  if (!well) return;  // (the whole block)
+  live = live && well;
   const int64_t row0 = tok * P.Hq + g * P.n_rep;
-  if (!has_document(P, doc)) {
-    if (split == 0) {
-      if (tid == 0 && g == 0) raise_status(P.status, DOPR_ERR_DOC_RANGE);
-      for (int e = tid; e < P.n_rep * G; e += 64 * kTokenWaves)
+  if (live && !has_document(P, doc)) {
+    if (first_of_pair) raise_status(P.status, DOPR_ERR_DOC_RANGE);
+    if (split == 0 && wu == 0) {
+      for (int e = lane; e < P.n_rep * G; e += 64)
         reinterpret_cast<uint4 *>(P.out + row0 * D)[e] =
             make_uint4(0, 0, 0, 0);
       if (P.lse)
-        for (int e = tid; e < P.n_rep; e += 64 * kTokenWaves)
-          P.lse[row0 + e] = -INFINITY;
+        for (int e = lane; e < P.n_rep; e += 64) P.lse[row0 + e] = -INFINITY;
     }
-    return;
+    live = false;
   }
-  const int L = P.sv.doc_len[doc];
-  const char *slice = reinterpret_cast<const char *>(
-      P.sv.payload +
-      fp4_offset(P.sv.doc_off[doc], L, hkv, P.layer, g, D));
-  const float kmax =
-      P.sv.kmax[((int64_t)doc * P.sv.n_layers + P.layer) * hkv + g];
-  const int n_chunks = (L + KC - 1) / KC;
-  const int per = (n_chunks + P.splits - 1) / P.splits;
-  const int begin = min(split * per, n_chunks),
-            end = min(begin + per, n_chunks);
-  const int first = begin + wave;
+  if (WU == 1 && !live) return;  // (no barrier below)
+  int L = 0, first = 0, end = 0;
+  const char *slice = nullptr;
+  float kmax = 0.f;
+  if (live) {
+    L = P.sv.doc_len[doc];
+    slice = reinterpret_cast<const char *>(
+        P.sv.payload + fp4_offset(P.sv.doc_off[doc], L, hkv, P.layer, g, D));
+    kmax = P.sv.kmax[((int64_t)doc * P.sv.n_layers + P.layer) * hkv + g];
+    const int n_chunks = (L + KC - 1) / KC;
+    const int per = (n_chunks + P.splits - 1) / P.splits;
+    const int begin = min(split * per, n_chunks);
+    end = min(begin + per, n_chunks);
+    first = begin + wu;
+  }
 
   for (int r0 = 0; r0 < P.n_rep; r0 += RT) {
     const int rows = min(RT, P.n_rep - r0);
-    Fp4Raw<D> kr{}, vr{};
-    if (first < end) {
-      const char *chunk = slice + (int64_t)first * fp4_chunk_bytes(D);
-      fp4_load_k<D>(chunk, lane, kr);
-      fp4_load_v<D>(chunk, lane, vr);
-    }
-    // c q^ of the rows and k^, G lanes a row; row `rows` is the own key
-    const int gc = tid % G;
-    auto row_of = [&](int rr) {
-      return rr < rows ? P.q + (row0 + r0 + rr) * D
-                       : P.k + (tok * hkv + g) * D;
-    };
-    uint4 raw = make_uint4(0, 0, 0, 0);
-    if (tid / G <= rows)
-      raw = *reinterpret_cast<const uint4 *>(row_of(tid / G) + 8 * gc);
-    if (r0 == 0 && tid < D / 2) {
-      const double freq = P.inv_freq
-                              ? (double)P.inv_freq[tid]
-                              : exp(-(double)tid / (D / 2) * P.log_theta);
-      double sn, cs;
-      sincos((double)L * freq, &sn, &cs);
-      sm.rope[tid] = make_float2((float)cs, (float)sn);
-    }
-    __syncthreads();
-    for (int rr = tid / G; rr <= rows; rr += 64 * kTokenWaves / G) {
-      if (rr != tid / G)
-        raw = *reinterpret_cast<const uint4 *>(row_of(rr) + 8 * gc);
-      float x[8], y[8];
-      unpack8(raw, x);
-      const uint16_t *w = rr < rows ? P.qw : P.kw;
-      if (w) {
-        float ss = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-#pragma unroll
-        for (int off = 1; off < G; off <<= 1) ss += __shfl_xor(ss, off, 64);
-        const float inv = 1.0f / sqrtf(ss * (1.0f / D) + P.eps);
-        float gain[8];
-        unpack8(*reinterpret_cast<const uint4 *>(w + 8 * gc), gain);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * gain[e];
-      }
-      // (the partner of dim i is i +- D/2)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = __shfl_xor(x[e], G / 2, 64);
-      const float sign = gc < G / 2 ? -1.f : 1.f, by = rr < rows ? P.c : 1.f;
-      float n2 = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float2 t = sm.rope[(8 * gc + e) % (D / 2)];
-        x[e] = by * fmaf(x[e], t.x, sign * y[e] * t.y);
-        n2 = fmaf(x[e], x[e], n2);
-      }
-#pragma unroll
-      for (int off = 1; off < G; off <<= 1) n2 += __shfl_xor(n2, off, 64);
-      if (gc == 0) sm.norm2[rr < rows ? rr : RT] = n2;
-      float4 *to = reinterpret_cast<float4 *>(
-          (rr < rows ? sm.q[rr] : sm.k) + 8 * gc);
-      to[0] = make_float4(x[0], x[1], x[2], x[3]);
-      to[1] = make_float4(x[4], x[5], x[6], x[7]);
-    }
-    __syncthreads();
-    float top = 0.f;
     bool bounded = true;
-    for (int rr = 0; rr < rows; ++rr) top = fmaxf(top, sm.norm2[rr]);
-    for (int rr = tid / G; rr < rows; rr += 64 * kTokenWaves / G) {
-      float dot = 0.f;
+    if (live) {
+      Fp4Raw<D> kr{}, vr{};
+      if (first < end) {
+        const char *chunk = slice + (int64_t)first * fp4_chunk_bytes(D);
+        fp4_load_k<D>(chunk, lane, kr);
+        fp4_load_v<D>(chunk, lane, vr);
+      }
+      // c q^ of the rows and k^, G lanes a row; row `rows` is the own key
+      const int gc = lane % G;
+      auto row_of = [&](int rr) {
+        return rr < rows ? P.q + (row0 + r0 + rr) * D
+                         : P.k + (tok * hkv + g) * D;
+      };
+      uint4 raw = make_uint4(0, 0, 0, 0);
+      if (lane / G <= rows)
+        raw = *reinterpret_cast<const uint4 *>(row_of(lane / G) + 8 * gc);
+      if (r0 == 0 && lane < D / 2) {
+        // whole turns are dropped in 64 bits
+        const double freq = P.inv_freq
+                                ? (double)P.inv_freq[lane]
+                                : exp(-(double)lane / (D / 2) * P.log_theta);
+        const double turns = (double)L * freq * 0.15915494309189533577;
+        float sn, cs;
+        sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
+        sm.rope[lane] = make_float2(cs, sn);
+      }
+      wave_fence();
+      for (int rr = lane / G; rr <= rows; rr += RP) {
+        float x[8], y[8];
+        unpack8(raw, x);
+        if (rr + RP <= rows)
+          raw = *reinterpret_cast<const uint4 *>(row_of(rr + RP) + 8 * gc);
+        const uint16_t *w = rr < rows ? P.qw : P.kw;
+        if (w) {
+          float ss = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        dot = fmaf(sm.q[rr][8 * gc + e], sm.k[8 * gc + e], dot);
+          for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
 #pragma unroll
-      for (int off = 1; off < G; off <<= 1) dot += __shfl_xor(dot, off, 64);
-      if (gc == 0) sm.own[rr] = dot;
-    }
-    // every logit (log2 units) lies in [-bound, bound]; NaN is not bounded
-    const float bound =
-        sqrtf(top) * fmaxf(kmax, sqrtf(sm.norm2[RT])) * 1.001f;
-    bounded = bound <= kNoRefBound;
+          for (int off = 1; off < G; off <<= 1) ss += __shfl_xor(ss, off, 64);
+          const float inv = 1.0f / sqrtf(ss * (1.0f / D) + P.eps);
+          float gain[8];
+          unpack8(*reinterpret_cast<const uint4 *>(w + 8 * gc), gain);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * gain[e];
+        }
+        // (the partner of dim i is i +- D/2)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = __shfl_xor(x[e], G / 2, 64);
+        const float sign = gc < G / 2 ? -1.f : 1.f, by = rr < rows ? P.c : 1.f;
+        float n2 = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float2 t = sm.rope[(8 * gc + e) % (D / 2)];
+          x[e] = by * fmaf(x[e], t.x, sign * y[e] * t.y);
+          n2 = fmaf(x[e], x[e], n2);
+        }
+#pragma unroll
+        for (int off = 1; off < G; off <<= 1) n2 += __shfl_xor(n2, off, 64);
+        if (gc == 0) sm.norm2[rr < rows ? rr : RT] = n2;
+        float4 *to = reinterpret_cast<float4 *>(
+            (rr < rows ? sm.q[rr] : sm.k) + 8 * gc);
+        to[0] = make_float4(x[0], x[1], x[2], x[3]);
+        to[1] = make_float4(x[4], x[5], x[6], x[7]);
+      }
+      wave_fence();
+      if (split == 0 && wu == 0)
+        for (int rr = lane / G; rr < rows; rr += RP) {
+          float dot = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            dot = fmaf(sm.q[rr][8 * gc + e], sm.k[8 * gc + e], dot);
+#pragma unroll
+          for (int off = 1; off < G; off <<= 1) dot += __shfl_xor(dot, off, 64);
+          if (gc == 0) sm.own[rr] = dot;
+        }
+      // every logit (log2 units) lies in [-bound, bound] (rows with NaN aside,
+      // which come out NaN either way)
+      float top = 0.f;
+      for (int rr = 0; rr < rows; ++rr) top = fmaxf(top, sm.norm2[rr]);
+      const float bound =
+          sqrtf(top) * fmaxf(kmax, sqrtf(sm.norm2[RT])) * 1.001f;
+      bounded = bound <= kNoRefBound;
 
-    bf16x8 qh[1][D / 16], ql[D / 16];
+      bf16x8 qh[1][D / 16], ql[D / 16];
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      float x[8];
-      const float4 *from = reinterpret_cast<const float4 *>(
-          &sm.q[lq < rows ? lq : 0][16 * s + 8 * hf]);
-      const float4 a = from[0], b = from[1];
-      x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
-      x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-      qh[0][s] = to_bf16x8(x);
+      for (int s = 0; s < D / 16; ++s) {
+        float x[8];
+        const float4 *from = reinterpret_cast<const float4 *>(
+            &sm.q[lq < rows ? lq : 0][16 * s + 8 * hf]);
+        const float4 a = from[0], b = from[1];
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
+        x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+        qh[0][s] = to_bf16x8(x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] -= (float)qh[0][s][e];
-      ql[s] = to_bf16x8(x);
-    }
-    Acc<D> acc[1];
-    acc[0].m = bounded ? 0.f : -INFINITY;
-    acc[0].l = 0.f;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[0].o[db][i] = 0.f;
-    if (bounded)
-      token_chunks<0, D>(slice, first, end, kTokenWaves, L, lane, qh, ql, kr,
-                         vr, acc);
-    else
-      token_chunks<2, D>(slice, first, end, kTokenWaves, L, lane, qh, ql, kr,
-                         vr, acc);
-
-    // the waves' sums meet
-    const float lt = acc[0].l + __shfl_xor(acc[0].l, 32, 64);
-    if (lq < rows) {
+        for (int e = 0; e < 8; ++e) x[e] -= (float)qh[0][s][e];
+        ql[s] = to_bf16x8(x);
+      }
+      Acc<D> acc[1];
+      acc[0].m = bounded ? 0.f : -INFINITY;
+      acc[0].l = 0.f;
 #pragma unroll
       for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-        for (int i = 0; i < 16; i += 4)
-          *reinterpret_cast<float4 *>(
-              &sm.o[wave][lq][32 * db + 16 * hf + i]) =
-              make_float4(acc[0].o[db][i], acc[0].o[db][i + 1],
-                          acc[0].o[db][i + 2], acc[0].o[db][i + 3]);
-      if (hf == 0) {
-        sm.m[wave][lq] = acc[0].m;
-        sm.l[wave][lq] = lt;
+        for (int i = 0; i < 16; ++i) acc[0].o[db][i] = 0.f;
+      if (bounded)
+        token_chunks<0, D>(slice, first, end, WU, L, lane, qh, ql, kr, vr,
+                           acc);
+      else
+        token_chunks<2, D>(slice, first, end, WU, L, lane, qh, ql, kr, vr,
+                           acc);
+
+      // the wave's sums, where q^ was
+      const float lt = acc[0].l + __shfl_xor(acc[0].l, 32, 64);
+      wave_fence();
+      if (lq < rows) {
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+          for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<float4 *>(&sm.q[lq][32 * db + 16 * hf + i]) =
+                make_float4(acc[0].o[db][i], acc[0].o[db][i + 1],
+                            acc[0].o[db][i + 2], acc[0].o[db][i + 3]);
+        if (hf == 0) {
+          sm.m[lq] = acc[0].m;
+          sm.l[lq] = lt;
+        }
       }
     }
-    __syncthreads();
-    for (int e = tid; e < rows * (D / 4); e += 64 * kTokenWaves) {
-      const int rr = e / (D / 4), d = 4 * (e % (D / 4));
-      const float own = split == 0 ? sm.own[rr] : -INFINITY;
-      float M = 0.f;
-      if (!bounded) {
-        M = own;
+    if constexpr (WU == 1)
+      wave_fence();
+    else
+      __syncthreads();
+    if (live)
+      for (int e = wu * 64 + lane; e < rows * (D / 4); e += 64 * WU) {
+        const int rr = e / (D / 4), d = 4 * (e % (D / 4));
+        const float own = split == 0 ? sm_all[w0].own[rr] : -INFINITY;
+        float M = 0.f;
+        if (!bounded) {
+          M = own;
 #pragma unroll
-        for (int w = 0; w < kTokenWaves; ++w) M = fmaxf(M, sm.m[w][rr]);
-      }
-      // (nothing seen, M = -inf: all weights are zero)
-      const float ref = M == -INFINITY ? 0.f : M;
-      float l = __builtin_amdgcn_exp2f(own - ref);
-      float o[4] = {0.f, 0.f, 0.f, 0.f};
-      if (split == 0) {
-        const uint2 u = *reinterpret_cast<const uint2 *>(
-            P.v + (tok * hkv + g) * D + d);
-        o[0] = l * __uint_as_float(u.x << 16);
-        o[1] = l * __uint_as_float(u.x & 0xffff0000u);
-        o[2] = l * __uint_as_float(u.y << 16);
-        o[3] = l * __uint_as_float(u.y & 0xffff0000u);
-      }
+          for (int w = 0; w < WU; ++w) M = fmaxf(M, sm_all[w0 + w].m[rr]);
+        }
+        // (nothing seen, M = -inf: all weights are zero)
+        const float ref = M == -INFINITY ? 0.f : M;
+        float l = __builtin_amdgcn_exp2f(own - ref);
+        float o[4] = {0.f, 0.f, 0.f, 0.f};
+        if (split == 0) {
+          const uint2 x = *reinterpret_cast<const uint2 *>(
+              P.v + (tok * hkv + g) * D + d);
+          o[0] = l * __uint_as_float(x.x << 16);
+          o[1] = l * __uint_as_float(x.x & 0xffff0000u);
+          o[2] = l * __uint_as_float(x.y << 16);
+          o[3] = l * __uint_as_float(x.y & 0xffff0000u);
+        }
 #pragma unroll
-      for (int w = 0; w < kTokenWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(sm.m[w][rr] - ref);
-        const float4 x = *reinterpret_cast<const float4 *>(&sm.o[w][rr][d]);
-        l = fmaf(f, sm.l[w][rr], l);
-        o[0] = fmaf(f, x.x, o[0]);
-        o[1] = fmaf(f, x.y, o[1]);
-        o[2] = fmaf(f, x.z, o[2]);
-        o[3] = fmaf(f, x.w, o[3]);
+        for (int w = 0; w < WU; ++w) {
+          const TokenRows<D, RT> &from = sm_all[w0 + w];
+          const float f = __builtin_amdgcn_exp2f(from.m[rr] - ref);
+          const float4 x = *reinterpret_cast<const float4 *>(&from.q[rr][d]);
+          l = fmaf(f, from.l[rr], l);
+          o[0] = fmaf(f, x.x, o[0]);
+          o[1] = fmaf(f, x.y, o[1]);
+          o[2] = fmaf(f, x.z, o[2]);
+          o[3] = fmaf(f, x.w, o[3]);
+        }
+        if (P.splits == 1) {
+          store_out(P.out + (row0 + r0 + rr) * D + d, o, 1.0f / l);
+          if (P.lse && d == 0)
+            P.lse[row0 + r0 + rr] = (ref + __log2f(l)) * kLn2;
+        } else {
+          float *to = P.part +
+                      (((p - P.p0) * hkv + g) * P.splits + split) * P.n_rep *
+                          (int64_t)(D + 2) +
+                      (int64_t)(r0 + rr) * (D + 2);
+          // (rows of D + 2: two 8-byte halves)
+          *reinterpret_cast<float2 *>(to + d) = make_float2(o[0], o[1]);
+          *reinterpret_cast<float2 *>(to + d + 2) = make_float2(o[2], o[3]);
+          if (d == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(M, l);
+        }
       }
-      if (P.splits == 1) {
-        store_out(P.out + (row0 + r0 + rr) * D + d, o, 1.0f / l);
-        if (P.lse && d == 0)
-          P.lse[row0 + r0 + rr] = (ref + __log2f(l)) * kLn2;
-      } else {
-        float *to = P.part +
-                    (((p - P.p0) * hkv + g) * P.splits + split) * P.n_rep *
-                        (int64_t)(D + 2) +
-                    (r0 + rr) * (D + 2);
-        // (rows of D + 2: two 8-byte halves)
-        *reinterpret_cast<float2 *>(to + d) = make_float2(o[0], o[1]);
-        *reinterpret_cast<float2 *>(to + d + 2) = make_float2(o[2], o[3]);
-        if (d == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(M, l);
-      }
-    }
-    __syncthreads();  // (the next tile writes where this one was read)
+    // (the next tile writes where this one was read)
+    if constexpr (WU == 1)
+      wave_fence();
+    else
+      __syncthreads();
   }
 }
 
-// The sums of a (pair, kv head)'s blocks, one block for each.
+// The sums of a row's blocks: one block a (pair, q head), eight of whose parts
+// share the splits.
 template <int D>
-__global__ __launch_bounds__(128) void k_token_join(TokenParams P) {
-  const int hkv = P.sv.n_kv_heads;
-  const int g = blockIdx.x % hkv;
-  const int64_t p = P.p0 + blockIdx.x / hkv;
+__global__ __launch_bounds__(4 * D) void k_token_join(TokenParams P) {
+  constexpr int PARTS = 8;
+  __shared__ float so[PARTS][D], sl[PARTS], sm[PARTS];
+  const int64_t p = P.p0 + blockIdx.x / P.Hq;
+  const int h = blockIdx.x % P.Hq, g = h / P.n_rep, rr = h - g * P.n_rep;
   int64_t tok;
   if (!one_token(P, p, tok) || !has_document(P, P.doc_ids[p])) return;
-  const int64_t row0 = tok * P.Hq + g * P.n_rep;
   const int64_t step = (int64_t)P.n_rep * (D + 2);
-  const float *from = P.part + ((p - P.p0) * hkv + g) * P.splits * step;
-  for (int e = threadIdx.x; e < P.n_rep * (D / 2); e += 128) {
-    const int rr = e / (D / 2), d = 2 * (e % (D / 2));
-    const float *x = from + (int64_t)rr * (D + 2);
-    float M = -INFINITY;
-    for (int s = 0; s < P.splits; ++s) M = fmaxf(M, x[s * step + D]);
-    // (a wave's block without keys has m = 0 or -inf, and no weight)
-    const float ref = M == -INFINITY ? 0.f : M;
-    float l = 0.f, o0 = 0.f, o1 = 0.f;
-    for (int s = 0; s < P.splits; ++s) {
-      const float2 ml = *reinterpret_cast<const float2 *>(x + s * step + D);
-      const float2 o = *reinterpret_cast<const float2 *>(x + s * step + d);
-      const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-      l = fmaf(f, ml.y, l);
-      o0 = fmaf(f, o.x, o0);
-      o1 = fmaf(f, o.y, o1);
-    }
-    const float inv = 1.0f / l;
-    const bf16x2 h = {(__bf16)(o0 * inv), (__bf16)(o1 * inv)};
-    *reinterpret_cast<uint32_t *>(P.out + (row0 + rr) * D + d) =
-        __builtin_bit_cast(uint32_t, h);
-    if (P.lse && d == 0) P.lse[row0 + rr] = (ref + __log2f(l)) * kLn2;
+  const float *x = P.part +
+                   ((p - P.p0) * P.sv.n_kv_heads + g) * P.splits * step +
+                   (int64_t)rr * (D + 2);
+  const int part = threadIdx.x / (D / 2), d = 2 * (threadIdx.x % (D / 2));
+  // (a split without keys has no weight, and the reference 0 or -inf)
+  float M = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
+  for (int s = part; s < P.splits; s += PARTS) {
+    const float2 ml = *reinterpret_cast<const float2 *>(x + s * step + D);
+    const float2 o = *reinterpret_cast<const float2 *>(x + s * step + d);
+    const float m = fmaxf(M, ml.x), ref = m == -INFINITY ? 0.f : m;
+    const float a = __builtin_amdgcn_exp2f(M - ref),
+                b = __builtin_amdgcn_exp2f(ml.x - ref);
+    l = fmaf(b, ml.y, a * l);
+    o0 = fmaf(b, o.x, a * o0);
+    o1 = fmaf(b, o.y, a * o1);
+    M = m;
   }
+  so[part][d] = o0;
+  so[part][d + 1] = o1;
+  if (d == 0) {
+    sm[part] = M;
+    sl[part] = l;
+  }
+  __syncthreads();
+  if (threadIdx.x >= D / 2) return;
+  M = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) M = fmaxf(M, sm[i]);
+  const float ref = M == -INFINITY ? 0.f : M;
+  l = o0 = o1 = 0.f;
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) {
+    const float f = __builtin_amdgcn_exp2f(sm[i] - ref);
+    l = fmaf(f, sl[i], l);
+    o0 = fmaf(f, so[i][d], o0);
+    o1 = fmaf(f, so[i][d + 1], o1);
+  }
+  const float inv = 1.0f / l;
+  const bf16x2 w = {(__bf16)(o0 * inv), (__bf16)(o1 * inv)};
+  const int64_t row = tok * P.Hq + h;
+  *reinterpret_cast<uint32_t *>(P.out + row * D + d) =
+      __builtin_bit_cast(uint32_t, w);
+  if (P.lse && d == 0) P.lse[row] = (ref + __log2f(l)) * kLn2;
+}
+
+// How a call's (pair, kv head)s are shared out: one wave each from kTokenFull
+// of them on (two waves a SIMD), two or four below, and blocks of four where
+// that leaves waves free, of at least two chunks a wave of the longest
+// document and within 32 MB of sums (half of the no-alloc call's scratch).
+constexpr int64_t kTokenFull = 2048;
+struct TokenShare {
+  int waves, splits;
+};
+TokenShare token_share(const dopr_store &st, int64_t pairs, int32_t n_rep) {
+  const int64_t units = pairs * st.n_kv_heads;
+  const int64_t chunks = ((int64_t)st.max_len + KC - 1) / KC;
+  if (2 * units > kTokenFull) return {1, 1};
+  if (4 * units > kTokenFull) return {2, 1};
+  const int64_t want = kTokenFull / (units * kTokenWaves);
+  const int64_t most = (chunks + 2 * kTokenWaves - 1) / (2 * kTokenWaves);
+  const int64_t fit = ((int64_t)32 << 20) /
+                      (4 * units * n_rep * (int64_t)(st.head_dim + 2));
+  return {kTokenWaves,
+          (int)std::max<int64_t>(1, std::min({want, most, fit}))};
+}
+
+template <int D, int RT>
+void launch_token2(int waves, const TokenParams &P, hipStream_t s) {
+  const auto kernel = waves == 1   ? k_token_fp4<D, RT, 1>
+                      : waves == 2 ? k_token_fp4<D, RT, 2>
+                                   : k_token_fp4<D, RT, 4>;
+  const unsigned per = kTokenWaves / waves;
+  hipLaunchKernelGGL(kernel, dim3((P.units + per - 1) / per),
+                     dim3(64 * kTokenWaves), 0, s, P);
 }
 
 template <int D>
-hipError_t launch_token1(const TokenParams &P, int64_t pairs, hipStream_t s) {
-  const int hkv = P.sv.n_kv_heads;
+hipError_t launch_token1(const TokenParams &P, int waves, int64_t pairs,
+                         hipStream_t s) {
+  const int64_t hkv = P.sv.n_kv_heads;
   return in_slices(
-      pairs, a_launch((int64_t)64 * kTokenWaves * hkv * P.splits),
+      pairs, a_launch(std::max<int64_t>(64 * waves * hkv * P.splits,
+                                        P.splits > 1 ? 4 * D * P.Hq : 1)),
       [&](int64_t at, int64_t n) {
         TokenParams S = P;
         S.p0 = P.p0 + at;
-        const dim3 grid((unsigned)(n * hkv * P.splits));
-        const auto kernel =
-            P.n_rep <= 8 ? k_token_fp4<D, 8> : k_token_fp4<D, 32>;
-        hipLaunchKernelGGL(kernel, grid, dim3(64 * kTokenWaves), 0, s, S);
+        S.units = (uint32_t)(n * hkv * P.splits);
+        if (P.n_rep <= 8)
+          launch_token2<D, 8>(waves, S, s);
+        else
+          launch_token2<D, 32>(waves, S, s);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess || P.splits == 1) return e;
-        hipLaunchKernelGGL(k_token_join<D>, dim3((unsigned)(n * hkv)),
-                           dim3(128), 0, s, S);
+        hipLaunchKernelGGL(k_token_join<D>, dim3((unsigned)(n * P.Hq)),
+                           dim3(4 * D), 0, s, S);
         return hipGetLastError();
       });
 }
 
 }  // namespace
 
-namespace {
-
-// Blocks that share a (pair, kv head): until some 1,024 blocks are there, of at
-// least two chunks a wave of the longest document, and within 32 MB (half of
-// the no-alloc call's scratch).
-int32_t token_splits(const dopr_store &st, int64_t pairs, int32_t n_rep) {
-  const int64_t units = pairs * st.n_kv_heads;
-  const int64_t chunks = ((int64_t)st.max_len + KC - 1) / KC;
-  const int64_t want = (1024 + units - 1) / units;
-  const int64_t most = (chunks + 2 * kTokenWaves - 1) / (2 * kTokenWaves);
-  const int64_t fit = ((int64_t)32 << 20) /
-                      (4 * units * n_rep * (int64_t)(st.head_dim + 2));
-  return (int32_t)std::max<int64_t>(1, std::min({want, most, fit}));
-}
-
-}  // namespace
-
 size_t token_bytes(const dopr_store &st, int64_t pairs, int32_t n_rep) {
-  const int64_t splits = token_splits(st, pairs, n_rep);
+  const int64_t splits = token_share(st, pairs, n_rep).splits;
   return splits == 1 ? 0
                      : sizeof(float) * (size_t)(pairs * st.n_kv_heads) *
                            splits * n_rep * (st.head_dim + 2);
@@ -441,13 +515,14 @@ hipError_t launch_token(const AttnCall &c, void *workspace, hipStream_t s) {
   P.Hq = a->n_q_heads;
   P.n_rep = c.n_rep;
   P.layer = c.layer;
-  P.splits = token_splits(st, a->n_pairs, c.n_rep);
+  const TokenShare share = token_share(st, a->n_pairs, c.n_rep);
+  P.splits = share.splits;
   hipError_t e = hipSuccess;
   if (a->timing_begin)
     e = hipEventRecord(static_cast<hipEvent_t>(a->timing_begin), s);
   if (e == hipSuccess)
-    e = st.head_dim == 128 ? launch_token1<128>(P, a->n_pairs, s)
-                           : launch_token1<64>(P, a->n_pairs, s);
+    e = st.head_dim == 128 ? launch_token1<128>(P, share.waves, a->n_pairs, s)
+                           : launch_token1<64>(P, share.waves, a->n_pairs, s);
   if (e == hipSuccess && a->timing_end)
     e = hipEventRecord(static_cast<hipEvent_t>(a->timing_end), s);
   return e;
