@@ -366,17 +366,6 @@ def dopr_store_put(store: Store, layer: int, doc_ids, src_cu_slots, k_src,
                                 _ptr(k_src), _ptr(v_src), _stream(stream)))
 
 
-def _put_heads(name, t, store, rows):
-    """(row, head) strides of k or v [rows, Hkv, D]."""
-    if t.dim() != 3 or tuple(t.shape) != (rows, store.n_kv_heads,
-                                          store.head_dim):
-        raise ValueError(f"{name} must be [rows, {store.n_kv_heads}, "
-                         f"{store.head_dim}], the rows of k")
-    if t.stride(2) != 1:
-        raise ValueError(f"{name} must have elements back to back")
-    return t.stride(0), t.stride(1)
-
-
 def dopr_store_put_rotary(store: Store, layer: int, doc_ids, src_cu_slots, k,
                           v, inv_freq, *, positions=None, k_norm_w=None,
                           interleaved=False, attention_factor=1.0,
@@ -386,40 +375,12 @@ def dopr_store_put_rotary(store: Store, layer: int, doc_ids, src_cu_slots, k,
     `positions` int32 [rows] (None: each document's slots 0, 1, ..), and v
     alike, rows and heads at any stride.  inv_freq fp32 [R/2] rotates the
     first R elements of a head."""
-    import torch
-    kinds = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
-    if k.dtype not in kinds:
-        raise ValueError("k must be bfloat16, float16 or float32")
-    rows = k.shape[0]
-    k_row, k_head = _put_heads("k", k, store, rows)
-    v_row, v_head = _put_heads("v", v, store, rows)
-    if v.dtype != k.dtype:
-        raise ValueError("v must have k's type")
-    n = doc_ids.numel()
-    for name, t, dtype, shape in (
-            ("doc_ids", doc_ids, torch.int32, (n,)),
-            ("src_cu_slots", src_cu_slots, torch.int64, (n + 1,)),
-            ("positions", positions, torch.int32, (rows,)),
-            ("k_norm_w", k_norm_w, k.dtype, (store.head_dim,)),
-            ("inv_freq", inv_freq, torch.float32, (inv_freq.numel(),)),
-            ("k", k, k.dtype, None), ("v", v, k.dtype, None)):
-        if t is None:
-            continue
-        if t.dtype != dtype:
-            raise ValueError(f"{name} must be {dtype}")
-        if shape is not None and (tuple(t.shape) != shape
-                                  or not t.is_contiguous()):
-            raise ValueError(f"{name} must be contiguous, of shape {shape}")
-        if t.device != store.pool.device:
-            raise ValueError(f"{name} must be on the store's device")
-    a = _PutRotaryArgs(int(layer), kinds[k.dtype], n, rows, _ptr(doc_ids),
-                       _ptr(src_cu_slots), _ptr(k), k_row, k_head, _ptr(v),
-                       v_row, v_head, _ptr(k_norm_w), _ptr(positions),
-                       _ptr(inv_freq), 2 * inv_freq.numel(),
-                       int(bool(interleaved)), float(attention_factor),
-                       float(rms_eps))
-    _check(lib().dopr_store_put_rotary(store.handle, ctypes.byref(a),
-                                       _stream(stream)))
+    pool = store.pool.device
+    _check(_compiled().store_put_rotary(
+        store.handle or 0, store.n_kv_heads, store.head_dim,
+        -1 if pool.index is None else pool.index, layer, doc_ids,
+        src_cu_slots, k, v, inv_freq, positions, k_norm_w, interleaved,
+        attention_factor, rms_eps, _handle(stream)))
 
 
 def dopr_store_destroy(store: Store):

@@ -1,6 +1,6 @@
-// binding.cpp -- the Python calls of the operators around the attention
-// (module _operators): checks tensors, fills the C ABI's argument structures
-// and calls it.
+// binding.cpp -- the Python calls of the operators around the attention and of
+// dopr_store_put_rotary (module _operators): checks tensors, fills the C ABI's
+// argument structures and calls it.
 //
 // The other entry points are marshalled in Python (ctypes).  These are a few
 // microseconds of GPU work at their smallest and take up to ten tensors of
@@ -264,6 +264,63 @@ PyObject *rotary(PyObject *const *a) {
   return PyLong_FromLong(dopr_rotary(&s, handle(a[12])));
 }
 
+int64_t whole(PyObject *o) {
+  const long long v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) throw Refused{};
+  return v;
+}
+
+PyObject *store_put_rotary(PyObject *const *a) {
+  // store's handle, kv heads, head dim and device, layer, doc_ids,
+  // src_cu_slots, k, v, inv_freq, positions, k_norm_w, interleaved,
+  // attention_factor, rms_eps, stream
+  dopr_put_rotary_args_t s{};
+  const int64_t hkv = whole(a[1]), d = whole(a[2]), device = whole(a[3]);
+  const int64_t layer = whole(a[4]);
+  s.layer = (int32_t)std::max<int64_t>(-1, std::min<int64_t>(layer,
+                                                             INT32_MAX));
+  const at::Tensor &k = tensor(a[7], "k");
+  if (k.dim() != 3) {
+    PyErr_SetString(PyExc_ValueError, "k must be [rows, kv heads, head dim]");
+    throw Refused{};
+  }
+  s.dtype = dtype_code(k, "k");
+  s.rows = k.size(0);
+  const ScalarType t = k.scalar_type();
+  expect(a[7], "k", t, {s.rows, hkv, d});
+  const at::Tensor &v = expect(a[8], "v", t, {s.rows, hkv, d});
+  s.k = k.data_ptr();
+  s.k_row_stride = k.stride(0);
+  s.k_head_stride = k.stride(1);
+  s.v = v.data_ptr();
+  s.v_row_stride = v.stride(0);
+  s.v_head_stride = v.stride(1);
+  s.n = tensor(a[5], "doc_ids").numel();
+  vector(a[5], "doc_ids", ScalarType::Int, s.n, s.doc_ids);
+  vector(a[6], "src_cu_slots", ScalarType::Long, s.n + 1, s.src_cu_slots);
+  const int64_t half = tensor(a[9], "inv_freq").numel();
+  vector(a[9], "inv_freq", ScalarType::Float, half, s.inv_freq);
+  s.rotary_dim = (int32_t)std::min<int64_t>(2 * half, INT32_MAX - 1);
+  vector(a[10], "positions", ScalarType::Int, s.rows, s.positions);
+  vector(a[11], "k_norm_w", t, d, s.k_norm_w);
+  const char *names[] = {"doc_ids", "src_cu_slots", "k",        "v",
+                         "inv_freq", "positions",    "k_norm_w"};
+  for (int i = 0; i < 7; ++i)
+    if (a[5 + i] != Py_None && tensor(a[5 + i], names[i]).device().index() !=
+                                   device) {
+      PyErr_Format(PyExc_ValueError, "%s must be on the store's device",
+                   names[i]);
+      throw Refused{};
+    }
+  s.interleaved = flag(a[12]);
+  s.attention_factor = real(a[13]);
+  s.rms_eps = real(a[14]);
+  void *store = PyLong_AsVoidPtr(a[0]);
+  if (!store && PyErr_Occurred()) throw Refused{};
+  return PyLong_FromLong(dopr_store_put_rotary(
+      static_cast<dopr_store_t>(store), &s, handle(a[15])));
+}
+
 template <PyObject *(*call)(PyObject *const *), Py_ssize_t count>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
   if (n != count) {
@@ -287,6 +344,7 @@ PyMethodDef methods[] = {DOPR_ENTRY(quantize_rows, 5),
                          DOPR_ENTRY(quant_matmul, 9),
                          DOPR_ENTRY(norm_residual, 12),
                          DOPR_ENTRY(rotary, 13),
+                         DOPR_ENTRY(store_put_rotary, 16),
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT,
