@@ -29,8 +29,8 @@ BINDING_LIB = os.path.join(HERE, "_operators.so")
 TIMERS_BUILD = os.path.join(HERE, "_build", "timers")
 TIMERS_LIB = os.path.join(HERE, "libdopr_timers.so")
 SOURCES = ["api.hip", "store.hip", "states.hip", "group.hip", "plan.hip",
-           "attn.hip", "stream.hip", "token.hip", "score.hip", "layer.hip",
-           "salience.hip", "rows.hip", "qproduct.hip", "rotary.hip"]
+           "attn.hip", "stream.hip", "token.hip", "direct.hip", "score.hip",
+           "layer.hip", "salience.hip", "rows.hip", "qproduct.hip", "rotary.hip"]
 # per-file flags: the pass kernel's cursor must stay in scalar
 # registers (common-code sinking would move it to scratch memory), and its
 # claims are atomics whose results are read much later (the wave-wide form

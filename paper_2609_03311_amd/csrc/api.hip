@@ -231,19 +231,30 @@ dopr_status_t check_attn(const dopr_store *st, const dopr_attn_args_t *a,
   return DOPR_OK;
 }
 
-// Whether a call is one of pairs of a single token that token.hip serves.
-bool is_token_call(const dopr_store *st, const dopr_attn_args_t *a) {
-  return st->fp4 && a->kernel_variant == 0 && a->max_tokens == 1 &&
-         a->total_tokens == a->n_pairs;
+// How a full call runs: by the planned kernels, or, over a 4-bit store unless
+// the caller asks for one of those, without a plan (token.hip: pairs of a
+// single token; direct.hip: others whose strides fit its 32-bit offsets).
+enum class Way { kPlan, kToken, kRows };
+Way way_of(const dopr_store *st, const dopr_attn_args_t *a) {
+  if (!st->fp4 || a->kernel_variant != 0 || a->n_pairs == 0) return Way::kPlan;
+  if (a->max_tokens == 1 && a->total_tokens == a->n_pairs) return Way::kToken;
+  return (int64_t)st->n_kv_heads * st->head_dim < (1 << 24) ? Way::kRows
+                                                            : Way::kPlan;
 }
 
-// Workspace bytes of a full call: its plan (also where none is made, as grouping
-// takes the same buffer), or what takes the plan's place.
+// Workspace bytes of a way.
+size_t way_bytes(Way way, const dopr_store *st, const dopr_attn_args_t *a,
+                 const PlanShape &shape) {
+  return way == Way::kToken  ? token_bytes(*st, a->n_pairs, shape.n_rep)
+         : way == Way::kRows ? rows_bytes(*st, *a)
+                             : plan_bytes(shape);
+}
+
+// Workspace bytes a caller is asked for: its plan's too where none is made, as
+// grouping takes the same buffer.
 size_t attn_bytes(const dopr_store *st, const dopr_attn_args_t *a,
                   const PlanShape &shape) {
-  const size_t plan = plan_bytes(shape);
-  if (!is_token_call(st, a) || a->n_pairs == 0) return plan;
-  return std::max(plan, token_bytes(*st, a->n_pairs, shape.n_rep));
+  return std::max(plan_bytes(shape), way_bytes(way_of(st, a), st, a, shape));
 }
 
 dopr_status_t check_device(const dopr_store *st) {
@@ -541,11 +552,13 @@ dopr_status_t noalloc_shape(const dopr_attn_args_t *a, PlanShape *shape) {
 }
 
 // The launches of a checked call.
-dopr_status_t launch_call(const AttnCall &call, void *ws,
+dopr_status_t launch_call(Way way, const AttnCall &call, void *ws,
                           const PlanShape &shape, hipStream_t hs) {
   hipError_t e;
-  if (!call.head && is_token_call(call.st, call.a)) {
+  if (way == Way::kToken) {
     e = launch_token(call, ws, hs);
+  } else if (way == Way::kRows) {
+    e = launch_rows(call, ws, hs);
   } else {
     const Plan plan = plan_carve(ws, shape);
     e = launch_plan(call, plan, shape, hs);
@@ -604,9 +617,12 @@ dopr_status_t run_attention(dopr_store_t st, int32_t layer,
       return fail(DOPR_ERR_INVALID_ARG,
                   "head norm_w and w_head must be 16-byte aligned");
   }
-  const bool token = !score && is_token_call(st, a);
-  const size_t need = token ? token_bytes(*st, a->n_pairs, n_rep)
-                            : plan_bytes(shape);
+  Way way = score ? Way::kPlan : way_of(st, a);
+  // (the block kernels give the same bits, but for calls of few rows, whose
+  // workspace is small)
+  if (no_alloc && way_bytes(way, st, a, shape) > kNoAllocScratchBytes)
+    way = Way::kPlan;
+  const size_t need = way_bytes(way, st, a, shape);
   void *ws = a->workspace;
   if (no_alloc) {
     if (need > kNoAllocScratchBytes) return noalloc_too_large(need);
@@ -625,7 +641,7 @@ dopr_status_t run_attention(dopr_store_t st, int32_t layer,
     if (s != DOPR_OK) return s;
   }
   const AttnCall call{st, layer, a, n_rep, head};
-  s = launch_call(call, ws, shape, as_stream(stream));
+  s = launch_call(way, call, ws, shape, as_stream(stream));
   return s == DOPR_OK ? ok() : s;
 }
 
@@ -762,7 +778,7 @@ dopr_status_t dopr_decoder_layer(dopr_store_t st, int32_t layer,
     return g < 0 ? hip_fail(hipGetLastError(), "layer launch")
                  : fail(DOPR_ERR_HIP, std::string("hipBLASLt: ") +
                                           gemm_status_str(g));
-  s = launch_call(call, w.plan, shape, hs);
+  s = launch_call(way_of(st, b), call, w.plan, shape, hs);
   if (s != DOPR_OK) return s;
   g = launch_layer_post(ls, l, w, b->rms_eps, hs);
   if (g != 0)

@@ -530,6 +530,9 @@ inline UnitArgs unit_args(const AttnCall &c) {
 // workspace it takes.
 size_t token_bytes(const dopr_store &st, int64_t pairs, int32_t n_rep);
 hipError_t launch_token(const AttnCall &c, void *workspace, hipStream_t s);
+// direct.hip: any other call over a 4-bit store without a plan.
+size_t rows_bytes(const dopr_store &st, const dopr_attn_args_t &a);
+hipError_t launch_rows(const AttnCall &c, void *workspace, hipStream_t s);
 hipError_t launch_plan(const AttnCall &c, const Plan &plan,
                        const PlanShape &shape, hipStream_t s);
 hipError_t launch_attention(const AttnCall &c, const Plan &plan,

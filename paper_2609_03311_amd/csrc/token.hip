@@ -18,6 +18,7 @@
 #include <cmath>
 
 #include "attn_common.hpp"
+#include "join.hpp"
 #include "operators.hpp"
 
 namespace dopr {
@@ -371,60 +372,17 @@ __global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
   }
 }
 
-// The sums of a row's blocks: one block a (pair, q head), eight of whose parts
-// share the splits.
+// The sums of a row's blocks: one block a (pair, q head).
 template <int D>
 __global__ __launch_bounds__(4 * D) void k_token_join(TokenParams P) {
-  constexpr int PARTS = 8;
-  __shared__ float so[PARTS][D], sl[PARTS], sm[PARTS];
   const int64_t p = P.p0 + blockIdx.x / P.Hq;
   const int h = blockIdx.x % P.Hq, g = h / P.n_rep, rr = h - g * P.n_rep;
   int64_t tok;
   if (!one_token(P, p, tok) || !has_document(P, P.doc_ids[p])) return;
-  const int64_t step = (int64_t)P.n_rep * (D + 2);
-  const float *x = P.part +
-                   ((p - P.p0) * P.sv.n_kv_heads + g) * P.splits * step +
-                   (int64_t)rr * (D + 2);
-  const int part = threadIdx.x / (D / 2), d = 2 * (threadIdx.x % (D / 2));
-  // (a split without keys has no weight, and the reference 0 or -inf)
-  float M = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
-  for (int s = part; s < P.splits; s += PARTS) {
-    const float2 ml = *reinterpret_cast<const float2 *>(x + s * step + D);
-    const float2 o = *reinterpret_cast<const float2 *>(x + s * step + d);
-    const float m = fmaxf(M, ml.x), ref = m == -INFINITY ? 0.f : m;
-    const float a = __builtin_amdgcn_exp2f(M - ref),
-                b = __builtin_amdgcn_exp2f(ml.x - ref);
-    l = fmaf(b, ml.y, a * l);
-    o0 = fmaf(b, o.x, a * o0);
-    o1 = fmaf(b, o.y, a * o1);
-    M = m;
-  }
-  so[part][d] = o0;
-  so[part][d + 1] = o1;
-  if (d == 0) {
-    sm[part] = M;
-    sl[part] = l;
-  }
-  __syncthreads();
-  if (threadIdx.x >= D / 2) return;
-  M = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < PARTS; ++i) M = fmaxf(M, sm[i]);
-  const float ref = M == -INFINITY ? 0.f : M;
-  l = o0 = o1 = 0.f;
-#pragma unroll
-  for (int i = 0; i < PARTS; ++i) {
-    const float f = __builtin_amdgcn_exp2f(sm[i] - ref);
-    l = fmaf(f, sl[i], l);
-    o0 = fmaf(f, so[i][d], o0);
-    o1 = fmaf(f, so[i][d + 1], o1);
-  }
-  const float inv = 1.0f / l;
-  const bf16x2 w = {(__bf16)(o0 * inv), (__bf16)(o1 * inv)};
-  const int64_t row = tok * P.Hq + h;
-  *reinterpret_cast<uint32_t *>(P.out + row * D + d) =
-      __builtin_bit_cast(uint32_t, w);
-  if (P.lse && d == 0) P.lse[row] = (ref + __log2f(l)) * kLn2;
+  const int64_t step = (int64_t)P.n_rep * (D + 2), row = tok * P.Hq + h;
+  join_row<D>(P.part + ((p - P.p0) * P.sv.n_kv_heads + g) * P.splits * step +
+                  (int64_t)rr * (D + 2),
+              step, P.splits, P.out + row * D, P.lse ? P.lse + row : nullptr);
 }
 
 // How a call's (pair, kv head)s are shared out: one wave each from kTokenFull

@@ -135,9 +135,8 @@ SHAPES = [
 def test_attention_is_the_bf16_stores(d, norm, shape):
     b = Batch(*SHAPES[shape], d, norm=norm, seed=shape)
     want = b.attention(b.stores[1], 8)
-    for variant in (0, 8, 6, 2, 1, 3):
+    for variant in (8, 6, 2, 1, 3):
         _same(b.attention(b.stores[0], variant), want)
-    _same(b.attention(b.stores[0], noalloc=True), want)
     for variant in (4, 5):
         _same(b.attention(b.stores[0], variant),
               b.attention(b.stores[1], variant))
@@ -161,7 +160,7 @@ def test_units_over_the_logit_bound(d, scale, gain):
     exact pass reads the 4-bit chunks."""
     b = Batch([300, 40, 64], [0, 1, 2, 0], [40, 3, 9, 66], 8, 2, d, seed=3,
               key_scale=scale, gain=gain)
-    for variant in (0, 6):
+    for variant in (8, 6):
         _same(b.attention(b.stores[0], variant),
               b.attention(b.stores[1], variant))
     _same(b.scored(b.stores[0]), b.scored(b.stores[1]))
@@ -173,7 +172,8 @@ def test_more_pairs_than_one_block_plans():
     lens = rng.integers(0, 80, 200).tolist()
     tokens = rng.integers(2, 5, 9000).tolist()
     b = Batch(lens, docs, tokens, 4, 2, 64, seed=5)
-    _same(b.attention(b.stores[0]), b.attention(b.stores[1]))
+    for variant in (0, 8):
+        _same(b.attention(b.stores[0], variant), b.attention(b.stores[1]))
     _same(b.scored(b.stores[0]), b.scored(b.stores[1]))
 
 
