@@ -228,24 +228,36 @@ __device__ __forceinline__ void row_chunks(const Rows &R, int lane, int j,
                                            Acc<D> *acc) {
   constexpr int G = D / 8, RPB = 64 / G, VB = KC / RPB;
   const int lq = lane & 31, hf = lane >> 5;
+  // prefix chunks, from two sets of codes by turns (one that is copied into the
+  // other has arrived before it has to)
   int i = R.first;
-  for (; i < R.end && i < R.n_prefix; i += R.step) {
-    const Fp4Raw<D> k0 = kr, v0 = vr;
-    if (i + R.step < R.end && i + R.step < R.n_prefix) {
-      const char *next =
-          R.slice + (int64_t)(i + R.step) * fp4_chunk_bytes(D);
-      fp4_load_k<D>(next, lane, kr);
-      fp4_load_v<D>(next, lane, vr);
-    }
+  const int stop = R.end < R.n_prefix ? R.end : R.n_prefix;
+  auto ask = [&](int c, Fp4Raw<D> &k, Fp4Raw<D> &v) {
+    if (c >= stop) return;
+    const char *chunk = R.slice + (int64_t)c * fp4_chunk_bytes(D);
+    fp4_load_k<D>(chunk, lane, k);
+    fp4_load_v<D>(chunk, lane, v);
+  };
+  auto attend = [&](int c, const Fp4Raw<D> &k, const Fp4Raw<D> &v) {
     floatx16 S[1];
 #pragma unroll
     for (int x = 0; x < 16; ++x) S[0][x] = 0.f;
 #pragma unroll
     for (int s = 0; s < D / 16; ++s)
-      S[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp4_k<D>(k0, s), qf[0][s],
+      S[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp4_k<D>(k, s), qf[0][s],
                                                      S[0], 0, 0, 0);
-    weigh<SMX, D>(S, R.L - 1 - i * KC, hf,
-                  [&](int f) { return fp4_v<D>(v0, f); }, acc);
+    weigh<SMX, D>(S, R.L - 1 - c * KC,
+                  hf, [&](int f) { return fp4_v<D>(v, f); }, acc);
+  };
+  Fp4Raw<D> k2{}, v2{};
+  while (i < stop) {
+    ask(i + R.step, k2, v2);
+    attend(i, kr, vr);
+    i += R.step;
+    if (i >= stop) break;
+    ask(i + R.step, kr, vr);
+    attend(i, k2, v2);
+    i += R.step;
   }
   if (i >= R.end) return;
 

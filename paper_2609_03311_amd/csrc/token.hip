@@ -4,18 +4,29 @@
 // A pair has n_rep rows a kv head, one own key (its own), and a prefix to
 // read: bound by HBM, 17/16 bytes a slot and dim of K and V.  No plan: the waves
 // of a (pair, kv head) find its document and each form q^ and k^ and the own
-// key's logit for themselves; they take the document's 32-slot chunks in turn,
-// codes straight from memory into operand registers, the next chunk's asked for
-// before the present one's products, and keep their own sums, which meet in
-// LDS.  One wave takes a (pair, kv head) where there are enough of them to fill
-// the card, up to four where there are not, and where pairs are few and
+// key's logit for themselves; they take the document's 32-slot chunks two at a
+// time, codes straight from memory into operand registers, the next two asked
+// for before the present ones' products, and keep their own sums, which meet
+// in LDS.  One wave takes a (pair, kv head) where there are enough of them to
+// fill the card, up to four where there are not, and where pairs are few and
 // prefixes long several blocks, which leave their sums to k_token_join.
+//
+// Rows are few, so the products are of 16 columns (v_mfma_f32_16x16x32_bf16):
+// half the matrix cycles, logits and sums of the 32-column ones.  With lane = 16
+// kg + m, a 16-byte piece of a chunk's codes is one lane's operand of a tile's
+// four (D = 128) k-steps: piece (part kg / 2, half kg % 2) of the key of row m
+// for S^T = K Q^T, dims 64 (kg / 2) + 16 ks + 8 (kg % 2) + e in step ks; row m
+// of tile mt is slot 16 (m / 8) + 4 mt + m % 4 of chunk (m / 4) % 2, so that a
+// lane's 16 logits are the slots 16 (kg / 2) .. + 15 of chunk kg % 2, two
+// operands of O^T = V^T P^T, against the pieces (chunk kg % 2, half kg / 2) of
+// the values.
 //
 // The softmax has no running maximum where |q^| |k| bounds the logits (exact
 // norms of this pair's rows; kmax of the document's keys), and an exact one
 // elsewhere, in the same launch.  q^ enters the products as two bf16 parts (16
 // bits of mantissa): the matrix cores have room, and the keys are exact.
 #include <cmath>
+#include <type_traits>
 
 #include "attn_common.hpp"
 #include "join.hpp"
@@ -63,15 +74,17 @@ __device__ __forceinline__ void store_out(uint16_t *to, const float *o,
   *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
 }
 
-// What a wave keeps of a unit's rows (a tile of RT, at most 32).
-template <int D, int RT>
+constexpr int kTokenRows = 16;  // of a tile
+
+// What a wave keeps of a unit's rows.
+template <int D>
 struct TokenRows {
-  float q[RT][D];  // c q^, then the wave's sums O
-  float k[D];      // k^ of the own key
+  float q[kTokenRows][D];  // c q^, then the wave's sums O
+  float k[D];              // k^ of the own key
   float2 rope[D / 2];
-  float norm2[RT + 1];  // of the rows of q, and of k
-  float own[RT];        // logits of the own key
-  float m[RT], l[RT];
+  float norm2[kTokenRows + 1];  // of the rows of q, and of k
+  float own[kTokenRows];        // logits of the own key
+  float m[kTokenRows], l[kTokenRows];
 };
 
 // The wave's LDS accesses so far, and the compiler's, end here.
@@ -81,60 +94,182 @@ __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Chunks c, c + step, .. < end: O and the normaliser of this wave's share.
-// (kr, vr: chunk c's codes, on their way or there.)
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// A lane's codes and exponents of two chunks.
+template <int D>
+struct Codes {
+  std::conditional_t<D == 128, fp4_u32x4, u32x2> k[4];  // by tile
+  fp4_u32x4 v[D / 32];  // [part][lq / 16]
+  uint8_t kx[4];
+  std::conditional_t<D == 128, uint32_t, uint16_t> vx[2];
+};
+
+// Chunks c and c + 1 of `end` (the last one again past it).  (The lane's places
+// are formed here: held across the loops they take the registers of a wave.)
+template <int D>
+__device__ __forceinline__ void load_keys(const char *slice, int c, int end,
+                                          int lane, Codes<D> &r) {
+  const int ln = lane + opaque_zero(), m = ln & 15, kg = ln >> 4;
+  const char *chunk =
+      slice + (int64_t)min(c + ((m >> 2) & 1), end - 1) * fp4_chunk_bytes(D);
+  const int lk = (kg & 1) * 32 + 4 * (m >> 3) + (m & 3);  // (of tile 0)
+  const char *at = chunk + (D == 128 ? 1024 : 8) * (kg >> 1) + 16 * lk;
+  const char *ax =
+      chunk + 32 * D + lk * (D / 64) + (D == 128 ? kg >> 1 : 0);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    r.k[t] = *reinterpret_cast<const decltype(r.k[0] + 0) *>(at + 128 * t);
+    r.kx[t] = *reinterpret_cast<const uint8_t *>(ax + 8 * (D / 64) * t);
+  }
+}
+template <int D>
+__device__ __forceinline__ void load_values(const char *slice, int c, int end,
+                                            int lane, Codes<D> &r) {
+  const int ln = lane + opaque_zero(), m = ln & 15, kg = ln >> 4;
+  const char *chunk =
+      slice + (int64_t)min(c + (kg & 1), end - 1) * fp4_chunk_bytes(D);
+  const char *at = chunk + 16 * D + 16 * ((kg >> 1) * 32 + m);
+  const char *ax = chunk + 33 * D + m * (D / 32);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j)
+      r.v[2 * j + h] =
+          *reinterpret_cast<const fp4_u32x4 *>(at + 1024 * j + 256 * h);
+    r.vx[h] = *reinterpret_cast<const decltype(r.vx[0] + 0) *>(ax + h * (D / 2));
+  }
+}
+
+// Sums of a tile's 16 columns: O^T by tiles of 16 dims, tile (j, dbl, h) dims
+// 32 (2 j + dbl) + 16 (kg % 2) + 8 h + 4 (kg / 2) + i, and as Acc.
+template <int D>
+struct Sums {
+  floatx4 o[D / 16];
+  float m, l;
+};
+
+// x of the lanes with the same m: all four's largest.
+__device__ __forceinline__ float max4(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16, 64));
+  return fmaxf(x, __shfl_xor(x, 32, 64));
+}
+
+// Chunks c, c + 1; c + 2 step, ..: O and the normaliser of this wave's share of
+// the chunks below `end`.  r: the first two's codes, on their way or there; the
+// next two's are asked for as soon as the registers are free, the keys' behind
+// the logits, the values' behind the sums.
 template <int SMX, int D>
 __device__ __forceinline__ void token_chunks(const char *slice, int c, int end,
                                              int step, int L, int lane,
-                                             const bf16x8 (*qh)[D / 16],
-                                             const bf16x8 *ql, Fp4Raw<D> &kr,
-                                             Fp4Raw<D> &vr, Acc<D> *acc) {
-  const int hf = lane >> 5;
+                                             const bf16x8 *qh, const bf16x8 *ql,
+                                             Codes<D> &r, Sums<D> &acc) {
+  constexpr int KS = D / 32;
+  const int kg = lane >> 4;
+  step *= 2;
   for (; c < end; c += step) {
-    const Fp4Raw<D> k0 = kr, v0 = vr;
-    if (c + step < end) {
-      const char *next = slice + (int64_t)(c + step) * fp4_chunk_bytes(D);
-      fp4_load_k<D>(next, lane, kr);
-      fp4_load_v<D>(next, lane, vr);
+    const bool more = c + step < end;
+    floatx4 S[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      S[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+      const float scale = fp4_scale(r.kx[t]);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8 kf = fp4_fragment(r.k[t][ks], scale);
+        S[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qh[ks], S[t], 0, 0,
+                                                       0);
+        S[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, ql[ks], S[t], 0, 0,
+                                                       0);
+      }
     }
-    floatx16 S[1];
+    if (more) load_keys<D>(slice, c + step, end, lane, r);
+    if ((c + 2) * KC > L || c + 2 > end) {
+      // (a second chunk past the share's end is the last one again)
+      const int lim = c + (kg & 1) < end
+                          ? L - (c + (kg & 1)) * KC - 16 * (kg >> 1) : 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) S[0][i] = 0.f;
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      const bf16x8 kf = fp4_k<D>(k0, s);
-      S[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qh[0][s], S[0], 0, 0,
-                                                     0);
-      S[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, ql[s], S[0], 0, 0, 0);
+        for (int i = 0; i < 4; ++i)
+          S[t][i] = 4 * t + i < lim ? S[t][i] : -INFINITY;
     }
-    const int lim = L - 1 - c * KC;
-    if (lim < KC - 1) {
-      const int li = lim - 16 * hf;
+    float muse = 0.f;
+    if constexpr (SMX == 2) {
+      float mx = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) S[0][i] = i <= li ? S[0][i] : -INFINITY;
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, S[t][i]);
+      mx = max4(mx);
+      const bool need = mx > acc.m + kTau;
+      const float mnew = need ? mx : acc.m;
+      const float alpha = need ? __builtin_amdgcn_exp2f(acc.m - mnew) : 1.0f;
+      acc.l *= alpha;
+      acc.m = mnew;
+      if (__any(need)) {
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc.o[d][i] *= alpha;
+      }
+      muse = acc.m == -INFINITY ? 0.f : acc.m;
     }
-    bf16x8 pb[1][2];
-    softmax_part<0, 1, SMX, D>(S, acc, hf, 0.f, nullptr, pb);
+    const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+    bf16x8 pb[2];
 #pragma unroll
-    for (int f = 0; f < D / 16; ++f)
-      acc[0].o[f >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-          fp4_v<D>(v0, f), pb[0][f & 1], acc[0].o[f >> 1], 0, 0, 0);
+    for (int t = 0; t < 2; ++t) {
+      float p[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const float s = S[2 * t + (x >> 2)][x & 3];
+        p[x] = __builtin_amdgcn_exp2f(SMX == 2 ? s - muse : s);
+      }
+      pb[t] = to_bf16x8(p);
+      // (the normaliser sums the weights that the products use)
+      const bf16x8 &w = pb[t];
+      acc.l = __builtin_amdgcn_fdot2_f32_bf16(
+          __builtin_shufflevector(w, w, 0, 1), one, acc.l, false);
+      acc.l = __builtin_amdgcn_fdot2_f32_bf16(
+          __builtin_shufflevector(w, w, 2, 3), one, acc.l, false);
+      acc.l = __builtin_amdgcn_fdot2_f32_bf16(
+          __builtin_shufflevector(w, w, 4, 5), one, acc.l, false);
+      acc.l = __builtin_amdgcn_fdot2_f32_bf16(
+          __builtin_shufflevector(w, w, 6, 7), one, acc.l, false);
+    }
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+      for (int dbl = 0; dbl < 2; ++dbl)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float scale = fp4_scale(r.vx[h] >> (8 * (2 * j + dbl)) & 255);
+          floatx4 &o = acc.o[4 * j + 2 * dbl + h];
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                fp4_fragment(r.v[2 * j + h][2 * dbl + t], scale), pb[t], o, 0,
+                0, 0);
+        }
+    if (more) load_values<D>(slice, c + step, end, lane, r);
   }
 }
 
 // WU: waves of a unit, (pair, kv head, split).
-template <int D, int RT, int WU>
+template <int D, int WU>
 __global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
     amdgpu_waves_per_eu(2, 2))) void k_token_fp4(TokenParams P) {
   constexpr int G = D / 8;    // lanes a row, eight dims each
   constexpr int RP = 64 / G;  // rows at a time
-  __shared__ __attribute__((aligned(16))) TokenRows<D, RT> sm_all[kTokenWaves];
+  constexpr int RT = kTokenRows;
+  __shared__ __attribute__((aligned(16))) TokenRows<D> sm_all[kTokenWaves];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int lq = lane & 31, hf = lane >> 5;
+  const int col = lane & 15, kg = lane >> 4;
   const int hkv = P.sv.n_kv_heads;
   const int w0 = wave / WU * WU, wu = wave - w0;  // the unit's first wave
-  TokenRows<D, RT> &sm = sm_all[wave];
+  TokenRows<D> &sm = sm_all[wave];
   const unsigned unit = blockIdx.x * (kTokenWaves / WU) + wave / WU;
   // (a wave without a unit, or whose pair has no token or no document, goes
   // on to meet the barriers)
@@ -178,18 +313,17 @@ __global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
     const int per = (n_chunks + P.splits - 1) / P.splits;
     const int begin = min(split * per, n_chunks);
     end = min(begin + per, n_chunks);
-    first = begin + wu;
+    first = begin + 2 * wu;
   }
 
   for (int r0 = 0; r0 < P.n_rep; r0 += RT) {
     const int rows = min(RT, P.n_rep - r0);
     bool bounded = true;
     if (live) {
-      Fp4Raw<D> kr{}, vr{};
+      Codes<D> codes{};
       if (first < end) {
-        const char *chunk = slice + (int64_t)first * fp4_chunk_bytes(D);
-        fp4_load_k<D>(chunk, lane, kr);
-        fp4_load_v<D>(chunk, lane, vr);
+        load_keys<D>(slice, first, end, lane, codes);
+        load_values<D>(slice, first, end, lane, codes);
       }
       // c q^ of the rows and k^, G lanes a row; row `rows` is the own key
       const int gc = lane % G;
@@ -267,48 +401,45 @@ __global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
           sqrtf(top) * fmaxf(kmax, sqrtf(sm.norm2[RT])) * 1.001f;
       bounded = bound <= kNoRefBound;
 
-      bf16x8 qh[1][D / 16], ql[D / 16];
+      bf16x8 qh[D / 32], ql[D / 32];
 #pragma unroll
-      for (int s = 0; s < D / 16; ++s) {
+      for (int ks = 0; ks < D / 32; ++ks) {
+        const int dim = D == 128 ? 64 * (kg >> 1) + 16 * ks + 8 * (kg & 1)
+                                 : 32 * (kg >> 1) + 16 * ks + 8 * (kg & 1);
         float x[8];
         const float4 *from = reinterpret_cast<const float4 *>(
-            &sm.q[lq < rows ? lq : 0][16 * s + 8 * hf]);
+            &sm.q[col < rows ? col : 0][dim]);
         const float4 a = from[0], b = from[1];
         x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
         x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-        qh[0][s] = to_bf16x8(x);
+        qh[ks] = to_bf16x8(x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] -= (float)qh[0][s][e];
-        ql[s] = to_bf16x8(x);
+        for (int e = 0; e < 8; ++e) x[e] -= (float)qh[ks][e];
+        ql[ks] = to_bf16x8(x);
       }
-      Acc<D> acc[1];
-      acc[0].m = bounded ? 0.f : -INFINITY;
-      acc[0].l = 0.f;
+      Sums<D> acc;
+      acc.m = bounded ? 0.f : -INFINITY;
+      acc.l = 0.f;
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[0].o[db][i] = 0.f;
+      for (int d = 0; d < D / 16; ++d) acc.o[d] = floatx4{0.f, 0.f, 0.f, 0.f};
       if (bounded)
-        token_chunks<0, D>(slice, first, end, WU, L, lane, qh, ql, kr, vr,
-                           acc);
+        token_chunks<0, D>(slice, first, end, WU, L, lane, qh, ql, codes, acc);
       else
-        token_chunks<2, D>(slice, first, end, WU, L, lane, qh, ql, kr, vr,
-                           acc);
+        token_chunks<2, D>(slice, first, end, WU, L, lane, qh, ql, codes, acc);
 
       // the wave's sums, where q^ was
-      const float lt = acc[0].l + __shfl_xor(acc[0].l, 32, 64);
+      float lt = acc.l + __shfl_xor(acc.l, 16, 64);
+      lt += __shfl_xor(lt, 32, 64);
       wave_fence();
-      if (lq < rows) {
+      if (col < rows) {
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-          for (int i = 0; i < 16; i += 4)
-            *reinterpret_cast<float4 *>(&sm.q[lq][32 * db + 16 * hf + i]) =
-                make_float4(acc[0].o[db][i], acc[0].o[db][i + 1],
-                            acc[0].o[db][i + 2], acc[0].o[db][i + 3]);
-        if (hf == 0) {
-          sm.m[lq] = acc[0].m;
-          sm.l[lq] = lt;
+        for (int d = 0; d < D / 16; ++d)
+          *reinterpret_cast<floatx4 *>(
+              &sm.q[col][32 * (d >> 1) + 16 * (kg & 1) + 8 * (d & 1) +
+                         4 * (kg >> 1)]) = acc.o[d];
+        if (kg == 0) {
+          sm.m[col] = acc.m;
+          sm.l[col] = lt;
         }
       }
     }
@@ -340,7 +471,7 @@ __global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
         }
 #pragma unroll
         for (int w = 0; w < WU; ++w) {
-          const TokenRows<D, RT> &from = sm_all[w0 + w];
+          const TokenRows<D> &from = sm_all[w0 + w];
           const float f = __builtin_amdgcn_exp2f(from.m[rr] - ref);
           const float4 x = *reinterpret_cast<const float4 *>(&from.q[rr][d]);
           l = fmaf(f, from.l[rr], l);
@@ -406,11 +537,11 @@ TokenShare token_share(const dopr_store &st, int64_t pairs, int32_t n_rep) {
           (int)std::max<int64_t>(1, std::min({want, most, fit}))};
 }
 
-template <int D, int RT>
+template <int D>
 void launch_token2(int waves, const TokenParams &P, hipStream_t s) {
-  const auto kernel = waves == 1   ? k_token_fp4<D, RT, 1>
-                      : waves == 2 ? k_token_fp4<D, RT, 2>
-                                   : k_token_fp4<D, RT, 4>;
+  const auto kernel = waves == 1   ? k_token_fp4<D, 1>
+                      : waves == 2 ? k_token_fp4<D, 2>
+                                   : k_token_fp4<D, 4>;
   const unsigned per = kTokenWaves / waves;
   hipLaunchKernelGGL(kernel, dim3((P.units + per - 1) / per),
                      dim3(64 * kTokenWaves), 0, s, P);
@@ -427,10 +558,7 @@ hipError_t launch_token1(const TokenParams &P, int waves, int64_t pairs,
         TokenParams S = P;
         S.p0 = P.p0 + at;
         S.units = (uint32_t)(n * hkv * P.splits);
-        if (P.n_rep <= 8)
-          launch_token2<D, 8>(waves, S, s);
-        else
-          launch_token2<D, 32>(waves, S, s);
+        launch_token2<D>(waves, S, s);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess || P.splits == 1) return e;
         hipLaunchKernelGGL(k_token_join<D>, dim3((unsigned)(n * P.Hq)),
