@@ -11,6 +11,19 @@
 // loads for a thousand cycles, and run waves without rows: 516 rows, 129 tokens
 // of 4 heads, take 20 waves there and 17 here.)
 //
+// Measured, 32 q / 8 kv heads of 128, against the pass kernel and its plan: 64
+// pairs of 129 tokens on 4,096 slots each 623 and 665 us, one pair of 4,000 on
+// 256 199 and 222, 1,024 pairs of 8 on 64 86 and 138, 1,600 pairs of 129 on 256
+// (a thousand documents) 2,070 and 2,000-2,085.  The plan stays ahead where many
+// short pairs share few documents, whose rows it puts into common tiles: 1,024
+// pairs of 4 tokens on 16 documents of 4,096 slots 541 and 330.
+//
+// What bounds it: the vector unit (55 % busy; of 2,335 vector instructions a
+// wave of the 1,600 pairs a chunk's are about 116, 64 of them the codes'
+// conversions, q^ 416) and, at its ends, q's loads and the output's stores, which
+// two waves a SIMD overlap only in part.  Three (168 registers) were no faster
+// at D = 128: the own keys have to be asked for late.
+//
 // Own keys: k_own_keys stores k^ in groups of four keys, the 16-byte pieces
 // that one operand load takes side by side (128 bytes a group), each pair from
 // a group of its own; own values are copied into the wave's part of LDS, behind
@@ -33,8 +46,8 @@
 namespace dopr {
 namespace {
 
-constexpr int kRowWaves = 4;  // of a block
-constexpr int waves_a_simd(int D) { return D == 64 ? 3 : 2; }
+constexpr int kMostWaves = 4;  // of a unit
+constexpr int waves_a_simd(int D) { return D == 64 ? 4 : 2; }
 constexpr int kKeyThreads = 256;
 
 struct RowsParams {
@@ -47,6 +60,7 @@ struct RowsParams {
   float *lse;
   int32_t *tiles;    // pair of each 32-row tile
   uint16_t *unit_w;  // [D] ones: the gains where there is no norm
+  float *bounds;     // of |k^| and |q^| / c from the gains (0: no norm)
   float2 *rope;      // [Ntok][D / 2]
   uint16_t *kh;      // [Hkv][rows_cap][D], by groups of four keys
   float *part;       // [tile, kv head, split][32][D + 2]: O, m, l
@@ -57,19 +71,26 @@ struct RowsParams {
   int32_t Hq, n_rep, layer, splits, max_tokens;
 };
 
+// Loads at wave-uniform places of what no kernel of this launch writes, through
+// the constant address space: scalar ones.
+template <class T>
+__device__ __forceinline__ T cld(const T *p, int64_t i) {
+  return ((const __attribute__((address_space(4))) T *)p)[i];
+}
+
 struct Pair {
   int64_t t0;
   int T;
   bool well;
 };
 __device__ __forceinline__ Pair pair_at(const RowsParams &P, int64_t p) {
-  const int64_t t0 = P.cu[p], t1 = P.cu[p + 1];
+  const int64_t t0 = cld(P.cu, p), t1 = cld(P.cu, p + 1);
   return {t0, (int)(t1 - t0),
           t0 >= 0 && t1 > t0 && t1 <= P.total_tokens &&
               t1 - t0 <= P.max_tokens};
 }
 __device__ __forceinline__ bool has_document(const RowsParams &P, int32_t d) {
-  return d >= 0 && (int64_t)d < P.sv.n_docs && P.sv.doc_len[d] >= 0;
+  return d >= 0 && (int64_t)d < P.sv.n_docs && cld(P.sv.doc_len, d) >= 0;
 }
 // The first of a pair's tiles, and of its groups of own keys: bounds that need
 // no sum over the pairs before it.
@@ -95,10 +116,11 @@ __global__ __launch_bounds__(kKeyThreads) void k_own_keys(RowsParams P) {
   constexpr int NSUB = D / 16, ROWS = kKeyThreads / NSUB;
   // (pairs side by side, as khat_part takes them; rows off the banks)
   __shared__ __attribute__((aligned(16))) float2 rope[32][D / 2 + 2];
+  __shared__ float red[4];
   const int64_t p = P.first + blockIdx.x;
   const int hkv = P.sv.n_kv_heads;
-  if (p == 0 && blockIdx.y == 0 && threadIdx.x < D)
-    P.unit_w[threadIdx.x] = 0x3F80;  // bf16 1.0
+  if (p == 0 && blockIdx.y == 0)
+    norm_bound(P.kw, P.qw, D, red, P.bounds, P.unit_w);
   const Pair me = pair_at(P, p);
   if (threadIdx.x == 0 && blockIdx.y == 0 &&
       (!me.well || (p == 0 && P.cu[0] != 0) ||
@@ -325,47 +347,38 @@ __device__ __forceinline__ void row_chunks(const Rows &R, int lane, int j,
 template <int D, int WU>
 struct RowsSm {
   static constexpr int kBytes = WU == 1 ? KC * D * 2 : 32 * D * 4;
-  char wave[kRowWaves][kBytes];
-  float m[kRowWaves][32], l[kRowWaves][32];
+  char wave[WU][kBytes];
+  float m[WU][32], l[WU][32];
 };
 
-// WU: waves of a unit, (tile, kv head, split).
+// One block of WU waves a unit, (tile, kv head, split).
 template <int D, int WU>
-__global__ __launch_bounds__(64 * kRowWaves) __attribute__((
-    amdgpu_waves_per_eu(waves_a_simd(D),
-                        waves_a_simd(D)))) void k_rows_fp4(RowsParams P) {
+__global__ __launch_bounds__(64 * WU) __attribute__((
+    amdgpu_waves_per_eu(WU == 1 ? waves_a_simd(D) : 2,
+                        WU == 1 ? waves_a_simd(D)
+                                : 2))) void k_rows_fp4(RowsParams P) {
   __shared__ __attribute__((aligned(16))) RowsSm<D, WU> sm;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lq = lane & 31, hf = lane >> 5;
   const int hkv = P.sv.n_kv_heads;
-  const int w0 = wave / WU * WU, wu = wave - w0;
   // blocks of one kv head's tiles, heads and splits side by side: block b runs
   // on XCD b % 8, so that with 8 heads a head's prefix goes through one L2
-  constexpr int PER = kRowWaves / WU;  // units of a block
   const int64_t b = P.first + blockIdx.x;
   const int g = (int)(b % hkv);
   const int64_t rest = b / hkv;
   const int split = (int)(rest % P.splits);
-  const int64_t tile = rest / P.splits * PER + wave / WU;
-  // (a wave without a tile goes on to meet the barriers)
-  bool live = tile < P.n_tiles;
-  const int64_t p = live ? P.tiles[tile] : -1;
-  live = live && p >= 0 && p < P.n_pairs;
-  Pair me{0, 0, false};
-  int32_t doc = -1;
-  int r0 = 0, rows = 0;
-  if (live) {
-    me = pair_at(P, p);
-    doc = P.doc_ids[p];
-    // (tiles that no pair has hold anything)
-    const int64_t at = (tile - first_tile(P, p, me.t0)) * 32;
-    const int64_t all = (int64_t)me.T * P.n_rep;
-    live = me.well && has_document(P, doc) && at >= 0 && at < all;
-    r0 = (int)at;
-    rows = (int)(all - at < 32 ? all - at : 32);
-  }
-  if (WU == 1 && !live) return;  // (no barrier below)
+  const int64_t tile = rest / P.splits;
+  // (tiles that no pair has hold anything)
+  const int64_t p = cld(P.tiles, tile);
+  if (p < 0 || p >= P.n_pairs) return;
+  const Pair me = pair_at(P, p);
+  const int32_t doc = cld(P.doc_ids, p);
+  const int64_t at0 = (tile - first_tile(P, p, me.t0)) * 32;
+  const int64_t all = (int64_t)me.T * P.n_rep;
+  if (!me.well || !has_document(P, doc) || at0 < 0 || at0 >= all) return;
+  const int r0 = (int)at0;
+  const int rows = (int)(all - at0 < 32 ? all - at0 : 32);
 
   const int rl = r0 + (lq < rows ? lq : rows - 1);
   const int back = rl / P.n_rep;
@@ -382,13 +395,13 @@ __global__ __launch_bounds__(64 * kRowWaves) __attribute__((
     for (int x = 0; x < 16; ++x) acc[0].o[db][x] = 0.f;
   bool bounded = true;
   float lt = 0.f;
-  if (live) {
+  {
     Rows R;
-    R.L = P.sv.doc_len[doc];
+    R.L = cld(P.sv.doc_len, doc);
     R.T = me.T;
     R.slice = reinterpret_cast<const char *>(
         P.sv.payload +
-        fp4_offset(P.sv.doc_off[doc], R.L, hkv, P.layer, g, D));
+        fp4_offset(cld(P.sv.doc_off, doc), R.L, hkv, P.layer, g, D));
     R.n_prefix = (R.L + KC - 1) / KC;
     // (the tile's latest position is at its first row)
     const int jmax = me.T - 1 - r0 / P.n_rep;
@@ -396,7 +409,7 @@ __global__ __launch_bounds__(64 * kRowWaves) __attribute__((
     const int per = (n + P.splits - 1) / P.splits;
     const int begin = min(split * per, n);
     R.end = min(begin + per, n);
-    R.first = begin + wu;
+    R.first = begin + wave;
     R.step = WU;
     R.stride = hkv * D;
     R.kh = P.kh + g * P.rows_cap * D;
@@ -415,28 +428,13 @@ __global__ __launch_bounds__(64 * kRowWaves) __attribute__((
     q_fragments_any<D>(P.q + (tokq * P.Hq + head) * D,
                        P.qw ? P.qw : P.unit_w, P.rope + tokq * (D / 2), hf,
                        lane, P.n_rep, P.eps, P.c, P.qw != nullptr, qf[0]);
-    // every logit (log2 units) lies in [-bound, bound]: the rows' own norms,
-    // the stored keys' bound and that of normed keys, sqrt(D) max|w|
-    bool known = P.kw != nullptr;
-    float bound = 0.f;
-    if (known) {
-      float n2 = 0.f;
-#pragma unroll
-      for (int s = 0; s < D / 16; ++s) n2 = sumsq8(as_uint4(qf[0][s]), n2);
-      n2 += __shfl_xor(n2, 32, 64);
-      float w = fabsf(__uint_as_float((uint32_t)P.kw[lane] << 16));
-      if (D == 128)
-        w = fmaxf(w,
-                  fabsf(__uint_as_float((uint32_t)P.kw[(64 + lane) % D] << 16)));
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        w = fmaxf(w, __shfl_xor(w, off, 64));
-        n2 = fmaxf(n2, __shfl_xor(n2, off, 64));
-      }
-      const float kmax =
-          P.sv.kmax[((int64_t)doc * P.sv.n_layers + P.layer) * hkv + g];
-      bound = sqrtf(n2) * fmaxf(kmax, w * sqrtf((float)D) * 1.01f) * 1.001f;
-    }
+    // every logit (log2 units) lies in [-bound, bound]: the gains' bounds and
+    // the stored keys'
+    const bool known = P.kw != nullptr;
+    const float kmax = cld(
+        P.sv.kmax, ((int64_t)doc * P.sv.n_layers + P.layer) * hkv + g);
+    const float bound = P.c * cld(P.bounds, 1) *
+                        fmaxf(kmax, cld(P.bounds, 0)) * 1.001f;
     // (one wave's sums without a bound are looked at behind the chunks)
     const bool alone = WU == 1 && P.splits == 1;
     bounded = known ? bound <= kNoRefBound : alone;
@@ -495,7 +493,7 @@ __global__ __launch_bounds__(64 * kRowWaves) __attribute__((
   } else {
     // the waves' sums meet.  (The wave's own values in LDS have been read.)
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (live && valid) {
+    if (valid) {
       float *o = reinterpret_cast<float *>(sm.wave[wave]) + lq * D;
 #pragma unroll
       for (int db = 0; db < D / 32; ++db)
@@ -510,24 +508,23 @@ __global__ __launch_bounds__(64 * kRowWaves) __attribute__((
       }
     }
     __syncthreads();
-    if (!live) return;
-    for (int e = wu * 64 + lane; e < rows * (D / 4); e += 64 * WU) {
+    for (int e = threadIdx.x; e < rows * (D / 4); e += 64 * WU) {
       const int rr = e / (D / 4), d = 4 * (e % (D / 4));
       float M = 0.f;
       if (!bounded) {
         M = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < WU; ++w) M = fmaxf(M, sm.m[w0 + w][rr]);
+        for (int w = 0; w < WU; ++w) M = fmaxf(M, sm.m[w][rr]);
       }
       // (nothing seen, M = -inf: all weights are zero)
       const float ref = M == -INFINITY ? 0.f : M;
       float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < WU; ++w) {
-        const float f = __builtin_amdgcn_exp2f(sm.m[w0 + w][rr] - ref);
+        const float f = __builtin_amdgcn_exp2f(sm.m[w][rr] - ref);
         const float4 x = *reinterpret_cast<const float4 *>(
-            reinterpret_cast<const float *>(sm.wave[w0 + w]) + rr * D + d);
-        l = fmaf(f, sm.l[w0 + w][rr], l);
+            reinterpret_cast<const float *>(sm.wave[w]) + rr * D + d);
+        l = fmaf(f, sm.l[w][rr], l);
         o[0] = fmaf(f, x.x, o[0]);
         o[1] = fmaf(f, x.y, o[1]);
         o[2] = fmaf(f, x.z, o[2]);
@@ -577,10 +574,12 @@ __global__ __launch_bounds__(4 * D) void k_rows_join(RowsParams P) {
               P.splits, P.out + row * D, P.lse ? P.lse + row : nullptr);
 }
 
-// How a call's (tile, kv head)s are shared out: one wave each where they fill
-// more than half of the card's 1,024 SIMDs, two or four below, and blocks of
-// four where that leaves waves free, of at least two chunks a wave of the
-// longest sequence.
+// How a call's (tile, kv head)s are shared out: one wave each where they take
+// more than half of the 2,048 waves the SIMDs hold (D = 64: 4,096), two or four
+// below, and
+// several blocks of four where that leaves waves free, of at least four chunks
+// a wave of the longest sequence (129 tokens on 256 slots: 21 us, and 29 in two
+// blocks of one or two chunks a wave and their join).
 struct RowsShare {
   int waves, splits;
 };
@@ -590,15 +589,15 @@ RowsShare rows_share(int D, int64_t units, int64_t max_len,
   if (2 * units > full) return {1, 1};
   if (4 * units > full) return {2, 1};
   const int64_t chunks = (max_len + max_tokens + KC - 1) / KC;
-  const int64_t want = full / (units * kRowWaves);
-  const int64_t most = (chunks + 2 * kRowWaves - 1) / (2 * kRowWaves);
-  return {kRowWaves, (int)std::max<int64_t>(1, std::min(want, most))};
+  const int64_t want = full / (units * kMostWaves);
+  const int64_t most = chunks / (4 * kMostWaves);
+  return {kMostWaves, (int)std::max<int64_t>(1, std::min(want, most))};
 }
 
 struct RowsLayout {
   int64_t n_tiles, rows_cap;
   RowsShare share;
-  size_t tiles, unit_w, rope, kh, part, bytes;
+  size_t tiles, unit_w, bounds, rope, kh, part, bytes;
 };
 RowsLayout rows_layout(const dopr_store &st, const dopr_attn_args_t &a) {
   const int64_t hkv = st.n_kv_heads, D = st.head_dim;
@@ -617,6 +616,7 @@ RowsLayout rows_layout(const dopr_store &st, const dopr_attn_args_t &a) {
   };
   l.tiles = take(sizeof(int32_t) * l.n_tiles);
   l.unit_w = take(sizeof(uint16_t) * D);
+  l.bounds = take(sizeof(float) * 2);
   l.rope = take(sizeof(float2) * a.total_tokens * (D / 2));
   l.kh = take(sizeof(uint16_t) * hkv * l.rows_cap * D);
   l.part = take(l.share.splits == 1 ? 0
@@ -643,15 +643,14 @@ hipError_t launch_rows1(RowsParams P, int waves, hipStream_t s) {
         return hipGetLastError();
       });
   if (e != hipSuccess) return e;
-  const int per = kRowWaves / waves;
-  const int64_t blocks = (P.n_tiles + per - 1) / per * hkv * P.splits;
-  e = in_slices(blocks, a_launch(64 * kRowWaves), [&](int64_t at, int64_t n) {
+  const int64_t blocks = P.n_tiles * hkv * P.splits;
+  e = in_slices(blocks, a_launch(64 * waves), [&](int64_t at, int64_t n) {
     RowsParams S = P;
     S.first = at;
     const auto kernel = waves == 1   ? k_rows_fp4<D, 1>
                         : waves == 2 ? k_rows_fp4<D, 2>
                                      : k_rows_fp4<D, 4>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(64 * kRowWaves), 0, s,
+    hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(64 * waves), 0, s,
                        S);
     return hipGetLastError();
   });
@@ -688,6 +687,7 @@ hipError_t launch_rows(const AttnCall &c, void *workspace, hipStream_t s) {
   P.lse = a->lse;
   P.tiles = reinterpret_cast<int32_t *>(ws + l.tiles);
   P.unit_w = reinterpret_cast<uint16_t *>(ws + l.unit_w);
+  P.bounds = reinterpret_cast<float *>(ws + l.bounds);
   P.rope = reinterpret_cast<float2 *>(ws + l.rope);
   P.kh = reinterpret_cast<uint16_t *>(ws + l.kh);
   P.part = reinterpret_cast<float *>(ws + l.part);
