@@ -1,6 +1,7 @@
-// binding.cpp -- the Python calls of the operators around the attention and of
-// dopr_store_put_rotary (module _operators): checks tensors, fills the C ABI's
-// argument structures and calls it.
+// binding.cpp -- the Python calls of the operators around the attention, of
+// dopr_store_put_rotary, dopr_prefix_attn and dopr_gather_prefix (module
+// _operators): checks tensors, fills the C ABI's argument structures and calls
+// it.
 //
 // The other entry points are marshalled in Python (ctypes).  These are a few
 // microseconds of GPU work at their smallest and take up to ten tensors of
@@ -14,6 +15,7 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <string>
 
 #include "dopr.h"
@@ -321,6 +323,90 @@ PyObject *store_put_rotary(PyObject *const *a) {
       static_cast<dopr_store_t>(store), &s, handle(a[15])));
 }
 
+// A tensor's address as it is (its caller keeps to the C ABI), NULL for None.
+template <typename P>
+void address(PyObject *o, const char *what, P &p) {
+  p = o == Py_None ? nullptr : static_cast<P>(tensor(o, what).data_ptr());
+}
+
+// An object's integer as the C type's lowest bits (as ctypes passes it), a
+// pointer's address with None for NULL.
+template <typename I>
+I bits(PyObject *o) {
+  PyObject *n = PyNumber_Long(o);
+  if (!n) throw Refused{};
+  const unsigned long long v = PyLong_AsUnsignedLongLongMask(n);
+  Py_DECREF(n);
+  if (v == ~0ull && PyErr_Occurred()) throw Refused{};
+  return (I)v;
+}
+
+void *pointer(PyObject *o) {
+  return o == Py_None ? nullptr : reinterpret_cast<void *>(bits<uintptr_t>(o));
+}
+
+PyObject *prefix_attn(PyObject *const *a) {
+  // store's handle, kv heads and head dim, layer, doc_ids, cu_seqlens, q, k, v,
+  // q_norm_w, k_norm_w, out, lse, workspace, max_tokens, total_tokens, rms_eps,
+  // rope_theta, softmax_scale, kernel_variant, timing begin and end,
+  // rope_inv_freq, rows_per_item, queue_order, stream
+  dopr_attn_args_t s{};
+  s.n_pairs = (int32_t)tensor(a[4], "doc_ids").numel();
+  address(a[4], "doc_ids", s.doc_ids);
+  address(a[5], "cu_seqlens", s.cu_seqlens);
+  s.n_q_heads = bits<int32_t>(a[1]);
+  if (a[6] != Py_None) {
+    const at::Tensor &q = tensor(a[6], "q");
+    if (q.dim() < 2) {
+      PyErr_SetString(PyExc_IndexError, "q must be [tokens, q heads, head dim]");
+      throw Refused{};
+    }
+    s.n_q_heads = (int32_t)q.size(1);
+    s.total_tokens = q.size(0);
+  }
+  address(a[6], "q", s.q);
+  address(a[7], "k", s.k);
+  address(a[8], "v", s.v);
+  address(a[9], "q_norm_w", s.q_norm_w);
+  address(a[10], "k_norm_w", s.k_norm_w);
+  address(a[11], "out", s.out);
+  address(a[12], "lse", s.lse);
+  address(a[13], "workspace", s.workspace);
+  if (s.workspace) s.workspace_bytes = tensor(a[13], "workspace").nbytes();
+  s.max_tokens = bits<int32_t>(a[14]);
+  if (a[15] != Py_None) s.total_tokens = bits<int64_t>(a[15]);
+  s.rms_eps = real(a[16]);
+  s.rope_theta = real(a[17]);
+  s.softmax_scale =
+      a[18] == Py_None
+          ? (float)std::pow((double)bits<int32_t>(a[2]), -0.5)
+          : real(a[18]);
+  s.kernel_variant = bits<int32_t>(a[19]);
+  s.timing_begin = pointer(a[20]);
+  s.timing_end = pointer(a[21]);
+  address(a[22], "rope_inv_freq", s.rope_inv_freq);
+  s.rows_per_item = bits<int32_t>(a[23]);
+  s.queue_order = bits<int32_t>(a[24]);
+  return PyLong_FromLong(
+      dopr_prefix_attn(static_cast<dopr_store_t>(pointer(a[0])),
+                       bits<int32_t>(a[3]), &s, handle(a[25])));
+}
+
+PyObject *gather_prefix(PyObject *const *a) {
+  // store's handle, layer, doc_ids, out_cu_slots, k_out, v_out, stream
+  const int32_t *doc_ids;
+  const int64_t *out_cu;
+  void *k, *v;
+  address(a[2], "doc_ids", doc_ids);
+  address(a[3], "out_cu_slots", out_cu);
+  address(a[4], "k_out", k);
+  address(a[5], "v_out", v);
+  return PyLong_FromLong(dopr_gather_prefix(
+      static_cast<dopr_store_t>(pointer(a[0])), bits<int32_t>(a[1]),
+      (int32_t)tensor(a[2], "doc_ids").numel(), doc_ids, out_cu, k, v,
+      handle(a[6])));
+}
+
 template <PyObject *(*call)(PyObject *const *), Py_ssize_t count>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
   if (n != count) {
@@ -345,6 +431,8 @@ PyMethodDef methods[] = {DOPR_ENTRY(quantize_rows, 5),
                          DOPR_ENTRY(norm_residual, 12),
                          DOPR_ENTRY(rotary, 13),
                          DOPR_ENTRY(store_put_rotary, 16),
+                         DOPR_ENTRY(prefix_attn, 26),
+                         DOPR_ENTRY(gather_prefix, 7),
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT,

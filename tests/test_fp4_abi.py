@@ -135,7 +135,7 @@ def test_put_launches():
     assert (got[1]["launches"][1]["gx"], got[1]["launches"][1]["gy"]) == \
         (2, 10)
     # (the last slice's five documents' chunks again)
-    assert names[2] == ["k_put_states"] * 2 + ["k_put_clear", "k_put_states"]
+    assert names[2] == ["k_put_states"] + ["k_put_clear", "k_put_states"]
     assert names[3] == ["k_put_clear", "k_put_states"]
     assert names[4] == ["k_gather_fp4"] and names[5] == ["k_gather_fp4"] * 3
     for g in got:
