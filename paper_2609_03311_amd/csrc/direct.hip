@@ -67,16 +67,10 @@ struct RowsParams {
   double log_theta;
   int64_t n_pairs, total_tokens, rows_cap, n_tiles;
   int64_t first;     // first pair, or block, of this launch
+  int32_t slab;      // tokens a block of k_own_keys takes at a time
   float eps, c;
   int32_t Hq, n_rep, layer, splits, max_tokens;
 };
-
-// Loads at wave-uniform places of what no kernel of this launch writes, through
-// the constant address space: scalar ones.
-template <class T>
-__device__ __forceinline__ T cld(const T *p, int64_t i) {
-  return ((const __attribute__((address_space(4))) T *)p)[i];
-}
 
 struct Pair {
   int64_t t0;
@@ -84,13 +78,13 @@ struct Pair {
   bool well;
 };
 __device__ __forceinline__ Pair pair_at(const RowsParams &P, int64_t p) {
-  const int64_t t0 = cld(P.cu, p), t1 = cld(P.cu, p + 1);
+  const int64_t t0 = uniform_load(P.cu, p), t1 = uniform_load(P.cu, p + 1);
   return {t0, (int)(t1 - t0),
           t0 >= 0 && t1 > t0 && t1 <= P.total_tokens &&
               t1 - t0 <= P.max_tokens};
 }
 __device__ __forceinline__ bool has_document(const RowsParams &P, int32_t d) {
-  return d >= 0 && (int64_t)d < P.sv.n_docs && cld(P.sv.doc_len, d) >= 0;
+  return d >= 0 && (int64_t)d < P.sv.n_docs && uniform_load(P.sv.doc_len, d) >= 0;
 }
 // The first of a pair's tiles, and of its groups of own keys: bounds that need
 // no sum over the pairs before it.
@@ -110,7 +104,8 @@ __device__ __forceinline__ int64_t key_piece(int64_t group0, int key, int s,
 }
 
 // k^ and the rotations of every token, the tiles' pairs, zero outputs of pairs
-// without a document.  A pair's tokens, 32 at a time, by gridDim.y blocks.
+// without a document.  A pair's tokens, `slab` (at most 32) at a time, by
+// gridDim.y blocks.
 template <int D>
 __global__ __launch_bounds__(kKeyThreads) void k_own_keys(RowsParams P) {
   constexpr int NSUB = D / 16, ROWS = kKeyThreads / NSUB;
@@ -148,8 +143,9 @@ __global__ __launch_bounds__(kKeyThreads) void k_own_keys(RowsParams P) {
     g0 = *reinterpret_cast<const uint4 *>(P.kw + 8 * sub);
     g1 = *reinterpret_cast<const uint4 *>(P.kw + D / 2 + 8 * sub);
   }
-  for (int j0 = 32 * blockIdx.y; j0 < me.T; j0 += 32 * gridDim.y) {
-    const int n = min(32, me.T - j0);
+  for (int64_t at = (int64_t)P.slab * blockIdx.y; at < me.T;
+       at += (int64_t)P.slab * gridDim.y) {
+    const int j0 = (int)at, n = min(P.slab, me.T - j0);
     __syncthreads();  // (the tokens before are done with the table)
     for (int e = threadIdx.x; e < n * (D / 2); e += kKeyThreads) {
       const int j = e / (D / 2), i = e % (D / 2);
@@ -370,10 +366,10 @@ __global__ __launch_bounds__(64 * WU) __attribute__((
   const int split = (int)(rest % P.splits);
   const int64_t tile = rest / P.splits;
   // (tiles that no pair has hold anything)
-  const int64_t p = cld(P.tiles, tile);
+  const int64_t p = uniform_load(P.tiles, tile);
   if (p < 0 || p >= P.n_pairs) return;
   const Pair me = pair_at(P, p);
-  const int32_t doc = cld(P.doc_ids, p);
+  const int32_t doc = uniform_load(P.doc_ids, p);
   const int64_t at0 = (tile - first_tile(P, p, me.t0)) * 32;
   const int64_t all = (int64_t)me.T * P.n_rep;
   if (!me.well || !has_document(P, doc) || at0 < 0 || at0 >= all) return;
@@ -397,11 +393,11 @@ __global__ __launch_bounds__(64 * WU) __attribute__((
   float lt = 0.f;
   {
     Rows R;
-    R.L = cld(P.sv.doc_len, doc);
+    R.L = uniform_load(P.sv.doc_len, doc);
     R.T = me.T;
     R.slice = reinterpret_cast<const char *>(
         P.sv.payload +
-        fp4_offset(cld(P.sv.doc_off, doc), R.L, hkv, P.layer, g, D));
+        fp4_offset(uniform_load(P.sv.doc_off, doc), R.L, hkv, P.layer, g, D));
     R.n_prefix = (R.L + KC - 1) / KC;
     // (the tile's latest position is at its first row)
     const int jmax = me.T - 1 - r0 / P.n_rep;
@@ -431,10 +427,10 @@ __global__ __launch_bounds__(64 * WU) __attribute__((
     // every logit (log2 units) lies in [-bound, bound]: the gains' bounds and
     // the stored keys'
     const bool known = P.kw != nullptr;
-    const float kmax = cld(
+    const float kmax = uniform_load(
         P.sv.kmax, ((int64_t)doc * P.sv.n_layers + P.layer) * hkv + g);
-    const float bound = P.c * cld(P.bounds, 1) *
-                        fmaxf(kmax, cld(P.bounds, 0)) * 1.001f;
+    const float bound = P.c * uniform_load(P.bounds, 1) *
+                        fmaxf(kmax, uniform_load(P.bounds, 0)) * 1.001f;
     // (one wave's sums without a bound are looked at behind the chunks)
     const bool alone = WU == 1 && P.splits == 1;
     bounded = known ? bound <= kNoRefBound : alone;
@@ -629,11 +625,13 @@ RowsLayout rows_layout(const dopr_store &st, const dopr_attn_args_t &a) {
 template <int D>
 hipError_t launch_rows1(RowsParams P, int waves, hipStream_t s) {
   const int64_t hkv = P.sv.n_kv_heads;
-  // (few pairs of many tokens: blocks share a pair's)
-  const int64_t per_pair = ((int64_t)P.max_tokens + 31) / 32;
-  const int64_t y = std::min<int64_t>(
-      std::min(per_pair, (P.total_tokens + 31) / 32),
-      std::max<int64_t>(1, 1024 / P.n_pairs));
+  // (few pairs of many tokens: blocks share a pair's, and few tokens are spread
+  // thinner, as each takes its sines in turn: one pair of 129: 4.5 us, and 9.0)
+  const int64_t most = std::min<int64_t>(P.max_tokens, P.total_tokens);
+  P.slab = P.n_pairs * ((most + 31) / 32) < 256 ? 8 : 32;
+  const int64_t y =
+      std::min((most + P.slab - 1) / P.slab,
+               std::max<int64_t>(1, 1024 / P.n_pairs));
   hipError_t e =
       in_slices(P.n_pairs, a_launch(kKeyThreads), [&](int64_t at, int64_t n) {
         RowsParams S = P;

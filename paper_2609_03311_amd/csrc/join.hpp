@@ -1,10 +1,18 @@
-// join.hpp -- sums of a softmax row that several blocks formed, put together.
+// join.hpp -- for the kernels that need no plan: uniform loads, and sums of a
+// softmax row that several blocks formed, put together.
 #pragma once
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
 
 namespace dopr {
+
+// Loads at wave-uniform places of what no kernel of this launch writes, through
+// the constant address space: scalar ones.
+template <class T>
+__device__ __forceinline__ T uniform_load(const T *p, int64_t i) {
+  return ((const __attribute__((address_space(4))) T *)p)[i];
+}
 
 constexpr int kJoinParts = 8;  // threads that share the splits of two dims
 

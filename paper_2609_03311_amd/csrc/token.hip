@@ -56,11 +56,12 @@ struct TokenParams {
 // Whether pair p has one token, and which.
 __device__ __forceinline__ bool one_token(const TokenParams &P, int64_t p,
                                           int64_t &t0) {
-  t0 = P.cu[p];
-  return t0 >= 0 && P.cu[p + 1] == t0 + 1 && t0 < P.total_tokens;
+  t0 = uniform_load(P.cu, p);
+  return t0 >= 0 && uniform_load(P.cu, p + 1) == t0 + 1 && t0 < P.total_tokens;
 }
 __device__ __forceinline__ bool has_document(const TokenParams &P, int32_t d) {
-  return d >= 0 && (int64_t)d < P.sv.n_docs && P.sv.doc_len[d] >= 0;
+  return d >= 0 && (int64_t)d < P.sv.n_docs &&
+         uniform_load(P.sv.doc_len, d) >= 0;
 }
 
 __device__ __forceinline__ void store_out(uint16_t *to, const float *o,
@@ -280,8 +281,8 @@ __global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
   const int split = rest % P.splits;
   const int64_t p = P.p0 + rest / P.splits;
   int64_t tok;
+  const int32_t doc = uniform_load(P.doc_ids, p);
   const bool well = one_token(P, p, tok);
-  const int32_t doc = P.doc_ids[p];
   const bool first_of_pair = lane == 0 && wu == 0 && g == 0 && split == 0;
   if (live && first_of_pair &&
       (!well || (p == 0 && P.cu[0] != 0) ||
@@ -301,14 +302,24 @@ __global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
     live = false;
   }
   if (WU == 1 && !live) return;  // (no barrier below)
+  // (asked for before what hangs on the pair)
+  float freq = 0.f;
+  if (P.inv_freq && lane < D / 2) freq = P.inv_freq[lane];
+  uint4 gain_q, gain_k;
+  if (P.qw) {
+    gain_q = *reinterpret_cast<const uint4 *>(P.qw + 8 * (lane % G));
+    gain_k = *reinterpret_cast<const uint4 *>(P.kw + 8 * (lane % G));
+  }
   int L = 0, first = 0, end = 0;
   const char *slice = nullptr;
   float kmax = 0.f;
   if (live) {
-    L = P.sv.doc_len[doc];
+    L = uniform_load(P.sv.doc_len, doc);
     slice = reinterpret_cast<const char *>(
-        P.sv.payload + fp4_offset(P.sv.doc_off[doc], L, hkv, P.layer, g, D));
-    kmax = P.sv.kmax[((int64_t)doc * P.sv.n_layers + P.layer) * hkv + g];
+        P.sv.payload + fp4_offset(uniform_load(P.sv.doc_off, doc), L, hkv,
+                                  P.layer, g, D));
+    kmax = uniform_load(P.sv.kmax,
+                        ((int64_t)doc * P.sv.n_layers + P.layer) * hkv + g);
     const int n_chunks = (L + KC - 1) / KC;
     const int per = (n_chunks + P.splits - 1) / P.splits;
     const int begin = min(split * per, n_chunks);
@@ -336,10 +347,10 @@ __global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
         raw = *reinterpret_cast<const uint4 *>(row_of(lane / G) + 8 * gc);
       if (r0 == 0 && lane < D / 2) {
         // whole turns are dropped in 64 bits
-        const double freq = P.inv_freq
-                                ? (double)P.inv_freq[lane]
-                                : exp(-(double)lane / (D / 2) * P.log_theta);
-        const double turns = (double)L * freq * 0.15915494309189533577;
+        const double by = P.inv_freq
+                              ? (double)freq
+                              : exp(-(double)lane / (D / 2) * P.log_theta);
+        const double turns = (double)L * by * 0.15915494309189533577;
         float sn, cs;
         sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
         sm.rope[lane] = make_float2(cs, sn);
@@ -350,8 +361,7 @@ __global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
         unpack8(raw, x);
         if (rr + RP <= rows)
           raw = *reinterpret_cast<const uint4 *>(row_of(rr + RP) + 8 * gc);
-        const uint16_t *w = rr < rows ? P.qw : P.kw;
-        if (w) {
+        if (P.qw) {
           float ss = 0.f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
@@ -359,7 +369,7 @@ __global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
           for (int off = 1; off < G; off <<= 1) ss += __shfl_xor(ss, off, 64);
           const float inv = 1.0f / sqrtf(ss * (1.0f / D) + P.eps);
           float gain[8];
-          unpack8(*reinterpret_cast<const uint4 *>(w + 8 * gc), gain);
+          unpack8(rr < rows ? gain_q : gain_k, gain);
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * gain[e];
         }
