@@ -802,7 +802,7 @@ unsigned stripes(int64_t n, int64_t chunks) {
 }
 
 // Blocks that share a chunk's heads, each forming its rotations again: until
-// 512 are there (one document of 32 slots, 8 heads: 16 -> 8 us).
+// 512 are there (one document of 32 slots, 8 heads: 16 -> 10 us).
 unsigned head_groups(int64_t blocks, int hkv) {
   const int64_t turns = (2 * (int64_t)hkv + kPutWaves - 1) / kPutWaves;
   const int64_t want = 512 / blocks;
