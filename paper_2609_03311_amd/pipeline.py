@@ -15,7 +15,7 @@ from . import (DOPR_STORE_BF16, dopr_decoder_layer,
                dopr_quant_matmul, dopr_quant_matmul_workspace,
                dopr_quantize_rows, dopr_rotary, dopr_rotary_frequencies,
                dopr_salience, dopr_salience_workspace, dopr_score_logits,
-               dopr_store_create, dopr_store_put)
+               dopr_store_create, dopr_store_put, dopr_store_put_rotary)
 
 HEAD_DIM = 128
 
@@ -302,15 +302,9 @@ class QuantLayerStep:
         dopr_norm_residual(x, pre_norm_w=gain, q=x8, q_scale=scale,
                            rms_eps=self.rms_eps, stream=stream)
 
-    def prefix_states(self, x, positions, k_norm_w, stream=None):
-        """Keys and values of this layer for prefix inputs x [slots, W] at
-        `positions` (int32 [slots]): bf16 [slots, Hkv, D] each, the keys
-        normed and rotated, as dopr_store_put takes them.  With a stream, they
-        and the scratch in between are allocated on it."""
+    def _prefix_products(self, x, stream):
+        """The 8-bit key and value products of prefix inputs x."""
         import torch
-        if stream is not None and stream != torch.cuda.current_stream():
-            with torch.cuda.stream(stream):
-                return self.prefix_states(x, positions, k_norm_w)
         n, d, hk = x.shape[0], self.store.head_dim, self.store.n_kv_heads
         x8 = self._int8(n, self.hidden, x.device)[:, :self.hidden]
         scale = torch.empty(n, dtype=torch.float32, device=x.device)
@@ -323,11 +317,41 @@ class QuantLayerStep:
             w, w_scale = self.w[name]
             dopr_quant_matmul(x8, scale, w, w_scale, out.flatten(1),
                               workspace=ws, stream=stream)
+        return k, v
+
+    def prefix_states(self, x, positions, k_norm_w, stream=None):
+        """Keys and values of this layer for prefix inputs x [slots, W] at
+        `positions` (int32 [slots]): bf16 [slots, Hkv, D] each, the keys
+        normed and rotated, as dopr_store_put takes them.  With a stream, they
+        and the scratch in between are allocated on it."""
+        import torch
+        if stream is not None and stream != torch.cuda.current_stream():
+            with torch.cuda.stream(stream):
+                return self.prefix_states(x, positions, k_norm_w)
+        k, v = self._prefix_products(x, stream)
         dopr_rotary(None, k, positions, self.inv_freq, None, k,
                     interleaved=self.interleaved,
                     attention_factor=self.attention_factor,
                     k_norm_w=k_norm_w, rms_eps=self.rms_eps, stream=stream)
         return k, v
+
+    def put_states(self, layer, doc_ids, src_cu_slots, x, positions, k_norm_w,
+                   stream=None):
+        """The keys and values of prefix inputs x [slots, W] at `positions`
+        into `layer` of the store, the keys normed and rotated on the way
+        (dopr_store_put_rotary; doc_ids and src_cu_slots as there).  The
+        scratch in between is allocated on `stream`."""
+        import torch
+        if stream is not None and stream != torch.cuda.current_stream():
+            with torch.cuda.stream(stream):
+                return self.put_states(layer, doc_ids, src_cu_slots, x,
+                                       positions, k_norm_w)
+        k, v = self._prefix_products(x, stream)
+        dopr_store_put_rotary(self.store, layer, doc_ids, src_cu_slots, k, v,
+                              self.inv_freq, positions=positions,
+                              k_norm_w=k_norm_w, interleaved=self.interleaved,
+                              attention_factor=self.attention_factor,
+                              rms_eps=self.rms_eps, stream=stream)
 
     def run(self, layer, doc_ids, cu_seqlens, x, positions, q_norm_w=None,
             k_norm_w=None, stream=None, softmax_scale=None):

@@ -21,7 +21,7 @@ sum=$R/gpurun_out/summaries
 mkdir -p "$out" "$sum"
 if [ "$path" = score ]; then
   tag=k_score_rows
-  kern="k_score_rows<$D>"
+  kern="k_score_rows<$D,"
 else
   tag=k_pass_attn
   kern="k_own_khat<$D>|k_plan_fill<$D>|k_pass_attn<$D,"

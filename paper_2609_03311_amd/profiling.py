@@ -47,9 +47,9 @@ SOURCE_SETS = {
 # k_own_khat) + pass kernel (full layer); one wave per 32-row
 # unit (score rows, every prefix at most 512 slots).  Same at head size 64.
 ATTN_KERNEL = r"k_own_khat<128>|k_plan_fill<128>|k_pass_attn<128,"
-SCORE_KERNEL = r"k_score_rows<128>"
+SCORE_KERNEL = r"k_score_rows<128,"
 ATTN_KERNEL_D64 = r"k_own_khat<64>|k_plan_fill<64>|k_pass_attn<64,"
-SCORE_KERNEL_D64 = r"k_score_rows<64>"
+SCORE_KERNEL_D64 = r"k_score_rows<64,"
 CALIB_KERNEL = r"bitwise_not"
 CALIB_BYTES = 1 << 30
 

@@ -6,10 +6,11 @@ are normed and rotated, and enter the store), then runs the online tokens of
 a batch of (query, document) pairs through the whole layer, once with bf16
 products (``pipeline.LayerStep``) and once with 8-bit ones
 (``pipeline.QuantLayerStep``), and prints both times and how far apart the
-outputs are.
+outputs are.  With --store fp4 the store holds the states in 4 bits, and the
+keys are normed and rotated on their way into it.
 
     python3 -m paper_2609_03311_amd.quant_layer [--config qwen3_0p6b]
-        [--pairs 800]
+        [--pairs 800] [--store bf16|fp4]
 
 Weights and states are random (seeded); the shapes are the named workload's.
 """
@@ -37,7 +38,8 @@ def main(argv=None):
     import torch
 
     import workloads
-    from . import dopr_check_status, dopr_store_create, dopr_store_put
+    from . import (DOPR_STORE_BF16, DOPR_STORE_FP4, dopr_check_status,
+                   dopr_store_create, dopr_store_put)
     from .pipeline import LayerStep, QuantLayerStep, online_positions
 
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
@@ -45,6 +47,7 @@ def main(argv=None):
                     choices=["tiny", "qwen3_0p6b", "qwen3_4b", "qwen3_8b"])
     ap.add_argument("--pairs", type=int, default=800)
     ap.add_argument("--steps", type=int, default=10)
+    ap.add_argument("--store", default="bf16", choices=["bf16", "fp4"])
     args = ap.parse_args(argv)
     dev = "cuda"
     full = workloads.make(args.config)
@@ -58,8 +61,10 @@ def main(argv=None):
     weights = workloads.layer_weights(st, hidden, inter, dev)
     prm = workloads.params(st, dev)
     x = workloads.hidden_states(st, hidden, dev)
+    fp4 = args.store == "fp4"
     store = dopr_store_create(1, st.n_kv_heads, st.head_dim, st.doc_len,
-                              device=dev)
+                              device=dev, format=DOPR_STORE_FP4 if fp4
+                              else DOPR_STORE_BF16)
     shape = dict(n_pairs=st.n_pairs, n_q_heads=st.n_q_heads,
                  total_tokens=st.n_tokens, max_tokens=int(st.seqlens.max()),
                  hidden=hidden, intermediate=inter, device=dev)
@@ -73,10 +78,13 @@ def main(argv=None):
                          device=dev).to(torch.bfloat16)
     pos = torch.from_numpy((np.arange(slots) - np.repeat(cu[:-1], st.doc_len))
                            .astype(np.int32)).to(dev)
-    k, v = quant.prefix_states(states, pos, prm["k_norm_w"])
-    dopr_store_put(store, 0, torch.arange(st.n_docs, dtype=torch.int32,
-                                          device=dev),
-                   torch.from_numpy(cu).to(dev), k, v)
+    ids = torch.arange(st.n_docs, dtype=torch.int32, device=dev)
+    src_cu = torch.from_numpy(cu).to(dev)
+    if fp4:
+        quant.put_states(0, ids, src_cu, states, pos, prm["k_norm_w"])
+    else:
+        k, v = quant.prefix_states(states, pos, prm["k_norm_w"])
+        dopr_store_put(store, 0, ids, src_cu, k, v)
 
     # online: the pairs' tokens through the layer
     doc_ids = torch.from_numpy(st.doc_ids).to(dev)
