@@ -549,12 +549,17 @@ __global__ __launch_bounds__(64 * WU) __attribute__((
   }
 }
 
-// The sums of a row's blocks: one block a (tile's row, kv head).
-template <int D>
-__global__ __launch_bounds__(4 * D) void k_rows_join(RowsParams P) {
+// The sums of a row's blocks, rows (tile, row of it, kv head).
+template <int D, int PARTS>
+__global__ __launch_bounds__(join_threads(D, PARTS)) void k_rows_join(
+    RowsParams P) {
   const int hkv = P.sv.n_kv_heads;
-  const int g = blockIdx.x % hkv, rr = blockIdx.x / hkv % 32;
-  const int64_t tile = blockIdx.x / hkv / 32;
+  const int64_t at =
+      PARTS > 1 ? blockIdx.x
+                : (int64_t)blockIdx.x * join_rows(D, 1) + threadIdx.x / (D / 2);
+  const int g = at % hkv, rr = at / hkv % 32;
+  const int64_t tile = at / hkv / 32;
+  if (tile >= P.n_tiles) return;
   const int64_t p = P.tiles[tile];
   if (p < 0 || p >= P.n_pairs) return;
   const Pair me = pair_at(P, p);
@@ -566,16 +571,18 @@ __global__ __launch_bounds__(4 * D) void k_rows_join(RowsParams P) {
   const int64_t row = (me.t0 + me.T - 1 - back) * P.Hq + g * P.n_rep +
                       (r - back * P.n_rep);
   const int64_t step = 32 * (D + 2);
-  join_row<D>(P.part + (tile * hkv + g) * P.splits * step + rr * (D + 2), step,
+  join_row<D, PARTS>(P.part + (tile * hkv + g) * P.splits * step + rr * (D + 2), step,
               P.splits, P.out + row * D, P.lse ? P.lse + row : nullptr);
 }
 
 // How a call's (tile, kv head)s are shared out: one wave each where they take
 // more than half of the 2,048 waves the SIMDs hold (D = 64: 4,096), two or four
-// below, and
-// several blocks of four where that leaves waves free, of at least four chunks
-// a wave of the longest sequence (129 tokens on 256 slots: 21 us, and 29 in two
-// blocks of one or two chunks a wave and their join).
+// below, and several blocks of four, of at least four chunks a wave of the
+// longest sequence, where that leaves waves free and saves more than the sums'
+// way through memory and their join cost: about where there are more chunks
+// than units and 32 more.  (32 q / 8 kv heads: 16 pairs of 8 tokens on 2,048
+// slots 24.5 us, in four blocks 31; one on 4,096 29, in eight 20; four on 4,096
+// 29 and 22.5.)
 struct RowsShare {
   int waves, splits;
 };
@@ -585,6 +592,7 @@ RowsShare rows_share(int D, int64_t units, int64_t max_len,
   if (2 * units > full) return {1, 1};
   if (4 * units > full) return {2, 1};
   const int64_t chunks = (max_len + max_tokens + KC - 1) / KC;
+  if (chunks <= 32 + units) return {kMostWaves, 1};
   const int64_t want = full / (units * kMostWaves);
   const int64_t most = chunks / (4 * kMostWaves);
   return {kMostWaves, (int)std::max<int64_t>(1, std::min(want, most))};
@@ -654,8 +662,11 @@ hipError_t launch_rows1(RowsParams P, int waves, hipStream_t s) {
   });
   if (e != hipSuccess || P.splits == 1) return e;
   // (units of several blocks are few: below 2^20 rows)
-  hipLaunchKernelGGL(k_rows_join<D>, dim3((unsigned)(P.n_tiles * 32 * hkv)),
-                     dim3(4 * D), 0, s, P);
+  const int parts = join_parts(P.splits), per = join_rows(D, parts);
+  const auto join = parts > 1 ? k_rows_join<D, kJoinParts> : k_rows_join<D, 1>;
+  hipLaunchKernelGGL(join,
+                     dim3((unsigned)((P.n_tiles * 32 * hkv + per - 1) / per)),
+                     dim3(join_threads(D, parts)), 0, s, P);
   return hipGetLastError();
 }
 

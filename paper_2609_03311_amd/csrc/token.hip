@@ -513,23 +513,30 @@ __global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
   }
 }
 
-// The sums of a row's blocks: one block a (pair, q head).
-template <int D>
-__global__ __launch_bounds__(4 * D) void k_token_join(TokenParams P) {
-  const int64_t p = P.p0 + blockIdx.x / P.Hq;
-  const int h = blockIdx.x % P.Hq, g = h / P.n_rep, rr = h - g * P.n_rep;
+// The sums of a row's blocks, rows (pair, q head).
+template <int D, int PARTS>
+__global__ __launch_bounds__(join_threads(D, PARTS)) void k_token_join(
+    TokenParams P) {
+  const unsigned at =
+      PARTS > 1 ? blockIdx.x
+                : blockIdx.x * join_rows(D, 1) + threadIdx.x / (D / 2);
+  const int64_t p = P.p0 + at / P.Hq;
+  if (p >= P.n_pairs) return;
+  const int h = at % P.Hq, g = h / P.n_rep, rr = h - g * P.n_rep;
   int64_t tok;
   if (!one_token(P, p, tok) || !has_document(P, P.doc_ids[p])) return;
   const int64_t step = (int64_t)P.n_rep * (D + 2), row = tok * P.Hq + h;
-  join_row<D>(P.part + ((p - P.p0) * P.sv.n_kv_heads + g) * P.splits * step +
+  join_row<D, PARTS>(P.part + ((p - P.p0) * P.sv.n_kv_heads + g) * P.splits * step +
                   (int64_t)rr * (D + 2),
               step, P.splits, P.out + row * D, P.lse ? P.lse + row : nullptr);
 }
 
 // How a call's (pair, kv head)s are shared out: one wave each from kTokenFull
-// of them on (two waves a SIMD), two or four below, and blocks of four where
-// that leaves waves free, of at least two chunks a wave of the longest
-// document and within 32 MB of sums (half of the no-alloc call's scratch).
+// of them on (two waves a SIMD), two or four below, and past 32 chunks several
+// blocks of four where that leaves waves free, of at least two chunks a wave of
+// the longest document and within 32 MB of sums (half of the no-alloc call's
+// scratch).  (One pair of 32 q / 8 kv heads: 512 slots 8.9 us, in two blocks
+// 11.4; 1,024 10.7 and 11.4; 2,048 14.4, in eight 11.1; 16,384 13.3 in 32.)
 constexpr int64_t kTokenFull = 2048;
 struct TokenShare {
   int waves, splits;
@@ -539,8 +546,9 @@ TokenShare token_share(const dopr_store &st, int64_t pairs, int32_t n_rep) {
   const int64_t chunks = ((int64_t)st.max_len + KC - 1) / KC;
   if (2 * units > kTokenFull) return {1, 1};
   if (4 * units > kTokenFull) return {2, 1};
+  if (chunks <= 32) return {kTokenWaves, 1};
   const int64_t want = kTokenFull / (units * kTokenWaves);
-  const int64_t most = (chunks + 2 * kTokenWaves - 1) / (2 * kTokenWaves);
+  const int64_t most = chunks / (2 * kTokenWaves);
   const int64_t fit = ((int64_t)32 << 20) /
                       (4 * units * n_rep * (int64_t)(st.head_dim + 2));
   return {kTokenWaves,
@@ -571,8 +579,11 @@ hipError_t launch_token1(const TokenParams &P, int waves, int64_t pairs,
         launch_token2<D>(waves, S, s);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess || P.splits == 1) return e;
-        hipLaunchKernelGGL(k_token_join<D>, dim3((unsigned)(n * P.Hq)),
-                           dim3(4 * D), 0, s, S);
+        const int parts = join_parts(P.splits), rows = join_rows(D, parts);
+        const auto join =
+            parts > 1 ? k_token_join<D, kJoinParts> : k_token_join<D, 1>;
+        hipLaunchKernelGGL(join, dim3((unsigned)((n * P.Hq + rows - 1) / rows)),
+                           dim3(join_threads(D, parts)), 0, s, S);
         return hipGetLastError();
       });
 }

@@ -141,3 +141,109 @@ def test_put_launches():
     for g in got:
         for x in g["launches"]:
             assert x["gx"] * x["bx"] < 1 << 32 and x["gy"] <= 65535
+
+
+ATTN = dict(_layer=0, n_pairs=1, n_q_heads=8, max_tokens=1, total_tokens=1,
+            doc_ids=256, cu_seqlens=256, q=256, k=256, v=256, rms_eps=1e-6,
+            rope_theta=1e6, softmax_scale=0.1, out=256, workspace=256,
+            workspace_bytes=1 << 60)
+
+
+def _attn(**more):
+    return ["dopr_prefix_attn", "_AttnArgs", ATTN | more]
+
+
+def _kernels(got):
+    for g in got:
+        assert g["status"] == 0, g["error"]
+        for x in g["launches"]:
+            assert x["gx"] * x["bx"] < 1 << 32 and x["gy"] <= 65535, x
+            assert x["lds"] <= 160 << 10
+    return [[x["kernel"].split("<")[0] for x in g["launches"]] for g in got]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_launches(d):
+    """Which kernels a call over a 4-bit store takes by itself, and their
+    grids at its largest."""
+    short = _kernels(store_calls((1, 2, d, [40, 300], 1), [
+        _attn(), _attn(n_pairs=5000, total_tokens=5000),
+        # a pair without the one token it has to have is not for them
+        _attn(max_tokens=2, total_tokens=2),
+        _attn(n_pairs=64, max_tokens=90, total_tokens=64 * 90),
+        _attn(n_pairs=0, max_tokens=5, total_tokens=0),
+        _attn(n_pairs=(1 << 24) + 3, total_tokens=(1 << 24) + 3),
+        _attn(n_pairs=(1 << 24) + 3, max_tokens=9, total_tokens=1 << 26),
+    ]))
+    rows = ["k_own_keys", "k_rows_fp4"]
+    assert short[:5] == [["k_token_fp4"], ["k_token_fp4"], rows, rows, []]
+    assert set(short[5]) == {"k_token_fp4"} and set(short[6]) == set(rows)
+    long = _kernels(store_calls((1, 2, d, [40, 60000], 1), [
+        _attn(), _attn(max_tokens=2, total_tokens=2),
+        _attn(n_pairs=5000, total_tokens=5000),
+        _attn(n_pairs=64, max_tokens=90, total_tokens=64 * 90)]))
+    assert long == [["k_token_fp4", "k_token_join"], rows + ["k_rows_join"],
+                    ["k_token_fp4"], rows]
+    # the planned kernels where they are asked for
+    for variant, name in ((8, "k_pass_attn"), (6, "k_prefix_attn"),
+                          (1, "k_prefix_attn"), (4, "k_prefix_attn")):
+        got = _kernels(store_calls((1, 2, d, [40, 300], 1), [
+            _attn(n_pairs=5, max_tokens=9, total_tokens=45,
+                  kernel_variant=variant)]))
+        assert name in got[0] and not set(got[0]) & set(rows), variant
+
+
+def test_attention_refusals():
+    D = _D()
+    doc_len = [40, 60000]
+    pool, _ = D.dopr_store_bytes(1, 2, 128, doc_len, D.DOPR_STORE_FP4)
+    desc, _keep = D._desc(1, 2, 128, doc_len)
+    shapes = [dict(), dict(max_tokens=5, total_tokens=5),
+              dict(n_pairs=900, max_tokens=50, total_tokens=45000)]
+    bad = [(dict(workspace_bytes=255), "workspace"),
+           (dict(workspace=257), "aligned"), (dict(workspace=None), ""),
+           (dict(q=None), "NULL"), (dict(doc_ids=None), "NULL"),
+           (dict(q=260), "aligned"), (dict(out=264), "aligned"),
+           (dict(n_q_heads=7), "n_q_heads"),
+           (dict(q_norm_w=256), "norm"), (dict(softmax_scale=0.0), "scale"),
+           (dict(softmax_scale=float("nan")), "scale"),
+           (dict(rms_eps=float("nan")), "rms_eps"),
+           (dict(kernel_variant=7), "kernel_variant"),
+           (dict(max_tokens=0), "max_tokens"), (dict(_layer=1), "layer"),
+           (dict(_layer=-1), "layer"), (dict(rope_inv_freq=258), "aligned")]
+    for shape in shapes:
+        got = store_calls((1, 2, 128, doc_len, 1),
+                          [_attn(**{**shape, **b}) for b, _ in bad])
+        for (b, text), g in zip(bad, got):
+            if b == dict(workspace_bytes=255) and not shape:
+                continue  # (may need less)
+            assert g["status"] in (INVALID, WORKSPACE), (b, g)
+            assert not g["launches"] and text in g["error"], (b, g)
+
+
+def test_put_rotary_checks_its_tensors():
+    """The binding names the argument; nothing of a CPU tensor reaches the
+    library."""
+    import torch
+    D = _D()
+
+    class Stand:
+        handle, n_kv_heads, head_dim = 0, 2, 64
+        pool = torch.empty(0)
+
+    k = torch.zeros(5, 2, 64, dtype=torch.bfloat16)
+    ids = torch.zeros(1, dtype=torch.int32)
+    cu = torch.tensor([0, 5])
+    freq = torch.ones(32)
+    good = [ids, cu, k, k, freq]
+    for i, what in enumerate(("doc_ids", "src_cu_slots", "k", "v",
+                              "inv_freq")):
+        for wrong in (None, 3, torch.zeros(2, 3, dtype=torch.int16)):
+            args = list(good)
+            args[i] = wrong
+            with pytest.raises(ValueError):
+                D.dopr_store_put_rotary(Stand(), 0, *args)
+    with pytest.raises(ValueError, match="k must be a"):
+        D.dopr_store_put_rotary(Stand(), 0, *good)  # (on the CPU)
+    with pytest.raises(ValueError, match="kv heads"):
+        D.dopr_store_put_rotary(Stand(), 0, ids, cu, k.flatten(1), k, freq)

@@ -121,6 +121,14 @@ def test_smaller_keys_in_place_of_large_ones(tokens):
     again.check(*want)
 
 
+@pytest.mark.parametrize("slots", [1024, 1025, 2047, 2100, 4200])
+@pytest.mark.parametrize("tokens", [[1, 1, 1], [3, 1, 20]])
+@pytest.mark.parametrize("d", [64, 128])
+def test_joins_of_few_blocks(slots, tokens, d):
+    r = Filled([slots, 40], [0, 1, 0], tokens, 6, 2, d, seed=slots)
+    r.check(*r.call())
+
+
 def test_two_streams_at_once():
     """Calls of two streams on one store, each with its own workspace, beside
     a put into the other layer."""
