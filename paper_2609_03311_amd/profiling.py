@@ -39,6 +39,9 @@ SOURCE_SETS = {
     "store": ("csrc/store.hip", "csrc/internal.hpp"),
     "operators": ("csrc/rows.hip", "csrc/qproduct.hip", "csrc/rotary.hip",
                   "csrc/rowio.hpp"),
+    "store4": ("csrc/states.hip", "csrc/token.hip", "csrc/direct.hip",
+               "csrc/fp4.hpp", "csrc/join.hpp", "csrc/attn_common.hpp",
+               "csrc/internal.hpp"),
     "layer": ("csrc/layer.hip", "csrc/group.hip", "csrc/score.hip")
     + KERNEL_SOURCES,
 }

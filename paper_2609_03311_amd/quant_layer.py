@@ -10,7 +10,7 @@ outputs are.  With --store fp4 the store holds the states in 4 bits, and the
 keys are normed and rotated on their way into it.
 
     python3 -m paper_2609_03311_amd.quant_layer [--config qwen3_0p6b]
-        [--pairs 800] [--store bf16|fp4]
+        [--pairs 800] [--tokens N] [--store bf16|fp4]
 
 Weights and states are random (seeded); the shapes are the named workload's.
 """
@@ -47,6 +47,8 @@ def main(argv=None):
                     choices=["tiny", "qwen3_0p6b", "qwen3_4b", "qwen3_8b"])
     ap.add_argument("--pairs", type=int, default=800)
     ap.add_argument("--steps", type=int, default=10)
+    ap.add_argument("--tokens", type=int, default=0,
+                    help="online tokens of every pair (0: the workload's)")
     ap.add_argument("--store", default="bf16", choices=["bf16", "fp4"])
     args = ap.parse_args(argv)
     dev = "cuda"
@@ -54,9 +56,11 @@ def main(argv=None):
     pairs = min(args.pairs, full.n_pairs)
     # the first pairs, over a store of just their documents
     docs, ids = np.unique(full.doc_ids[:pairs], return_inverse=True)
-    st = workloads.custom(full.doc_len[docs], ids.astype(np.int32),
-                          full.seqlens[:pairs], full.n_q_heads,
-                          full.n_kv_heads, name=args.config)
+    seqlens = full.seqlens[:pairs]
+    if args.tokens > 0:
+        seqlens = np.full_like(seqlens, args.tokens)
+    st = workloads.custom(full.doc_len[docs], ids.astype(np.int32), seqlens,
+                          full.n_q_heads, full.n_kv_heads, name=args.config)
     hidden, inter = workloads.layer_dims(full)
     weights = workloads.layer_weights(st, hidden, inter, dev)
     prm = workloads.params(st, dev)
