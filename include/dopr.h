@@ -10,7 +10,7 @@
  *
  *   dopr_store_*       the HBM-resident prefix store of per-document K/V
  *                      states (Sec. 3.3: query-independent, reused across
- *                      queries; bf16 per Table 7).
+ *                      queries; bf16 per Table 7, or 4 bits a value).
  *   dopr_prefix_attn   batched GQA attention in which each pair's online
  *                      tokens attend to [that document's prefix ; their own
  *                      causal keys] (Sec. 3.4; the query/score tokens see the
@@ -251,7 +251,10 @@ typedef struct {
                                4 = exact running-max softmax for every row
                                (slower; the reference for the fast path);
                                5 = self-check: the fast pass queues every
-                               work unit for the exact pass (tests only)   */
+                               work unit for the exact pass (tests only).
+                               Over a 4-bit store 0 runs kernels that need
+                               no plan (see dopr_prefix_attn), and 1, 2 and
+                               3 run shape 6                               */
   int64_t total_tokens;     /* Ntok = cu_seqlens[P]                         */
   const int32_t *doc_ids;   /* dev int32 [P]                                */
   const int32_t *cu_seqlens;/* dev int32 [P+1], cu[0] = 0, T_p >= 1         */
@@ -303,7 +306,8 @@ typedef struct {
                                values are INVALID_ARG.                      */
 } dopr_attn_args_t;
 
-/* Workspace bytes needed by dopr_prefix_attn for these arguments (host). */
+/* Workspace bytes needed by dopr_prefix_attn for these arguments (host).
+ * Never fewer than a plan for them takes, also where none is made.         */
 dopr_status_t dopr_prefix_attn_workspace(dopr_store_t st,
                                          const dopr_attn_args_t *args,
                                          size_t *bytes);
@@ -311,7 +315,21 @@ dopr_status_t dopr_prefix_attn_workspace(dopr_store_t st,
 /* Run the online attention of one layer for a batch of pairs.  Pairs that
  * share a document are grouped on the device so that the document's prefix
  * is read from HBM once per group and reused from LDS.  Pairs with a bad doc
- * id get zero outputs (lse = -inf) and a deferred DOC_RANGE status.        */
+ * id get zero outputs (lse = -inf) and a deferred DOC_RANGE status.
+ *
+ * Over a 4-bit store the automatic choice makes no plan and groups nothing.
+ * Pairs of several tokens: every 32 stacked rows of a (pair, kv head) stream
+ * the document's codes by themselves.  Where such units are many, each is one
+ * wave's, and its rows are bit for bit those of the planned kernels; where they
+ * are few, waves and blocks share a unit's keys and add their sums, so that a
+ * row's last bits go by how many units a call has.  Pairs of one token each
+ * (max_tokens 1 and total_tokens = n_pairs): a unit is a (pair, kv head), and
+ * q^ and k^ stay in 32 bits (q^ enters the products as two bf16 parts), so the
+ * outputs are nearer to the definition than the planned kernels', and not their
+ * bits.  Many short pairs that share few documents run faster by a plan, whose
+ * items hold rows of several pairs: kernel_variant 8 (4,096 single tokens on 64
+ * documents of 512 slots 187 us, and 288; 1,024 pairs of 4 tokens on 16 of
+ * 4,096 330 us, and 541).                                                  */
 dopr_status_t dopr_prefix_attn(dopr_store_t st, int32_t layer,
                                const dopr_attn_args_t *args, void *stream);
 
@@ -330,13 +348,17 @@ dopr_status_t dopr_prefix_attn(dopr_store_t st, int32_t layer,
  *     is run only when asked for and its plan fits (its work items counted
  *     with up to 2048 rows and 32 bytes each per kv head; when only the
  *     128-row items it is run with do not fit, the block kernels run, with
- *     the same outputs);
+ *     the same outputs).  Over a 4-bit store the automatic choice is
+ *     dopr_prefix_attn's while its keys fit (2 Hkv D + 4 D bytes a token), else
+ *     the block kernels;
  *   - the call allocates nothing: no hipMalloc, hipFree or allocating
  *     library routine.
  * Every call on one device shares that device's scratch: calls that overlap
  * on one device (other streams, other threads) race and must be ordered by
  * the caller.  The plan's kernels clear what must start at zero.  Outputs
- * are bitwise identical to dopr_prefix_attn's for the same inputs.        */
+ * are bitwise identical to dopr_prefix_attn's for the same inputs.  (Over a
+ * 4-bit store, past those bytes: to kernel_variant 6's, and to the automatic
+ * choice's where its units are one wave's.)                                */
 #define DOPR_NOALLOC_SCRATCH_BYTES ((size_t)64 << 20)
 dopr_status_t dopr_prefix_attn_noalloc(dopr_store_t st, int32_t layer,
                                        const dopr_attn_args_t *args,
