@@ -35,7 +35,7 @@
 namespace dopr {
 namespace {
 
-constexpr int kTokenWaves = 4;  // of a block
+constexpr int kTokenWaves = 4;  // of a unit, at most
 
 struct TokenParams {
   StoreView sv;
@@ -257,25 +257,22 @@ __device__ __forceinline__ void token_chunks(const char *slice, int c, int end,
   }
 }
 
-// WU: waves of a unit, (pair, kv head, split).
+// One block of WU waves a unit, (pair, kv head, split).  (With four units of
+// one wave in a block, whose waves and LDS come free together, 4,096 pairs on 64
+// to 512 slots take 307 us for 290.)
 template <int D, int WU>
-__global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
+__global__ __launch_bounds__(64 * WU) __attribute__((
     amdgpu_waves_per_eu(2, 2))) void k_token_fp4(TokenParams P) {
   constexpr int G = D / 8;    // lanes a row, eight dims each
   constexpr int RP = 64 / G;  // rows at a time
   constexpr int RT = kTokenRows;
-  __shared__ __attribute__((aligned(16))) TokenRows<D> sm_all[kTokenWaves];
+  __shared__ __attribute__((aligned(16))) TokenRows<D> sm_all[WU];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, kg = lane >> 4;
   const int hkv = P.sv.n_kv_heads;
-  const int w0 = wave / WU * WU, wu = wave - w0;  // the unit's first wave
   TokenRows<D> &sm = sm_all[wave];
-  const unsigned unit = blockIdx.x * (kTokenWaves / WU) + wave / WU;
-  // (a wave without a unit, or whose pair has no token or no document, goes
-  // on to meet the barriers)
-  bool live = unit < P.units;
-  const unsigned u = live ? unit : 0;
+  const unsigned u = blockIdx.x;
   const int g = u % hkv;
   const unsigned rest = u / hkv;
   const int split = rest % P.splits;
@@ -283,25 +280,24 @@ __global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
   int64_t tok;
   const int32_t doc = uniform_load(P.doc_ids, p);
   const bool well = one_token(P, p, tok);
-  const bool first_of_pair = lane == 0 && wu == 0 && g == 0 && split == 0;
-  if (live && first_of_pair &&
+  const bool first_of_pair = lane == 0 && wave == 0 && g == 0 && split == 0;
+  if (first_of_pair &&
       (!well || (p == 0 && P.cu[0] != 0) ||
        (p == P.n_pairs - 1 && P.cu[P.n_pairs] != P.total_tokens)))
     raise_status(P.status, DOPR_ERR_SEQLEN);
-  live = live && well;
+  if (!well) return;  // (the whole block)
   const int64_t row0 = tok * P.Hq + g * P.n_rep;
-  if (live && !has_document(P, doc)) {
+  if (!has_document(P, doc)) {
     if (first_of_pair) raise_status(P.status, DOPR_ERR_DOC_RANGE);
-    if (split == 0 && wu == 0) {
+    if (split == 0 && wave == 0) {
       for (int e = lane; e < P.n_rep * G; e += 64)
         reinterpret_cast<uint4 *>(P.out + row0 * D)[e] =
             make_uint4(0, 0, 0, 0);
       if (P.lse)
         for (int e = lane; e < P.n_rep; e += 64) P.lse[row0 + e] = -INFINITY;
     }
-    live = false;
+    return;
   }
-  if (WU == 1 && !live) return;  // (no barrier below)
   // (asked for before what hangs on the pair)
   float freq = 0.f;
   if (P.inv_freq && lane < D / 2) freq = P.inv_freq[lane];
@@ -310,201 +306,192 @@ __global__ __launch_bounds__(64 * kTokenWaves) __attribute__((
     gain_q = *reinterpret_cast<const uint4 *>(P.qw + 8 * (lane % G));
     gain_k = *reinterpret_cast<const uint4 *>(P.kw + 8 * (lane % G));
   }
-  int L = 0, first = 0, end = 0;
-  const char *slice = nullptr;
-  float kmax = 0.f;
-  if (live) {
-    L = uniform_load(P.sv.doc_len, doc);
-    slice = reinterpret_cast<const char *>(
-        P.sv.payload + fp4_offset(uniform_load(P.sv.doc_off, doc), L, hkv,
-                                  P.layer, g, D));
-    kmax = uniform_load(P.sv.kmax,
-                        ((int64_t)doc * P.sv.n_layers + P.layer) * hkv + g);
-    const int n_chunks = (L + KC - 1) / KC;
-    const int per = (n_chunks + P.splits - 1) / P.splits;
-    const int begin = min(split * per, n_chunks);
-    end = min(begin + per, n_chunks);
-    first = begin + 2 * wu;
-  }
+  const int L = uniform_load(P.sv.doc_len, doc);
+  const char *slice = reinterpret_cast<const char *>(
+      P.sv.payload + fp4_offset(uniform_load(P.sv.doc_off, doc), L, hkv,
+                                P.layer, g, D));
+  const float kmax = uniform_load(
+      P.sv.kmax, ((int64_t)doc * P.sv.n_layers + P.layer) * hkv + g);
+  const int n_chunks = (L + KC - 1) / KC;
+  const int per = (n_chunks + P.splits - 1) / P.splits;
+  const int begin = min(split * per, n_chunks);
+  const int end = min(begin + per, n_chunks), first = begin + 2 * wave;
 
   for (int r0 = 0; r0 < P.n_rep; r0 += RT) {
     const int rows = min(RT, P.n_rep - r0);
     bool bounded = true;
-    if (live) {
-      Codes<D> codes{};
-      if (first < end) {
-        load_keys<D>(slice, first, end, lane, codes);
-        load_values<D>(slice, first, end, lane, codes);
+    Codes<D> codes{};
+    if (first < end) {
+      load_keys<D>(slice, first, end, lane, codes);
+      load_values<D>(slice, first, end, lane, codes);
+    }
+    // c q^ of the rows and k^, G lanes a row; row `rows` is the own key
+    const int gc = lane % G;
+    auto row_of = [&](int rr) {
+      return rr < rows ? P.q + (row0 + r0 + rr) * D
+                       : P.k + (tok * hkv + g) * D;
+    };
+    uint4 raw = make_uint4(0, 0, 0, 0);
+    if (lane / G <= rows)
+      raw = *reinterpret_cast<const uint4 *>(row_of(lane / G) + 8 * gc);
+    if (r0 == 0 && lane < D / 2) {
+      // whole turns are dropped in 64 bits
+      const double by = P.inv_freq
+                            ? (double)freq
+                            : exp(-(double)lane / (D / 2) * P.log_theta);
+      const double turns = (double)L * by * 0.15915494309189533577;
+      float sn, cs;
+      sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
+      sm.rope[lane] = make_float2(cs, sn);
+    }
+    wave_fence();
+    for (int rr = lane / G; rr <= rows; rr += RP) {
+      float x[8], y[8];
+      unpack8(raw, x);
+      if (rr + RP <= rows)
+        raw = *reinterpret_cast<const uint4 *>(row_of(rr + RP) + 8 * gc);
+      if (P.qw) {
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+#pragma unroll
+        for (int off = 1; off < G; off <<= 1) ss += __shfl_xor(ss, off, 64);
+        const float inv = 1.0f / sqrtf(ss * (1.0f / D) + P.eps);
+        float gain[8];
+        unpack8(rr < rows ? gain_q : gain_k, gain);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * gain[e];
       }
-      // c q^ of the rows and k^, G lanes a row; row `rows` is the own key
-      const int gc = lane % G;
-      auto row_of = [&](int rr) {
-        return rr < rows ? P.q + (row0 + r0 + rr) * D
-                         : P.k + (tok * hkv + g) * D;
-      };
-      uint4 raw = make_uint4(0, 0, 0, 0);
-      if (lane / G <= rows)
-        raw = *reinterpret_cast<const uint4 *>(row_of(lane / G) + 8 * gc);
-      if (r0 == 0 && lane < D / 2) {
-        // whole turns are dropped in 64 bits
-        const double by = P.inv_freq
-                              ? (double)freq
-                              : exp(-(double)lane / (D / 2) * P.log_theta);
-        const double turns = (double)L * by * 0.15915494309189533577;
-        float sn, cs;
-        sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
-        sm.rope[lane] = make_float2(cs, sn);
+      // (the partner of dim i is i +- D/2)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = __shfl_xor(x[e], G / 2, 64);
+      const float sign = gc < G / 2 ? -1.f : 1.f, by = rr < rows ? P.c : 1.f;
+      float n2 = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float2 t = sm.rope[(8 * gc + e) % (D / 2)];
+        x[e] = by * fmaf(x[e], t.x, sign * y[e] * t.y);
+        n2 = fmaf(x[e], x[e], n2);
       }
-      wave_fence();
-      for (int rr = lane / G; rr <= rows; rr += RP) {
-        float x[8], y[8];
-        unpack8(raw, x);
-        if (rr + RP <= rows)
-          raw = *reinterpret_cast<const uint4 *>(row_of(rr + RP) + 8 * gc);
-        if (P.qw) {
-          float ss = 0.f;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+      for (int off = 1; off < G; off <<= 1) n2 += __shfl_xor(n2, off, 64);
+      if (gc == 0) sm.norm2[rr < rows ? rr : RT] = n2;
+      float4 *to = reinterpret_cast<float4 *>(
+          (rr < rows ? sm.q[rr] : sm.k) + 8 * gc);
+      to[0] = make_float4(x[0], x[1], x[2], x[3]);
+      to[1] = make_float4(x[4], x[5], x[6], x[7]);
+    }
+    wave_fence();
+    if (split == 0 && wave == 0)
+      for (int rr = lane / G; rr < rows; rr += RP) {
+        float dot = 0.f;
 #pragma unroll
-          for (int off = 1; off < G; off <<= 1) ss += __shfl_xor(ss, off, 64);
-          const float inv = 1.0f / sqrtf(ss * (1.0f / D) + P.eps);
-          float gain[8];
-          unpack8(rr < rows ? gain_q : gain_k, gain);
+        for (int e = 0; e < 8; ++e)
+          dot = fmaf(sm.q[rr][8 * gc + e], sm.k[8 * gc + e], dot);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * gain[e];
-        }
-        // (the partner of dim i is i +- D/2)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = __shfl_xor(x[e], G / 2, 64);
-        const float sign = gc < G / 2 ? -1.f : 1.f, by = rr < rows ? P.c : 1.f;
-        float n2 = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float2 t = sm.rope[(8 * gc + e) % (D / 2)];
-          x[e] = by * fmaf(x[e], t.x, sign * y[e] * t.y);
-          n2 = fmaf(x[e], x[e], n2);
-        }
-#pragma unroll
-        for (int off = 1; off < G; off <<= 1) n2 += __shfl_xor(n2, off, 64);
-        if (gc == 0) sm.norm2[rr < rows ? rr : RT] = n2;
-        float4 *to = reinterpret_cast<float4 *>(
-            (rr < rows ? sm.q[rr] : sm.k) + 8 * gc);
-        to[0] = make_float4(x[0], x[1], x[2], x[3]);
-        to[1] = make_float4(x[4], x[5], x[6], x[7]);
+        for (int off = 1; off < G; off <<= 1) dot += __shfl_xor(dot, off, 64);
+        if (gc == 0) sm.own[rr] = dot;
       }
-      wave_fence();
-      if (split == 0 && wu == 0)
-        for (int rr = lane / G; rr < rows; rr += RP) {
-          float dot = 0.f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            dot = fmaf(sm.q[rr][8 * gc + e], sm.k[8 * gc + e], dot);
-#pragma unroll
-          for (int off = 1; off < G; off <<= 1) dot += __shfl_xor(dot, off, 64);
-          if (gc == 0) sm.own[rr] = dot;
-        }
-      // every logit (log2 units) lies in [-bound, bound] (rows with NaN aside,
-      // which come out NaN either way)
-      float top = 0.f;
-      for (int rr = 0; rr < rows; ++rr) top = fmaxf(top, sm.norm2[rr]);
-      const float bound =
-          sqrtf(top) * fmaxf(kmax, sqrtf(sm.norm2[RT])) * 1.001f;
-      bounded = bound <= kNoRefBound;
+    // every logit (log2 units) lies in [-bound, bound] (rows with NaN aside,
+    // which come out NaN either way)
+    float top = 0.f;
+    for (int rr = 0; rr < rows; ++rr) top = fmaxf(top, sm.norm2[rr]);
+    const float bound =
+        sqrtf(top) * fmaxf(kmax, sqrtf(sm.norm2[RT])) * 1.001f;
+    bounded = bound <= kNoRefBound;
 
-      bf16x8 qh[D / 32], ql[D / 32];
+    bf16x8 qh[D / 32], ql[D / 32];
 #pragma unroll
-      for (int ks = 0; ks < D / 32; ++ks) {
-        const int dim = D == 128 ? 64 * (kg >> 1) + 16 * ks + 8 * (kg & 1)
-                                 : 32 * (kg >> 1) + 16 * ks + 8 * (kg & 1);
-        float x[8];
-        const float4 *from = reinterpret_cast<const float4 *>(
-            &sm.q[col < rows ? col : 0][dim]);
-        const float4 a = from[0], b = from[1];
-        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
-        x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-        qh[ks] = to_bf16x8(x);
+    for (int ks = 0; ks < D / 32; ++ks) {
+      const int dim = D == 128 ? 64 * (kg >> 1) + 16 * ks + 8 * (kg & 1)
+                               : 32 * (kg >> 1) + 16 * ks + 8 * (kg & 1);
+      float x[8];
+      const float4 *from = reinterpret_cast<const float4 *>(
+          &sm.q[col < rows ? col : 0][dim]);
+      const float4 a = from[0], b = from[1];
+      x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
+      x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+      qh[ks] = to_bf16x8(x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] -= (float)qh[ks][e];
-        ql[ks] = to_bf16x8(x);
-      }
-      Sums<D> acc;
-      acc.m = bounded ? 0.f : -INFINITY;
-      acc.l = 0.f;
+      for (int e = 0; e < 8; ++e) x[e] -= (float)qh[ks][e];
+      ql[ks] = to_bf16x8(x);
+    }
+    Sums<D> acc;
+    acc.m = bounded ? 0.f : -INFINITY;
+    acc.l = 0.f;
 #pragma unroll
-      for (int d = 0; d < D / 16; ++d) acc.o[d] = floatx4{0.f, 0.f, 0.f, 0.f};
-      if (bounded)
-        token_chunks<0, D>(slice, first, end, WU, L, lane, qh, ql, codes, acc);
-      else
-        token_chunks<2, D>(slice, first, end, WU, L, lane, qh, ql, codes, acc);
+    for (int d = 0; d < D / 16; ++d) acc.o[d] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (bounded)
+      token_chunks<0, D>(slice, first, end, WU, L, lane, qh, ql, codes, acc);
+    else
+      token_chunks<2, D>(slice, first, end, WU, L, lane, qh, ql, codes, acc);
 
-      // the wave's sums, where q^ was
-      float lt = acc.l + __shfl_xor(acc.l, 16, 64);
-      lt += __shfl_xor(lt, 32, 64);
-      wave_fence();
-      if (col < rows) {
+    // the wave's sums, where q^ was
+    float lt = acc.l + __shfl_xor(acc.l, 16, 64);
+    lt += __shfl_xor(lt, 32, 64);
+    wave_fence();
+    if (col < rows) {
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d)
-          *reinterpret_cast<floatx4 *>(
-              &sm.q[col][32 * (d >> 1) + 16 * (kg & 1) + 8 * (d & 1) +
-                         4 * (kg >> 1)]) = acc.o[d];
-        if (kg == 0) {
-          sm.m[col] = acc.m;
-          sm.l[col] = lt;
-        }
+      for (int d = 0; d < D / 16; ++d)
+        *reinterpret_cast<floatx4 *>(
+            &sm.q[col][32 * (d >> 1) + 16 * (kg & 1) + 8 * (d & 1) +
+                       4 * (kg >> 1)]) = acc.o[d];
+      if (kg == 0) {
+        sm.m[col] = acc.m;
+        sm.l[col] = lt;
       }
     }
     if constexpr (WU == 1)
       wave_fence();
     else
       __syncthreads();
-    if (live)
-      for (int e = wu * 64 + lane; e < rows * (D / 4); e += 64 * WU) {
-        const int rr = e / (D / 4), d = 4 * (e % (D / 4));
-        const float own = split == 0 ? sm_all[w0].own[rr] : -INFINITY;
-        float M = 0.f;
-        if (!bounded) {
-          M = own;
+    for (int e = threadIdx.x; e < rows * (D / 4); e += 64 * WU) {
+      const int rr = e / (D / 4), d = 4 * (e % (D / 4));
+      const float own = split == 0 ? sm_all[0].own[rr] : -INFINITY;
+      float M = 0.f;
+      if (!bounded) {
+        M = own;
 #pragma unroll
-          for (int w = 0; w < WU; ++w) M = fmaxf(M, sm_all[w0 + w].m[rr]);
-        }
-        // (nothing seen, M = -inf: all weights are zero)
-        const float ref = M == -INFINITY ? 0.f : M;
-        float l = __builtin_amdgcn_exp2f(own - ref);
-        float o[4] = {0.f, 0.f, 0.f, 0.f};
-        if (split == 0) {
-          const uint2 x = *reinterpret_cast<const uint2 *>(
-              P.v + (tok * hkv + g) * D + d);
-          o[0] = l * __uint_as_float(x.x << 16);
-          o[1] = l * __uint_as_float(x.x & 0xffff0000u);
-          o[2] = l * __uint_as_float(x.y << 16);
-          o[3] = l * __uint_as_float(x.y & 0xffff0000u);
-        }
-#pragma unroll
-        for (int w = 0; w < WU; ++w) {
-          const TokenRows<D> &from = sm_all[w0 + w];
-          const float f = __builtin_amdgcn_exp2f(from.m[rr] - ref);
-          const float4 x = *reinterpret_cast<const float4 *>(&from.q[rr][d]);
-          l = fmaf(f, from.l[rr], l);
-          o[0] = fmaf(f, x.x, o[0]);
-          o[1] = fmaf(f, x.y, o[1]);
-          o[2] = fmaf(f, x.z, o[2]);
-          o[3] = fmaf(f, x.w, o[3]);
-        }
-        if (P.splits == 1) {
-          store_out(P.out + (row0 + r0 + rr) * D + d, o, 1.0f / l);
-          if (P.lse && d == 0)
-            P.lse[row0 + r0 + rr] = (ref + __log2f(l)) * kLn2;
-        } else {
-          float *to = P.part +
-                      (((p - P.p0) * hkv + g) * P.splits + split) * P.n_rep *
-                          (int64_t)(D + 2) +
-                      (int64_t)(r0 + rr) * (D + 2);
-          // (rows of D + 2: two 8-byte halves)
-          *reinterpret_cast<float2 *>(to + d) = make_float2(o[0], o[1]);
-          *reinterpret_cast<float2 *>(to + d + 2) = make_float2(o[2], o[3]);
-          if (d == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(M, l);
-        }
+        for (int w = 0; w < WU; ++w) M = fmaxf(M, sm_all[w].m[rr]);
       }
+      // (nothing seen, M = -inf: all weights are zero)
+      const float ref = M == -INFINITY ? 0.f : M;
+      float l = __builtin_amdgcn_exp2f(own - ref);
+      float o[4] = {0.f, 0.f, 0.f, 0.f};
+      if (split == 0) {
+        const uint2 x = *reinterpret_cast<const uint2 *>(
+            P.v + (tok * hkv + g) * D + d);
+        o[0] = l * __uint_as_float(x.x << 16);
+        o[1] = l * __uint_as_float(x.x & 0xffff0000u);
+        o[2] = l * __uint_as_float(x.y << 16);
+        o[3] = l * __uint_as_float(x.y & 0xffff0000u);
+      }
+#pragma unroll
+      for (int w = 0; w < WU; ++w) {
+        const TokenRows<D> &from = sm_all[w];
+        const float f = __builtin_amdgcn_exp2f(from.m[rr] - ref);
+        const float4 x = *reinterpret_cast<const float4 *>(&from.q[rr][d]);
+        l = fmaf(f, from.l[rr], l);
+        o[0] = fmaf(f, x.x, o[0]);
+        o[1] = fmaf(f, x.y, o[1]);
+        o[2] = fmaf(f, x.z, o[2]);
+        o[3] = fmaf(f, x.w, o[3]);
+      }
+      if (P.splits == 1) {
+        store_out(P.out + (row0 + r0 + rr) * D + d, o, 1.0f / l);
+        if (P.lse && d == 0)
+          P.lse[row0 + r0 + rr] = (ref + __log2f(l)) * kLn2;
+      } else {
+        float *to = P.part +
+                    (((p - P.p0) * hkv + g) * P.splits + split) * P.n_rep *
+                        (int64_t)(D + 2) +
+                    (int64_t)(r0 + rr) * (D + 2);
+        // (rows of D + 2: two 8-byte halves)
+        *reinterpret_cast<float2 *>(to + d) = make_float2(o[0], o[1]);
+        *reinterpret_cast<float2 *>(to + d + 2) = make_float2(o[2], o[3]);
+        if (d == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(M, l);
+      }
+    }
     // (the next tile writes where this one was read)
     if constexpr (WU == 1)
       wave_fence();
@@ -526,9 +513,10 @@ __global__ __launch_bounds__(join_threads(D, PARTS)) void k_token_join(
   int64_t tok;
   if (!one_token(P, p, tok) || !has_document(P, P.doc_ids[p])) return;
   const int64_t step = (int64_t)P.n_rep * (D + 2), row = tok * P.Hq + h;
-  join_row<D, PARTS>(P.part + ((p - P.p0) * P.sv.n_kv_heads + g) * P.splits * step +
-                  (int64_t)rr * (D + 2),
-              step, P.splits, P.out + row * D, P.lse ? P.lse + row : nullptr);
+  join_row<D, PARTS>(
+      P.part + ((p - P.p0) * P.sv.n_kv_heads + g) * P.splits * step +
+          (int64_t)rr * (D + 2),
+      step, P.splits, P.out + row * D, P.lse ? P.lse + row : nullptr);
 }
 
 // How a call's (pair, kv head)s are shared out: one wave each from kTokenFull
@@ -560,9 +548,7 @@ void launch_token2(int waves, const TokenParams &P, hipStream_t s) {
   const auto kernel = waves == 1   ? k_token_fp4<D, 1>
                       : waves == 2 ? k_token_fp4<D, 2>
                                    : k_token_fp4<D, 4>;
-  const unsigned per = kTokenWaves / waves;
-  hipLaunchKernelGGL(kernel, dim3((P.units + per - 1) / per),
-                     dim3(64 * kTokenWaves), 0, s, P);
+  hipLaunchKernelGGL(kernel, dim3(P.units), dim3(64 * waves), 0, s, P);
 }
 
 template <int D>
