@@ -329,7 +329,9 @@ dopr_status_t dopr_prefix_attn_workspace(dopr_store_t st,
  * bits.  Many short pairs that share few documents run faster by a plan, whose
  * items hold rows of several pairs: kernel_variant 8 (4,096 single tokens on 64
  * documents of 512 slots 187 us, and 288; 1,024 pairs of 4 tokens on 16 of
- * 4,096 330 us, and 541).                                                  */
+ * 4,096 330 us, and 541).  A value v that is not finite makes its dim NaN in
+ * the rows of the tokens before it too, whose weight of zero it meets in the same
+ * 32 keys; other pairs' rows stay as they are.                             */
 dopr_status_t dopr_prefix_attn(dopr_store_t st, int32_t layer,
                                const dopr_attn_args_t *args, void *stream);
 

@@ -192,6 +192,45 @@ def test_graphs_that_share_a_workspace():
             calls[0].call(workspace=ws)
 
 
+@pytest.mark.parametrize("tokens", [[1] * 4, [5, 40, 3, 17], [90] * 4])
+@pytest.mark.parametrize("pairs", [1, 70])
+def test_values_that_are_not_finite(tokens, pairs):
+    """A pair's own keys and values leave other pairs' rows alone, and a
+    document's the rows over other documents; keys that a mask hides change
+    nothing before them."""
+    lens, docs = [40, 70, 33], [0, 1, 0, 2] * pairs
+    args = (lens, docs, tokens * pairs, 4, 2, 128)
+    r = Filled(*args, seed=6)
+    out, lse = r.call()
+    rows = [(int(a), int(b)) for a, b in zip(r.cu[:-1], r.cu[1:])]
+    a, b = rows[1]
+    r.v[b - 1, 0, 5] = float("inf")
+    r.k[b - 1, 1, 7] = float("nan")
+    got, got_lse = r.call()
+    keep = torch.ones(r.total, dtype=torch.bool)
+    keep[a:b] = False
+    _same((got[keep], got_lse[keep]), (out[keep], lse[keep]))
+    # the first kv head's rows: one dim that is not finite, the rest as before
+    mine, dims = got[a:b, :2].float(), torch.arange(128) != 5
+    assert not torch.isfinite(mine[-1, :, 5]).any()
+    _same((got[a:b, :2][..., dims],), (out[a:b, :2][..., dims],))
+    # the second's: the token with the key, and none before
+    assert torch.isnan(got[b - 1, 2:].float()).all()
+    _same((got[a:b - 1, 2:],), (out[a:b - 1, 2:],))
+    # a stored value: its dim, over its document
+    r = Filled(*args, seed=6)
+    r.states[41, 1, 9] = float("nan")  # (the second document's second slot)
+    r.put(r.gain)
+    got, _ = r.call()
+    of = torch.zeros(r.total, dtype=torch.bool)
+    for p, (a, b) in enumerate(rows):
+        of[a:b] = docs[p] == 1
+    hit = torch.zeros((r.total, 4, 128), dtype=torch.bool)
+    hit[of, 2:, 9] = True
+    assert torch.equal(torch.isnan(got.cpu().float()), hit)
+    _same((got.cpu()[~hit],), (out.cpu()[~hit],))
+
+
 def _step(fmt, **rotary):
     from paper_2609_03311_amd import dopr_store_create, pipeline
     st = workloads.custom(np.array([70, 5, 33], np.int32),
