@@ -144,7 +144,7 @@ typedef enum { DOPR_STORE_BF16 = 0, DOPR_STORE_FP4 = 1 } dopr_store_format_t;
 
 /* dopr_store_bytes and dopr_store_create for a format.  *payload_bytes of a
  * 4-bit store: codes and exponents of the documents' slots; its pool holds
- * whole chunks of 32 slots.                                                */
+ * whole chunks of 32 slots, and a document has at most 2^31 - 64.          */
 dopr_status_t dopr_store_bytes_as(const dopr_store_desc_t *desc,
                                   int32_t format, size_t *pool_bytes,
                                   size_t *payload_bytes);
@@ -328,7 +328,7 @@ dopr_status_t dopr_prefix_attn_workspace(dopr_store_t st,
  * outputs are nearer to the definition than the planned kernels', and not their
  * bits.  Many short pairs that share few documents run faster by a plan, whose
  * items hold rows of several pairs: kernel_variant 8 (4,096 single tokens on 64
- * documents of 512 slots 187 us, and 288; 1,024 pairs of 4 tokens on 16 of
+ * documents of 512 slots 187 us, and 275; 1,024 pairs of 4 tokens on 16 of
  * 4,096 330 us, and 541).  A value v that is not finite makes its dim NaN in
  * the rows of the tokens before it too, whose weight of zero it meets in the same
  * 32 keys; other pairs' rows stay as they are.                             */

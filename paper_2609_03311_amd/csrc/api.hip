@@ -95,15 +95,19 @@ dopr_status_t layout_store(const dopr_store_desc_t *d, int32_t format,
       return fail(DOPR_ERR_INVALID_ARG,
                   "doc_len entries must be >= 0, or -1 (not resident)");
     if (L < 0) continue;
+    // (its last chunk's slots are counted in 32 bits)
+    if (fp4 && L > INT32_MAX - 63)
+      return fail(DOPR_ERR_UNSUPPORTED,
+                  "a document of a 4-bit store has at most 2^31 - 64 slots");
     if (doc_off) (*doc_off)[i] = elems;
     elems += (int64_t)d->n_layers *
              layer_block_elems(L, d->n_kv_heads, d->head_dim, fp4);
     // (4 bits a value, and a byte for 32 values of a key, for up to 32 slots
     // of a value's dim)
+    const size_t D = d->head_dim, slots = L;
     const size_t per_head =
-        fp4 ? ((size_t)L + (size_t)L / 32 + (((size_t)L + 31) / 32)) *
-                  d->head_dim
-            : (size_t)L * d->head_dim * 2 * 2;
+        fp4 ? slots * D + slots * (D / 32) + (slots + 31) / 32 * D
+            : slots * D * 2 * 2;
     canon += per_head * d->n_layers * d->n_kv_heads;
     if (L > max_len) max_len = L;
   }

@@ -30,7 +30,8 @@ def test_store_bytes_closed_form():
         chunks = -(-n // 32)
         # half a byte a value of K and V, a byte for 32 dims of a key and for
         # a chunk's slots of a value's dim
-        assert payload == layers * hkv * d * (n + n // 32 + chunks).sum()
+        assert payload == layers * hkv * (n * d + n * (d // 32)
+                                          + chunks * d).sum()
         index = (12 + 4 * layers * hkv) * len(lens)
         held = 34 * d * chunks.sum() * layers * hkv
         assert held + index <= pool <= held + index + 5 * 256
@@ -50,6 +51,14 @@ def test_store_refusals():
     with pytest.raises(D.DoprError) as e:
         D.dopr_store_bytes(1, 8, 96, [4], D.DOPR_STORE_FP4)
     assert e.value.status == UNSUPPORTED
+    for longest, good in ((2 ** 31 - 64, True), (2 ** 31 - 63, False)):
+        if good:
+            assert D.dopr_store_bytes(1, 1, 64, [longest],
+                                      D.DOPR_STORE_FP4)[0] > 68 * longest
+            continue
+        with pytest.raises(D.DoprError) as e:
+            D.dopr_store_bytes(1, 1, 64, [longest], D.DOPR_STORE_FP4)
+        assert e.value.status == UNSUPPORTED
     L = D.lib()
     desc, _keep = D._desc(1, 8, 128, [4])
     h = ctypes.c_void_p(0)
