@@ -246,3 +246,25 @@ def test_put_rotary_rows_outside_the_source():
         D.dopr_store_put_rotary(store, 0, ids,
                                 torch.tensor(cu, device=DEV), k, k, freq)
         assert D.dopr_check_status(store) == D.DOPR_ERR_DOC_RANGE
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_angles_of_any_size(fmt):
+    """Positions of either sign up to the type's ends, and frequencies past
+    any model's."""
+    D = _D()
+    lens, hkv, d = [70], 2, 64
+    cu = _cu(lens)
+    k, v = (torch.randn((70, hkv, d), generator=_gen(s)) for s in (21, 22))
+    pos = torch.randint(-2 ** 31, 2 ** 31, (70,), generator=_gen(23),
+                        dtype=torch.int64).to(torch.int32)
+    pos[:3] = torch.tensor([2 ** 31 - 1, -2 ** 31, 0])
+    freq = 10.0 ** torch.linspace(-12, 9, d // 2)
+    store = _store(D, lens, hkv, d, fmt)
+    D.dopr_store_put_rotary(
+        store, 0, torch.zeros(1, dtype=torch.int32, device=DEV),
+        torch.from_numpy(cu).to(DEV), k.to(DEV), v.to(DEV), freq.to(DEV),
+        positions=pos.to(DEV))
+    want = _expected(k, v, cu, fmt, D, positions=pos, inv_freq=freq)
+    got = _gather(D, store, 0, [0], cu, hkv, d)
+    assert _same(got[0], want[0]) and _same(got[1], want[1])
