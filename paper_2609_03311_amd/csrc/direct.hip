@@ -49,6 +49,7 @@ namespace {
 constexpr int kMostWaves = 4;  // of a unit
 constexpr int waves_a_simd(int D) { return D == 64 ? 4 : 2; }
 constexpr int kKeyThreads = 256;
+constexpr int kSlab = 8;  // tokens that a block of k_own_keys takes at a time
 
 struct RowsParams {
   StoreView sv;
@@ -67,7 +68,6 @@ struct RowsParams {
   double log_theta;
   int64_t n_pairs, total_tokens, rows_cap, n_tiles;
   int64_t first;     // first pair, or block, of this launch
-  int32_t slab;      // tokens a block of k_own_keys takes at a time
   float eps, c;
   int32_t Hq, n_rep, layer, splits, max_tokens;
 };
@@ -104,13 +104,16 @@ __device__ __forceinline__ int64_t key_piece(int64_t group0, int key, int s,
 }
 
 // k^ and the rotations of every token, the tiles' pairs, zero outputs of pairs
-// without a document.  A pair's tokens, `slab` (at most 32) at a time, by
-// gridDim.y blocks.
+// without a document.  A pair's tokens, kSlab at a time, by gridDim.y blocks.
+// (Few at a time, and up to 4,096 blocks of a call: what a block waits for is
+// its tokens' sines and loads in turn.  32 tokens a block and 1,024 blocks: one
+// pair of 129 21 us with the attention for 16, 512 ragged ones 321 for 310, 1,600
+// of 129 2,078 for 2,056.)
 template <int D>
 __global__ __launch_bounds__(kKeyThreads) void k_own_keys(RowsParams P) {
   constexpr int NSUB = D / 16, ROWS = kKeyThreads / NSUB;
   // (pairs side by side, as khat_part takes them; rows off the banks)
-  __shared__ __attribute__((aligned(16))) float2 rope[32][D / 2 + 2];
+  __shared__ __attribute__((aligned(16))) float2 rope[kSlab][D / 2 + 2];
   __shared__ float red[4];
   const int64_t p = P.first + blockIdx.x;
   const int hkv = P.sv.n_kv_heads;
@@ -143,9 +146,9 @@ __global__ __launch_bounds__(kKeyThreads) void k_own_keys(RowsParams P) {
     g0 = *reinterpret_cast<const uint4 *>(P.kw + 8 * sub);
     g1 = *reinterpret_cast<const uint4 *>(P.kw + D / 2 + 8 * sub);
   }
-  for (int64_t at = (int64_t)P.slab * blockIdx.y; at < me.T;
-       at += (int64_t)P.slab * gridDim.y) {
-    const int j0 = (int)at, n = min(P.slab, me.T - j0);
+  for (int64_t at = (int64_t)kSlab * blockIdx.y; at < me.T;
+       at += (int64_t)kSlab * gridDim.y) {
+    const int j0 = (int)at, n = min(kSlab, me.T - j0);
     __syncthreads();  // (the tokens before are done with the table)
     for (int e = threadIdx.x; e < n * (D / 2); e += kKeyThreads) {
       const int j = e / (D / 2), i = e % (D / 2);
@@ -633,13 +636,10 @@ RowsLayout rows_layout(const dopr_store &st, const dopr_attn_args_t &a) {
 template <int D>
 hipError_t launch_rows1(RowsParams P, int waves, hipStream_t s) {
   const int64_t hkv = P.sv.n_kv_heads;
-  // (few pairs of many tokens: blocks share a pair's, and few tokens are spread
-  // thinner, as each takes its sines in turn: one pair of 129: 4.5 us, and 9.0)
+  // (few pairs of many tokens: blocks share a pair's)
   const int64_t most = std::min<int64_t>(P.max_tokens, P.total_tokens);
-  P.slab = P.n_pairs * ((most + 31) / 32) < 256 ? 8 : 32;
-  const int64_t y =
-      std::min((most + P.slab - 1) / P.slab,
-               std::max<int64_t>(1, 1024 / P.n_pairs));
+  const int64_t y = std::min((most + kSlab - 1) / kSlab,
+                             std::max<int64_t>(1, 4096 / P.n_pairs));
   hipError_t e =
       in_slices(P.n_pairs, a_launch(kKeyThreads), [&](int64_t at, int64_t n) {
         RowsParams S = P;
