@@ -187,10 +187,12 @@ __device__ __forceinline__ void round8(const Raw8<T> &x, uint32_t *w) {
   for (int i = 0; i < 4; ++i) w[i] = pack2<bf16_t>(f[2 * i], f[2 * i + 1]);
 }
 
-// A value times its gain: exact in fp32 for two 16-bit types.
+// A value times its gain, exact: in fp32 for two fp16 values; the product of two
+// bf16 values fits fp32's bits, but not its range.  (1,024 documents of 256 slots
+// in bf16 381 -> 389 us for it.)
 template <typename T>
 __device__ __forceinline__ double times(float x, float w) {
-  return sizeof(T) == 2 ? (double)(x * w) : (double)x * w;
+  return std::is_same_v<T, _Float16> ? (double)(x * w) : (double)x * w;
 }
 
 // What a wave knows of its chunk.
@@ -343,7 +345,12 @@ __device__ __forceinline__ float put_keys(const PutParams &P, const Share<T> &h,
         float f[8];
         cur[j].get(f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[j][e] = times<T>(f[e], gain[j][e]);
+        for (int e = 0; e < 8; ++e) {
+          // (bf16 gains widened here: 64-bit ones held across the rows spill)
+          if constexpr (std::is_same_v<T, bf16_t>)
+            asm volatile("" : "+v"(gain[j][e]));
+          x[j][e] = times<T>(f[e], gain[j][e]);
+        }
       }
       // (turned, then by 1 / rms)
       if constexpr (MODE == kWholeHalf && D == 128) {
