@@ -11,9 +11,12 @@
 // each step.  What is stored is laid out in the wave's part of LDS and leaves
 // in whole lines.
 //
-// Keys are normed and turned in 64 bits and rounded once, to bf16: a 4-bit
-// store quantises that value, and a key off by fp32's rounding would now and
-// then land on another code, half a step of the block away.
+// Keys are normed and turned in 64 bits and rounded at the end, to fp32 and from
+// there to bf16, as a framework's conversion from 64 bits does it: a 4-bit store
+// quantises that value, and a key off by a sum's order would now and then land on
+// another code, half a step of the block away.  (Where fp32 rounds to the middle
+// of two bf16 values, one normal value in 130,000, the key may be the farther one
+// of the two.)
 #include <type_traits>
 
 #include "fp4.hpp"

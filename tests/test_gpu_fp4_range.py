@@ -81,3 +81,24 @@ def test_products_with_gains_that_leave_fp32(d, rotated, inter, eps):
     for gain in (torch.full((d,), 1.25), 40 * about_one, about_one * 2e-30,
                  torch.ldexp(about_one.double(), spread)):
         _check(k, gain.to(torch.bfloat16), d, rotated, inter, eps)
+
+
+def test_keys_next_to_the_middle_of_two_bf16_values():
+    """A key's two roundings, 64 bits to fp32 and from there to bf16: what fp32
+    rounds to the middle of two bf16 values goes to the even one.  k times the
+    factor is m (1 - 2^-13) (1 + 2^-13) = m (1 - 2^-26), less than an eighth of
+    fp32's step below the middle m."""
+    D = _D()
+    d, rows = 128, 127
+    m = torch.arange(128, 255).double() + 0.5
+    k = (m * (1 - 2.0 ** -13)).float()
+    assert (k.double() == m * (1 - 2.0 ** -13)).all()
+    k = k[:, None, None].expand(rows, 1, d).contiguous().to(DEV)
+    store = _store(D, [rows], 1, d, D.DOPR_STORE_BF16)
+    D.dopr_store_put_rotary(
+        store, 0, torch.zeros(1, dtype=torch.int32, device=DEV),
+        torch.tensor([0, rows], device=DEV), k, k,
+        torch.zeros(d // 2, device=DEV), attention_factor=1 + 2.0 ** -13)
+    got, _ = _gather(D, store, 0, [0], _cu([rows]), 1, d)
+    even = 2 * ((m + 0.5) / 2).floor()
+    assert (got[:, 0].double() == even[:, None]).all()
