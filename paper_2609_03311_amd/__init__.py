@@ -465,12 +465,23 @@ def dopr_prefix_attn(store: Store, layer: int, doc_ids, cu_seqlens, q, k, v,
     item size; queue_order 0/1/2 is the automatic, natural or
     longest-first order of the work queues."""
     begin, end = timing if timing is not None else (None, None)
-    _check(_compiled().prefix_attn(
+    status = _compiled().prefix_attn(
         store.handle, store.n_kv_heads, store.head_dim, layer, doc_ids,
         cu_seqlens, q, k, v, q_norm_w, k_norm_w, out, lse, workspace,
         max_tokens, total_tokens, rms_eps, rope_theta, softmax_scale,
         kernel_variant, begin, end, rope_inv_freq, rows_per_item,
-        queue_order, _handle(stream)))
+        queue_order, _handle(stream))
+    if status is None:  # (arguments that only ctypes takes, or names)
+        a = _attn_args(store, doc_ids, cu_seqlens, q, k, v, q_norm_w,
+                       k_norm_w, out, lse, workspace, max_tokens=max_tokens,
+                       total_tokens=total_tokens, rms_eps=rms_eps,
+                       rope_theta=rope_theta, softmax_scale=softmax_scale,
+                       kernel_variant=kernel_variant, timing=timing,
+                       rope_inv_freq=rope_inv_freq,
+                       rows_per_item=rows_per_item, queue_order=queue_order)
+        status = lib().dopr_prefix_attn(store.handle, layer, ctypes.byref(a),
+                                        _stream(stream))
+    _check(status)
 
 
 def dopr_prefix_attn_noalloc(store: Store, layer: int, doc_ids, cu_seqlens,
@@ -594,9 +605,15 @@ def dopr_group_pairs(store: Store, doc_ids, workspace, stream=None):
 
 def dopr_gather_prefix(store: Store, layer: int, doc_ids, out_cu_slots,
                        k_out, v_out, stream=None):
-    _check(_compiled().gather_prefix(store.handle, layer, doc_ids,
-                                     out_cu_slots, k_out, v_out,
-                                     _handle(stream)))
+    status = _compiled().gather_prefix(store.handle, layer, doc_ids,
+                                       out_cu_slots, k_out, v_out,
+                                       _handle(stream))
+    if status is None:  # (arguments that only ctypes takes, or names)
+        status = lib().dopr_gather_prefix(store.handle, layer,
+                                          doc_ids.numel(), _ptr(doc_ids),
+                                          _ptr(out_cu_slots), _ptr(k_out),
+                                          _ptr(v_out), _stream(stream))
+    _check(status)
 
 
 def _salience_args(n_docs, max_doclen, n_q_heads, n_kv_heads, top_p,

@@ -10,7 +10,7 @@
 //
 // Every function takes its arguments by position, None for an absent tensor,
 // and a stream handle last (None: the current stream), and returns the call's
-// status.
+// status, or None where it has not been made (see Elsewhere).
 #include <Python.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -323,20 +323,31 @@ PyObject *store_put_rotary(PyObject *const *a) {
       static_cast<dopr_store_t>(store), &s, handle(a[15])));
 }
 
+// The calls below are also marshalled in Python, which takes more than they do
+// (other objects with a tensor's methods, numbers and handles in other forms) and
+// names what it refuses; an argument of another kind than a tensor, an int or a
+// float leaves the call to that.
+struct Elsewhere {};
+
 // A tensor's address as it is (its caller keeps to the C ABI), NULL for None.
 template <typename P>
-void address(PyObject *o, const char *what, P &p) {
-  p = o == Py_None ? nullptr : static_cast<P>(tensor(o, what).data_ptr());
+void address(PyObject *o, P &p) {
+  if (o != Py_None && !THPVariable_Check(o)) throw Elsewhere{};
+  p = o == Py_None ? nullptr
+                   : static_cast<P>(THPVariable_Unpack(o).data_ptr());
 }
 
-// An object's integer as the C type's lowest bits (as ctypes passes it), a
-// pointer's address with None for NULL.
+const at::Tensor &plain_tensor(PyObject *o) {
+  if (!THPVariable_Check(o)) throw Elsewhere{};
+  return THPVariable_Unpack(o);
+}
+
+// An int's lowest bits as the C type (as ctypes passes it), a handle's with None
+// for NULL.
 template <typename I>
 I bits(PyObject *o) {
-  PyObject *n = PyNumber_Long(o);
-  if (!n) throw Refused{};
-  const unsigned long long v = PyLong_AsUnsignedLongLongMask(n);
-  Py_DECREF(n);
+  if (!PyLong_Check(o)) throw Elsewhere{};
+  const unsigned long long v = PyLong_AsUnsignedLongLongMask(o);
   if (v == ~0ull && PyErr_Occurred()) throw Refused{};
   return (I)v;
 }
@@ -345,51 +356,59 @@ void *pointer(PyObject *o) {
   return o == Py_None ? nullptr : reinterpret_cast<void *>(bits<uintptr_t>(o));
 }
 
+float plain_real(PyObject *o) {
+  if (!PyFloat_Check(o) && !PyLong_Check(o)) throw Elsewhere{};
+  return real(o);
+}
+
+void *plain_handle(PyObject *o) {
+  return o == Py_None ? handle(o) : pointer(o);
+}
+
 PyObject *prefix_attn(PyObject *const *a) {
   // store's handle, kv heads and head dim, layer, doc_ids, cu_seqlens, q, k, v,
   // q_norm_w, k_norm_w, out, lse, workspace, max_tokens, total_tokens, rms_eps,
   // rope_theta, softmax_scale, kernel_variant, timing begin and end,
   // rope_inv_freq, rows_per_item, queue_order, stream
   dopr_attn_args_t s{};
-  s.n_pairs = (int32_t)tensor(a[4], "doc_ids").numel();
-  address(a[4], "doc_ids", s.doc_ids);
-  address(a[5], "cu_seqlens", s.cu_seqlens);
+  s.n_pairs = (int32_t)plain_tensor(a[4]).numel();
+  address(a[4], s.doc_ids);
+  address(a[5], s.cu_seqlens);
   s.n_q_heads = bits<int32_t>(a[1]);
   if (a[6] != Py_None) {
-    const at::Tensor &q = tensor(a[6], "q");
-    if (q.dim() < 2) {
-      PyErr_SetString(PyExc_IndexError, "q must be [tokens, q heads, head dim]");
-      throw Refused{};
-    }
+    const at::Tensor &q = plain_tensor(a[6]);
+    if (q.dim() < 2) throw Elsewhere{};
     s.n_q_heads = (int32_t)q.size(1);
     s.total_tokens = q.size(0);
+  } else if (a[15] == Py_None) {
+    throw Elsewhere{};
   }
-  address(a[6], "q", s.q);
-  address(a[7], "k", s.k);
-  address(a[8], "v", s.v);
-  address(a[9], "q_norm_w", s.q_norm_w);
-  address(a[10], "k_norm_w", s.k_norm_w);
-  address(a[11], "out", s.out);
-  address(a[12], "lse", s.lse);
-  address(a[13], "workspace", s.workspace);
-  if (s.workspace) s.workspace_bytes = tensor(a[13], "workspace").nbytes();
+  address(a[6], s.q);
+  address(a[7], s.k);
+  address(a[8], s.v);
+  address(a[9], s.q_norm_w);
+  address(a[10], s.k_norm_w);
+  address(a[11], s.out);
+  address(a[12], s.lse);
+  address(a[13], s.workspace);
+  if (s.workspace) s.workspace_bytes = plain_tensor(a[13]).nbytes();
   s.max_tokens = bits<int32_t>(a[14]);
   if (a[15] != Py_None) s.total_tokens = bits<int64_t>(a[15]);
-  s.rms_eps = real(a[16]);
-  s.rope_theta = real(a[17]);
+  s.rms_eps = plain_real(a[16]);
+  s.rope_theta = plain_real(a[17]);
   s.softmax_scale =
       a[18] == Py_None
           ? (float)std::pow((double)bits<int32_t>(a[2]), -0.5)
-          : real(a[18]);
+          : plain_real(a[18]);
   s.kernel_variant = bits<int32_t>(a[19]);
   s.timing_begin = pointer(a[20]);
   s.timing_end = pointer(a[21]);
-  address(a[22], "rope_inv_freq", s.rope_inv_freq);
+  address(a[22], s.rope_inv_freq);
   s.rows_per_item = bits<int32_t>(a[23]);
   s.queue_order = bits<int32_t>(a[24]);
   return PyLong_FromLong(
       dopr_prefix_attn(static_cast<dopr_store_t>(pointer(a[0])),
-                       bits<int32_t>(a[3]), &s, handle(a[25])));
+                       bits<int32_t>(a[3]), &s, plain_handle(a[25])));
 }
 
 PyObject *gather_prefix(PyObject *const *a) {
@@ -397,14 +416,14 @@ PyObject *gather_prefix(PyObject *const *a) {
   const int32_t *doc_ids;
   const int64_t *out_cu;
   void *k, *v;
-  address(a[2], "doc_ids", doc_ids);
-  address(a[3], "out_cu_slots", out_cu);
-  address(a[4], "k_out", k);
-  address(a[5], "v_out", v);
+  address(a[2], doc_ids);
+  address(a[3], out_cu);
+  address(a[4], k);
+  address(a[5], v);
   return PyLong_FromLong(dopr_gather_prefix(
       static_cast<dopr_store_t>(pointer(a[0])), bits<int32_t>(a[1]),
-      (int32_t)tensor(a[2], "doc_ids").numel(), doc_ids, out_cu, k, v,
-      handle(a[6])));
+      (int32_t)plain_tensor(a[2]).numel(), doc_ids, out_cu, k, v,
+      plain_handle(a[6])));
 }
 
 template <PyObject *(*call)(PyObject *const *), Py_ssize_t count>
@@ -415,6 +434,8 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
   }
   try {
     return call(args);
+  } catch (const Elsewhere &) {
+    Py_RETURN_NONE;
   } catch (const Refused &) {
   } catch (const std::exception &e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
