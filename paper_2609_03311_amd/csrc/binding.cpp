@@ -122,6 +122,21 @@ int32_t flag(PyObject *o) {
   return v;
 }
 
+// The status of a C call, which other Python threads run beside: it waits where
+// the stream's queue is full.
+template <typename Call>
+PyObject *status_of(Call call) {
+  struct Unlocked {
+    PyThreadState *state = PyEval_SaveThread();
+    ~Unlocked() { PyEval_RestoreThread(state); }
+  };
+  const auto made = [&] {
+    const Unlocked here;
+    return call();
+  };
+  return PyLong_FromLong(made());
+}
+
 PyObject *quantize_rows(PyObject *const *a) {
   dopr_quantize_args_t s{};
   const at::Tensor &x = tensor(a[0], "x");
@@ -134,7 +149,8 @@ PyObject *quantize_rows(PyObject *const *a) {
   matrix(a[1], "q", ScalarType::Char, s.rows, s.width, s.q, s.q_row_stride);
   vector(a[2], "scale", ScalarType::Float, s.rows, s.scale);
   matrix(a[3], "up", t, s.rows, s.width, s.up, s.up_row_stride);
-  return PyLong_FromLong(dopr_quantize_rows(&s, handle(a[4])));
+  void *stream = handle(a[4]);
+  return status_of([&] { return dopr_quantize_rows(&s, stream); });
 }
 
 PyObject *quant_matmul(PyObject *const *a) {
@@ -166,7 +182,8 @@ PyObject *quant_matmul(PyObject *const *a) {
     s.workspace = ws.data_ptr();
     s.workspace_bytes = ws.nbytes();
   }
-  return PyLong_FromLong(dopr_quant_matmul(&s, handle(a[8])));
+  void *stream = handle(a[8]);
+  return status_of([&] { return dopr_quant_matmul(&s, stream); });
 }
 
 PyObject *norm_residual(PyObject *const *a) {
@@ -202,7 +219,8 @@ PyObject *norm_residual(PyObject *const *a) {
   matrix(a[8], "q", ScalarType::Char, s.rows, s.width, s.q, s.q_row_stride);
   vector(a[9], "q_scale", ScalarType::Float, s.rows, s.q_scale);
   s.rms_eps = real(a[10]);
-  return PyLong_FromLong(dopr_norm_residual(&s, handle(a[11])));
+  void *stream = handle(a[11]);
+  return status_of([&] { return dopr_norm_residual(&s, stream); });
 }
 
 // [rows, heads, d] and its output
@@ -263,7 +281,8 @@ PyObject *rotary(PyObject *const *a) {
   vector(a[9], "q_norm_w", t, s.head_dim, s.q_norm_w);
   vector(a[10], "k_norm_w", t, s.head_dim, s.k_norm_w);
   s.rms_eps = real(a[11]);
-  return PyLong_FromLong(dopr_rotary(&s, handle(a[12])));
+  void *stream = handle(a[12]);
+  return status_of([&] { return dopr_rotary(&s, stream); });
 }
 
 int64_t whole(PyObject *o) {
@@ -319,8 +338,10 @@ PyObject *store_put_rotary(PyObject *const *a) {
   s.rms_eps = real(a[14]);
   void *store = PyLong_AsVoidPtr(a[0]);
   if (!store && PyErr_Occurred()) throw Refused{};
-  return PyLong_FromLong(dopr_store_put_rotary(
-      static_cast<dopr_store_t>(store), &s, handle(a[15])));
+  void *stream = handle(a[15]);
+  return status_of([&] {
+    return dopr_store_put_rotary(static_cast<dopr_store_t>(store), &s, stream);
+  });
 }
 
 // The calls below are also marshalled in Python, which takes more than they do
@@ -406,9 +427,10 @@ PyObject *prefix_attn(PyObject *const *a) {
   address(a[22], s.rope_inv_freq);
   s.rows_per_item = bits<int32_t>(a[23]);
   s.queue_order = bits<int32_t>(a[24]);
-  return PyLong_FromLong(
-      dopr_prefix_attn(static_cast<dopr_store_t>(pointer(a[0])),
-                       bits<int32_t>(a[3]), &s, plain_handle(a[25])));
+  const auto store = static_cast<dopr_store_t>(pointer(a[0]));
+  const int32_t layer = bits<int32_t>(a[3]);
+  void *stream = plain_handle(a[25]);
+  return status_of([&] { return dopr_prefix_attn(store, layer, &s, stream); });
 }
 
 PyObject *gather_prefix(PyObject *const *a) {
@@ -420,10 +442,13 @@ PyObject *gather_prefix(PyObject *const *a) {
   address(a[3], out_cu);
   address(a[4], k);
   address(a[5], v);
-  return PyLong_FromLong(dopr_gather_prefix(
-      static_cast<dopr_store_t>(pointer(a[0])), bits<int32_t>(a[1]),
-      (int32_t)plain_tensor(a[2]).numel(), doc_ids, out_cu, k, v,
-      plain_handle(a[6])));
+  const auto store = static_cast<dopr_store_t>(pointer(a[0]));
+  const int32_t layer = bits<int32_t>(a[1]);
+  const int32_t n = (int32_t)plain_tensor(a[2]).numel();
+  void *stream = plain_handle(a[6]);
+  return status_of([&] {
+    return dopr_gather_prefix(store, layer, n, doc_ids, out_cu, k, v, stream);
+  });
 }
 
 template <PyObject *(*call)(PyObject *const *), Py_ssize_t count>
