@@ -159,12 +159,13 @@ dopr_status_t dopr_store_create_as(const dopr_store_desc_t *desc,
  *   pos = positions[r], or j when positions is NULL
  * the rotation being dopr_rotary's (rotary_dim, interleaved, inv_freq,
  * attention_factor).  k' is formed in 64 bits and rounded to fp32 and from there
- * to bf16, v is rounded to bf16, and both go into the store, of either format, as
- * dopr_store_put would put them.  Rows and heads lie any distance apart (k and v may be parts
- * of one buffer).  A document whose rows do not lie in [0, rows), whose slot
- * count differs from L_d, or that is out of range or not resident, is skipped
- * and reported by dopr_check_status as DOC_RANGE.  A call names a document
- * once.                                                                    */
+ * to bf16, v is rounded to bf16, and both go into the store, of either format,
+ * as dopr_store_put would put them.  Rows and heads lie any distance apart (k
+ * and v may be parts of one buffer).  A document whose rows do not lie in
+ * [0, rows), whose slot count differs from L_d, or that is out of range or not
+ * resident, is skipped and reported by dopr_check_status as DOC_RANGE.  Where
+ * rows is 0 (documents without slots), k and v may be NULL.  A call names a
+ * document once.                                                           */
 typedef struct {
   int32_t layer;
   int32_t dtype;            /* of k, v and k_norm_w (dopr_dtype_t: bf16, fp16

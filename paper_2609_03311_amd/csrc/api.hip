@@ -439,7 +439,8 @@ dopr_status_t dopr_store_put_rotary(dopr_store_t st,
       a->v_head_stride < 0)
     return fail(DOPR_ERR_INVALID_ARG, "strides must be >= 0");
   if (a->n == 0) return ok();
-  if (!a->doc_ids || !a->src_cu_slots || !a->inv_freq || !a->k || !a->v)
+  if (!a->doc_ids || !a->src_cu_slots || !a->inv_freq ||
+      (a->rows > 0 && (!a->k || !a->v)))
     return fail(DOPR_ERR_INVALID_ARG, "NULL buffer");
   if (!aligned_to(a->k, a->dtype) || !aligned_to(a->v, a->dtype) ||
       !aligned_to(a->k_norm_w, a->dtype) ||
