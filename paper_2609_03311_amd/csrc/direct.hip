@@ -435,7 +435,7 @@ __global__ __launch_bounds__(64 * WU) __attribute__((
     const float bound = P.c * uniform_load(P.bounds, 1) *
                         fmaxf(kmax, uniform_load(P.bounds, 0)) * 1.001f;
     // (one wave's sums without a bound are looked at behind the chunks)
-    const bool alone = WU == 1 && P.splits == 1;
+    const bool alone = WU == 1;  // (never of several blocks)
     bounded = known ? bound <= kNoRefBound : alone;
     uint16_t *lds = reinterpret_cast<uint16_t *>(sm.wave[wave]);
     const uint32_t at = (uint32_t)(uintptr_t)(
@@ -463,20 +463,6 @@ __global__ __launch_bounds__(64 * WU) __attribute__((
   if constexpr (WU == 1) {
     if (!valid) return;
     const int64_t orow = tokq * P.Hq + head;
-    if (P.splits > 1) {
-      float *to = P.part + ((tile * hkv + g) * P.splits + split) *
-                               (int64_t)(32 * (D + 2)) +
-                  lq * (D + 2);
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int x = 0; x < 16; x += 2)
-          *reinterpret_cast<float2 *>(to + 32 * db + 16 * hf + x) =
-              make_float2(acc[0].o[db][x], acc[0].o[db][x + 1]);
-      if (hf == 0)
-        *reinterpret_cast<float2 *>(to + D) = make_float2(acc[0].m, lt);
-      return;
-    }
     const float inv = 1.0f / lt;
     uint16_t *op = P.out + orow * D;
 #pragma unroll
