@@ -136,7 +136,8 @@ dopr_status_t dopr_store_destroy(dopr_store_t st);
  *                    dim of 32 slots (32 s .. 32 s + 31 of the document, fewer
  *                    at its end).  No value is off by more than 2^e (beyond
  *                    7 * 2^125, by more).  A block with a value that is not
- *                    finite reads as NaN.
+ *                    finite reads as NaN.  A dopr_store_put names a document
+ *                    once.
  * What is held are bf16 values, and a call on a 4-bit store computes what it
  * computes on a bf16 store that holds those values: the same bits wherever the
  * same kernels run (not the pairs of one token, see dopr_prefix_attn).  */
@@ -332,7 +333,9 @@ dopr_status_t dopr_prefix_attn_workspace(dopr_store_t st,
  * documents of 512 slots 187 us, and 275; 1,024 pairs of 4 tokens on 16 of
  * 4,096 330 us, and 541).  A value v that is not finite makes its dim NaN in
  * the rows of the tokens before it too, whose weight of zero it meets in the same
- * 32 keys; other pairs' rows stay as they are.                             */
+ * 32 keys; other pairs' rows stay as they are.  (The planned kernels, over a
+ * store of either format, pass it on to the rows of other pairs of the document
+ * that share its work unit as well.)                                       */
 dopr_status_t dopr_prefix_attn(dopr_store_t st, int32_t layer,
                                const dopr_attn_args_t *args, void *stream);
 

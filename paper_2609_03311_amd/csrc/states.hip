@@ -126,8 +126,8 @@ __device__ __attribute__((noinline)) double2 cos_sin_far(double x) {
 
 // sin and cos of x in 64 bits: x less its quarter turns (pi / 2 in two parts,
 // to 2^-106 of itself) and the Taylor series, whose first terms left out are
-// under 2^-60 at pi / 4.  Past 2^45 quarter turns (frequencies no model has)
-// the library's.
+// under 2^-60 at pi / 4.  From |x| = 2^45 on (frequencies no model has) the
+// library's.
 __device__ __forceinline__ double2 cos_sin(double x) {
   if (!(fabs(x) < 0x1p45)) return cos_sin_far(x);
   const double n = rint(x * 0.63661977236758134308);
