@@ -18,7 +18,7 @@
 // short pairs share few documents, whose rows it puts into common tiles: 1,024
 // pairs of 4 tokens on 16 documents of 4,096 slots 541 and 330.
 //
-// What bounds it: the vector unit (50 % busy; of 2,132 vector instructions a
+// What bounds it: the vector unit (51 % busy; of 2,127 vector instructions a
 // wave of the 1,600 pairs, beside 169 products, a chunk's are about 116, 64 of
 // them the codes' conversions, q^ 416) and, at its ends, q's loads and the
 // output's stores, which two waves a SIMD overlap only in part.  Three (168 registers) were no faster
